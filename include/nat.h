@@ -7,6 +7,10 @@
  * laws inside the same estimator), nat_prefix_pack (the truncated batch for the model
  * body), nat_loss_fwd_bwd_kl (token loss with the KL term, entropy), nat_logp_fwd (the
  * forward pass alone).
+ * In the model body: nat_attn_fwd / nat_attn_bwd (attention over the packed sequences of
+ * nat_prefix_pack).  Where the rollouts are written: nat_sample (the next token and its
+ * behaviour log-prob), nat_kv_write / nat_kv_read / nat_attn_decode (a paged key-value cache
+ * and attention of one new token over it).
  *
  * Notation follows the paper: P prompts, G rollouts per prompt, B = P*G
  * rollouts, T_i response length of rollout i, t = 1..T_i token position,
@@ -385,6 +389,147 @@ nat_status nat_loss_fwd_bwd_kl(const void* d_hidden_k, const void* d_W, const in
                                float* d_loss, float* d_logp_k, float* d_kl_k, float* d_entropy_k,
                                int32_t* d_diag, void* d_dH_k, float* d_dW, int32_t accumulate_dw,
                                void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Attention over packed sequences with grouped heads: what the model body runs over the rows of
+ * nat_prefix_pack, or over whole prompts.
+ *     S_ij = scale q_i . k_j,  lse_i = log sum_j exp(S_ij),  out_i = sum_j exp(S_ij - lse_i) v_j
+ * over the keys j that query i sees: of its own sequence, all of them, or (causal) the first
+ * t + 1 + (keys - queries) for the query at place t, so that the last query sees all keys: with as many
+ * keys as queries its own and those before it; with more, queries behind a cached prefix; with fewer,
+ * the first queries see none.  A query that sees no key has out = 0 and lse = -inf, and adds nothing to
+ * any gradient.  What lies in masked places of keys, values, queries or gradients (infinities and NaN
+ * too) has no influence.
+ *   n_seqs       sequences;  n_q, n_k: rows of the query and key arrays (at most 2^31 - 1);
+ *   n_q_heads    a multiple of n_kv_heads; query head h reads key head h / (n_q_heads / n_kv_heads);
+ *   head_dim     64 or 128;  dtype NAT_DTYPE_BF16;  causal 0 or 1;  scale > 0 and finite;
+ *   *_stride     elements from row to row (a row holds its heads back to back), a multiple of 8, at least
+ *                heads * head_dim and below 2^31; 0 = exactly that.  q, k, v may be parts of one array.
+ */
+typedef struct nat_attn_params {
+  int32_t n_seqs, n_q_heads, n_kv_heads, head_dim, dtype, causal;
+  float scale;
+  int64_t n_q, n_k;
+  int64_t q_stride, k_stride, v_stride, out_stride;
+  int64_t dout_stride, dq_stride, dk_stride, dv_stride;      /* nat_attn_bwd */
+} nat_attn_params;
+
+/*
+ *   d_q [n_q, n_q_heads, head_dim], d_k, d_v [n_k, n_kv_heads, head_dim] bf16;
+ *   d_cu_q, d_cu_k [n_seqs+1] int32: non-decreasing row offsets (d_cu_packed of nat_prefix_pack); values
+ *                outside [0, n_q] / [0, n_k] are clamped;
+ *   d_out [n_q, n_q_heads, head_dim] bf16 out;  d_lse [n_q_heads, n_q] float out.  Rows of no sequence
+ *                are not written.
+ * Products of queries and keys and all sums are held in fp32; the probabilities are rounded to bf16 for
+ * the product with the values.  Results do not change from run to run.
+ * Errors: NULL pointer, negative count, causal not 0 / 1, scale out of range, a pointer (other than lse and
+ * offsets) that is not 16-byte aligned -> NAT_INVALID_ARG; head counts, head_dim or a stride out of range, or
+ * n_q * (n_q_heads / n_kv_heads) >= 2^30 -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE.
+ * n_seqs = 0 and n_q = 0 are valid and do nothing.
+ */
+nat_status nat_attn_fwd(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v,
+                        const int32_t* d_cu_q, const int32_t* d_cu_k, void* d_out, float* d_lse, void* stream);
+
+/*
+ * Its gradients: with P_ij = exp(S_ij - lse_i), dS_ij = P_ij (dout_i . v_j - dout_i . out_i),
+ *     dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i,
+ * the sums for dk, dv over all query heads that share the key head.
+ *   d_out, d_lse from nat_attn_fwd;  d_dout [n_q, n_q_heads, head_dim] bf16;
+ *   d_dq like d_q, d_dk, d_dv like d_k: bf16 out (rows of no sequence are not written);
+ *   d_ws / ws_bytes: at least nat_attn_bwd_workspace_bytes, 256-byte aligned.
+ * P and dS are rounded to bf16 for the products that they enter.  No atomics: results do not change from
+ * run to run.  Errors as nat_attn_fwd, plus NAT_WORKSPACE_TOO_SMALL.  With n_q = 0, dk and dv are zeros.
+ */
+size_t nat_attn_bwd_workspace_bytes(int64_t n_q, int32_t n_q_heads);
+nat_status nat_attn_bwd(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v,
+                        const void* d_out, const float* d_lse, const void* d_dout, const int32_t* d_cu_q,
+                        const int32_t* d_cu_k, void* d_dq, void* d_dk, void* d_dv,
+                        void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * A paged key-value cache, owned by the caller.  Token t of a sequence lies in page block_table[t / page_size]
+ * at place t % page_size; slot = page * page_size + place.
+ *   d_k, d_v     [n_pages, n_kv_heads, page_size, head_dim] in `format`: NAT_KV_BF16, or NAT_KV_FP8: 8 bits with 4
+ *                exponent and 3 mantissa bits (largest value 448, no infinities);
+ *   d_k_exp, d_v_exp [n_pages, n_kv_heads, page_size] uint8, NAT_KV_FP8 only: row (token, head) stands for its
+ *                8-bit values times 2^(exp - 127);
+ *   page_size    16, 32, 64, 128 or 256;  head_dim 64 or 128.  All four arrays 16-byte aligned.
+ */
+enum { NAT_KV_BF16 = 0, NAT_KV_FP8 = 1 };
+typedef struct nat_kv_cache {
+  void *d_k, *d_v;
+  uint8_t *d_k_exp, *d_v_exp;
+  int32_t n_pages, n_kv_heads, page_size, head_dim, format;
+} nat_kv_cache;
+
+/*
+ * Write rows into the cache.
+ *   d_k, d_v     [n_rows, n_kv_heads, head_dim] bf16, strides as in nat_attn_params;
+ *   d_slots      [n_rows] int64: the slot of each row.  Rows with a slot outside [0, n_pages * page_size) (-1: a row
+ *                of padding) are skipped; the other slots must differ from one another.
+ * NAT_KV_FP8: the exponent of a row is the smallest e >= -126 with max |x| <= 448 * 2^e over its finite elements, and
+ * its values are x / 2^e rounded to nearest, ties to even; elements that are not finite are stored as NaN.
+ * Errors: NULL or misaligned pointer, negative count, n_pages <= 0 -> NAT_INVALID_ARG; page_size, head_dim, heads or stride
+ * out of range -> NAT_BAD_SHAPE; format -> NAT_UNSUPPORTED_DTYPE.
+ */
+nat_status nat_kv_write(const nat_kv_cache* cache, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
+                        const int64_t* d_slots, int64_t n_rows, void* stream);
+
+/*
+ * Read sequences back as packed bf16 rows (the keys and values of nat_attn_fwd for queries behind a cached prefix).
+ *   d_block_table [n_seqs, table_width] int32;  d_cu_k [n_seqs+1] int32 row offsets of the output;
+ *   d_k, d_v     [n_rows, n_kv_heads, head_dim] out: row cu_k[b] + t is token t of sequence b.  Tokens beyond the
+ *                table's width or with a page outside [0, n_pages) are zeros; rows of no sequence are not written.
+ * Reading back is exact as far as bf16 goes: 3 mantissa bits and a power of two.  Errors as nat_kv_write.
+ */
+nat_status nat_kv_read(const nat_kv_cache* cache, const int32_t* d_block_table, int32_t table_width,
+                       const int32_t* d_cu_k, int32_t n_seqs, int64_t n_rows, void* d_k, int64_t k_stride,
+                       void* d_v, int64_t v_stride, void* stream);
+
+/*
+ * Attention of one new token per sequence over its cached tokens (the new token's own key and value written before).
+ *   d_q          [n_seqs, n_q_heads, head_dim] bf16;  d_seq_lens [n_seqs] int32: cached tokens that count, the first ones
+ *                (clamped to [0, table_width * page_size]); tokens whose page lies outside [0, n_pages) do not count;
+ *   d_out        [n_seqs, n_q_heads, head_dim] bf16 out;  d_lse [n_seqs, n_q_heads] float out.  Without any token out = 0
+ *                and lse = -inf.  What is stored in places beyond a sequence's length has no influence;
+ *   d_ws / ws_bytes: nat_attn_decode_workspace_bytes(.., max_tokens = table_width * page_size), 256-byte aligned; 0 for
+ *                short tables, which need none.
+ * Long sequences are cut into chunks for different workgroups and joined by a second kernel; how depends on the sizes
+ * alone, so results do not change from run to run.
+ * Errors: as nat_kv_write, plus scale out of range -> NAT_INVALID_ARG, NAT_WORKSPACE_TOO_SMALL.
+ */
+size_t nat_attn_decode_workspace_bytes(int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                       int64_t max_tokens);
+nat_status nat_attn_decode(const nat_kv_cache* cache, const void* d_q, int64_t q_stride, int32_t n_seqs, int32_t n_q_heads,
+                           const int32_t* d_block_table, int32_t table_width, const int32_t* d_seq_lens, float scale,
+                           void* d_out, int64_t out_stride, float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Draw the next token of every row from its logits (Sec. 2: the rollouts o_i ~ pi_theta_old).
+ * Token v of a row has the whole-number weight a_v = round(2^40 * 2^y), y = (z_v - max z) * (log2(e) / temperature) in fp32.
+ * In order of falling logits, equal ones by index:
+ *     top_k     the first top_k stay (<= 0: all);
+ *     top_p     of these, the first ones up to the one with which their weight reaches
+ *               max(1, (floor(top_p * 2^32) * total weight) >> 32)  (>= 1: all; <= 0: the first);
+ *     min_p     of these, those with a_v >= ceil(min_p * 2^40), i.e. at least min_p of the likeliest one's probability
+ *               (<= 0: all; above 1 it counts as 1).
+ * The drawn token is the first, in order of index, at which the running sum of the weights that stay exceeds
+ * (random * their sum) >> 32.  Everything in whole numbers: the draw does not depend on the order of any sum.
+ * temperature <= 0 (or NaN) draws the first of the largest logits.  NaN logits count as -inf, which is never drawn; a row
+ * without any other logit gets token -1 and NaN log-probabilities.
+ *   d_logits [n_rows, V] f32 or bf16, row_stride elements from row to row (0: V; any alignment of rows);
+ *   d_random [n_rows] uint32: uniform words (e.g. of Philox4x32-10);
+ *   d_temperature, d_top_p, d_min_p [n_rows] float, d_top_k [n_rows] int32: each may be NULL (1, 1, 0, 0);
+ *   d_ids [n_rows] int32 out;
+ *   d_logp [n_rows] float out or NULL: log soft-max of the logits at the token (temperature 1, whole vocabulary): the
+ *                behaviour log-prob that nat_loss_fwd_bwd takes as d_old_logp;
+ *   d_logq [n_rows] float out or NULL: log of the probability with which the token was drawn.
+ * Errors: NULL required pointer, n_rows < 0, logits not aligned to their element -> NAT_INVALID_ARG; V outside [1, 2^20],
+ * 0 < row_stride < V -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE.
+ */
+nat_status nat_sample(const void* d_logits, int64_t row_stride, int32_t n_rows, int32_t V, int32_t dtype,
+                      const uint32_t* d_random, const float* d_temperature, const int32_t* d_top_k, const float* d_top_p,
+                      const float* d_min_p, int32_t* d_ids, float* d_logp, float* d_logq, void* stream);
 
 /*
  * Per-kernel timing (measurement aid, off by default).  When enabled, every

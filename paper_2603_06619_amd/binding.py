@@ -11,6 +11,7 @@ _lib = None
 FULL, URS, RPC, DET = 0, 1, 2, 3
 DTYPE_F32, DTYPE_BF16 = 0, 1
 KL_LOG_RATIO, KL_NONNEG = 0, 1
+KV_BF16, KV_FP8 = 0, 1
 DIAG_BAD_ID, DIAG_SHIFT_RANGE, DIAG_CLIPPED, DIAG_NONZERO_ADV, DIAG_WORDS = 0, 1, 2, 3, 4
 
 
@@ -25,6 +26,18 @@ class _CSelectParams(ctypes.Structure):
                 ("trunc_frac", ctypes.c_double), ("seed", ctypes.c_uint64), ("step", ctypes.c_uint32),
                 ("rollout_id_base", ctypes.c_int32), ("d_scheme_per_rollout", ctypes.c_void_p),
                 ("d_drop_zero_adv", ctypes.c_void_p)]
+
+
+class _CAttnParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seqs", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "causal")] + \
+               [("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("n_q", "n_k", "q_stride", "k_stride", "v_stride", "out_stride", "dout_stride",
+                                              "dq_stride", "dk_stride", "dv_stride")]
+
+
+class _CKvCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("d_k", "d_v", "d_k_exp", "d_v_exp")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "n_kv_heads", "page_size", "head_dim", "format")]
 
 
 class SelectParams:
@@ -103,6 +116,23 @@ def load_library():
         getattr(lib, name).argtypes = [i32, i32, i32, i32]
     lib.nat_logp_fwd.restype = i32
     lib.nat_logp_fwd.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    pa, pc = ctypes.POINTER(_CAttnParams), ctypes.POINTER(_CKvCache)
+    lib.nat_attn_fwd.restype = i32
+    lib.nat_attn_fwd.argtypes = [pa, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.nat_attn_bwd_workspace_bytes.restype = sz
+    lib.nat_attn_bwd_workspace_bytes.argtypes = [i64, i32]
+    lib.nat_attn_bwd.restype = i32
+    lib.nat_attn_bwd.argtypes = [pa, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.nat_kv_write.restype = i32
+    lib.nat_kv_write.argtypes = [pc, vp, i64, vp, i64, vp, i64, vp]
+    lib.nat_kv_read.restype = i32
+    lib.nat_kv_read.argtypes = [pc, vp, i32, vp, i32, i64, vp, i64, vp, i64, vp]
+    lib.nat_attn_decode_workspace_bytes.restype = sz
+    lib.nat_attn_decode_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
+    lib.nat_attn_decode.restype = i32
+    lib.nat_attn_decode.argtypes = [pc, vp, i64, i32, i32, vp, i32, vp, f32, vp, i64, vp, vp, sz, vp]
+    lib.nat_sample.restype = i32
+    lib.nat_sample.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.nat_probe_mfma_scratch_bytes.restype = sz
     lib.nat_probe_mfma_scratch_bytes.argtypes = []
     lib.nat_probe_mfma_bf16.restype = i32
@@ -299,6 +329,143 @@ def nat_logp_fwd(hidden_k, W, ids_k, N_k, logp_out, entropy_out, workspace, diag
         _ptr(hidden_k), _ptr(W), _ptr(ids_k), N_k, H, V, _dtype_code(W), _ptr(logp_out), _ptr(entropy_out),
         _ptr(diag_out), _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()),
         "nat_logp_fwd")
+
+
+def _rows(t, name, shape=None, dtype=torch.bfloat16):
+    """A [rows, heads, head_dim] tensor whose heads lie back to back; returns its row stride.  What the kernels need and the
+    library cannot see (device, element type, extents) is checked here."""
+    if t.dtype != dtype or t.dim() != 3 or not t.is_cuda:
+        raise TypeError(f"{name}: expected a {dtype} device tensor [rows, heads, head_dim]")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    row, head, one = t.stride()
+    n, heads, dim = t.shape
+    if n == 0 or heads == 0 or dim == 0:
+        return 0
+    if (dim > 1 and one != 1) or (heads > 1 and head != dim):
+        raise ValueError(f"{name}: the heads of a row must lie back to back")
+    return row if n > 1 else 0
+
+
+def _vector(t, dtype, n, name):
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_cuda or t.numel() != n or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous {dtype} device tensor of {n} elements")
+    return t.data_ptr()
+
+
+def _attn_params(q, k, v, cu_q, cu_k, causal, scale):
+    n_q, hq, dim = q.shape
+    n_k, hkv, _ = k.shape
+    n_seqs = max(cu_q.numel() - 1, 0)
+    _vector(cu_q, torch.int32, n_seqs + 1, "cu_q")
+    _vector(cu_k, torch.int32, n_seqs + 1, "cu_k")
+    p = _CAttnParams(n_seqs, hq, hkv, dim, DTYPE_BF16, int(causal), float(scale), n_q, n_k, _rows(q, "q"), _rows(k, "k", (n_k, hkv, dim)),
+                     _rows(v, "v", (n_k, hkv, dim)))
+    return p
+
+
+def nat_attn_fwd(q, k, v, cu_q, cu_k, causal, scale, out, lse):
+    """q [n_q, q heads, D], k, v [n_k, kv heads, D] bf16 (any row stride); cu_q, cu_k int32 [n_seqs + 1]; out like q, lse float32
+    [q heads, n_q]."""
+    p = _attn_params(q, k, v, cu_q, cu_k, causal, scale)
+    p.out_stride = _rows(out, "out", q.shape)
+    _raise(load_library().nat_attn_fwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k), _ptr(out),
+                                       _vector(lse, torch.float32, p.n_q_heads * p.n_q, "lse"), _stream()), "nat_attn_fwd")
+
+
+def attn_bwd_workspace_bytes(n_q, n_q_heads):
+    return int(load_library().nat_attn_bwd_workspace_bytes(int(n_q), int(n_q_heads)))
+
+
+def nat_attn_bwd(q, k, v, out, lse, dout, cu_q, cu_k, causal, scale, dq, dk, dv, workspace):
+    """The gradients of nat_attn_fwd; dq like q, dk and dv like k (any row stride)."""
+    p = _attn_params(q, k, v, cu_q, cu_k, causal, scale)
+    p.out_stride, p.dout_stride = _rows(out, "out", q.shape), _rows(dout, "dout", q.shape)
+    p.dq_stride, p.dk_stride, p.dv_stride = _rows(dq, "dq", q.shape), _rows(dk, "dk", k.shape), _rows(dv, "dv", k.shape)
+    _raise(load_library().nat_attn_bwd(
+        ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _vector(lse, torch.float32, p.n_q_heads * p.n_q, "lse"), _ptr(dout),
+        _ptr(cu_q), _ptr(cu_k), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
+        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_attn_bwd")
+
+
+class KvCache:
+    """The arrays of a paged cache: k, v [n_pages, kv heads, page_size, D] in bfloat16, or in float8_e4m3fn with the exponents
+    k_exp, v_exp [n_pages, kv heads, page_size] uint8 (see nat_kv_cache in nat.h)."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        fp8 = k.dtype == torch.float8_e4m3fn
+        if k.dim() != 4 or not (fp8 or k.dtype == torch.bfloat16):
+            raise TypeError("k: expected a bfloat16 or float8_e4m3fn tensor [n_pages, heads, page_size, head_dim]")
+        for name, t in (("k", k), ("v", v)):
+            if t.shape != k.shape or t.dtype != k.dtype or not t.is_contiguous() or not t.is_cuda:
+                raise TypeError(f"{name}: expected a contiguous {k.dtype} device tensor {tuple(k.shape)}")
+        if fp8:
+            for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
+                if t is None or t.shape != k.shape[:3] or t.dtype != torch.uint8 or not t.is_contiguous() or not t.is_cuda:
+                    raise TypeError(f"{name}: expected a contiguous uint8 device tensor {tuple(k.shape[:3])}")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        n_pages, heads, page_size, dim = k.shape
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = n_pages, heads, page_size, dim
+        self._c = _CKvCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if fp8 else None, v_exp.data_ptr() if fp8 else None,
+                            n_pages, heads, page_size, dim, KV_FP8 if fp8 else KV_BF16)
+
+
+def nat_kv_write(cache, k, v, slots):
+    """k, v [rows, kv heads, D] bf16; slots int64 [rows], -1 for rows that are skipped."""
+    n = k.shape[0]
+    shape = (n, cache.n_kv_heads, cache.head_dim)
+    _raise(load_library().nat_kv_write(ctypes.byref(cache._c), _ptr(k), _rows(k, "k", shape), _ptr(v), _rows(v, "v", shape),
+                                       _vector(slots, torch.int64, n, "slots"), n, _stream()), "nat_kv_write")
+
+
+def _table(block_table, n_seqs):
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or not block_table.is_contiguous() or not block_table.is_cuda or \
+            block_table.shape[0] != n_seqs:
+        raise TypeError(f"block_table: expected a contiguous int32 device tensor [{n_seqs}, pages]")
+    return block_table.shape[1]
+
+
+def nat_kv_read(cache, block_table, cu_k, k, v):
+    """block_table int32 [n_seqs, pages], cu_k int32 [n_seqs + 1]; k, v [rows, kv heads, D] bf16 out."""
+    n_seqs = max(cu_k.numel() - 1, 0)
+    shape = (k.shape[0], cache.n_kv_heads, cache.head_dim)
+    width = _table(block_table, n_seqs)
+    _raise(load_library().nat_kv_read(ctypes.byref(cache._c), _ptr(block_table), width, _vector(cu_k, torch.int32, n_seqs + 1, "cu_k"), n_seqs,
+                                      k.shape[0], _ptr(k), _rows(k, "k", shape), _ptr(v), _rows(v, "v", shape), _stream()), "nat_kv_read")
+
+
+def attn_decode_workspace_bytes(n_seqs, n_q_heads, n_kv_heads, head_dim, max_tokens):
+    return int(load_library().nat_attn_decode_workspace_bytes(int(n_seqs), int(n_q_heads), int(n_kv_heads), int(head_dim), int(max_tokens)))
+
+
+def nat_attn_decode(cache, q, block_table, seq_lens, scale, out, lse, workspace):
+    """q [n_seqs, q heads, D] bf16, block_table int32 [n_seqs, pages], seq_lens int32 [n_seqs]; out like q, lse float32 [n_seqs, q heads]."""
+    n_seqs, hq, _ = q.shape
+    width = _table(block_table, n_seqs)
+    shape = (n_seqs, hq, cache.head_dim)
+    _raise(load_library().nat_attn_decode(
+        ctypes.byref(cache._c), _ptr(q), _rows(q, "q", shape), n_seqs, hq, _ptr(block_table), width,
+        _vector(seq_lens, torch.int32, n_seqs, "seq_lens"), float(scale), _ptr(out), _rows(out, "out", shape),
+        _vector(lse, torch.float32, n_seqs * hq, "lse"), _ptr(workspace),
+        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_attn_decode")
+
+
+def nat_sample(logits, random, temperature, top_k, top_p, min_p, ids_out, logp_out=None, logq_out=None):
+    """logits [rows, V] float32 or bfloat16 (any row stride), random int32 [rows] (the 32 bits are read as unsigned); temperature,
+    top_p, min_p float32 [rows] and top_k int32 [rows], each or None; ids int32, logp and logq float32 [rows] out."""
+    if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise TypeError("logits: expected a device tensor [rows, vocabulary] with its rows contiguous")
+    n, V = logits.shape
+    if logits.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("logits must be float32 or bfloat16")
+    _raise(load_library().nat_sample(
+        _ptr(logits), logits.stride(0) if n > 1 else 0, n, V, _dtype_code(logits), _vector(random, torch.int32, n, "random"),
+        _vector(temperature, torch.float32, n, "temperature"), _vector(top_k, torch.int32, n, "top_k"),
+        _vector(top_p, torch.float32, n, "top_p"), _vector(min_p, torch.float32, n, "min_p"),
+        _vector(ids_out, torch.int32, n, "ids_out"), _vector(logp_out, torch.float32, n, "logp_out"),
+        _vector(logq_out, torch.float32, n, "logq_out"), _stream()), "nat_sample")
 
 
 def probe_mfma_scratch_bytes():

@@ -1,0 +1,547 @@
+// Attention over packed sequences with grouped heads, forward and backward, bf16 on the matrix cores.
+//
+//   S_ij = scale q_i . k_j,  P_ij = exp(S_ij - lse_i),  lse_i = log sum_j exp(S_ij),  out_i = sum_j P_ij v_j       over the keys j that i sees
+//   dP_ij = dout_i . v_j,  delta_i = dout_i . out_i,  dS_ij = P_ij (dP_ij - delta_i)
+//   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i
+//
+// The G query heads that share a key head are rows of one matrix: row r of a sequence is query r / G, head r % G of the group.
+// A tile of rows then reads its keys once for all heads, covers few queries (so little of the causal mask's edge is computed in vain),
+// and dk, dv of a shared head are plain sums over rows.  Every wavefront owns 32 rows (forward, dq) or 32 keys (dk, dv) as the columns of its
+// products: a lane holds results of one column, so that row maxima and sums stay in the lane but for one exchange of the wavefront's halves, and the
+// probabilities are the next product's operand without leaving the registers (mfma_tile.hip.h).
+// Nothing is added by atomics: results do not change from run to run.
+#include "nat_internal.h"
+#include "mfma_tile.hip.h"
+
+namespace nat {
+namespace {
+
+constexpr float kLog2E = 1.4426950408889634f;
+constexpr int kRowTile = 128;             // rows per workgroup: 4 wavefronts of 32
+constexpr int kKeyTile = 64;              // keys per step of the forward and dq kernels
+constexpr int kDkvKeys = 128;             // keys per workgroup of the dk, dv kernel
+constexpr int kDkvRows = 64;              // rows per step of it
+
+struct AttnArgs {
+  const uint16_t *q, *k, *v;
+  uint16_t* out;
+  float* lse;
+  const int32_t *cu_q, *cu_k;
+  int n_seqs, hq, hkv, group, causal;
+  int64_t n_q, n_k, q_stride, k_stride, v_stride, out_stride;
+  float scale;
+  // backward
+  const uint16_t* dout;
+  float* delta;                  // [hq, n_q]
+  uint16_t *dq, *dk, *dv;
+  int64_t dout_stride, dq_stride, dk_stride, dv_stride;
+  int slots;                     // tile slots per key head
+};
+
+// Offsets come from device memory: clamped to the arrays, and a sequence never has a negative length.
+__device__ __forceinline__ int64_t offset_at(const int32_t* cu, int i, int64_t n) {
+  const int64_t c = cu[i];
+  return c < 0 ? 0 : c < n ? c : n;
+}
+
+// Sequence of a slot.  Sequence b with `mult` rows per packed row owns the slots floor(cu[b] mult / tile) + b up to that of b + 1: at least as many as
+// it has tiles, so a grid of floor(n mult / tile) + n_seqs slots needs no lengths on the host and the search no prefix sums.  The wavefront looks at 64
+// sequences at a time.
+__device__ __forceinline__ int sequence_of_slot(const int32_t* cu, int n_seqs, int64_t n, int mult, int tile, int64_t slot, int64_t* first) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n_seqs;                // the last b in [lo, hi) with first(b) <= slot
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) >> 6, b = lo + lane * step;
+    const bool le = b < hi && offset_at(cu, b, n) * mult / tile + b <= slot;
+    const int below = __popcll(__ballot(le));
+    if (below == 0) break;
+    const int next = lo + (below - 1) * step;
+    hi = next + step < hi ? next + step : hi;
+    lo = next;
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  *first = offset_at(cu, lo, n) * mult / tile + lo;
+  return lo;
+}
+
+struct Sequence {
+  int64_t q0, k0;                // first packed rows
+  int n_q, n_k, ahead;           // lengths; query t sees the keys 0 .. t + ahead, or all
+};
+__device__ __forceinline__ Sequence sequence(const AttnArgs& a, int b) {
+  Sequence s;
+  s.q0 = offset_at(a.cu_q, b, a.n_q);
+  s.k0 = offset_at(a.cu_k, b, a.n_k);
+  const int64_t q1 = offset_at(a.cu_q, b + 1, a.n_q), k1 = offset_at(a.cu_k, b + 1, a.n_k);
+  s.n_q = q1 > s.q0 ? (int)(q1 - s.q0) : 0;
+  s.n_k = k1 > s.k0 ? (int)(k1 - s.k0) : 0;
+  s.ahead = s.n_k - s.n_q;
+  return s;
+}
+// last key that query t sees (below 0: none)
+__device__ __forceinline__ int last_key(const AttnArgs& a, const Sequence& s, int t) {
+  const int l = a.causal ? t + s.ahead : s.n_k - 1;
+  return l < s.n_k ? l : s.n_k - 1;
+}
+
+// Block id -> (key head, slot).  Blocks are dealt to the 8 XCDs in turn: those of one key head go to as few XCDs as possible, whose L2 then
+// holds its keys and values.  Where the number of heads and 8 do not divide each other the heads just alternate.
+__device__ __forceinline__ void head_and_slot(int id, int heads, int slots, int& head, int& slot) {
+  if (heads % 8 == 0) {
+    const int at = id >> 3;
+    head = (id & 7) + 8 * (at / slots);
+    slot = at % slots;
+  } else if (8 % heads == 0) {
+    const int per = 8 / heads;
+    head = (id & 7) % heads;
+    slot = (id >> 3) * per + (id & 7) / heads;       // the grid is a whole number of 8: may pass the end
+  } else {
+    head = id % heads;
+    slot = id / heads;
+  }
+}
+unsigned grid_of(int heads, int64_t slots) {
+  return (unsigned)((heads % 8 != 0 && 8 % heads == 0) ? (slots * heads + 7) / 8 * 8 : slots * heads);
+}
+
+// kRows rows of D elements, staged through registers: fetched one step ahead, written to LDS when the step begins.  Rows at or beyond `end` are zeros,
+// so what lies behind a sequence's end never meets a product.
+template <int D, int kRows>
+struct RowLoader {
+  static constexpr int kLoads = kRows * D / 8 / 256;
+  uint4 x[kLoads];
+  __device__ __forceinline__ void fetch(const uint16_t* base, int64_t stride, int first, int end) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = threadIdx.x + 256 * i, row = first + at / (D / 8);
+      x[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (row < end) x[i] = *(const uint4*)(base + row * stride + at % (D / 8) * 8);
+    }
+  }
+  // rows r of a group's matrix: query r / group, head r % group
+  __device__ __forceinline__ void fetch_grouped(const uint16_t* base, int64_t stride, int group, int first, int end) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = threadIdx.x + 256 * i, row = first + at / (D / 8);
+      x[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (row < end) x[i] = *(const uint4*)(base + (row / group) * stride + row % group * D + at % (D / 8) * 8);
+    }
+  }
+  __device__ __forceinline__ void store(char* tile) const {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = threadIdx.x + 256 * i;
+      *(uint4*)(tile + RowTile<D>::chunk_at(at / (D / 8), at % (D / 8))) = x[i];
+    }
+  }
+};
+
+template <int D>
+struct RowFragments {            // 32 rows as an operand, one row per lane, in registers
+  bf16x8 f[D / 16];
+  __device__ __forceinline__ void load(const uint16_t* row, int lane) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) f[s] = *(const bf16x8*)(row + 16 * s + 8 * (lane >> 5));
+  }
+};
+
+// Columns of a result, 32 elements db of this lane's column n, as bf16 to its row
+template <int D>
+__device__ __forceinline__ void store_columns(uint16_t* row, const f32x16 (&acc)[D / 32], float factor, int lane) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 x = {acc[db][4 * i] * factor, acc[db][4 * i + 1] * factor, acc[db][4 * i + 2] * factor, acc[db][4 * i + 3] * factor};
+      *(bf16x4*)(row + 32 * db + 8 * i + 4 * (lane >> 5)) = __builtin_convertvector(x, bf16x4);
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
+  __shared__ __attribute__((aligned(16))) char tiles[2][2][kKeyTile * D * 2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  int head, slot;
+  head_and_slot(blockIdx.x, a.hkv, a.slots, head, slot);
+  if (slot >= a.slots) return;
+  slot = a.slots - 1 - slot;                 // causal: the last tiles of a sequence have the most keys, and go first
+  int64_t first_slot;
+  const Sequence s = sequence(a, sequence_of_slot(a.cu_q, a.n_seqs, a.n_q, a.group, kRowTile, slot, &first_slot));
+  const int n_rows = s.n_q * a.group, tile_row = (int)(slot - first_slot) * kRowTile;
+  if (slot < first_slot || tile_row >= n_rows) return;
+
+  const int row = tile_row + wave * 32 + (lane & 31), safe_row = row < n_rows ? row : n_rows - 1;
+  const int query = safe_row / a.group, of_group = safe_row - query * a.group;
+  RowFragments<D> q;
+  q.load(a.q + (s.q0 + query) * a.q_stride + (head * a.group + of_group) * D, lane);
+  const int tile_end = tile_row + kRowTile < n_rows ? tile_row + kRowTile : n_rows;
+  const int n_keys = last_key(a, s, (tile_end - 1) / a.group) + 1;      // of the tile
+  const int last = last_key(a, s, query);                              // of this lane's row
+  const int wave_row = tile_row + wave * 32 < n_rows ? tile_row + wave * 32 : n_rows - 1, wave_end = wave_row + 32 < n_rows ? wave_row + 32 : n_rows;
+  const int wave_least = last_key(a, s, wave_row / a.group);           // keys up to here are seen by all rows of the wavefront
+  const int wave_last = last_key(a, s, (wave_end - 1) / a.group);
+  const uint16_t *k = a.k + s.k0 * a.k_stride + head * D, *v = a.v + s.k0 * a.v_stride + head * D;
+
+  const float to_log2 = a.scale * kLog2E;
+  float m = -INFINITY, sum = 0.f;            // running maximum of q.k, sum of this lane's half
+  f32x16 acc[D / 32] = {};
+  RowLoader<D, kKeyTile> kl, vl;
+  kl.fetch(k, a.k_stride, 0, n_keys);
+  vl.fetch(v, a.v_stride, 0, n_keys);
+  for (int key0 = 0, buf = 0; key0 < n_keys; key0 += kKeyTile, buf ^= 1) {
+    char *kt = tiles[buf][0], *vt = tiles[buf][1];
+    kl.store(kt);
+    vl.store(vt);
+    __syncthreads();                         // the other buffer is read before this by all
+    if (key0 + kKeyTile < n_keys) {
+      kl.fetch(k, a.k_stride, key0 + kKeyTile, n_keys);
+      vl.fetch(v, a.v_stride, key0 + kKeyTile, n_keys);
+    }
+    if (key0 > wave_last) continue;
+    f32x16 st[2] = {};
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) st[rb] = mfma32(row_fragment<D>(kt, lane, rb, i), q.f[i], st[rb]);
+    if (key0 + kKeyTile - 1 > wave_least) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (key0 + 32 * rb + result_row(i, half) > last) st[rb][i] = -INFINITY;
+    }
+    float top = m;
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, st[rb][i]);
+    top = max_halves(top);
+    if (__any(top > m)) {
+      const float f = top == -INFINITY ? 1.f : exp2_fast((m - top) * to_log2);
+      sum *= f;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) acc[db] *= f;
+      m = top;
+    }
+    const float shift = m == -INFINITY ? 0.f : m * to_log2;
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        st[rb][i] = exp2_fast(fmaf(st[rb][i], to_log2, -shift));
+        sum += st[rb][i];
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8 p = fragment_of_result(st[rb], h);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(transposed_fragment<D>(vt, lane, db, 2 * rb + h), p, acc[db]);
+      }
+    }
+  }
+  sum = sum_halves(sum);
+  if (row >= n_rows) return;
+  const int64_t at = s.q0 + query;
+  const int qh = head * a.group + of_group;
+  store_columns<D>(a.out + at * a.out_stride + qh * D, acc, sum == 0.f ? 0.f : 1.f / sum, lane);
+  if (half == 0) a.lse[qh * a.n_q + at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, __logf(sum));
+}
+
+// dq, and delta for the dk, dv kernel behind it.
+template <int D>
+__global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
+  __shared__ __attribute__((aligned(16))) char tiles[2][2][kKeyTile * D * 2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  int head, slot;
+  head_and_slot(blockIdx.x, a.hkv, a.slots, head, slot);
+  if (slot >= a.slots) return;
+  slot = a.slots - 1 - slot;
+  int64_t first_slot;
+  const Sequence s = sequence(a, sequence_of_slot(a.cu_q, a.n_seqs, a.n_q, a.group, kRowTile, slot, &first_slot));
+  const int n_rows = s.n_q * a.group, tile_row = (int)(slot - first_slot) * kRowTile;
+  if (slot < first_slot || tile_row >= n_rows) return;
+
+  const int row = tile_row + wave * 32 + (lane & 31), safe_row = row < n_rows ? row : n_rows - 1;
+  const int query = safe_row / a.group, of_group = safe_row - query * a.group;
+  const int64_t at = s.q0 + query;
+  const int qh = head * a.group + of_group;
+  RowFragments<D> q, d;
+  q.load(a.q + at * a.q_stride + qh * D, lane);
+  d.load(a.dout + at * a.dout_stride + qh * D, lane);
+  float delta = 0.f;
+  {
+    RowFragments<D> o;
+    o.load(a.out + at * a.out_stride + qh * D, lane);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf((float)o.f[i][e], (float)d.f[i][e], delta);
+    delta = sum_halves(delta);
+  }
+  if (row < n_rows && half == 0) a.delta[qh * a.n_q + at] = delta;
+  const int tile_end = tile_row + kRowTile < n_rows ? tile_row + kRowTile : n_rows;
+  const int n_keys = last_key(a, s, (tile_end - 1) / a.group) + 1;
+  const int last = last_key(a, s, query);
+  const int wave_row = tile_row + wave * 32 < n_rows ? tile_row + wave * 32 : n_rows - 1, wave_end = wave_row + 32 < n_rows ? wave_row + 32 : n_rows;
+  const int wave_least = last_key(a, s, wave_row / a.group), wave_last = last_key(a, s, (wave_end - 1) / a.group);
+  const uint16_t *k = a.k + s.k0 * a.k_stride + head * D, *v = a.v + s.k0 * a.v_stride + head * D;
+  const float to_log2 = a.scale * kLog2E, lse = a.lse[qh * a.n_q + at], shift = lse == -INFINITY ? INFINITY : lse * kLog2E;
+
+  f32x16 acc[D / 32] = {};
+  RowLoader<D, kKeyTile> kl, vl;
+  kl.fetch(k, a.k_stride, 0, n_keys);
+  vl.fetch(v, a.v_stride, 0, n_keys);
+  for (int key0 = 0, buf = 0; key0 < n_keys; key0 += kKeyTile, buf ^= 1) {
+    char *kt = tiles[buf][0], *vt = tiles[buf][1];
+    kl.store(kt);
+    vl.store(vt);
+    __syncthreads();
+    if (key0 + kKeyTile < n_keys) {
+      kl.fetch(k, a.k_stride, key0 + kKeyTile, n_keys);
+      vl.fetch(v, a.v_stride, key0 + kKeyTile, n_keys);
+    }
+    if (key0 > wave_last) continue;
+    const bool edge = key0 + kKeyTile - 1 > wave_least;
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      f32x16 st = {}, dp = {};
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        st = mfma32(row_fragment<D>(kt, lane, rb, i), q.f[i], st);
+        dp = mfma32(row_fragment<D>(vt, lane, rb, i), d.f[i], dp);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st[i] = exp2_fast(fmaf(st[i], to_log2, -shift)) * (dp[i] - delta);
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (key0 + 32 * rb + result_row(i, half) > last) st[i] = 0.f;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8 p = fragment_of_result(st, h);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(transposed_fragment<D>(kt, lane, db, 2 * rb + h), p, acc[db]);
+      }
+    }
+  }
+  if (row < n_rows) store_columns<D>(a.dq + at * a.dq_stride + qh * D, acc, a.scale, lane);
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
+  struct RowWords { float shift[kDkvRows], delta[kDkvRows]; int last[kDkvRows]; };
+  __shared__ __attribute__((aligned(16))) char tiles[2][2][kDkvRows * D * 2];
+  __shared__ __attribute__((aligned(16))) RowWords words[2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  int head, slot;
+  head_and_slot(blockIdx.x, a.hkv, a.slots, head, slot);
+  if (slot >= a.slots) return;
+  int64_t first_slot;
+  const Sequence s = sequence(a, sequence_of_slot(a.cu_k, a.n_seqs, a.n_k, 1, kDkvKeys, slot, &first_slot));
+  const int tile_key = (int)(slot - first_slot) * kDkvKeys;
+  if (slot < first_slot || tile_key >= s.n_k) return;
+
+  const int key = tile_key + wave * 32 + (lane & 31), safe_key = key < s.n_k ? key : s.n_k - 1;
+  RowFragments<D> k, v;
+  k.load(a.k + (s.k0 + safe_key) * a.k_stride + head * D, lane);
+  v.load(a.v + (s.k0 + safe_key) * a.v_stride + head * D, lane);
+  const int n_rows = s.n_q * a.group, wave_key = tile_key + wave * 32;
+  // the first row that sees the tile's first key
+  const int first_query = a.causal && tile_key > s.ahead ? tile_key - s.ahead : 0;
+  const int first_row = first_query < s.n_q ? first_query * a.group : n_rows;
+  const int wave_first = a.causal ? wave_key - s.ahead : 0;            // the first query that sees the wavefront's first key
+  const int wave_all = a.causal ? wave_key + 31 - s.ahead : 0;         // queries from here on see all its keys
+  const uint16_t *q = a.q + s.q0 * a.q_stride + head * a.group * D, *d = a.dout + s.q0 * a.dout_stride + head * a.group * D;
+  const float *lse = a.lse + (int64_t)head * a.group * a.n_q + s.q0, *delta = a.delta + (int64_t)head * a.group * a.n_q + s.q0;
+  const float to_log2 = a.scale * kLog2E;
+
+  f32x16 dk[D / 32] = {}, dv[D / 32] = {};
+  RowLoader<D, kDkvRows> ql, dl;
+  float row_shift = INFINITY, row_delta = 0.f;
+  int row_last = -1;
+  auto fetch = [&](int row0) {
+    ql.fetch_grouped(q, a.q_stride, a.group, row0, n_rows);
+    dl.fetch_grouped(d, a.dout_stride, a.group, row0, n_rows);
+    if (threadIdx.x < kDkvRows) {
+      const int r = row0 + threadIdx.x, t = r / a.group;
+      row_shift = INFINITY;                  // probability 0: rows past the end, and rows that see no key
+      row_delta = 0.f;
+      row_last = -1;
+      if (r < n_rows) {
+        const int64_t at = (r - t * a.group) * a.n_q + t;
+        const float l = lse[at];
+        row_shift = l == -INFINITY ? INFINITY : l * kLog2E;
+        row_delta = delta[at];
+        row_last = last_key(a, s, t);
+      }
+    }
+  };
+  fetch(first_row);
+  for (int row0 = first_row, buf = 0; row0 < n_rows; row0 += kDkvRows, buf ^= 1) {
+    char *qt = tiles[buf][0], *dt = tiles[buf][1];
+    RowWords& w = words[buf];
+    ql.store(qt);
+    dl.store(dt);
+    if (threadIdx.x < kDkvRows) {
+      w.shift[threadIdx.x] = row_shift;
+      w.delta[threadIdx.x] = row_delta;
+      w.last[threadIdx.x] = row_last;
+    }
+    __syncthreads();
+    if (row0 + kDkvRows < n_rows) fetch(row0 + kDkvRows);
+    if ((row0 + kDkvRows - 1) / a.group < wave_first) continue;
+    const bool edge = row0 / a.group < wave_all;
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      f32x16 p = {}, dp = {};
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        p = mfma32(row_fragment<D>(qt, lane, rb, i), k.f[i], p);
+        dp = mfma32(row_fragment<D>(dt, lane, rb, i), v.f[i], dp);
+      }
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const f32x4 shift = *(const f32x4*)(w.shift + 32 * rb + 8 * i4 + 4 * half), del = *(const f32x4*)(w.delta + 32 * rb + 8 * i4 + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * i4 + e;
+          p[i] = exp2_fast(fmaf(p[i], to_log2, -shift[e]));
+          dp[i] = p[i] * (dp[i] - del[e]);
+        }
+      }
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (key > w.last[32 * rb + result_row(i, half)]) p[i] = dp[i] = 0.f;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8 pf = fragment_of_result(p, h), df = fragment_of_result(dp, h);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+          dv[db] = mfma32(transposed_fragment<D>(dt, lane, db, 2 * rb + h), pf, dv[db]);
+          dk[db] = mfma32(transposed_fragment<D>(qt, lane, db, 2 * rb + h), df, dk[db]);
+        }
+      }
+    }
+  }
+  if (key >= s.n_k) return;
+  store_columns<D>(a.dk + (s.k0 + key) * a.dk_stride + head * D, dk, a.scale, lane);
+  store_columns<D>(a.dv + (s.k0 + key) * a.dv_stride + head * D, dv, 1.f, lane);
+}
+
+bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
+
+// Checks of what forward and backward share; fills `a`.
+nat_status attn_args(const nat_attn_params* p, const void* d_q, const void* d_k, const void* d_v, const int32_t* d_cu_q, const int32_t* d_cu_k,
+                     AttnArgs* a) {
+  if (!p) return NAT_INVALID_ARG;
+  if (p->dtype != NAT_DTYPE_BF16) return NAT_UNSUPPORTED_DTYPE;
+  if (p->n_seqs < 0 || p->n_q < 0 || p->n_k < 0 || p->n_q > INT32_MAX || p->n_k > INT32_MAX) return NAT_INVALID_ARG;
+  if (!(p->scale > 0.f) || !(p->scale < INFINITY)) return NAT_INVALID_ARG;
+  if (p->causal != 0 && p->causal != 1) return NAT_INVALID_ARG;
+  if ((p->head_dim != 64 && p->head_dim != 128) || p->n_kv_heads <= 0 || p->n_q_heads <= 0 || p->n_q_heads % p->n_kv_heads != 0 ||
+      p->n_q_heads > 4096)
+    return NAT_BAD_SHAPE;
+  const int64_t q_row = (int64_t)p->n_q_heads * p->head_dim, k_row = (int64_t)p->n_kv_heads * p->head_dim;
+  const int group = p->n_q_heads / p->n_kv_heads;
+  // rows of a group's matrix and tile slots are counted in 32 bits
+  if (p->n_q * group > INT32_MAX / 2 || (p->n_q * group / kRowTile + p->n_seqs) * p->n_kv_heads > INT32_MAX / 2 ||
+      (p->n_k / kDkvKeys + p->n_seqs) * p->n_kv_heads > INT32_MAX / 2)
+    return NAT_BAD_SHAPE;
+  auto stride_ok = [](int64_t s, int64_t row) { return s == 0 || (s >= row && s % 8 == 0 && s <= INT32_MAX); };
+  if (!stride_ok(p->q_stride, q_row) || !stride_ok(p->out_stride, q_row) || !stride_ok(p->dout_stride, q_row) || !stride_ok(p->dq_stride, q_row) ||
+      !stride_ok(p->k_stride, k_row) || !stride_ok(p->v_stride, k_row) || !stride_ok(p->dk_stride, k_row) || !stride_ok(p->dv_stride, k_row))
+    return NAT_BAD_SHAPE;
+  *a = AttnArgs{};
+  a->n_seqs = p->n_seqs;
+  if (p->n_seqs == 0) return NAT_OK;
+  if (!d_cu_q || !d_cu_k || (p->n_q > 0 && !d_q) || (p->n_k > 0 && (!d_k || !d_v))) return NAT_INVALID_ARG;
+  if (misaligned(d_q) || misaligned(d_k) || misaligned(d_v)) return NAT_INVALID_ARG;
+  auto or_row = [](int64_t s, int64_t row) { return s ? s : row; };
+  a->q = (const uint16_t*)d_q;
+  a->k = (const uint16_t*)d_k;
+  a->v = (const uint16_t*)d_v;
+  a->cu_q = d_cu_q;
+  a->cu_k = d_cu_k;
+  a->hq = p->n_q_heads;
+  a->hkv = p->n_kv_heads;
+  a->group = group;
+  a->causal = p->causal;
+  a->n_q = p->n_q;
+  a->n_k = p->n_k;
+  a->scale = p->scale;
+  a->q_stride = or_row(p->q_stride, q_row);
+  a->out_stride = or_row(p->out_stride, q_row);
+  a->dout_stride = or_row(p->dout_stride, q_row);
+  a->dq_stride = or_row(p->dq_stride, q_row);
+  a->k_stride = or_row(p->k_stride, k_row);
+  a->v_stride = or_row(p->v_stride, k_row);
+  a->dk_stride = or_row(p->dk_stride, k_row);
+  a->dv_stride = or_row(p->dv_stride, k_row);
+  return NAT_OK;
+}
+
+}  // namespace
+}  // namespace nat
+
+using namespace nat;
+
+extern "C" nat_status nat_attn_fwd(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v, const int32_t* d_cu_q,
+                                   const int32_t* d_cu_k, void* d_out, float* d_lse, void* stream) {
+  AttnArgs a;
+  const nat_status st = attn_args(params, d_q, d_k, d_v, d_cu_q, d_cu_k, &a);
+  if (st != NAT_OK || a.n_seqs == 0 || a.n_q == 0) return st;
+  if (!d_out || !d_lse || misaligned(d_out)) return NAT_INVALID_ARG;
+  a.out = (uint16_t*)d_out;
+  a.lse = d_lse;
+  a.slots = (int)(a.n_q * a.group / kRowTile + a.n_seqs);
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope prof(PC_ATTN_FWD, s);
+  if (params->head_dim == 128) attn_fwd_kernel<128><<<grid_of(a.hkv, a.slots), 256, 0, s>>>(a);
+  else attn_fwd_kernel<64><<<grid_of(a.hkv, a.slots), 256, 0, s>>>(a);
+  NAT_LAUNCH_CHECK();
+  return NAT_OK;
+}
+
+extern "C" size_t nat_attn_bwd_workspace_bytes(int64_t n_q, int32_t n_q_heads) {
+  if (n_q <= 0 || n_q_heads <= 0 || n_q > INT32_MAX || n_q_heads > 4096) return 0;
+  return ((size_t)n_q * (size_t)n_q_heads * 4 + 255) / 256 * 256;
+}
+
+extern "C" nat_status nat_attn_bwd(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v, const void* d_out,
+                                   const float* d_lse, const void* d_dout, const int32_t* d_cu_q, const int32_t* d_cu_k, void* d_dq, void* d_dk,
+                                   void* d_dv, void* d_ws, size_t ws_bytes, void* stream) {
+  AttnArgs a;
+  const nat_status st = attn_args(params, d_q, d_k, d_v, d_cu_q, d_cu_k, &a);
+  if (st != NAT_OK || a.n_seqs == 0) return st;
+  if (a.n_q > 0 && (!d_out || !d_lse || !d_dout || !d_dq)) return NAT_INVALID_ARG;
+  if (a.n_k > 0 && (!d_dk || !d_dv)) return NAT_INVALID_ARG;
+  if (misaligned(d_out) || misaligned(d_dout) || misaligned(d_dq) || misaligned(d_dk) || misaligned(d_dv)) return NAT_INVALID_ARG;
+  if (a.n_q > 0 && (!d_ws || ws_bytes < nat_attn_bwd_workspace_bytes(a.n_q, a.hq))) return NAT_WORKSPACE_TOO_SMALL;
+  if ((uintptr_t)d_ws & 255) return NAT_INVALID_ARG;
+  a.out = (uint16_t*)const_cast<void*>(d_out);
+  a.lse = const_cast<float*>(d_lse);
+  a.dout = (const uint16_t*)d_dout;
+  a.delta = (float*)d_ws;
+  a.dq = (uint16_t*)d_dq;
+  a.dk = (uint16_t*)d_dk;
+  a.dv = (uint16_t*)d_dv;
+  hipStream_t s = (hipStream_t)stream;
+  if (a.n_q > 0) {
+    ProfScope prof(PC_ATTN_BWD, s);
+    a.slots = (int)(a.n_q * a.group / kRowTile + a.n_seqs);
+    if (params->head_dim == 128) attn_dq_kernel<128><<<grid_of(a.hkv, a.slots), 256, 0, s>>>(a);
+    else attn_dq_kernel<64><<<grid_of(a.hkv, a.slots), 256, 0, s>>>(a);
+    NAT_LAUNCH_CHECK();
+  }
+  if (a.n_k > 0) {
+    ProfScope prof(PC_ATTN_BWD, s);
+    a.slots = (int)(a.n_k / kDkvKeys + a.n_seqs);
+    if (params->head_dim == 128) attn_dkv_kernel<128><<<grid_of(a.hkv, a.slots), 256, 0, s>>>(a);
+    else attn_dkv_kernel<64><<<grid_of(a.hkv, a.slots), 256, 0, s>>>(a);
+    NAT_LAUNCH_CHECK();
+  }
+  return NAT_OK;
+}
