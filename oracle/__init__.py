@@ -16,6 +16,9 @@ Modules
   grpo     group-relative advantage (Eq. 2), ratio (Eq. 1), clipped surrogate
            (Eq. 3), sequence-mean objective (Eq. 5) and its gradient w.r.t.
            hidden states and the LM-head matrix (App. A)
+  attention  attention over packed sequences, its gradients, attention of one token over a paged cache
+  kv_cache   the 8-bit format of cached rows
+  sampling   temperature, top-k, top-p, min-p and the draw, in whole numbers
   drivers  exhaustive-enumeration and Monte-Carlo expectations of the masked
            estimator (Prop. 1), and the closed-form variances (App. B)
 

@@ -19,6 +19,7 @@ namespace {
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr int kRowTile = 128;             // rows per workgroup: 4 wavefronts of 32
 constexpr int kKeyTile = 64;              // keys per step of the forward and dq kernels
+constexpr int kFewKeys = 64;             // see attn_dq_kernel
 constexpr int kDkvKeys = 128;             // keys per workgroup of the dk, dv kernel
 constexpr int kDkvRows = 64;              // rows per step of it
 
@@ -134,7 +135,51 @@ struct RowLoader {
       *(uint4*)(tile + RowTile<D>::chunk_at(at / (D / 8), at % (D / 8))) = x[i];
     }
   }
+  // an element of this thread's is infinite or NaN
+  __device__ __forceinline__ bool not_finite() const {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+    }
+    return any;
+  }
 };
+
+// The workgroup's barrier; at the mask's edge it tells whether any of the rows on the way to LDS holds what is not finite.
+template <class... Loaders>
+__device__ __forceinline__ bool wait_at_edge(bool edge, const Loaders&... l) {
+  if (edge) return __syncthreads_or((l.not_finite() || ...));
+  __syncthreads();
+  return false;
+}
+
+// Where a mask cuts through a tile, a product multiplies masked rows by 0, and infinities or NaN in them would come through.  Such a tile (looked for
+// only at the mask's edge, where the workgroup agrees on it at its barrier) gets zeros in their places before it enters the product, and the columns that see
+// them have them added by hand.
+template <int D, int kRows, class Sees>
+__device__ __forceinline__ void take_out_not_finite(char* tile, f32x16 (&acc)[D / 32], int half, const Sees& sees) {
+  for (int row = 0; row < kRows; ++row) {
+    if (!sees(row)) continue;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint16_t* x = (const uint16_t*)(tile + RowTile<D>::chunk_at(row, 4 * db + i) + 8 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if ((x[e] & 0x7f80) == 0x7f80) acc[db][4 * i + e] += __builtin_bit_cast(float, (uint32_t)x[e] << 16);
+      }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kRows * D; i += 256) {
+    uint16_t* x = (uint16_t*)tile + i;
+    if ((*x & 0x7f80) == 0x7f80) *x = 0;
+  }
+  __syncthreads();
+}
 
 template <int D>
 struct RowFragments {            // 32 rows as an operand, one row per lane, in registers
@@ -176,6 +221,7 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   q.load(a.q + (s.q0 + query) * a.q_stride + (head * a.group + of_group) * D, lane);
   const int tile_end = tile_row + kRowTile < n_rows ? tile_row + kRowTile : n_rows;
   const int n_keys = last_key(a, s, (tile_end - 1) / a.group) + 1;      // of the tile
+  const int tile_least = last_key(a, s, tile_row / a.group);           // seen by all rows of the tile
   const int last = last_key(a, s, query);                              // of this lane's row
   const int wave_row = tile_row + wave * 32 < n_rows ? tile_row + wave * 32 : n_rows - 1, wave_end = wave_row + 32 < n_rows ? wave_row + 32 : n_rows;
   const int wave_least = last_key(a, s, wave_row / a.group);           // keys up to here are seen by all rows of the wavefront
@@ -192,7 +238,9 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
     char *kt = tiles[buf][0], *vt = tiles[buf][1];
     kl.store(kt);
     vl.store(vt);
-    __syncthreads();                         // the other buffer is read before this by all
+    // the barrier: the other buffer is read before this by all
+    if (__builtin_expect(wait_at_edge(key0 + kKeyTile - 1 > tile_least, vl), 0))
+      take_out_not_finite<D, kKeyTile>(vt, acc, half, [&](int i) { return key0 + i <= last; });
     if (key0 + kKeyTile < n_keys) {
       kl.fetch(k, a.k_stride, key0 + kKeyTile, n_keys);
       vl.fetch(v, a.v_stride, key0 + kKeyTile, n_keys);
@@ -247,7 +295,9 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   if (half == 0) a.lse[qh * a.n_q + at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, __logf(sum));
 }
 
-// dq, and delta for the dk, dv kernel behind it.
+// dq, and delta for the dk, dv kernel behind it.  delta = dout . out takes `out` as it was rounded, which for rows of few keys is an error that dq does not
+// average out (of the 2-norm about 1.7e-3 / sqrt(keys), where the rounding of dS is 1.7e-3; a single such row a few per cent).  Tiles with a row of fewer than
+// kFewKeys keys go over their keys once more for it: delta = sum_j P_ij dP_ij.
 template <int D>
 __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) char tiles[2][2][kKeyTile * D * 2];
@@ -278,9 +328,8 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
       for (int e = 0; e < 8; ++e) delta = fmaf((float)o.f[i][e], (float)d.f[i][e], delta);
     delta = sum_halves(delta);
   }
-  if (row < n_rows && half == 0) a.delta[qh * a.n_q + at] = delta;
   const int tile_end = tile_row + kRowTile < n_rows ? tile_row + kRowTile : n_rows;
-  const int n_keys = last_key(a, s, (tile_end - 1) / a.group) + 1;
+  const int n_keys = last_key(a, s, (tile_end - 1) / a.group) + 1, tile_least = last_key(a, s, tile_row / a.group);
   const int last = last_key(a, s, query);
   const int wave_row = tile_row + wave * 32 < n_rows ? tile_row + wave * 32 : n_rows - 1, wave_end = wave_row + 32 < n_rows ? wave_row + 32 : n_rows;
   const int wave_least = last_key(a, s, wave_row / a.group), wave_last = last_key(a, s, (wave_end - 1) / a.group);
@@ -289,43 +338,65 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
 
   f32x16 acc[D / 32] = {};
   RowLoader<D, kKeyTile> kl, vl;
-  kl.fetch(k, a.k_stride, 0, n_keys);
-  vl.fetch(v, a.v_stride, 0, n_keys);
-  for (int key0 = 0, buf = 0; key0 < n_keys; key0 += kKeyTile, buf ^= 1) {
-    char *kt = tiles[buf][0], *vt = tiles[buf][1];
-    kl.store(kt);
-    vl.store(vt);
-    __syncthreads();
-    if (key0 + kKeyTile < n_keys) {
-      kl.fetch(k, a.k_stride, key0 + kKeyTile, n_keys);
-      vl.fetch(v, a.v_stride, key0 + kKeyTile, n_keys);
+  const bool two_passes = tile_least < kFewKeys - 1;
+  float p_sum = 0.f, p_dp = 0.f;
+  for (int pass = two_passes ? 0 : 1; pass < 2; ++pass) {
+    kl.fetch(k, a.k_stride, 0, n_keys);
+    vl.fetch(v, a.v_stride, 0, n_keys);
+    for (int key0 = 0, buf = 0; key0 < n_keys; key0 += kKeyTile, buf ^= 1) {
+      char *kt = tiles[buf][0], *vt = tiles[buf][1];
+      kl.store(kt);
+      vl.store(vt);
+      if (__builtin_expect(wait_at_edge(key0 + kKeyTile - 1 > tile_least, kl), 0))
+        take_out_not_finite<D, kKeyTile>(kt, acc, half, [&](int i) { return key0 + i <= last; });
+      if (key0 + kKeyTile < n_keys) {
+        kl.fetch(k, a.k_stride, key0 + kKeyTile, n_keys);
+        vl.fetch(v, a.v_stride, key0 + kKeyTile, n_keys);
+      }
+      if (key0 > wave_last) continue;
+      const bool edge = key0 + kKeyTile - 1 > wave_least;
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        f32x16 st = {}, dp = {};
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          st = mfma32(row_fragment<D>(kt, lane, rb, i), q.f[i], st);
+          dp = mfma32(row_fragment<D>(vt, lane, rb, i), d.f[i], dp);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[i] = exp2_fast(fmaf(st[i], to_log2, -shift));
+        if (edge) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (key0 + 32 * rb + result_row(i, half) > last) st[i] = dp[i] = 0.f;
+        }
+        if (pass == 0) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            p_sum += st[i];
+            p_dp = fmaf(st[i], dp[i], p_dp);
+          }
+          continue;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[i] *= dp[i] - delta;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bf16x8 p = fragment_of_result(st, h);
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(transposed_fragment<D>(kt, lane, db, 2 * rb + h), p, acc[db]);
+        }
+      }
     }
-    if (key0 > wave_last) continue;
-    const bool edge = key0 + kKeyTile - 1 > wave_least;
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-      f32x16 st = {}, dp = {};
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        st = mfma32(row_fragment<D>(kt, lane, rb, i), q.f[i], st);
-        dp = mfma32(row_fragment<D>(vt, lane, rb, i), d.f[i], dp);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) st[i] = exp2_fast(fmaf(st[i], to_log2, -shift)) * (dp[i] - delta);
-      if (edge) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (key0 + 32 * rb + result_row(i, half) > last) st[i] = 0.f;
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bf16x8 p = fragment_of_result(st, h);
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(transposed_fragment<D>(kt, lane, db, 2 * rb + h), p, acc[db]);
-      }
+    if (pass == 0) {
+      p_sum = sum_halves(p_sum);
+      delta = p_sum > 0.f ? sum_halves(p_dp) / p_sum : 0.f;
+      __syncthreads();                       // the first tile is overwritten next
     }
   }
-  if (row < n_rows) store_columns<D>(a.dq + at * a.dq_stride + qh * D, acc, a.scale, lane);
+  if (row >= n_rows) return;
+  if (half == 0) a.delta[qh * a.n_q + at] = delta;
+  store_columns<D>(a.dq + at * a.dq_stride + qh * D, acc, a.scale, lane);
 }
 
 template <int D>
@@ -351,6 +422,7 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
   const int first_query = a.causal && tile_key > s.ahead ? tile_key - s.ahead : 0;
   const int first_row = first_query < s.n_q ? first_query * a.group : n_rows;
   const int wave_first = a.causal ? wave_key - s.ahead : 0;            // the first query that sees the wavefront's first key
+  const int tile_all = a.causal ? tile_key + kDkvKeys - 1 - s.ahead : 0;
   const int wave_all = a.causal ? wave_key + 31 - s.ahead : 0;         // queries from here on see all its keys
   const uint16_t *q = a.q + s.q0 * a.q_stride + head * a.group * D, *d = a.dout + s.q0 * a.dout_stride + head * a.group * D;
   const float *lse = a.lse + (int64_t)head * a.group * a.n_q + s.q0, *delta = a.delta + (int64_t)head * a.group * a.n_q + s.q0;
@@ -388,7 +460,11 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
       w.delta[threadIdx.x] = row_delta;
       w.last[threadIdx.x] = row_last;
     }
-    __syncthreads();
+    const bool tile_edge = row0 / a.group < tile_all;
+    if (__builtin_expect(wait_at_edge(tile_edge, ql, dl), 0)) {
+      take_out_not_finite<D, kDkvRows>(qt, dk, half, [&](int i) { return key <= w.last[i]; });
+      take_out_not_finite<D, kDkvRows>(dt, dv, half, [&](int i) { return key <= w.last[i]; });
+    }
     if (row0 + kDkvRows < n_rows) fetch(row0 + kDkvRows);
     if ((row0 + kDkvRows - 1) / a.group < wave_first) continue;
     const bool edge = row0 / a.group < wave_all;

@@ -1,0 +1,285 @@
+"""nat_kv_write / nat_kv_read bit for bit against the oracle, nat_attn_decode within the limits of bf16 probabilities and results
+(oracle/attention.py)."""
+import numpy as np
+import pytest
+import torch
+
+from nat_testlib import DEV
+from oracle import attention as oattn
+from oracle import kv_cache as okv
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def stage():
+    from paper_2603_06619_amd.rollout import RolloutStage
+    return RolloutStage(DEV)
+
+
+def new_cache(n_pages, heads, page, D, fp8, fill=None):
+    from paper_2603_06619_amd.rollout import PagedCache
+    c = PagedCache.empty(n_pages, heads, page, D, fp8, DEV)
+    for x in (c.k, c.v, c.k_exp, c.v_exp):
+        if x is not None and fill is not None:
+            x.view(torch.uint8).fill_(fill)
+    return c
+
+
+def values(cache, name):
+    """float64 values of a whole cache."""
+    x, e = getattr(cache, name), getattr(cache, name + "_exp")
+    if e is None:
+        return x.double().cpu().numpy()
+    return okv.row_values(x.view(torch.uint8).cpu().numpy(), e.cpu().numpy())
+
+
+def rows(seed, n, heads, D, pad=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn((n, heads * D + pad), generator=g, device=DEV) * torch.exp(4 * torch.randn((n, 1), generator=g, device=DEV))
+    return x.bfloat16()[:, :heads * D].unflatten(1, (heads, D))
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("heads,D,page,n", [(1, 64, 16, 1), (2, 128, 16, 50), (3, 64, 32, 333), (8, 128, 64, 1000), (5, 128, 256, 700)])
+def test_write_bit_for_bit(stage, fp8, heads, D, page, n):
+    n_pages = 2 * n // page + 3
+    cache = new_cache(n_pages, heads, page, D, fp8, fill=0x2a)
+    k, v = rows(1, n, heads, D), rows(2, n, heads, D, pad=16)
+    rng = np.random.default_rng(3)
+    slots = rng.permutation(n_pages * page)[:n].astype(np.int64)
+    if n > 4:
+        slots[[1, n // 2]] = -1                                 # rows of padding
+        slots[2] = n_pages * page                               # outside the cache
+        slots[3] = 2 ** 40
+    before = {x: getattr(cache, x).view(torch.uint8).cpu().numpy().copy() for x in (("k", "v", "k_exp", "v_exp") if fp8 else ("k", "v"))}
+    stage.write_cache(cache, k, v, torch.from_numpy(slots).to(DEV))
+    torch.cuda.synchronize()
+    live = (slots >= 0) & (slots < n_pages * page)
+    for name, x in (("k", k), ("v", v)):
+        want = before[name]
+        at = (slots[live] // page, slice(None), slots[live] % page)
+        if fp8:
+            codes, exps = okv.quantise_rows(x.float().cpu().numpy())
+            want[at], before[name + "_exp"][at] = codes[live], exps[live]
+            assert np.array_equal(getattr(cache, name + "_exp").cpu().numpy(), before[name + "_exp"])
+        else:
+            want[at] = x.contiguous().view(torch.uint8).cpu().numpy()[live]
+        assert np.array_equal(getattr(cache, name).view(torch.uint8).cpu().numpy(), want), name
+
+
+def test_write_of_zeros_extremes_and_not_finite(stage):
+    D, inf, nan = 64, float("inf"), float("nan")
+    x = torch.zeros((8, 1, D))
+    x[1, 0, :4] = torch.tensor([448.0, -448.0, 1.0, 2.0 ** -9])
+    x[2, 0, :3] = torch.tensor([450.0, 0.5, -450.0])
+    x[3, 0, :3] = torch.tensor([3.3895313892515355e38, 1.0, -1e38])        # the largest bf16
+    x[4, 0, :3] = torch.tensor([2.0 ** -133, -2.0 ** -130, 2.0 ** -126])   # below the normal range
+    x[5, 0, :4] = torch.tensor([inf, 1.0, -inf, nan])
+    x[6, 0, :] = nan
+    x[7, 0, :] = -0.0
+    x = x.bfloat16().to(DEV)
+    cache = new_cache(1, 1, 16, D, True, fill=0)
+    stage.write_cache(cache, x, x, torch.arange(8, device=DEV))
+    codes, exps = okv.quantise_rows(x.float().cpu().numpy())
+    got, e = cache.k.view(torch.uint8).cpu().numpy()[0, 0, :8], cache.k_exp.cpu().numpy()[0, 0, :8]
+    assert np.array_equal(e, exps[:, 0])
+    nans = (codes[:, 0] & 127) == 127
+    assert np.array_equal(got[~nans], codes[:, 0][~nans]) and np.all((got[nans] & 127) == 127)
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("heads,D,page", [(1, 64, 16), (3, 128, 64), (2, 64, 256)])
+def test_read_back(stage, fp8, heads, D, page):
+    import paper_2603_06619_amd as nat
+    lens = [1, page, 0, 3 * page + 5, page - 1]
+    n = sum(lens)
+    need = [-(-l // page) for l in lens]
+    order = np.random.default_rng(4).permutation(sum(need) + 2)
+    table = np.full((len(lens), max(need) + 1), -1, np.int32)
+    at = 0
+    for i, c in enumerate(need):
+        table[i, :c] = order[at:at + c]
+        at += c
+    cu = np.cumsum([0] + lens)
+    cache = new_cache(sum(need) + 2, heads, page, D, fp8, fill=0x55)
+    k, v = rows(5, n, heads, D), rows(6, n, heads, D)
+    slots = np.concatenate([table[i][np.arange(l) // page].astype(np.int64) * page + np.arange(l) % page for i, l in enumerate(lens)])
+    stage.write_cache(cache, k, v, torch.from_numpy(slots).to(DEV))
+    dev = lambda x: torch.from_numpy(x.astype(np.int32)).to(DEV)
+    gk, gv = stage.read_cache(cache, dev(table), dev(cu), n)
+    for got, x in ((gk, k), (gv, v)):
+        if fp8:
+            want = torch.from_numpy(okv.row_values(*okv.quantise_rows(x.float().cpu().numpy()))).bfloat16()
+            assert torch.equal(got.cpu(), want)
+        else:
+            assert torch.equal(got, x)
+    # a page that is not there reads as zeros; rows of no sequence are left alone; a row stride
+    table[3, 1] = 10 ** 6
+    whole = torch.full((n + 3, heads * D + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+    part = whole[:, :heads * D].unflatten(1, (heads, D))
+    part2 = part.clone()
+    nat.nat_kv_read(cache, dev(table), dev(cu), part, part2)
+    gone = slice(cu[3] + page, cu[3] + 2 * page)
+    assert bool((part[gone] == 0).all()) and torch.equal(part[:gone.start], gk[:gone.start]) and torch.equal(part[gone.stop:n], gk[gone.stop:])
+    assert bool((part[n:] == 7).all()) and bool((whole[:, heads * D:] == 7).all())
+
+
+def decode_case(seed, lens, hq, hkv, D, page, fp8, width=None, fill=0xff):
+    """A cache whose unwritten places hold NaN (fill 0xff) and a table with pages in no order."""
+    rng = np.random.default_rng(seed)
+    need = [-(-max(l, 0) // page) for l in lens]
+    width = width or max(need + [1])
+    n_pages = sum(need) + 1
+    order = rng.permutation(n_pages)
+    table = np.full((len(lens), width), -1, np.int32)
+    at = 0
+    for i, c in enumerate(need):
+        table[i, :c] = order[at:at + c]
+        at += c
+    from paper_2603_06619_amd.rollout import RolloutStage
+    cache = new_cache(n_pages, hkv, page, D, fp8, fill)
+    n = sum(max(l, 0) for l in lens)
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    new = lambda r, h: torch.randn((r, h, D), generator=g, device=DEV, dtype=torch.bfloat16)
+    if n:
+        slots = np.concatenate([table[i][np.arange(l) // page].astype(np.int64) * page + np.arange(l) % page for i, l in enumerate(lens) if l > 0])
+        RolloutStage(DEV).write_cache(cache, new(n, hkv), new(n, hkv), torch.from_numpy(slots).to(DEV))
+    return dict(cache=cache, q=new(len(lens), hq), table=torch.from_numpy(table).to(DEV), lens=torch.tensor(lens, dtype=torch.int32, device=DEV))
+
+
+def check_decode(c, out, lse, scale=None):
+    k, v = values(c["cache"], "k"), values(c["cache"], "v")
+    ref = oattn.decode(c["q"].double().cpu().numpy(), k, v, c["table"].cpu().numpy(), c["lens"].cpu().numpy(), scale, bounds=True)
+    got, l = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert np.isfinite(got).all() and np.array_equal(np.isneginf(l), np.isneginf(ref["lse"]))
+    assert np.all(np.abs(got - ref["out"]) <= ref["e_out"] + 1e-30)
+    fine = np.isfinite(ref["lse"])
+    assert np.all(np.abs(l[fine] - ref["lse"][fine]) <= ref["e_lse"][fine])
+    norm = np.linalg.norm(ref["out"])
+    assert norm == 0 or np.linalg.norm(got - ref["out"]) <= 4e-3 * norm
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+@pytest.mark.parametrize("hq,hkv,D", [(1, 1, 64), (4, 4, 128), (8, 1, 64), (28, 4, 128), (16, 1, 128), (40, 2, 64), (17, 1, 128)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_decode(stage, fp8, hq, hkv, D, page):
+    lens = [1, 0, 15, 16, 17, 33, 257, 700, 31, 2000]
+    c = decode_case(7, lens, hq, hkv, D, page, fp8)
+    out, lse = stage.decode(c["q"], c["cache"], c["table"], c["lens"])
+    check_decode(c, out, lse)
+
+
+@pytest.mark.parametrize("page,width", [(16, 1), (32, 3), (256, 1), (128, 40)])
+def test_decode_short_tables_and_wide_ones(stage, page, width):
+    lens = [min(page * width, n) for n in (3, page, page * width, 1)]
+    c = decode_case(8, lens, 6, 2, 128, page, True, width=width)
+    check_decode(c, *stage.decode(c["q"], c["cache"], c["table"], c["lens"], scale=0.3), scale=0.3)
+
+
+def test_decode_lengths_are_clamped_and_missing_pages_do_not_count(stage):
+    c = decode_case(9, [64, 100, 300], 4, 2, 64, 16, False)
+    c["lens"] = torch.tensor([64, -7, 300], dtype=torch.int32, device=DEV)
+    c["table"][2, 3] = -1
+    c["table"][2, 7] = 1 << 20
+    c["table"][2, 18] = -(1 << 31)
+    check_decode(c, *stage.decode(c["q"], c["cache"], c["table"], c["lens"]))
+    full = decode_case(10, [48], 4, 2, 64, 16, False)
+    want = stage.decode(full["q"], full["cache"], full["table"], full["lens"])
+    full["lens"].fill_(1 << 30)                       # more than the table holds: the table's tokens
+    got = stage.decode(full["q"], full["cache"], full["table"], full["lens"])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_decode_strides_streams_and_runs(stage, fp8):
+    c = decode_case(11, [5000, 40, 1234], 8, 2, 128, 64, fp8)
+    out, lse = stage.decode(c["q"], c["cache"], c["table"], c["lens"])
+    check_decode(c, out, lse)
+    wide = torch.full((3, 9 * 128 + 8), float("nan"), dtype=torch.bfloat16, device=DEV)
+    q = wide[:, 128:9 * 128].unflatten(1, (8, 128))
+    q.copy_(c["q"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = stage.decode(q, c["cache"], c["table"], c["lens"])
+    side.synchronize()
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+def test_decode_agrees_with_attention_over_the_rows_read_back(stage):
+    c = decode_case(12, [777, 64, 130], 12, 4, 128, 32, True)
+    out, lse = stage.decode(c["q"], c["cache"], c["table"], c["lens"])
+    cu_k = torch.tensor([0, 777, 841, 971], dtype=torch.int32, device=DEV)
+    k, v = stage.read_cache(c["cache"], c["table"], cu_k, 971)
+    ref, ref_lse = stage.attention(c["q"], k, v, torch.arange(4, dtype=torch.int32, device=DEV), cu_k)
+    assert float((out.float() - ref.float()).norm() / ref.float().norm()) <= 6e-3           # both within 4e-3, mostly the same roundings
+    assert float((lse - ref_lse.t()).abs().max()) <= 1e-4
+
+
+@pytest.mark.parametrize("fp8", [True, False])
+def test_pages_beyond_32_bit_offsets(stage, fp8):
+    """The last pages of caches of 5 * 2^30 elements."""
+    D, page, hkv = 128, 256, 8
+    n_pages = 5 * 2 ** 30 // (D * page * hkv)
+    cache = new_cache(n_pages, hkv, page, D, fp8)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, v = (torch.randn((600, hkv, D), generator=g, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    pages = torch.tensor([[n_pages - 1, 0, n_pages - 2]], dtype=torch.int32, device=DEV)
+    t = torch.arange(600, device=DEV)
+    stage.write_cache(cache, k, v, pages[0].long()[t // page] * page + t % page)
+    small = new_cache(3, hkv, page, D, fp8)
+    order = torch.tensor([[0, 1, 2]], dtype=torch.int32, device=DEV)
+    stage.write_cache(small, k, v, t)
+    cu = torch.tensor([0, 600], dtype=torch.int32, device=DEV)
+    for a, b in zip(stage.read_cache(cache, pages, cu, 600), stage.read_cache(small, order, cu, 600)):
+        assert torch.equal(a, b)
+    q, lens = torch.randn((1, 16, D), generator=g, device=DEV, dtype=torch.bfloat16), torch.tensor([600], dtype=torch.int32, device=DEV)
+    for a, b in zip(stage.decode(q, cache, pages, lens), stage.decode(q, small, order, lens)):
+        assert torch.equal(a, b)
+
+
+def test_a_step_replays_from_a_graph(stage):
+    """Write the new rows, attend, draw: recorded once, replayed with other inputs in the same buffers."""
+    import paper_2603_06619_amd as nat
+    lens = [700, 65]
+    c = decode_case(13, lens, 8, 2, 64, 32, True, width=32)
+    cache, D, V = c["cache"], 64, 5000
+    head = torch.randn((8 * D, V), device=DEV) * 0.05
+    bufs = dict(q=torch.randn((2, 8, D), device=DEV, dtype=torch.bfloat16), k=torch.randn((2, 2, D), device=DEV, dtype=torch.bfloat16),
+                v=torch.randn((2, 2, D), device=DEV, dtype=torch.bfloat16), word=torch.tensor([5, -77], dtype=torch.int32, device=DEV))
+    place = [(l - 1) for l in lens]                  # the last token's slot is rewritten
+    slots = torch.tensor([int(c["table"][i, p // 32]) * 32 + p % 32 for i, p in enumerate(place)], device=DEV)
+    ws = torch.empty(max(nat.attn_decode_workspace_bytes(2, 8, 2, D, 32 * 32), 256), dtype=torch.uint8, device=DEV)
+    new = lambda: dict(out=torch.empty_like(bufs["q"]), lse=torch.empty((2, 8), device=DEV), ids=torch.empty(2, dtype=torch.int32, device=DEV),
+                       logp=torch.empty(2, device=DEV), logq=torch.empty(2, device=DEV), logits=torch.empty((2, V), device=DEV))
+
+    def call(o):
+        nat.nat_kv_write(cache, bufs["k"], bufs["v"], slots)
+        nat.nat_attn_decode(cache, bufs["q"], c["table"], c["lens"], D ** -0.5, o["out"], o["lse"], ws)
+        torch.mm(o["out"].flatten(1).float(), head, out=o["logits"])
+        nat.nat_sample(o["logits"], bufs["word"], None, None, None, None, o["ids"], o["logp"], o["logq"])
+    o = new()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(o)
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(o)
+    for rep in range(4):
+        for x in bufs.values():
+            x.copy_(torch.randn(x.shape, device=DEV) * 1e9 if x.dtype == torch.int32 else torch.randn(x.shape, device=DEV))
+        for x in o.values():
+            x.fill_(1)
+        ws.fill_(rep)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        got = {n: x.clone() for n, x in o.items()}
+        eager = new()
+        call(eager)
+        torch.cuda.synchronize()
+        for n in got:
+            assert torch.equal(got[n], eager[n]), (rep, n)
