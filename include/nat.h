@@ -404,7 +404,7 @@ nat_status nat_loss_fwd_bwd_kl(const void* d_hidden_k, const void* d_W, const in
  *   n_q_heads    a multiple of n_kv_heads; query head h reads key head h / (n_q_heads / n_kv_heads);
  *   head_dim     64 or 128;  dtype NAT_DTYPE_BF16;  causal 0 or 1;  scale > 0 and finite;
  *   *_stride     elements from row to row (a row holds its heads back to back), a multiple of 8, at least
- *                heads * head_dim and below 2^31; 0 = exactly that.  q, k, v may be parts of one array.
+ *                heads * head_dim and below 2^24; 0 = exactly that.  q, k, v may be parts of one array.
  */
 typedef struct nat_attn_params {
   int32_t n_seqs, n_q_heads, n_kv_heads, head_dim, dtype, causal;

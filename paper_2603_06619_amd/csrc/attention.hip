@@ -13,6 +13,8 @@
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
 
+#include <type_traits>
+
 namespace nat {
 namespace {
 
@@ -20,6 +22,8 @@ constexpr float kLog2E = 1.4426950408889634f;
 constexpr int kRowTile = 128;             // rows per workgroup: 4 wavefronts of 32
 constexpr int kKeyTile = 64;              // keys per step of the forward and dq kernels
 constexpr int kFewKeys = 64;             // see attn_dq_kernel
+constexpr float kSlack = 8.f;
+constexpr int64_t kMaxStride = 1 << 24;   // elements: 64 rows are then within the 32-bit offsets of a buffer descriptor
 constexpr int kDkvKeys = 128;             // keys per workgroup of the dk, dv kernel
 constexpr int kDkvRows = 64;              // rows per step of it
 
@@ -37,7 +41,11 @@ struct AttnArgs {
   uint16_t *dq, *dk, *dv;
   int64_t dout_stride, dq_stride, dk_stride, dv_stride;
   int slots;                     // tile slots per key head
+  uint32_t group_inverse;        // see small_quotient
 };
+
+// x / group for 0 <= x < 2^13: inverse = floor(2^32 / group) + 1 is too large by less than 1 / group in 2^32 / x
+__device__ __forceinline__ int small_quotient(int x, int group, uint32_t inverse) { return group == 1 ? x : (int)__umulhi((uint32_t)x, inverse); }
 
 // Offsets come from device memory: clamped to the arrays, and a sequence never has a negative length.
 __device__ __forceinline__ int64_t offset_at(const int32_t* cu, int i, int64_t n) {
@@ -71,9 +79,11 @@ struct Sequence {
 };
 __device__ __forceinline__ Sequence sequence(const AttnArgs& a, int b) {
   Sequence s;
-  s.q0 = offset_at(a.cu_q, b, a.n_q);
-  s.k0 = offset_at(a.cu_k, b, a.n_k);
-  const int64_t q1 = offset_at(a.cu_q, b + 1, a.n_q), k1 = offset_at(a.cu_k, b + 1, a.n_k);
+  // the same for all lanes, and said so: what is made of them stays in scalar registers
+  auto at = [](const int32_t* cu, int i, int64_t n) { return (int64_t)__builtin_amdgcn_readfirstlane((int)offset_at(cu, i, n)); };
+  s.q0 = at(a.cu_q, b, a.n_q);
+  s.k0 = at(a.cu_k, b, a.n_k);
+  const int64_t q1 = at(a.cu_q, b + 1, a.n_q), k1 = at(a.cu_k, b + 1, a.n_k);
   s.n_q = q1 > s.q0 ? (int)(q1 - s.q0) : 0;
   s.n_k = k1 > s.k0 ? (int)(k1 - s.k0) : 0;
   s.ahead = s.n_k - s.n_q;
@@ -105,60 +115,44 @@ unsigned grid_of(int heads, int64_t slots) {
   return (unsigned)((heads % 8 != 0 && 8 % heads == 0) ? (slots * heads + 7) / 8 * 8 : slots * heads);
 }
 
-// kRows rows of D elements, staged through registers: fetched one step ahead, written to LDS when the step begins.  Rows at or beyond `end` are zeros,
-// so what lies behind a sequence's end never meets a product.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// kRows rows of D elements, staged through registers: fetched one step ahead, written to LDS when the step begins.  Loads go through a buffer descriptor
+// of the rows that there are: what lies behind them (behind a sequence's end) is read as zeros by the hardware's bounds check and never meets a product.
 template <int D, int kRows>
 struct RowLoader {
-  static constexpr int kLoads = kRows * D / 8 / 256;
-  uint4 x[kLoads];
-  __device__ __forceinline__ void fetch(const uint16_t* base, int64_t stride, int first, int end) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = threadIdx.x + 256 * i, row = first + at / (D / 8);
-      x[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (row < end) x[i] = *(const uint4*)(base + row * stride + at % (D / 8) * 8);
-    }
+  static constexpr int kLanes = D / 8, kLoads = kRows * kLanes / 256, kStep = 256 / kLanes;
+  u32x4 x[kLoads];
+  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const uint16_t* base, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes > 0 ? (int)(uint32_t)bytes : 0, 0x00027000);
   }
-  // rows r of a group's matrix: query r / group, head r % group
-  __device__ __forceinline__ void fetch_grouped(const uint16_t* base, int64_t stride, int group, int first, int end) {
+  __device__ __forceinline__ void fetch(const uint16_t* base, int64_t stride, int first, int end) {
+    const int rows = end - first < kRows ? end - first : kRows;
+    const auto r = rows_at(base + first * stride, rows > 0 ? (rows - 1) * stride * 2 + D * 2 : 0);
+    const uint32_t row = (uint32_t)stride * 2, at = threadIdx.x / kLanes * row + threadIdx.x % kLanes * 16;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, at + i * kStep * row, 0, 0);
+  }
+  // rows of a group's matrix from head `head` of query `query` on, `rows` of them (the rest: zeros)
+  __device__ __forceinline__ void fetch_grouped(const uint16_t* base, int64_t stride, int group, uint32_t group_inverse, int64_t query, int head, int rows) {
+    const int live = rows < kRows ? rows : kRows;
+    const auto r = rows_at(base + query * stride, live > 0 ? small_quotient(head + live - 1, group, group_inverse) * stride * 2 + group * D * 2 : 0);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int at = threadIdx.x + 256 * i, row = first + at / (D / 8);
-      x[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (row < end) x[i] = *(const uint4*)(base + (row / group) * stride + row % group * D + at % (D / 8) * 8);
+      const int row = threadIdx.x / kLanes + i * kStep, at = head + row, t = small_quotient(at, group, group_inverse);
+      const uint32_t offset = t * ((uint32_t)stride * 2) + (at - t * group) * (D * 2) + threadIdx.x % kLanes * 16;
+      x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, row < live ? offset : 0x80000000u, 0, 0);
     }
   }
   __device__ __forceinline__ void store(char* tile) const {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = threadIdx.x + 256 * i;
-      *(uint4*)(tile + RowTile<D>::chunk_at(at / (D / 8), at % (D / 8))) = x[i];
-    }
-  }
-  // an element of this thread's is infinite or NaN
-  __device__ __forceinline__ bool not_finite() const {
-    bool any = false;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) any |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
-    }
-    return any;
+    for (int i = 0; i < kLoads; ++i) *(u32x4*)(tile + RowTile<D>::chunk_at(threadIdx.x / kLanes + i * kStep, threadIdx.x % kLanes)) = x[i];
   }
 };
 
-// The workgroup's barrier; at the mask's edge it tells whether any of the rows on the way to LDS holds what is not finite.
-template <class... Loaders>
-__device__ __forceinline__ bool wait_at_edge(bool edge, const Loaders&... l) {
-  if (edge) return __syncthreads_or((l.not_finite() || ...));
-  __syncthreads();
-  return false;
-}
-
-// Where a mask cuts through a tile, a product multiplies masked rows by 0, and infinities or NaN in them would come through.  Such a tile (looked for
-// only at the mask's edge, where the workgroup agrees on it at its barrier) gets zeros in their places before it enters the product, and the columns that see
-// them have them added by hand.
+// Where a mask cuts through a tile, a product multiplies masked rows by 0, and infinities or NaN in them come through as NaN.  Results that are not finite
+// are therefore computed once more, carefully: at the mask's edge such a tile gets zeros in their places before it enters the product, and the columns
+// that see them have them added by hand.
 template <int D, int kRows, class Sees>
 __device__ __forceinline__ void take_out_not_finite(char* tile, f32x16 (&acc)[D / 32], int half, const Sees& sees) {
   for (int row = 0; row < kRows; ++row) {
@@ -190,6 +184,40 @@ struct RowFragments {            // 32 rows as an operand, one row per lane, in 
   }
 };
 
+template <int D>
+__device__ __forceinline__ bool not_finite(const f32x16 (&acc)[D / 32]) {
+  float x = 0.f;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x += acc[db][i];
+  return !(fabsf(x) < INFINITY);             // (sums that overflow are looked at again too)
+}
+
+// C[32 rb ..][n] = rows of a tile of 64 rows times the columns b: fragments are read four at a time while the four before them are multiplied (the
+// compiler by itself reads one and waits for it).
+template <int D>
+__device__ __forceinline__ void tile_times_columns(const char* tile, const bf16x8 (&b)[D / 16], f32x16 (&c)[2], int lane) {
+  constexpr int kSteps = D / 16, kGroups = 2 * kSteps / 4;
+  bf16x8 f[2][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[0][i] = row_fragment<D>(tile, lane, i / kSteps, i % kSteps);
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    if (g + 1 < kGroups) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[(g + 1) & 1][i] = row_fragment<D>(tile, lane, (4 * g + 4 + i) / kSteps, (4 * g + 4 + i) % kSteps);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = 4 * g + i;
+      c[at / kSteps] = mfma32(f[g & 1][i], b[at % kSteps], c[at / kSteps]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
 // Columns of a result, 32 elements db of this lane's column n, as bf16 to its row
 template <int D>
 __device__ __forceinline__ void store_columns(uint16_t* row, const f32x16 (&acc)[D / 32], float factor, int lane) {
@@ -205,7 +233,7 @@ __device__ __forceinline__ void store_columns(uint16_t* row, const f32x16 (&acc)
 template <int D>
 __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) char tiles[2][2][kKeyTile * D * 2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   int head, slot;
   head_and_slot(blockIdx.x, a.hkv, a.slots, head, slot);
   if (slot >= a.slots) return;
@@ -229,28 +257,26 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   const uint16_t *k = a.k + s.k0 * a.k_stride + head * D, *v = a.v + s.k0 * a.v_stride + head * D;
 
   const float to_log2 = a.scale * kLog2E;
-  float m = -INFINITY, sum = 0.f;            // running maximum of q.k, sum of this lane's half
-  f32x16 acc[D / 32] = {};
+  // What exponents are shifted by, and the sum (of this lane's half).  m follows the maximum of q.k only when that has grown by a factor of 2^kSlack in the
+  // exponentials: they and their sums have room for it, and the results are seldom scaled
+  float m, sum;
+  const float slack = kSlack / to_log2;
+  f32x16 acc[D / 32];
   RowLoader<D, kKeyTile> kl, vl;
-  kl.fetch(k, a.k_stride, 0, n_keys);
-  vl.fetch(v, a.v_stride, 0, n_keys);
-  for (int key0 = 0, buf = 0; key0 < n_keys; key0 += kKeyTile, buf ^= 1) {
-    char *kt = tiles[buf][0], *vt = tiles[buf][1];
+  auto step = [&](int key0, char* kt, char* vt, auto careful) __attribute__((always_inline)) {
     kl.store(kt);
     vl.store(vt);
-    // the barrier: the other buffer is read before this by all
-    if (__builtin_expect(wait_at_edge(key0 + kKeyTile - 1 > tile_least, vl), 0))
-      take_out_not_finite<D, kKeyTile>(vt, acc, half, [&](int i) { return key0 + i <= last; });
+    __syncthreads();                         // the other buffer is read before this by all
     if (key0 + kKeyTile < n_keys) {
       kl.fetch(k, a.k_stride, key0 + kKeyTile, n_keys);
       vl.fetch(v, a.v_stride, key0 + kKeyTile, n_keys);
     }
-    if (key0 > wave_last) continue;
+    if constexpr (decltype(careful)::value) {
+      if (key0 + kKeyTile - 1 > tile_least) take_out_not_finite<D, kKeyTile>(vt, acc, half, [&](int i) { return key0 + i <= last; });
+    }
+    if (key0 > wave_last) return;
     f32x16 st[2] = {};
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) st[rb] = mfma32(row_fragment<D>(kt, lane, rb, i), q.f[i], st[rb]);
+    tile_times_columns<D>(kt, q.f, st, lane);
     if (key0 + kKeyTile - 1 > wave_least) {
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb)
@@ -264,29 +290,52 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, st[rb][i]);
     top = max_halves(top);
-    if (__any(top > m)) {
-      const float f = top == -INFINITY ? 1.f : exp2_fast((m - top) * to_log2);
+    const bool grown = top > m + slack;
+    if (__any(grown)) {                      // each row by its own: what its neighbours hold does not change its rounding
+      const float f = grown ? exp2_fast((m - top) * to_log2) : 1.f;
       sum *= f;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) acc[db] *= f;
-      m = top;
+      m = grown ? top : m;
     }
     const float shift = m == -INFINITY ? 0.f : m * to_log2;
+    // probabilities of 16 keys at a time, while those of the 16 before them are multiplied
+    bf16x8 p[2], vf[2][D / 32];
+    auto ready = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        st[rb][i] = exp2_fast(fmaf(st[rb][i], to_log2, -shift));
-        sum += st[rb][i];
+      for (int i = 0; i < 8; ++i) {
+        const int e = 8 * (g & 1) + i;
+        st[g >> 1][e] = exp2_fast(fmaf(st[g >> 1][e], to_log2, -shift));
+        sum += st[g >> 1][e];
       }
+      p[g & 1] = fragment_of_result(st[g >> 1], g & 1);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bf16x8 p = fragment_of_result(st[rb], h);
+      for (int db = 0; db < D / 32; ++db) vf[g & 1][db] = transposed_fragment<D>(vt, lane, db, g);
+    };
+    ready(0);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(transposed_fragment<D>(vt, lane, db, 2 * rb + h), p, acc[db]);
-      }
+    for (int g = 0; g < 4; ++g) {
+      if (g < 3) ready(g + 1);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(vf[g & 1][db], p[g & 1], acc[db]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-  }
+  };
+  auto pass = [&](auto careful) __attribute__((always_inline)) {
+    m = -INFINITY;
+    sum = 0.f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) acc[db] = f32x16{};
+    kl.fetch(k, a.k_stride, 0, n_keys);
+    vl.fetch(v, a.v_stride, 0, n_keys);
+    for (int key0 = 0; key0 < n_keys; key0 += 2 * kKeyTile) {
+      step(key0, tiles[0][0], tiles[0][1], careful);
+      if (key0 + kKeyTile < n_keys) step(key0 + kKeyTile, tiles[1][0], tiles[1][1], careful);
+    }
+  };
+  pass(std::false_type{});
+  if (__syncthreads_or(not_finite<D>(acc))) pass(std::true_type{});
   sum = sum_halves(sum);
   if (row >= n_rows) return;
   const int64_t at = s.q0 + query;
@@ -295,13 +344,15 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   if (half == 0) a.lse[qh * a.n_q + at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, __logf(sum));
 }
 
+enum class Pass { kDelta, kPlain, kCareful };
+
 // dq, and delta for the dk, dv kernel behind it.  delta = dout . out takes `out` as it was rounded, which for rows of few keys is an error that dq does not
 // average out (of the 2-norm about 1.7e-3 / sqrt(keys), where the rounding of dS is 1.7e-3; a single such row a few per cent).  Tiles with a row of fewer than
 // kFewKeys keys go over their keys once more for it: delta = sum_j P_ij dP_ij.
 template <int D>
 __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) char tiles[2][2][kKeyTile * D * 2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   int head, slot;
   head_and_slot(blockIdx.x, a.hkv, a.slots, head, slot);
   if (slot >= a.slots) return;
@@ -336,64 +387,85 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
   const uint16_t *k = a.k + s.k0 * a.k_stride + head * D, *v = a.v + s.k0 * a.v_stride + head * D;
   const float to_log2 = a.scale * kLog2E, lse = a.lse[qh * a.n_q + at], shift = lse == -INFINITY ? INFINITY : lse * kLog2E;
 
-  f32x16 acc[D / 32] = {};
+  f32x16 acc[D / 32];
   RowLoader<D, kKeyTile> kl, vl;
-  const bool two_passes = tile_least < kFewKeys - 1;
   float p_sum = 0.f, p_dp = 0.f;
-  for (int pass = two_passes ? 0 : 1; pass < 2; ++pass) {
+  auto step = [&](int key0, char* kt, char* vt, auto kind) __attribute__((always_inline)) {
+    constexpr Pass kPass = decltype(kind)::value;
+    kl.store(kt);
+    vl.store(vt);
+    __syncthreads();
+    if (key0 + kKeyTile < n_keys) {
+      kl.fetch(k, a.k_stride, key0 + kKeyTile, n_keys);
+      vl.fetch(v, a.v_stride, key0 + kKeyTile, n_keys);
+    }
+    if constexpr (kPass == Pass::kCareful) {
+      if (key0 + kKeyTile - 1 > tile_least) take_out_not_finite<D, kKeyTile>(kt, acc, half, [&](int i) { return key0 + i <= last; });
+    }
+    if (key0 > wave_last) return;
+    f32x16 st[2] = {}, dp[2] = {};
+    tile_times_columns<D>(kt, q.f, st, lane);
+    tile_times_columns<D>(vt, d.f, dp, lane);
+    if (key0 + kKeyTile - 1 > wave_least) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (key0 + 32 * rb + result_row(i, half) > last) {
+            st[rb][i] = -INFINITY;
+            dp[rb][i] = 0.f;
+          }
+    }
+    if constexpr (kPass == Pass::kDelta) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float p = exp2_fast(fmaf(st[rb][i], to_log2, -shift));
+          p_sum += p;
+          p_dp = fmaf(p, dp[rb][i], p_dp);
+        }
+    } else {
+      bf16x8 p[2], kf[2][D / 32];
+      auto ready = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int e = 8 * (g & 1) + i;
+          st[g >> 1][e] = exp2_fast(fmaf(st[g >> 1][e], to_log2, -shift)) * (dp[g >> 1][e] - delta);
+        }
+        p[g & 1] = fragment_of_result(st[g >> 1], g & 1);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) kf[g & 1][db] = transposed_fragment<D>(kt, lane, db, g);
+      };
+      ready(0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        if (g < 3) ready(g + 1);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(kf[g & 1][db], p[g & 1], acc[db]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+  auto pass = [&](auto kind) __attribute__((always_inline)) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) acc[db] = f32x16{};
     kl.fetch(k, a.k_stride, 0, n_keys);
     vl.fetch(v, a.v_stride, 0, n_keys);
-    for (int key0 = 0, buf = 0; key0 < n_keys; key0 += kKeyTile, buf ^= 1) {
-      char *kt = tiles[buf][0], *vt = tiles[buf][1];
-      kl.store(kt);
-      vl.store(vt);
-      if (__builtin_expect(wait_at_edge(key0 + kKeyTile - 1 > tile_least, kl), 0))
-        take_out_not_finite<D, kKeyTile>(kt, acc, half, [&](int i) { return key0 + i <= last; });
-      if (key0 + kKeyTile < n_keys) {
-        kl.fetch(k, a.k_stride, key0 + kKeyTile, n_keys);
-        vl.fetch(v, a.v_stride, key0 + kKeyTile, n_keys);
-      }
-      if (key0 > wave_last) continue;
-      const bool edge = key0 + kKeyTile - 1 > wave_least;
-#pragma unroll
-      for (int rb = 0; rb < 2; ++rb) {
-        f32x16 st = {}, dp = {};
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          st = mfma32(row_fragment<D>(kt, lane, rb, i), q.f[i], st);
-          dp = mfma32(row_fragment<D>(vt, lane, rb, i), d.f[i], dp);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) st[i] = exp2_fast(fmaf(st[i], to_log2, -shift));
-        if (edge) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (key0 + 32 * rb + result_row(i, half) > last) st[i] = dp[i] = 0.f;
-        }
-        if (pass == 0) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            p_sum += st[i];
-            p_dp = fmaf(st[i], dp[i], p_dp);
-          }
-          continue;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) st[i] *= dp[i] - delta;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const bf16x8 p = fragment_of_result(st, h);
-#pragma unroll
-          for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(transposed_fragment<D>(kt, lane, db, 2 * rb + h), p, acc[db]);
-        }
-      }
+    for (int key0 = 0; key0 < n_keys; key0 += 2 * kKeyTile) {
+      step(key0, tiles[0][0], tiles[0][1], kind);
+      if (key0 + kKeyTile < n_keys) step(key0 + kKeyTile, tiles[1][0], tiles[1][1], kind);
     }
-    if (pass == 0) {
-      p_sum = sum_halves(p_sum);
-      delta = p_sum > 0.f ? sum_halves(p_dp) / p_sum : 0.f;
-      __syncthreads();                       // the first tile is overwritten next
-    }
+  };
+  if (tile_least < kFewKeys - 1) {
+    pass(std::integral_constant<Pass, Pass::kDelta>{});
+    p_sum = sum_halves(p_sum);
+    delta = p_sum > 0.f ? sum_halves(p_dp) / p_sum : 0.f;
+    __syncthreads();                         // before the first tile is overwritten
   }
+  pass(std::integral_constant<Pass, Pass::kPlain>{});
+  if (__syncthreads_or(not_finite<D>(acc))) pass(std::integral_constant<Pass, Pass::kCareful>{});
   if (row >= n_rows) return;
   if (half == 0) a.delta[qh * a.n_q + at] = delta;
   store_columns<D>(a.dq + at * a.dq_stride + qh * D, acc, a.scale, lane);
@@ -404,7 +476,7 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
   struct RowWords { float shift[kDkvRows], delta[kDkvRows]; int last[kDkvRows]; };
   __shared__ __attribute__((aligned(16))) char tiles[2][2][kDkvRows * D * 2];
   __shared__ __attribute__((aligned(16))) RowWords words[2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   int head, slot;
   head_and_slot(blockIdx.x, a.hkv, a.slots, head, slot);
   if (slot >= a.slots) return;
@@ -428,31 +500,31 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
   const float *lse = a.lse + (int64_t)head * a.group * a.n_q + s.q0, *delta = a.delta + (int64_t)head * a.group * a.n_q + s.q0;
   const float to_log2 = a.scale * kLog2E;
 
-  f32x16 dk[D / 32] = {}, dv[D / 32] = {};
+  f32x16 dk[D / 32], dv[D / 32];
   RowLoader<D, kDkvRows> ql, dl;
   float row_shift = INFINITY, row_delta = 0.f;
   int row_last = -1;
-  auto fetch = [&](int row0) {
-    ql.fetch_grouped(q, a.q_stride, a.group, row0, n_rows);
-    dl.fetch_grouped(d, a.dout_stride, a.group, row0, n_rows);
+  // the rows from `row0` on; query and head of row0 are kept as they go
+  int next_query, next_head, query = 0, head_of_group = 0;
+  const int query_step = kDkvRows / a.group, head_step = kDkvRows - query_step * a.group;
+  auto fetch = [&](int row0) __attribute__((always_inline)) {
+    ql.fetch_grouped(q, a.q_stride, a.group, a.group_inverse, next_query, next_head, n_rows - row0);
+    dl.fetch_grouped(d, a.dout_stride, a.group, a.group_inverse, next_query, next_head, n_rows - row0);
     if (threadIdx.x < kDkvRows) {
-      const int r = row0 + threadIdx.x, t = r / a.group;
+      const int at = next_head + threadIdx.x, of = small_quotient(at, a.group, a.group_inverse), t = next_query + of;
       row_shift = INFINITY;                  // probability 0: rows past the end, and rows that see no key
       row_delta = 0.f;
       row_last = -1;
-      if (r < n_rows) {
-        const int64_t at = (r - t * a.group) * a.n_q + t;
-        const float l = lse[at];
+      if (row0 + (int)threadIdx.x < n_rows) {
+        const int64_t w = (at - of * a.group) * a.n_q + t;
+        const float l = lse[w];
         row_shift = l == -INFINITY ? INFINITY : l * kLog2E;
-        row_delta = delta[at];
+        row_delta = delta[w];
         row_last = last_key(a, s, t);
       }
     }
   };
-  fetch(first_row);
-  for (int row0 = first_row, buf = 0; row0 < n_rows; row0 += kDkvRows, buf ^= 1) {
-    char *qt = tiles[buf][0], *dt = tiles[buf][1];
-    RowWords& w = words[buf];
+  auto step = [&](int row0, char* qt, char* dt, RowWords& w, auto careful) __attribute__((always_inline)) {
     ql.store(qt);
     dl.store(dt);
     if (threadIdx.x < kDkvRows) {
@@ -460,48 +532,79 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
       w.delta[threadIdx.x] = row_delta;
       w.last[threadIdx.x] = row_last;
     }
-    const bool tile_edge = row0 / a.group < tile_all;
-    if (__builtin_expect(wait_at_edge(tile_edge, ql, dl), 0)) {
-      take_out_not_finite<D, kDkvRows>(qt, dk, half, [&](int i) { return key <= w.last[i]; });
-      take_out_not_finite<D, kDkvRows>(dt, dv, half, [&](int i) { return key <= w.last[i]; });
+    __syncthreads();
+    query = next_query;
+    head_of_group = next_head;
+    next_query += query_step;
+    next_head += head_step;
+    if (next_head >= a.group) {
+      next_head -= a.group;
+      ++next_query;
     }
     if (row0 + kDkvRows < n_rows) fetch(row0 + kDkvRows);
-    if ((row0 + kDkvRows - 1) / a.group < wave_first) continue;
-    const bool edge = row0 / a.group < wave_all;
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-      f32x16 p = {}, dp = {};
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        p = mfma32(row_fragment<D>(qt, lane, rb, i), k.f[i], p);
-        dp = mfma32(row_fragment<D>(dt, lane, rb, i), v.f[i], dp);
-      }
-#pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        const f32x4 shift = *(const f32x4*)(w.shift + 32 * rb + 8 * i4 + 4 * half), del = *(const f32x4*)(w.delta + 32 * rb + 8 * i4 + 4 * half);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 4 * i4 + e;
-          p[i] = exp2_fast(fmaf(p[i], to_log2, -shift[e]));
-          dp[i] = p[i] * (dp[i] - del[e]);
-        }
-      }
-      if (edge) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (key > w.last[32 * rb + result_row(i, half)]) p[i] = dp[i] = 0.f;
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bf16x8 pf = fragment_of_result(p, h), df = fragment_of_result(dp, h);
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) {
-          dv[db] = mfma32(transposed_fragment<D>(dt, lane, db, 2 * rb + h), pf, dv[db]);
-          dk[db] = mfma32(transposed_fragment<D>(qt, lane, db, 2 * rb + h), df, dk[db]);
-        }
+    if constexpr (decltype(careful)::value) {
+      if (query < tile_all) {
+        take_out_not_finite<D, kDkvRows>(qt, dk, half, [&](int i) { return key <= w.last[i]; });
+        take_out_not_finite<D, kDkvRows>(dt, dv, half, [&](int i) { return key <= w.last[i]; });
       }
     }
-  }
+    if (query + small_quotient(head_of_group + kDkvRows - 1, a.group, a.group_inverse) < wave_first) return;
+    f32x16 p[2] = {}, dp[2] = {};
+    tile_times_columns<D>(qt, k.f, p, lane);
+    tile_times_columns<D>(dt, v.f, dp, lane);
+    const bool edge = query < wave_all;
+    bf16x8 pf[2], df[2], dof[2][D / 32], qf[2][D / 32];
+    auto ready = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i4 = 0; i4 < 2; ++i4) {
+        const int row = 16 * g + 8 * i4 + 4 * half;
+        const f32x4 shift = *(const f32x4*)(w.shift + row), del = *(const f32x4*)(w.delta + row);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 8 * (g & 1) + 4 * i4 + e;
+          p[g >> 1][i] = exp2_fast(fmaf(p[g >> 1][i], to_log2, -shift[e]));
+          dp[g >> 1][i] = p[g >> 1][i] * (dp[g >> 1][i] - del[e]);
+        }
+        if (edge) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (key > w.last[row + e]) p[g >> 1][8 * (g & 1) + 4 * i4 + e] = dp[g >> 1][8 * (g & 1) + 4 * i4 + e] = 0.f;
+        }
+      }
+      pf[g & 1] = fragment_of_result(p[g >> 1], g & 1);
+      df[g & 1] = fragment_of_result(dp[g >> 1], g & 1);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        dof[g & 1][db] = transposed_fragment<D>(dt, lane, db, g);
+        qf[g & 1][db] = transposed_fragment<D>(qt, lane, db, g);
+      }
+    };
+    ready(0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (g < 3) ready(g + 1);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        dv[db] = mfma32(dof[g & 1][db], pf[g & 1], dv[db]);
+        dk[db] = mfma32(qf[g & 1][db], df[g & 1], dk[db]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto pass = [&](auto careful) __attribute__((always_inline)) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) dk[db] = dv[db] = f32x16{};
+    next_query = first_query;
+    next_head = 0;
+    fetch(first_row);
+    for (int row0 = first_row; row0 < n_rows; row0 += 2 * kDkvRows) {
+      step(row0, tiles[0][0], tiles[0][1], words[0], careful);
+      if (row0 + kDkvRows < n_rows) step(row0 + kDkvRows, tiles[1][0], tiles[1][1], words[1], careful);
+    }
+  };
+  pass(std::false_type{});
+  if (__syncthreads_or(not_finite<D>(dk) || not_finite<D>(dv))) pass(std::true_type{});
   if (key >= s.n_k) return;
   store_columns<D>(a.dk + (s.k0 + key) * a.dk_stride + head * D, dk, a.scale, lane);
   store_columns<D>(a.dv + (s.k0 + key) * a.dv_stride + head * D, dv, 1.f, lane);
@@ -526,7 +629,7 @@ nat_status attn_args(const nat_attn_params* p, const void* d_q, const void* d_k,
   if (p->n_q * group > INT32_MAX / 2 || (p->n_q * group / kRowTile + p->n_seqs) * p->n_kv_heads > INT32_MAX / 2 ||
       (p->n_k / kDkvKeys + p->n_seqs) * p->n_kv_heads > INT32_MAX / 2)
     return NAT_BAD_SHAPE;
-  auto stride_ok = [](int64_t s, int64_t row) { return s == 0 || (s >= row && s % 8 == 0 && s <= INT32_MAX); };
+  auto stride_ok = [](int64_t s, int64_t row) { return s == 0 || (s >= row && s % 8 == 0 && s < kMaxStride); };
   if (!stride_ok(p->q_stride, q_row) || !stride_ok(p->out_stride, q_row) || !stride_ok(p->dout_stride, q_row) || !stride_ok(p->dq_stride, q_row) ||
       !stride_ok(p->k_stride, k_row) || !stride_ok(p->v_stride, k_row) || !stride_ok(p->dk_stride, k_row) || !stride_ok(p->dv_stride, k_row))
     return NAT_BAD_SHAPE;
@@ -544,6 +647,7 @@ nat_status attn_args(const nat_attn_params* p, const void* d_q, const void* d_k,
   a->hq = p->n_q_heads;
   a->hkv = p->n_kv_heads;
   a->group = group;
+  a->group_inverse = (uint32_t)((1ull << 32) / group + 1);
   a->causal = p->causal;
   a->n_q = p->n_q;
   a->n_k = p->n_k;
