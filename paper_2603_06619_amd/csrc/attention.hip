@@ -123,24 +123,24 @@ template <int D, int kRows>
 struct RowLoader {
   static constexpr int kLanes = D / 8, kLoads = kRows * kLanes / 256, kStep = 256 / kLanes;
   u32x4 x[kLoads];
-  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const uint16_t* base, int64_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes > 0 ? (int)(uint32_t)bytes : 0, 0x00027000);
+  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const char* base, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000);
   }
-  __device__ __forceinline__ void fetch(const uint16_t* base, int64_t stride, int first, int end) {
-    const int rows = end - first < kRows ? end - first : kRows;
-    const auto r = rows_at(base + first * stride, rows > 0 ? (rows - 1) * stride * 2 + D * 2 : 0);
-    const uint32_t row = (uint32_t)stride * 2, at = threadIdx.x / kLanes * row + threadIdx.x % kLanes * 16;
+  // `rows` rows from `base` on (more than kRows: kRows), row_bytes apart
+  __device__ __forceinline__ void fetch(const char* base, int row_bytes, int rows) {
+    const auto r = rows_at(base, rows > 0 ? ((rows < kRows ? rows : kRows) - 1) * row_bytes + D * 2 : 0);
+    const int at = threadIdx.x / kLanes * row_bytes + threadIdx.x % kLanes * 16;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, at + i * kStep * row, 0, 0);
+    for (int i = 0; i < kLoads; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, at + i * kStep * row_bytes, 0, 0);
   }
-  // rows of a group's matrix from head `head` of query `query` on, `rows` of them (the rest: zeros)
-  __device__ __forceinline__ void fetch_grouped(const uint16_t* base, int64_t stride, int group, uint32_t group_inverse, int64_t query, int head, int rows) {
+  // rows of a group's matrix: `rows` of them from head `head` of the query at `base` on
+  __device__ __forceinline__ void fetch_grouped(const char* base, int row_bytes, int group, uint32_t group_inverse, int head, int rows) {
     const int live = rows < kRows ? rows : kRows;
-    const auto r = rows_at(base + query * stride, live > 0 ? small_quotient(head + live - 1, group, group_inverse) * stride * 2 + group * D * 2 : 0);
+    const auto r = rows_at(base, live > 0 ? small_quotient(head + live - 1, group, group_inverse) * row_bytes + group * D * 2 : 0);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int row = threadIdx.x / kLanes + i * kStep, at = head + row, t = small_quotient(at, group, group_inverse);
-      const uint32_t offset = t * ((uint32_t)stride * 2) + (at - t * group) * (D * 2) + threadIdx.x % kLanes * 16;
+      const int offset = t * row_bytes + (at - t * group) * (D * 2) + threadIdx.x % kLanes * 16;
       x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, row < live ? offset : 0x80000000u, 0, 0);
     }
   }
@@ -254,7 +254,8 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   const int wave_row = tile_row + wave * 32 < n_rows ? tile_row + wave * 32 : n_rows - 1, wave_end = wave_row + 32 < n_rows ? wave_row + 32 : n_rows;
   const int wave_least = last_key(a, s, wave_row / a.group);           // keys up to here are seen by all rows of the wavefront
   const int wave_last = last_key(a, s, (wave_end - 1) / a.group);
-  const uint16_t *k = a.k + s.k0 * a.k_stride + head * D, *v = a.v + s.k0 * a.v_stride + head * D;
+  const char *k = (const char*)(a.k + s.k0 * a.k_stride + head * D), *v = (const char*)(a.v + s.k0 * a.v_stride + head * D);
+  const int k_bytes = (int)a.k_stride * 2, v_bytes = (int)a.v_stride * 2;
 
   const float to_log2 = a.scale * kLog2E;
   // What exponents are shifted by, and the sum (of this lane's half).  m follows the maximum of q.k only when that has grown by a factor of 2^kSlack in the
@@ -263,13 +264,16 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   const float slack = kSlack / to_log2;
   f32x16 acc[D / 32];
   RowLoader<D, kKeyTile> kl, vl;
+  const char *next_k, *next_v;
   auto step = [&](int key0, char* kt, char* vt, auto careful) __attribute__((always_inline)) {
     kl.store(kt);
     vl.store(vt);
     __syncthreads();                         // the other buffer is read before this by all
     if (key0 + kKeyTile < n_keys) {
-      kl.fetch(k, a.k_stride, key0 + kKeyTile, n_keys);
-      vl.fetch(v, a.v_stride, key0 + kKeyTile, n_keys);
+      next_k += (int64_t)kKeyTile * k_bytes;
+      next_v += (int64_t)kKeyTile * v_bytes;
+      kl.fetch(next_k, k_bytes, n_keys - key0 - kKeyTile);
+      vl.fetch(next_v, v_bytes, n_keys - key0 - kKeyTile);
     }
     if constexpr (decltype(careful)::value) {
       if (key0 + kKeyTile - 1 > tile_least) take_out_not_finite<D, kKeyTile>(vt, acc, half, [&](int i) { return key0 + i <= last; });
@@ -327,8 +331,10 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
     sum = 0.f;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) acc[db] = f32x16{};
-    kl.fetch(k, a.k_stride, 0, n_keys);
-    vl.fetch(v, a.v_stride, 0, n_keys);
+    next_k = k;
+    next_v = v;
+    kl.fetch(k, k_bytes, n_keys);
+    vl.fetch(v, v_bytes, n_keys);
     for (int key0 = 0; key0 < n_keys; key0 += 2 * kKeyTile) {
       step(key0, tiles[0][0], tiles[0][1], careful);
       if (key0 + kKeyTile < n_keys) step(key0 + kKeyTile, tiles[1][0], tiles[1][1], careful);
@@ -384,11 +390,13 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
   const int last = last_key(a, s, query);
   const int wave_row = tile_row + wave * 32 < n_rows ? tile_row + wave * 32 : n_rows - 1, wave_end = wave_row + 32 < n_rows ? wave_row + 32 : n_rows;
   const int wave_least = last_key(a, s, wave_row / a.group), wave_last = last_key(a, s, (wave_end - 1) / a.group);
-  const uint16_t *k = a.k + s.k0 * a.k_stride + head * D, *v = a.v + s.k0 * a.v_stride + head * D;
+  const char *k = (const char*)(a.k + s.k0 * a.k_stride + head * D), *v = (const char*)(a.v + s.k0 * a.v_stride + head * D);
+  const int k_bytes = (int)a.k_stride * 2, v_bytes = (int)a.v_stride * 2;
   const float to_log2 = a.scale * kLog2E, lse = a.lse[qh * a.n_q + at], shift = lse == -INFINITY ? INFINITY : lse * kLog2E;
 
   f32x16 acc[D / 32];
   RowLoader<D, kKeyTile> kl, vl;
+  const char *next_k, *next_v;
   float p_sum = 0.f, p_dp = 0.f;
   auto step = [&](int key0, char* kt, char* vt, auto kind) __attribute__((always_inline)) {
     constexpr Pass kPass = decltype(kind)::value;
@@ -396,8 +404,10 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     vl.store(vt);
     __syncthreads();
     if (key0 + kKeyTile < n_keys) {
-      kl.fetch(k, a.k_stride, key0 + kKeyTile, n_keys);
-      vl.fetch(v, a.v_stride, key0 + kKeyTile, n_keys);
+      next_k += (int64_t)kKeyTile * k_bytes;
+      next_v += (int64_t)kKeyTile * v_bytes;
+      kl.fetch(next_k, k_bytes, n_keys - key0 - kKeyTile);
+      vl.fetch(next_v, v_bytes, n_keys - key0 - kKeyTile);
     }
     if constexpr (kPass == Pass::kCareful) {
       if (key0 + kKeyTile - 1 > tile_least) take_out_not_finite<D, kKeyTile>(kt, acc, half, [&](int i) { return key0 + i <= last; });
@@ -451,8 +461,10 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
   auto pass = [&](auto kind) __attribute__((always_inline)) {
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) acc[db] = f32x16{};
-    kl.fetch(k, a.k_stride, 0, n_keys);
-    vl.fetch(v, a.v_stride, 0, n_keys);
+    next_k = k;
+    next_v = v;
+    kl.fetch(k, k_bytes, n_keys);
+    vl.fetch(v, v_bytes, n_keys);
     for (int key0 = 0; key0 < n_keys; key0 += 2 * kKeyTile) {
       step(key0, tiles[0][0], tiles[0][1], kind);
       if (key0 + kKeyTile < n_keys) step(key0 + kKeyTile, tiles[1][0], tiles[1][1], kind);
@@ -496,7 +508,8 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
   const int wave_first = a.causal ? wave_key - s.ahead : 0;            // the first query that sees the wavefront's first key
   const int tile_all = a.causal ? tile_key + kDkvKeys - 1 - s.ahead : 0;
   const int wave_all = a.causal ? wave_key + 31 - s.ahead : 0;         // queries from here on see all its keys
-  const uint16_t *q = a.q + s.q0 * a.q_stride + head * a.group * D, *d = a.dout + s.q0 * a.dout_stride + head * a.group * D;
+  const char *q = (const char*)(a.q + s.q0 * a.q_stride + head * a.group * D), *d = (const char*)(a.dout + s.q0 * a.dout_stride + head * a.group * D);
+  const int q_bytes = (int)a.q_stride * 2, d_bytes = (int)a.dout_stride * 2;
   const float *lse = a.lse + (int64_t)head * a.group * a.n_q + s.q0, *delta = a.delta + (int64_t)head * a.group * a.n_q + s.q0;
   const float to_log2 = a.scale * kLog2E;
 
@@ -508,8 +521,8 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
   int next_query, next_head, query = 0, head_of_group = 0;
   const int query_step = kDkvRows / a.group, head_step = kDkvRows - query_step * a.group;
   auto fetch = [&](int row0) __attribute__((always_inline)) {
-    ql.fetch_grouped(q, a.q_stride, a.group, a.group_inverse, next_query, next_head, n_rows - row0);
-    dl.fetch_grouped(d, a.dout_stride, a.group, a.group_inverse, next_query, next_head, n_rows - row0);
+    ql.fetch_grouped(q + (int64_t)next_query * q_bytes, q_bytes, a.group, a.group_inverse, next_head, n_rows - row0);
+    dl.fetch_grouped(d + (int64_t)next_query * d_bytes, d_bytes, a.group, a.group_inverse, next_head, n_rows - row0);
     if (threadIdx.x < kDkvRows) {
       const int at = next_head + threadIdx.x, of = small_quotient(at, a.group, a.group_inverse), t = next_query + of;
       row_shift = INFINITY;                  // probability 0: rows past the end, and rows that see no key
