@@ -523,13 +523,17 @@ nat_status nat_attn_decode(const nat_kv_cache* cache, const void* d_q, int64_t q
  *   d_ids [n_rows] int32 out;
  *   d_logp [n_rows] float out or NULL: log soft-max of the logits at the token (temperature 1, whole vocabulary): the
  *                behaviour log-prob that nat_loss_fwd_bwd takes as d_old_logp;
- *   d_logq [n_rows] float out or NULL: log of the probability with which the token was drawn.
+ *   d_logq [n_rows] float out or NULL: log of the probability with which the token was drawn;
+ *   d_ws / ws_bytes: at least nat_sample_workspace_bytes, 256-byte aligned; 0 for as many rows as fill the chip.
+ * 2^y is taken to a relative error of 2^-44 before it is rounded to a weight.
  * Errors: NULL required pointer, n_rows < 0, logits not aligned to their element -> NAT_INVALID_ARG; V outside [1, 2^20],
- * 0 < row_stride < V -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE.
+ * 0 < row_stride < V -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE; NAT_WORKSPACE_TOO_SMALL.
  */
+size_t nat_sample_workspace_bytes(int32_t n_rows, int32_t V, int32_t dtype);
 nat_status nat_sample(const void* d_logits, int64_t row_stride, int32_t n_rows, int32_t V, int32_t dtype,
                       const uint32_t* d_random, const float* d_temperature, const int32_t* d_top_k, const float* d_top_p,
-                      const float* d_min_p, int32_t* d_ids, float* d_logp, float* d_logq, void* stream);
+                      const float* d_min_p, int32_t* d_ids, float* d_logp, float* d_logq, void* d_ws, size_t ws_bytes,
+                      void* stream);
 
 /*
  * Per-kernel timing (measurement aid, off by default).  When enabled, every

@@ -132,7 +132,9 @@ def load_library():
     lib.nat_attn_decode.restype = i32
     lib.nat_attn_decode.argtypes = [pc, vp, i64, i32, i32, vp, i32, vp, f32, vp, i64, vp, vp, sz, vp]
     lib.nat_sample.restype = i32
-    lib.nat_sample.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.nat_sample.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.nat_sample_workspace_bytes.restype = sz
+    lib.nat_sample_workspace_bytes.argtypes = [i32, i32, i32]
     lib.nat_probe_mfma_scratch_bytes.restype = sz
     lib.nat_probe_mfma_scratch_bytes.argtypes = []
     lib.nat_probe_mfma_bf16.restype = i32
@@ -452,7 +454,11 @@ def nat_attn_decode(cache, q, block_table, seq_lens, scale, out, lse, workspace)
         workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_attn_decode")
 
 
-def nat_sample(logits, random, temperature, top_k, top_p, min_p, ids_out, logp_out=None, logq_out=None):
+def sample_workspace_bytes(n_rows, V, dtype):
+    return int(load_library().nat_sample_workspace_bytes(int(n_rows), int(V), int(dtype)))
+
+
+def nat_sample(logits, random, temperature, top_k, top_p, min_p, ids_out, logp_out=None, logq_out=None, workspace=None):
     """logits [rows, V] float32 or bfloat16 (any row stride), random int32 [rows] (the 32 bits are read as unsigned); temperature,
     top_p, min_p float32 [rows] and top_k int32 [rows], each or None; ids int32, logp and logq float32 [rows] out."""
     if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
@@ -465,7 +471,8 @@ def nat_sample(logits, random, temperature, top_k, top_p, min_p, ids_out, logp_o
         _vector(temperature, torch.float32, n, "temperature"), _vector(top_k, torch.int32, n, "top_k"),
         _vector(top_p, torch.float32, n, "top_p"), _vector(min_p, torch.float32, n, "min_p"),
         _vector(ids_out, torch.int32, n, "ids_out"), _vector(logp_out, torch.float32, n, "logp_out"),
-        _vector(logq_out, torch.float32, n, "logq_out"), _stream()), "nat_sample")
+        _vector(logq_out, torch.float32, n, "logq_out"), _ptr(workspace),
+        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_sample")
 
 
 def probe_mfma_scratch_bytes():

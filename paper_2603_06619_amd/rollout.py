@@ -81,5 +81,6 @@ class RolloutStage:
         n = logits.shape[0]
         new = lambda dt: torch.empty(n, dtype=dt, device=logits.device)
         out = dict(ids=new(torch.int32), logp=new(torch.float32), logq=new(torch.float32))
-        nb.nat_sample(logits, random, temperature, top_k, top_p, min_p, out["ids"], out["logp"], out["logq"])
+        ws = self._buf("sample", nb.sample_workspace_bytes(n, logits.shape[1], nb._dtype_code(logits)))
+        nb.nat_sample(logits, random, temperature, top_k, top_p, min_p, out["ids"], out["logp"], out["logq"], ws)
         return out

@@ -251,6 +251,7 @@ def test_a_step_replays_from_a_graph(stage):
     place = [(l - 1) for l in lens]                  # the last token's slot is rewritten
     slots = torch.tensor([int(c["table"][i, p // 32]) * 32 + p % 32 for i, p in enumerate(place)], device=DEV)
     ws = torch.empty(max(nat.attn_decode_workspace_bytes(2, 8, 2, D, 32 * 32), 256), dtype=torch.uint8, device=DEV)
+    sample_ws = torch.empty(max(nat.sample_workspace_bytes(2, V, nat.DTYPE_F32), 256), dtype=torch.uint8, device=DEV)
     new = lambda: dict(out=torch.empty_like(bufs["q"]), lse=torch.empty((2, 8), device=DEV), ids=torch.empty(2, dtype=torch.int32, device=DEV),
                        logp=torch.empty(2, device=DEV), logq=torch.empty(2, device=DEV), logits=torch.empty((2, V), device=DEV))
 
@@ -258,7 +259,7 @@ def test_a_step_replays_from_a_graph(stage):
         nat.nat_kv_write(cache, bufs["k"], bufs["v"], slots)
         nat.nat_attn_decode(cache, bufs["q"], c["table"], c["lens"], D ** -0.5, o["out"], o["lse"], ws)
         torch.mm(o["out"].flatten(1).float(), head, out=o["logits"])
-        nat.nat_sample(o["logits"], bufs["word"], None, None, None, None, o["ids"], o["logp"], o["logq"])
+        nat.nat_sample(o["logits"], bufs["word"], None, None, None, None, o["ids"], o["logp"], o["logq"], sample_ws)
     o = new()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())

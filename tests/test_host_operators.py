@@ -128,12 +128,16 @@ def test_decode_refusals(nat):
 def test_sample_refusals(nat):
     lib = nat.load_library()
 
-    def call(logits=fake, stride=0, n=3, V=1000, dtype=1, word=fake, ids=fake):
-        return lib.nat_sample(logits, stride, n, V, dtype, word, None, None, None, None, ids, None, None, None)
+    def call(logits=fake, stride=0, n=3, V=1000, dtype=1, word=fake, ids=fake, ws=fake, ws_bytes=1 << 30):
+        return lib.nat_sample(logits, stride, n, V, dtype, word, None, None, None, None, ids, None, None, ws, ws_bytes, None)
     assert call(dtype=5) == DTYPE
     assert call(n=-1) == call(logits=None) == call(word=None) == call(ids=None) == call(logits=fake + 1) == call(logits=fake + 2, dtype=0) == INVALID
     assert call(V=0) == call(V=-3) == call(V=(1 << 20) + 1) == call(stride=999) == call(stride=-1) == SHAPE
     assert call(n=0, logits=None, word=None, ids=None) == OK
+    need = nat.sample_workspace_bytes(3, 150000, nat.DTYPE_BF16)
+    assert need > 0 and need % 256 == 0 and nat.sample_workspace_bytes(1000, 150000, nat.DTYPE_BF16) == 0
+    assert call(V=150000, ws=None) == call(V=150000, ws_bytes=need - 1) == WORKSPACE and call(V=150000, ws=fake + 128) == INVALID
+    assert nat.sample_workspace_bytes(0, 10, 0) == nat.sample_workspace_bytes(5, 0, 0) == nat.sample_workspace_bytes(5, 10, 3) == 0
 
 
 def test_binding_refuses_what_the_library_cannot_see(nat):
