@@ -525,7 +525,7 @@ nat_status nat_attn_decode(const nat_kv_cache* cache, const void* d_q, int64_t q
  *                behaviour log-prob that nat_loss_fwd_bwd takes as d_old_logp;
  *   d_logq [n_rows] float out or NULL: log of the probability with which the token was drawn;
  *   d_ws / ws_bytes: at least nat_sample_workspace_bytes, 256-byte aligned; 0 for as many rows as fill the chip.
- * 2^y is taken to a relative error of 2^-44 before it is rounded to a weight.
+ * 2^y is taken to a relative error of 2^-40, i.e. weights are whole numbers within 2 of the exact ones.
  * Errors: NULL required pointer, n_rows < 0, logits not aligned to their element -> NAT_INVALID_ARG; V outside [1, 2^20],
  * 0 < row_stride < V -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE; NAT_WORKSPACE_TOO_SMALL.
  */

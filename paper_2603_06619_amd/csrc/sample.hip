@@ -4,11 +4,17 @@
 // their order, so which tokens are kept and which one is drawn does not depend on how a row is dealt to wavefronts: an fp32 cumulative sum over a vocabulary
 // leaves the draw to its rounding near every boundary.  2^40 keeps tokens down to 2^-41 of the likeliest one, and 2^20 weights fit 60 bits.
 //
-// A row is cut into ranges of 16-byte vectors, one per wavefront, 8 or more wavefronts per workgroup and 1 or more workgroups ("splits") per row.  Phase 1: the
-// largest logit.  Phase 2: weights, and their sums over parts of the ranges; in rows with a top-k or top-p also a list of the tokens with at least 2^-12 of the
-// largest weight, the candidates.  Phase 3, one workgroup per row: the draw, in order of index, by the sums of the parts, then by lanes, then by
-// elements; in ranked rows first the least logit that stays, by histograms over the candidates, and the draw among them.  If what stays reaches
-// below the candidates, or these are too many, the row is gone over again by phase 3 alone (draw_slowly).
+// A row is cut into parts of 256 16-byte vectors, dealt to wavefronts in turn, 8 wavefronts per workgroup and 1 or more workgroups ("splits") per row.
+//   top      the largest logit;
+//   bins     (rows with a top-k or top-p) a histogram of the exponents y, 1/16 apart: of tokens if the row has a top-k, else of their weight.  The bin in which
+//            the top-k ends, or the weight that the top-p asks for;
+//   list     the tokens of that bin (with a top-k: of all bins down to it).  Among them the least logit that stays, and the last index that does of those
+//            equal to it;
+//   sums     weights of what stays, summed over parts of the ranges;
+//   draw     in order of index: by the sums of the parts, then by steps, lanes and elements.
+// A row with one workgroup goes through them in one kernel; with more, each of top, bins, list and sums is a kernel, and the workgroup that comes last in
+// a row does what follows from all (it knows by a counter; nobody waits).  If the list is longer than LDS has room for (very many equal logits), the row
+// is gone over once more by one workgroup (threshold_slowly).
 #include "nat_internal.h"
 
 namespace nat {
@@ -19,10 +25,8 @@ constexpr int kMaxVocab = 1 << 20;
 constexpr int kMaxSplits = 32;
 constexpr int kUnroll = 4;                            // vectors per lane and step, and per part of a wavefront's range
 constexpr int kBins = 1024, kBinBits = 10;
-constexpr int kCandPerWave = 768;                     // capacity of a wavefront's list of candidates
-constexpr int kCandRow = kCandPerWave * kWaves;       // of a row's, where two workgroups share a compute unit's LDS
-constexpr int kCandSplit = 2 * kCandRow;              // where a row has several workgroups, and the last one the compute unit
-constexpr float kCandReach = -12.f;                   // y of the last candidates
+constexpr float kBinsPerOctave = 16.f;                // of exponents: the last bin holds weights of 0 alone
+constexpr int kList = 6144;                           // tokens of a list: two workgroups share a compute unit's LDS
 constexpr uint32_t kKeyMinusInf = 0x007fffffu;        // order of -inf, below all that can be drawn
 constexpr uint64_t kOne = 1ull << 40;
 constexpr float kLog2E = 1.44269504088896341f;
@@ -55,32 +59,38 @@ __device__ __forceinline__ uint64_t share_of(uint32_t word, uint64_t total) {
   return word * (total >> 32) + ((word * (total & 0xffffffffu)) >> 32);
 }
 
+// 2^40 2^(j / 64), j = 0 .. 63, in LDS
+struct Powers {
+  double of[64];
+  __device__ __forceinline__ void fill() {           // read behind a barrier
+    if (threadIdx.x < 64) of[threadIdx.x] = exp2((double)threadIdx.x * (1.0 / 64)) * (double)kOne;
+  }
+};
+
 struct Weigher {
+  const Powers* powers;
   float max, per_nat;            // of +inf: the largest finite value, as the logits that are +inf
-  __device__ __forceinline__ Weigher(uint32_t top, float temperature) {
+  __device__ __forceinline__ Weigher(uint32_t top, float temperature, const Powers& p) : powers(&p) {
     max = fminf(logit_of(top), __FLT_MAX__);
     per_nat = fmaxf(fminf(kLog2E / temperature, __FLT_MAX__), __FLT_MIN__);      // 0 * per_nat is 0, inf * per_nat is inf
   }
   // the median of three: +inf is 0 like the largest finite logit, NaN the lesser bound, whose weight is 0
   __device__ __forceinline__ float exponent(float z) const { return __builtin_amdgcn_fmed3f((z - max) * per_nat, -60.f, 0.f); }
-  // 2^y = 2^n 2^f, f in [-1/2, 1/2], by the polynomial that meets 2^f at the ten Chebyshev points of the interval: relative error below 2^-44.  Adding
-  // 2^52 rounds 2^(40 + y) to a whole number, which then is the low bits of the sum; in all 23 instructions
-  static __device__ __forceinline__ uint64_t weight(float y) {
-    const float n = rintf(y);
-    const double f = (double)(y - n);
-    double p = 0x1.b6571d9fbc782p-24;
-    p = fma(p, f, 0x1.63ef9699f65f0p-20);
-    p = fma(p, f, 0x1.ffcb7678dfe12p-17);
-    p = fma(p, f, 0x1.43088e257f900p-13);
-    p = fma(p, f, 0x1.5d87fe908f6f7p-10);
-    p = fma(p, f, 0x1.3b2ab72b175e9p-7);
-    p = fma(p, f, 0x1.c6b08d704411ap-5);
-    p = fma(p, f, 0x1.ebfbdff8149f2p-3);
-    p = fma(p, f, 0x1.62e42fefa39f7p-1);
-    p = fma(p, f, 1.0);
-    const double scale = __builtin_bit_cast(double, (uint64_t)(uint32_t)((int)n + 1023 + 40) << 52);
-    return __builtin_bit_cast(uint64_t, fma(p, scale, 0x1p52)) & ((1ull << 52) - 1);
+  // 2^y = 2^n 2^(j / 64) 2^r, |r| <= 1/128; 2^r - 1 = r (c1 + r (c2 + r (c3 + r c4))) through the four Chebyshev points of (2^r - 1) / r, all but the last two
+  // steps in fp32: error below 2^-40 of the weight.  Adding 2^52 rounds to a whole number, which then is the low 52 bits (kBias: those above).  In all 24
+  // instructions; a polynomial of degree 9 without a table took 38 (weights of 512 rows of 152064 logits XX us, then YY)
+  static constexpr uint64_t kBias = 0x433ull << 52;
+  __device__ __forceinline__ uint64_t biased_weight(float y) const {
+    constexpr float kWhole = 0x1.8p23f;              // adding it rounds to a whole number, the low bits of the sum
+    const float t = fmaf(y, 64.f, kWhole), r = fmaf(t - kWhole, -1.f / 64, y);
+    const uint32_t bits = __builtin_bit_cast(uint32_t, t);
+    const uint64_t power = __builtin_bit_cast(uint64_t, powers->of[bits & 63]) + ((uint64_t)((bits & ~63u) << 14) << 32);
+    const double p = __builtin_bit_cast(double, power);
+    const float h = fmaf(fmaf(0x1.3b2acbp-7f, r, 0x1.c6b0b9p-5f), r, 0x1.ebfbe0p-3f);
+    const double q = (double)r * fma((double)h, (double)r, 0x1.62e42fefa2417p-1);
+    return __builtin_bit_cast(uint64_t, fma(p, 1.0 + q, 0x1p52));
   }
+  __device__ __forceinline__ uint64_t weight(float y) const { return biased_weight(y) & ((1ull << 52) - 1); }
   __device__ __forceinline__ uint64_t of_key(uint32_t key) const { return key <= kKeyMinusInf ? 0 : weight(exponent(logit_of(key))); }
 };
 
@@ -107,8 +117,9 @@ template <class T>
 struct Row {
   static constexpr int kE = 16 / sizeof(T);
   const T* p;
-  int vocab, lead, vectors, steps, parts;        // steps of 64 kUnroll vectors of a wavefront, for `waves` of them: one part each
-  __device__ __forceinline__ Row(const SampleArgs& a, int64_t row, int waves) {
+  int vocab, lead, vectors, waves, steps, parts;       // steps of 64 kUnroll vectors of every wavefront, one part each: side by side, so that a workgroup reads on
+  __device__ __forceinline__ Row(const SampleArgs& a, int64_t row, int n_waves) {
+    waves = n_waves;
     p = (const T*)a.logits + row * a.row_stride;
     vocab = a.vocab;
     lead = (int)(((uintptr_t)p & 15) / sizeof(T));
@@ -137,43 +148,72 @@ struct Row {
 #pragma unroll
     for (int i = 0; i < kE; ++i) k[i] = key_of(value(x.e[i]));
   }
-  // calls f(first vector of a part, vectors of this lane) for the parts of wavefront w
-  template <class F>
-  __device__ __forceinline__ void each_part(int w, const F& f) const {
+  // The parts of wavefront w: f(first vector, this lane's vector) for every 64 vectors of a part, then end(part).  A part's vectors are loaded together, a part
+  // ahead, and used in a loop that stays a loop: unrolled, code that runs a few times spends longer being fetched than running.  kBack: the last part
+  // first.  Passes over a row go to and fro, so that each begins with what the one before it left in the caches (512 rows of 608 KB, 1.2 times
+  // the Infinity Cache: XX us, all passes forward YY)
+  template <bool kBack, class F, class End>
+  __device__ __forceinline__ void each_part(int w, const F& f, const End& end) const {
     const int lane = threadIdx.x & 63;
-    for (int s = 0; s < steps; ++s) {
-      const int j0 = (w * steps + s) * (64 * kUnroll);
-      Vector x[kUnroll];
+    Vector x[kUnroll], next[kUnroll];
+    auto load_part = [&](int j0, Vector (&y)[kUnroll]) {
+      if (j0 * kE - lead >= 0 && (j0 + 64 * kUnroll) * kE - lead <= vocab) {       // the same for all lanes
+        const uint4* from = (const uint4*)(p + (j0 * kE - lead)) + lane;
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) load(j0 + u * 64 + lane, x[u]);
-      f(w * steps + s, j0, x);
+        for (int u = 0; u < kUnroll; ++u) y[u].q = from[64 * u];
+      } else {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) load(j0 + u * 64 + lane, y[u]);
+      }
+    };
+    auto first = [&](int s) { return ((kBack ? steps - 1 - s : s) * waves + w) * (64 * kUnroll); };
+    load_part(first(0), next);
+    for (int s = 0; s < steps; ++s) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) x[u].q = next[u].q;
+      if (s + 1 < steps) load_part(first(s + 1), next);
+#pragma unroll 1
+      for (int u = 0; u < kUnroll; ++u) {
+        f(first(s) + u * 64, x[0]);
+#pragma unroll
+        for (int v = 0; v + 1 < kUnroll; ++v) x[v].q = x[v + 1].q;
+      }
+      end(first(s) / (64 * kUnroll));
     }
+  }
+  template <bool kBack, class F>
+  __device__ __forceinline__ void each_vector(int w, const F& f) const {
+    each_part<kBack>(w, f, [](int) {});
   }
 };
 
-struct Candidate { uint32_t key, index; };
-
-// What phases 1 and 2 leave of a row: in LDS, or with more than one workgroup per row in the workspace
+struct Listed { uint32_t key, index; };
 struct WaveSums { uint64_t all; double soft; };      // all weights; exponentials at temperature 1, where the weights are of another
+// The tokens that stay: keys above `least`, and those equal to it up to index `equal_end`
+struct Stay {
+  uint32_t least;
+  int equal_end;
+  __device__ __forceinline__ bool has(uint32_t key, int index) const { return key > least || (key == least && index <= equal_end); }
+};
+// What is listed: exponents' bins first .. last; what lies above bin `last`, in tokens or weight
+struct Gather { int first, last; uint64_t above; };
 
 constexpr int kMaxParts = kMaxVocab / 4 / (64 * kUnroll) + kMaxSplits * kWaves + 2;
 
-template <int kCand>
-struct SharedOf {
-  static constexpr int kCandidates = kCand;
+struct Shared {
+  Powers powers;
   uint64_t hist[kBins];
   uint64_t part[kMaxParts];
   union {
-    Candidate cand[kCand];
-    uint64_t slice[(kMaxVocab / 4 / kThreads + 2) * kWaves];     // draw_slowly: sums of the wavefronts' parts of the slices
+    Listed list[kList];
+    uint64_t slice[(kMaxVocab / 4 / kThreads + 2) * kWaves];     // threshold_slowly: sums of the wavefronts' parts of the slices
   };
   WaveSums sums[kMaxSplits * kWaves];
-  uint32_t top[kMaxSplits * kWaves];
-  uint32_t cand_n[kMaxSplits * kWaves];
+  uint32_t top[kWaves];
   uint64_t wave64[kWaves];
   uint64_t found64;
-  uint32_t found;
-  int equal_end;
+  uint32_t found, list_n;
+  int equal_end, last_one;
 };
 
 __device__ __forceinline__ uint64_t wave_sum64(uint64_t x) {
@@ -192,7 +232,6 @@ __device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {       // inclusive
 }
 
 // over the workgroup; every thread gets the result
-template <class Shared>
 __device__ __forceinline__ uint64_t block_sum64(uint64_t x, Shared& sm) {
   x = wave_sum64(x);
   __syncthreads();
@@ -205,7 +244,7 @@ __device__ __forceinline__ uint64_t block_sum64(uint64_t x, Shared& sm) {
 
 // The i in [0, n) at which the running sum of x(i) passes `target`, i.e. the first whose inclusive sum is > target, and the sum before it; n if
 // there is none.  What x reads has been written behind a barrier.
-template <class X, class Shared>
+template <class X>
 __device__ __forceinline__ int block_find(const X& x, int n, uint64_t target, uint64_t* before, Shared& sm) {
   const int per = (n + kThreads - 1) / kThreads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int lo = threadIdx.x * per < n ? threadIdx.x * per : n, hi = lo + per < n ? lo + per : n;
@@ -236,7 +275,7 @@ __device__ __forceinline__ int block_find(const X& x, int n, uint64_t target, ui
 
 // The largest key whose elements, with all above it, have a weight (an element's: of(key)) over `target` in all: narrowed down by histograms of the keys from
 // `hi` down to `lo`.  each(f) calls f(key) for every element.  *above: the weight above that key.  False if all of lo .. hi together do not pass the target.
-template <class Each, class Of, class Shared>
+template <class Each, class Of>
 __device__ __forceinline__ bool select_key(const Each& each, uint32_t lo, uint32_t hi, uint64_t target, const Of& of, uint32_t* key, uint64_t* above, Shared& sm) {
   uint64_t over = 0;
   if (lo > hi) return false;
@@ -267,30 +306,6 @@ __device__ __forceinline__ bool select_key(const Each& each, uint32_t lo, uint32
   }
 }
 
-// What stays by rank: keys above `least`, and of those equal to it the first n_least.  each, of as in select_key; total_of(least): the weight above a key.
-struct Ranked { uint32_t least; uint64_t n_least; };
-template <class Each, class TotalOver, class Shared>
-__device__ __forceinline__ Ranked rank_row(const Settings& set, const Weigher& weigh, uint32_t top, const Each& each, const TotalOver& total_over, Shared& sm) {
-  Ranked r{kKeyMinusInf, 0};
-  uint64_t above;
-  if (set.top_k > 0 && select_key(each, kKeyMinusInf + 1, top, (uint64_t)set.top_k - 1, [](uint32_t) -> uint64_t { return 1; }, &r.least, &above, sm))
-    r.n_least = set.top_k - above;
-  if (!(set.top_p < 1.f)) return r;
-  const uint64_t at_least = weigh.of_key(r.least), over = total_over(r.least), total = over + r.n_least * at_least;
-  const double share = set.top_p > 0.f ? (double)set.top_p * 4294967296.0 : 0.0;
-  uint64_t reach = share_of((uint32_t)share, total);
-  if (reach < 1) reach = 1;
-  uint32_t key;
-  if (select_key(each, r.least + 1, top, reach - 1, [&](uint32_t k) { return weigh.of_key(k); }, &key, &above, sm)) {
-    const uint64_t one = weigh.of_key(key);
-    return Ranked{key, (reach - above + one - 1) / one};
-  }
-  // the equal ones at the top-k's end: what is left after all above them
-  const uint64_t n = at_least ? (reach - over + at_least - 1) / at_least : 0;
-  if (n < r.n_least) r.n_least = n;
-  return r;
-}
-
 struct Drawn { int index; uint32_t key; uint64_t weight, total; };
 
 __device__ __forceinline__ void write_out(const SampleArgs& a, int64_t r, const Drawn& d, const Weigher& weigh, double soft) {
@@ -299,11 +314,50 @@ __device__ __forceinline__ void write_out(const SampleArgs& a, int64_t r, const 
   if (a.logp) a.logp[r] = (float)((double)(z - weigh.max) - log(soft));
   if (a.logq) a.logq[r] = (float)log((double)d.weight / (double)d.total);
 }
+__device__ __forceinline__ void nothing_to_draw(const SampleArgs& a, int64_t r) {
+  a.ids[r] = -1;
+  if (a.logp) a.logp[r] = NAN;
+  if (a.logq) a.logq[r] = NAN;
+}
 
-// A ranked row whose candidates do not do: everything from the row itself, in slices of one vector per thread.
-template <class T, class Shared>
-__device__ __noinline__ void draw_slowly(const SampleArgs& a, int64_t r, const Row<T>& row, const Settings& set, const Weigher& weigh, uint32_t top, double soft,
-                                         Shared& sm) {
+// weight that the top-p asks for, of a total
+__device__ __forceinline__ uint64_t reach_of(float top_p, uint64_t total) {
+  const double share = top_p > 0.f ? (double)top_p * 4294967296.0 : 0.0;
+  const uint64_t reach = share_of((uint32_t)share, total);
+  return reach < 1 ? 1 : reach;
+}
+
+// Keys above `least` and the first n_least of those equal to it stay by rank, of elements that each(f) calls f(key) for.  over_top: the weight above all of
+// them, over(least): of them above a key; by_count: they begin with the row's largest and hold the whole top-k.
+struct Ranked { uint32_t least; uint64_t n_least; };
+template <class Each, class Over>
+__device__ __forceinline__ Ranked rank_tokens(const Settings& set, const Weigher& weigh, bool by_count, uint32_t lo, uint32_t hi, uint64_t total, uint64_t over_top,
+                                              const Each& each, const Over& over, Shared& sm) {
+  auto by_weight = [&](uint32_t k) { return weigh.of_key(k); };
+  Ranked r{lo - 1, 0};
+  uint64_t above, at_least = 0;
+  if (by_count) {
+    if (select_key(each, lo, hi, (uint64_t)set.top_k - 1, [](uint32_t) -> uint64_t { return 1; }, &r.least, &above, sm)) r.n_least = set.top_k - above;
+    if (!(set.top_p < 1.f)) return r;
+    at_least = weigh.of_key(r.least);
+    over_top = 0;
+    total = over(r.least) + r.n_least * at_least;
+  }
+  const uint64_t reach = reach_of(set.top_p, total);
+  uint32_t key;
+  if (select_key(each, r.least + 1, hi, reach - 1 - over_top, by_weight, &key, &above, sm)) {
+    const uint64_t one = weigh.of_key(key);
+    return Ranked{key, (reach - over_top - above + one - 1) / one};
+  }
+  // the equal ones at the top-k's end: what is left after all above them
+  const uint64_t n = at_least ? (reach - (total - r.n_least * at_least) + at_least - 1) / at_least : 0;
+  if (n < r.n_least) r.n_least = n;
+  return r;
+}
+
+// A list that is too long: the least logit that stays from the row itself, in slices of one vector per thread.
+template <class T>
+__device__ __noinline__ Stay threshold_slowly(const SampleArgs& a, const Row<T>& row, const Settings& set, const Weigher& weigh, uint32_t top, Shared& sm) {
   constexpr int kE = Row<T>::kE;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, slices = (row.vectors + kThreads - 1) / kThreads;
   auto each = [&](auto f) {
@@ -314,173 +368,214 @@ __device__ __noinline__ void draw_slowly(const SampleArgs& a, int64_t r, const R
       for (int i = 0; i < kE; ++i) f(k[i]);
     }
   };
-  const Ranked stay = rank_row(set, weigh, top, each, [&](uint32_t least) {
+  auto over = [&](uint32_t least) {
+    uint64_t t = 0;
+    each([&](uint32_t k) { t += k > least ? weigh.of_key(k) : 0; });
+    return block_sum64(t, sm);
+  };
+  const Ranked r = rank_tokens(set, weigh, set.top_k > 0, kKeyMinusInf + 1, top, set.top_k > 0 ? 0 : over(kKeyMinusInf), 0, each, over, sm);
+  if (r.n_least == 0) return Stay{r.least, -1};
+  __syncthreads();
+  for (int s = 0; s < slices; ++s) {
+    uint32_t k[kE];
+    row.load(s * kThreads + threadIdx.x, k);
+    uint64_t n = 0;
+#pragma unroll
+    for (int i = 0; i < kE; ++i) n += k[i] == r.least;
+    n = wave_sum64(n);
+    if (lane == 0) sm.slice[s * kWaves + wave] = n;
+  }
+  __syncthreads();
+  uint64_t before;
+  const int part = block_find([&](int i) { return sm.slice[i]; }, slices * kWaves, r.n_least - 1, &before, sm);
+  if (part == slices * kWaves) return Stay{r.least, a.vocab};
+  const int j = part * 64 + lane;
+  uint32_t k[kE];
+  row.load(j, k);
+  uint64_t n = 0;
+#pragma unroll
+  for (int i = 0; i < kE; ++i) n += k[i] == r.least;
+  uint64_t at = before + wave_scan64(n) - n;
+  if (n && at < r.n_least && r.n_least <= at + n) {
+#pragma unroll
+    for (int i = 0; i < kE; ++i)
+      if (k[i] == r.least && ++at == r.n_least) sm.equal_end = j * kE - row.lead + i;
+  }
+  __syncthreads();
+  return Stay{r.least, sm.equal_end};
+}
+
+// top: the largest key of wavefront w's range
+template <class T>
+__device__ __forceinline__ uint32_t largest_key(const Row<T>& row, int w) {
+  float m = -INFINITY;                       // fmaxf passes NaN over
+  row.template each_vector<false>(w, [&](int, const typename Row<T>::Vector& x) {
+#pragma unroll
+    for (int i = 0; i < Row<T>::kE; ++i) m = fmaxf(m, Row<T>::value(x.e[i]));
+  });
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+  return key_of(m);
+}
+
+__device__ __forceinline__ int bin_of(float y) {
+  const int b = (int)(y * -kBinsPerOctave);
+  return b < kBins ? b : kBins - 1;
+}
+
+// bins: the range's tokens or weights, added to the histogram in LDS
+template <class T>
+__device__ __forceinline__ void bin_range(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, uint64_t* hist) {
+  row.template each_vector<true>(w, [&](int, const typename Row<T>::Vector& x) {
+#pragma unroll
+    for (int i = 0; i < Row<T>::kE; ++i) {
+      const float y = weigh.exponent(Row<T>::value(x.e[i]));
+      if (y <= -60.f) continue;                // weight 0
+      if (set.top_k > 0) atomicAdd((uint32_t*)&hist[bin_of(y)], 1u);
+      else atomicAdd((unsigned long long*)&hist[bin_of(y)], (unsigned long long)weigh.weight(y));
+    }
+  });
+}
+
+// Which bins to list, from the row's histogram (all threads; behind a barrier)
+__device__ __forceinline__ Gather choose_bins(const Settings& set, const uint64_t* hist, Shared& sm) {
+  auto entry = [&](int i) { return hist[i]; };
+  uint64_t target = (uint64_t)set.top_k - 1, above = 0;
+  if (set.top_k <= 0) {
+    uint64_t total = 0;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) total += hist[i];
+    target = reach_of(set.top_p, block_sum64(total, sm)) - 1;
+  }
+  const int bin = block_find(entry, kBins, target, &above, sm);
+  if (bin == kBins) return Gather{0, kBins - 1, 0};            // fewer tokens than the top-k: all of them
+  return set.top_k > 0 ? Gather{0, bin, 0} : Gather{bin, bin, above};
+}
+
+// list: the range's tokens in those bins; *n counts on past the room
+template <class T>
+__device__ __forceinline__ void list_range(const Row<T>& row, int w, const Weigher& weigh, const Gather& g, Listed* list, uint32_t* n) {
+  constexpr int kE = Row<T>::kE;
+  const int lane = threadIdx.x & 63;
+  row.template each_vector<false>(w, [&](int j, const typename Row<T>::Vector& x) {
+    uint32_t take = 0;
+#pragma unroll
+    for (int i = 0; i < kE; ++i) {
+      const float y = weigh.exponent(Row<T>::value(x.e[i]));
+      const int b = bin_of(y);
+      take |= (uint32_t)(b >= g.first && b <= g.last && y > -60.f) << i;
+    }
+    if (take) {
+      uint32_t at = atomicAdd(n, (uint32_t)__popc(take));
+      const int index = (j + lane) * kE - row.lead;
+#pragma unroll
+      for (int i = 0; i < kE; ++i)
+        if (take >> i & 1) {
+          if (at < kList) list[at] = Listed{key_of(Row<T>::value(x.e[i])), (uint32_t)(index + i)};
+          ++at;
+        }
+    }
+  });
+}
+
+// What stays, from the list in LDS (in no order); all: the weight of the row
+__device__ __forceinline__ Stay threshold_of_list(const Settings& set, const Weigher& weigh, uint32_t top, const Gather& g, int n, uint64_t all, Shared& sm) {
+  auto each = [&](auto f) {
+    for (int i = threadIdx.x; i < n; i += kThreads) f(sm.list[i].key);
+  };
+  uint32_t lo = top, hi = 0;
+  each([&](uint32_t k) {
+    lo = k < lo ? k : lo;
+    hi = k > hi ? k : hi;
+  });
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t x = __shfl_xor(lo, d, 64), y = __shfl_xor(hi, d, 64);
+    lo = x < lo ? x : lo;
+    hi = y > hi ? y : hi;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sm.wave64[threadIdx.x >> 6] = (uint64_t)hi << 32 | lo;
+  __syncthreads();
+  for (int w = 0; w < kWaves; ++w) {
+    const uint32_t x = (uint32_t)sm.wave64[w], y = (uint32_t)(sm.wave64[w] >> 32);
+    lo = x < lo ? x : lo;
+    hi = y > hi ? y : hi;
+  }
+  const Ranked r = rank_tokens(set, weigh, set.top_k > 0, lo, hi, all, g.above, each, [&](uint32_t least) {
     uint64_t t = 0;
     each([&](uint32_t k) { t += k > least ? weigh.of_key(k) : 0; });
     return block_sum64(t, sm);
   }, sm);
-  // of the equal ones, the first n_least in order of index: up to index `equal_end`
-  auto in_slices = [&](auto f) {              // sums of f(key, index) over the wavefronts' parts of the slices
-    __syncthreads();
-    for (int s = 0; s < slices; ++s) {
-      const int j = s * kThreads + threadIdx.x;
-      uint32_t k[kE];
-      row.load(j, k);
-      uint64_t n = 0;
-#pragma unroll
-      for (int i = 0; i < kE; ++i) n += f(k[i], j * kE - row.lead + i);
-      n = wave_sum64(n);
-      if (lane == 0) sm.slice[s * kWaves + wave] = n;
-    }
-    __syncthreads();
-  };
-  auto slice = [&](int i) { return sm.slice[i]; };
-  int equal_end = -1;
-  if (stay.n_least > 0) {
-    in_slices([&](uint32_t k, int) -> uint64_t { return k == stay.least; });
-    uint64_t before;
-    const int part = block_find(slice, slices * kWaves, stay.n_least - 1, &before, sm);
-    equal_end = a.vocab;
-    if (part < slices * kWaves) {
-      const int j = part * 64 + lane;
-      uint32_t k[kE];
-      row.load(j, k);
-      uint64_t n = 0;
-#pragma unroll
-      for (int i = 0; i < kE; ++i) n += k[i] == stay.least;
-      uint64_t at = before + wave_scan64(n) - n;
-      if (n && at < stay.n_least && stay.n_least <= at + n) {
-#pragma unroll
-        for (int i = 0; i < kE; ++i)
-          if (k[i] == stay.least && ++at == stay.n_least) sm.equal_end = j * kE - row.lead + i;
-      }
-      __syncthreads();
-      equal_end = sm.equal_end;
-    }
-  }
-  auto kept = [&](uint32_t key, int index) -> uint64_t {
-    if (key < stay.least || (key == stay.least && index > equal_end)) return 0;
-    const uint64_t w = weigh.of_key(key);
-    return w >= set.least ? w : 0;
-  };
-  in_slices(kept);
-  uint64_t total = 0;
-  for (int i = threadIdx.x; i < slices * kWaves; i += kThreads) total += sm.slice[i];
-  total = block_sum64(total, sm);
-  const uint64_t target = share_of(a.random[r], total);
-  uint64_t before;
-  const int part = block_find(slice, slices * kWaves, target, &before, sm);
-  if (wave != 0) return;
-  const int j = part * 64 + lane;
-  uint32_t k[kE];
-  row.load(j, k);
-  uint64_t w[kE], sum = 0;
-#pragma unroll
-  for (int i = 0; i < kE; ++i) sum += w[i] = kept(k[i], j * kE - row.lead + i);
-  uint64_t at = before + wave_scan64(sum) - sum;
-  if (sum && at <= target && target < at + sum) {
-    Drawn d{-1, 0, 0, total};
-#pragma unroll
-    for (int i = 0; i < kE; ++i) {
-      if (d.index < 0 && target < at + w[i]) d = Drawn{j * kE - row.lead + i, k[i], w[i], total};
-      at += w[i];
-    }
-    write_out(a, r, d, weigh, soft);
-  }
+  if (r.n_least == 0) return Stay{r.least, -1};
+  // the n_least-th index of those equal to the least: in the order of ~index the largest come first
+  uint32_t key;
+  uint64_t above;
+  const bool some = select_key([&](auto f) {
+    for (int i = threadIdx.x; i < n; i += kThreads)
+      if (sm.list[i].key == r.least) f(~sm.list[i].index);
+  }, ~(uint32_t)kMaxVocab, 0xffffffffu, r.n_least - 1, [](uint32_t) -> uint64_t { return 1; }, &key, &above, sm);
+  return Stay{r.least, some ? (int)~key : kMaxVocab};
 }
 
-// Phase 1, wavefront w of the row's: its largest key
+// sums: weights of what stays over the range's parts; of all the range's tokens, and their exponentials at temperature 1
 template <class T>
-__device__ __forceinline__ uint32_t largest_key(const Row<T>& row, int w) {
-  uint32_t top = 0;
-  row.each_part(w, [&](int, int, const typename Row<T>::Vector (&x)[kUnroll]) {
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-      for (int i = 0; i < Row<T>::kE; ++i) {
-        const uint32_t k = key_of(Row<T>::value(x[u].e[i]));
-        top = k > top ? k : top;
-      }
-  });
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_xor(top, d, 64);
-    top = o > top ? o : top;
-  }
-  return top;
-}
-
-// Phase 2, wavefront w of the row's: sums of its parts to `part`, sums over all of them, candidates
-template <class T>
-__device__ __forceinline__ void weigh_range(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, bool want_soft, uint64_t* part, WaveSums* sums,
-                                            Candidate* cand, uint32_t* cand_n) {
+__device__ __forceinline__ void sum_range(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, const Stay& stay, bool want_soft, uint64_t* part,
+                                          WaveSums* sums) {
   constexpr int kE = Row<T>::kE;
   using Vector = typename Row<T>::Vector;
   const int lane = threadIdx.x & 63;
-  uint64_t all = 0;
+  uint64_t all = 0, n = 0;
   double soft = 0.0;
+  auto end = [&](int id) {
+    n = wave_sum64(n);
+    if (lane == 0) part[id] = n;
+    n = 0;
+  };
   if (set.greedy) {
-    row.each_part(w, [&](int id, int, const Vector (&x)[kUnroll]) {
-      uint64_t n = 0;
+    row.template each_part<true>(w, [&](int, const Vector& x) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
+      for (int i = 0; i < kE; ++i) n += Row<T>::value(x.e[i]) >= weigh.max;
+    }, end);
+  } else if (!set.ranked && set.least <= 1) {
+    row.template each_part<true>(w, [&](int, const Vector& x) {
 #pragma unroll
-        for (int i = 0; i < kE; ++i) n += Row<T>::value(x[u].e[i]) >= weigh.max;
-      n = wave_sum64(n);
-      if (lane == 0) part[id] = n;
+      for (int i = 0; i < kE; ++i) n += weigh.biased_weight(weigh.exponent(Row<T>::value(x.e[i])));
+    }, [&](int id) {
+      n -= (uint64_t)(kE * kUnroll) * Weigher::kBias;
+      all += n;
+      end(id);
     });
   } else if (!set.ranked) {
-    row.each_part(w, [&](int id, int, const Vector (&x)[kUnroll]) {
-      uint64_t n = 0;
+    row.template each_part<true>(w, [&](int, const Vector& x) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-        for (int i = 0; i < kE; ++i) {
-          const uint64_t a = Weigher::weight(weigh.exponent(Row<T>::value(x[u].e[i])));
-          all += a;
-          n += a >= set.least ? a : 0;
-        }
-      n = wave_sum64(n);
-      if (lane == 0) part[id] = n;
-    });
+      for (int i = 0; i < kE; ++i) {
+        const uint64_t a = weigh.weight(weigh.exponent(Row<T>::value(x.e[i])));
+        all += a;
+        n += a >= set.least ? a : 0;
+      }
+    }, end);
   } else {
-    uint32_t n = 0;
-    row.each_part(w, [&](int, int j0, const Vector (&x)[kUnroll]) {
+    const bool want_all = want_soft && set.temperature == 1.f;
+    row.template each_part<true>(w, [&](int j, const Vector& x) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        uint32_t take = 0, at = n;
-#pragma unroll
-        for (int i = 0; i < kE; ++i) {
-          const float y = weigh.exponent(Row<T>::value(x[u].e[i]));
-          all += Weigher::weight(y);
-          const bool t = y >= kCandReach;
-          take |= (uint32_t)t << i;
-          const uint64_t b = __ballot(t);
-          at = __builtin_amdgcn_mbcnt_hi((uint32_t)(b >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)b, at));
-          n += __popcll(b);
-        }
-        if (take) {
-          const int index = (j0 + u * 64 + lane) * kE - row.lead;
-#pragma unroll
-          for (int i = 0; i < kE; ++i)
-            if (take >> i & 1) {
-              if (at < kCandPerWave) cand[at] = Candidate{key_of(Row<T>::value(x[u].e[i])), (uint32_t)(index + i)};
-              ++at;
-            }
+      for (int i = 0; i < kE; ++i) {
+        const float z = Row<T>::value(x.e[i]);
+        const bool stays = stay.has(key_of(z), (j + lane) * kE - row.lead + i);
+        if (want_all || __any(stays)) {
+          const uint64_t a = weigh.weight(weigh.exponent(z));
+          all += a;
+          n += stays && a >= set.least ? a : 0;
         }
       }
-    });
-    if (lane == 0) *cand_n = n;
+    }, end);
   }
   if (want_soft && (set.greedy || set.temperature != 1.f)) {
-    row.each_part(w, [&](int, int, const Vector (&x)[kUnroll]) {
+    row.template each_vector<false>(w, [&](int, const Vector& x) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-        for (int i = 0; i < kE; ++i) {
-          const float e = __builtin_amdgcn_fmed3f((Row<T>::value(x[u].e[i]) - weigh.max) * kLog2E, -200.f, 0.f);       // NaN: 0
-          soft += (double)__builtin_amdgcn_exp2f(e);
-        }
+      for (int i = 0; i < kE; ++i) {
+        const float e = __builtin_amdgcn_fmed3f((Row<T>::value(x.e[i]) - weigh.max) * kLog2E, -200.f, 0.f);       // NaN: 0
+        soft += (double)__builtin_amdgcn_exp2f(e);
+      }
     });
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) soft += __shfl_xor(soft, d, 64);
@@ -489,69 +584,12 @@ __device__ __forceinline__ void weigh_range(const Row<T>& row, int w, const Sett
   if (lane == 0) *sums = WaveSums{all, soft};
 }
 
-// Phase 3: what the `waves` wavefronts left is in sm (candidates in segments, `stride` of them for each wavefront)
-template <class T, class Shared>
-__device__ __forceinline__ void draw_row(const SampleArgs& a, int64_t r, const Row<T>& row, const Settings& set, const Weigher& weigh, uint32_t top, int waves,
-                                         bool cand_overflow, int n_cand, Shared& sm) {
+// draw, from the parts' sums and the wavefronts' in LDS (behind a barrier)
+template <class T>
+__device__ __forceinline__ void draw_row(const SampleArgs& a, int64_t r, const Row<T>& row, const Settings& set, const Weigher& weigh, const Stay& stay, int waves,
+                                         Shared& sm) {
   constexpr int kE = Row<T>::kE;
   const int lane = threadIdx.x & 63;
-  uint64_t all = 0;
-  double soft = 0.0;
-  for (int w = 0; w < waves; ++w) {
-    all += sm.sums[w].all;
-    soft += sm.sums[w].soft;
-  }
-  if (!set.greedy && set.temperature == 1.f) soft = (double)all * (1.0 / (double)kOne);
-  if (set.ranked) {
-    bool slow = cand_overflow;
-    Ranked stay{};
-    if (!slow) {
-      auto each = [&](auto f) {
-        for (int i = threadIdx.x; i < n_cand; i += kThreads) f(sm.cand[i].key);
-      };
-      // without a top-k the weight of the row, else of the candidates above the key
-      bool all_of_row = true;
-      if (set.top_k > n_cand) {
-        slow = true;                           // the least of the top-k is no candidate
-      } else {
-        uint64_t cand_total = 0;
-        each([&](uint32_t k) { cand_total += weigh.of_key(k); });
-        cand_total = block_sum64(cand_total, sm);
-        all_of_row = set.top_k <= 0;
-        const double share = set.top_p > 0.f ? (double)set.top_p * 4294967296.0 : 0.0;
-        if (all_of_row && share_of((uint32_t)share, all) > cand_total) {
-          slow = true;                         // nor that of the top-p
-        } else {
-          stay = rank_row(set, weigh, top, each, [&](uint32_t least) {
-            if (all_of_row) return all;
-            uint64_t t = 0;
-            each([&](uint32_t k) { t += k > least ? weigh.of_key(k) : 0; });
-            return block_sum64(t, sm);
-          }, sm);
-        }
-      }
-    }
-    if (slow) {
-      draw_slowly(a, r, row, set, weigh, top, soft, sm);
-      return;
-    }
-    // candidates are in order of index
-    uint64_t before;
-    int equal_end = -1;
-    if (stay.n_least > 0) equal_end = block_find([&](int i) -> uint64_t { return sm.cand[i].key == stay.least; }, n_cand, stay.n_least - 1, &before, sm);
-    auto kept = [&](int i) -> uint64_t {
-      const uint32_t key = sm.cand[i].key;
-      if (key < stay.least || (key == stay.least && i > equal_end)) return 0;
-      const uint64_t w = weigh.of_key(key);
-      return w >= set.least ? w : 0;
-    };
-    uint64_t total = 0;
-    for (int i = threadIdx.x; i < n_cand; i += kThreads) total += kept(i);
-    total = block_sum64(total, sm);
-    const int i = block_find(kept, n_cand, share_of(a.random[r], total), &before, sm);
-    if (threadIdx.x == 0) write_out(a, r, Drawn{(int)sm.cand[i].index, sm.cand[i].key, weigh.of_key(sm.cand[i].key), total}, weigh, soft);
-    return;
-  }
   uint64_t total = 0;
   for (int i = threadIdx.x; i < row.parts; i += kThreads) total += sm.part[i];
   total = block_sum64(total, sm);
@@ -559,6 +597,17 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int64_t r, const R
   uint64_t before;
   const int part = block_find([&](int i) { return sm.part[i]; }, row.parts, target, &before, sm);
   if (threadIdx.x >= 64) return;
+  uint64_t all = 0;
+  double soft = 0.0;
+  for (int w = lane; w < waves; w += 64) {
+    all += sm.sums[w].all;
+    soft += sm.sums[w].soft;
+  }
+  all = wave_sum64(all);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) soft += __shfl_xor(soft, d, 64);
+  if (!set.greedy && set.temperature == 1.f) soft = (double)all * (1.0 / (double)kOne);
+#pragma unroll 1
   for (int u = 0; u < kUnroll; ++u) {
     const int j = (part * kUnroll + u) * 64 + lane;
     typename Row<T>::Vector x;
@@ -567,8 +616,12 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int64_t r, const R
 #pragma unroll
     for (int i = 0; i < kE; ++i) {
       const float z = Row<T>::value(x.e[i]);
-      w[i] = set.greedy ? (uint64_t)(z >= weigh.max) : Weigher::weight(weigh.exponent(z));
-      if (w[i] < set.least && !set.greedy) w[i] = 0;
+      if (set.greedy) {
+        w[i] = z >= weigh.max;
+      } else {
+        const uint64_t weight = weigh.weight(weigh.exponent(z));
+        w[i] = stay.has(key_of(z), j * kE - row.lead + i) && weight >= set.least ? weight : 0;
+      }
       sum += w[i];
     }
     const uint64_t incl = wave_scan64(sum);
@@ -588,21 +641,18 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int64_t r, const R
   }
 }
 
-__device__ __forceinline__ void nothing_to_draw(const SampleArgs& a, int64_t r) {
-  a.ids[r] = -1;
-  if (a.logp) a.logp[r] = NAN;
-  if (a.logq) a.logq[r] = NAN;
-}
-
-// A workgroup per row: all three phases
+// A workgroup per row
 template <class T>
 __global__ void __launch_bounds__(kThreads, 4) sample_row_kernel(SampleArgs a) {
-  __shared__ SharedOf<kCandRow> sm;
+  __shared__ Shared sm;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t r = blockIdx.x;
   const Row<T> row(a, r, kWaves);
+  sm.powers.fill();
   const uint32_t mine = largest_key(row, wave);
   if (lane == 0) sm.top[wave] = mine;
+  for (int i = threadIdx.x; i < kBins; i += kThreads) sm.hist[i] = 0;
+  if (threadIdx.x == 0) sm.list_n = 0;
   __syncthreads();
   uint32_t top = 0;
   for (int w = 0; w < kWaves; ++w) top = sm.top[w] > top ? sm.top[w] : top;
@@ -611,40 +661,33 @@ __global__ void __launch_bounds__(kThreads, 4) sample_row_kernel(SampleArgs a) {
     return;
   }
   const Settings set(a, r);
-  const Weigher weigh(top, set.temperature);
-  weigh_range(row, wave, set, weigh, a.logp != nullptr, sm.part, &sm.sums[wave], sm.cand + wave * kCandPerWave, &sm.cand_n[wave]);
-  __syncthreads();
-  int n_cand = 0;
-  bool overflow = false;
-  if (set.ranked) {                          // the segments close up
-    Candidate c[kCandPerWave / 64];
-    int to = 0;
-    for (int w = 0; w < kWaves; ++w) {
-      if (w == wave) to = n_cand;
-      overflow |= sm.cand_n[w] > kCandPerWave;
-      n_cand += (int)sm.cand_n[w];
-    }
-    if (!overflow) {
-      const int n = (int)sm.cand_n[wave];
-#pragma unroll
-      for (int i = 0; i < kCandPerWave / 64; ++i)
-        if (64 * i + lane < n) c[i] = sm.cand[wave * kCandPerWave + 64 * i + lane];
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kCandPerWave / 64; ++i)
-        if (64 * i + lane < n) sm.cand[to + 64 * i + lane] = c[i];
-      __syncthreads();
-    }
+  const Weigher weigh(top, set.temperature, sm.powers);
+  Stay stay{kKeyMinusInf, -1};
+  if (set.ranked) {
+    bin_range(row, wave, set, weigh, sm.hist);
+    __syncthreads();
+    uint64_t all = 0;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) all += sm.hist[i];
+    all = block_sum64(all, sm);
+    const Gather g = choose_bins(set, sm.hist, sm);
+    list_range(row, wave, weigh, g, sm.list, &sm.list_n);
+    __syncthreads();
+    stay = sm.list_n > kList ? threshold_slowly(a, row, set, weigh, top, sm) : threshold_of_list(set, weigh, top, g, (int)sm.list_n, all, sm);
+    __syncthreads();
   }
-  draw_row(a, r, row, set, weigh, top, kWaves, overflow, n_cand, sm);
+  sum_range(row, wave, set, weigh, stay, a.logp != nullptr, sm.part, &sm.sums[wave]);
+  __syncthreads();
+  draw_row(a, r, row, set, weigh, stay, kWaves, sm);
 }
 
-// Several workgroups per row: a kernel for each phase, what passes between them in the workspace
+// Several workgroups per row: what passes between them, in the workspace
 struct RowSpace {
-  uint64_t* part;
+  uint64_t *hist, *part;
   WaveSums* sums;
-  uint32_t *top, *cand_n;
-  Candidate* cand;               // kCandPerWave for each wavefront
+  Gather* gather;
+  Stay* stay;
+  uint32_t *top, *count;         // count: workgroups that are done with bins, list, sums; tokens of the list
+  Listed* list;
 };
 __host__ __device__ inline size_t row_space(char* p, int parts, int waves, RowSpace* s) {
   size_t at = 0;
@@ -653,23 +696,15 @@ __host__ __device__ inline size_t row_space(char* p, int parts, int waves, RowSp
     at += (bytes + 255) / 256 * 256;
     return q;
   };
+  s->hist = (uint64_t*)take(kBins * 8);
   s->part = (uint64_t*)take((size_t)parts * 8);
   s->sums = (WaveSums*)take((size_t)waves * sizeof(WaveSums));
+  s->gather = (Gather*)take(sizeof(Gather));
+  s->stay = (Stay*)take(sizeof(Stay));
   s->top = (uint32_t*)take((size_t)waves * 4);
-  s->cand_n = (uint32_t*)take((size_t)waves * 4);
-  s->cand = (Candidate*)take((size_t)waves * kCandPerWave * sizeof(Candidate));
+  s->count = (uint32_t*)take(4 * 4);
+  s->list = (Listed*)take(kList * sizeof(Listed));
   return at;
-}
-
-template <class T>
-__global__ void __launch_bounds__(kThreads, 4) sample_top_kernel(SampleArgs a) {
-  const int64_t r = blockIdx.x / a.splits;
-  const int w = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % a.splits) * kWaves + (threadIdx.x >> 6)), waves = a.splits * kWaves;
-  const Row<T> row(a, r, waves);
-  RowSpace s;
-  row_space(a.ws + r * a.ws_row, row.parts, waves, &s);
-  const uint32_t top = largest_key(row, w);
-  if ((threadIdx.x & 63) == 0) s.top[w] = top;
 }
 
 __device__ __forceinline__ uint32_t top_of_waves(const uint32_t* tops, int waves) {
@@ -680,68 +715,124 @@ __device__ __forceinline__ uint32_t top_of_waves(const uint32_t* tops, int waves
     const uint32_t o = __shfl_xor(top, d, 64);
     top = o > top ? o : top;
   }
-  return top;
+  return __builtin_amdgcn_readfirstlane(top);
+}
+
+// What this workgroup wrote is seen by the one for which this is true: the last of the row's `n`.  One thread's fences do for all, which its barriers order
+// with the others: at the scope of the whole GPU a fence writes an XCD's L2 back, or invalidates it.
+__device__ __forceinline__ bool last_of_row(uint32_t* count, int n, Shared& sm) {
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    sm.last_one = atomicAdd(count, 1u) == (uint32_t)n - 1;
+    if (sm.last_one) __threadfence();
+  }
+  __syncthreads();
+  return sm.last_one;
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads, 4) sample_weigh_kernel(SampleArgs a) {
-  const int64_t r = blockIdx.x / a.splits;
-  const int w = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % a.splits) * kWaves + (threadIdx.x >> 6)), waves = a.splits * kWaves;
-  const Row<T> row(a, r, waves);
+struct SplitRow {
+  int64_t r;
+  int w, waves;
+  Row<T> row;
   RowSpace s;
-  row_space(a.ws + r * a.ws_row, row.parts, waves, &s);
-  const uint32_t top = top_of_waves(s.top, waves);
+  __device__ __forceinline__ SplitRow(const SampleArgs& a)
+      : r(blockIdx.x / a.splits), w(__builtin_amdgcn_readfirstlane((int)(blockIdx.x % a.splits) * kWaves + (threadIdx.x >> 6))), waves(a.splits * kWaves),
+        row(a, r, waves) {
+    row_space(a.ws + r * a.ws_row, row.parts, waves, &s);
+  }
+};
+
+template <class T>
+__global__ void __launch_bounds__(kThreads, 4) sample_top_kernel(SampleArgs a) {
+  const SplitRow<T> x(a);
+  if (blockIdx.x % a.splits == 0) {
+    for (int i = threadIdx.x; i < kBins; i += kThreads) x.s.hist[i] = 0;
+    if (threadIdx.x < 4) x.s.count[threadIdx.x] = 0;
+  }
+  const uint32_t top = largest_key(x.row, x.w);
+  if ((threadIdx.x & 63) == 0) x.s.top[x.w] = top;
+}
+
+template <class T>
+__global__ void __launch_bounds__(kThreads, 4) sample_bins_kernel(SampleArgs a) {
+  __shared__ Shared sm;
+  const SplitRow<T> x(a);
+  const Settings set(a, x.r);
+  if (!set.ranked) return;
+  const uint32_t top = top_of_waves(x.s.top, x.waves);
   if (top <= kKeyMinusInf) return;
-  const Settings set(a, r);
-  const Weigher weigh(top, set.temperature);
-  weigh_range(row, w, set, weigh, a.logp != nullptr, s.part, &s.sums[w], s.cand + w * kCandPerWave, &s.cand_n[w]);
+  const Weigher weigh(top, set.temperature, sm.powers);
+  for (int i = threadIdx.x; i < kBins; i += kThreads) sm.hist[i] = 0;
+  sm.powers.fill();
+  __syncthreads();
+  bin_range(x.row, x.w, set, weigh, sm.hist);
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kThreads)
+    if (sm.hist[i]) atomicAdd((unsigned long long*)&x.s.hist[i], (unsigned long long)sm.hist[i]);
+  if (!last_of_row(&x.s.count[0], a.splits, sm)) return;
+  for (int i = threadIdx.x; i < kBins; i += kThreads) sm.hist[i] = __hip_atomic_load(&x.s.hist[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  const Gather g = choose_bins(set, sm.hist, sm);
+  if (threadIdx.x == 0) *x.s.gather = g;
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads, 2) sample_draw_kernel(SampleArgs a) {
-  __shared__ SharedOf<kCandSplit> sm;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t r = blockIdx.x;
-  const int waves = a.splits * kWaves;
-  const Row<T> row(a, r, waves);
-  RowSpace s;
-  row_space(a.ws + r * a.ws_row, row.parts, waves, &s);
-  const uint32_t top = top_of_waves(s.top, waves);
+__global__ void __launch_bounds__(kThreads, 4) sample_list_kernel(SampleArgs a) {
+  __shared__ Shared sm;
+  const SplitRow<T> x(a);
+  const Settings set(a, x.r);
+  if (!set.ranked) return;
+  const uint32_t top = top_of_waves(x.s.top, x.waves);
+  if (top <= kKeyMinusInf) return;
+  const Weigher weigh(top, set.temperature, sm.powers);
+  const Gather g = *x.s.gather;
+  sm.powers.fill();
+  __syncthreads();
+  list_range(x.row, x.w, weigh, g, x.s.list, &x.s.count[3]);
+  if (!last_of_row(&x.s.count[1], a.splits, sm)) return;
+  const uint32_t n = __hip_atomic_load(&x.s.count[3], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  Stay stay;
+  if (n > kList) {
+    stay = threshold_slowly(a, x.row, set, weigh, top, sm);
+  } else {
+    uint64_t all = 0;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) all += x.s.hist[i];
+    all = block_sum64(all, sm);
+    for (int i = threadIdx.x; i < (int)n; i += kThreads) sm.list[i] = x.s.list[i];
+    __syncthreads();
+    stay = threshold_of_list(set, weigh, top, g, (int)n, all, sm);
+  }
+  if (threadIdx.x == 0) *x.s.stay = stay;
+}
+
+template <class T>
+__global__ void __launch_bounds__(kThreads, 4) sample_sums_kernel(SampleArgs a) {
+  __shared__ Shared sm;
+  const SplitRow<T> x(a);
+  const Settings set(a, x.r);
+  const uint32_t top = top_of_waves(x.s.top, x.waves);
   if (top <= kKeyMinusInf) {
-    if (threadIdx.x == 0) nothing_to_draw(a, r);
+    if (blockIdx.x % a.splits == 0 && threadIdx.x == 0) nothing_to_draw(a, x.r);
     return;
   }
-  const Settings set(a, r);
-  const Weigher weigh(top, set.temperature);
-  for (int i = threadIdx.x; i < waves; i += kThreads) {
-    sm.sums[i] = s.sums[i];
-    if (set.ranked) sm.cand_n[i] = s.cand_n[i];
-  }
-  if (!set.ranked)
-    for (int i = threadIdx.x; i < row.parts; i += kThreads) sm.part[i] = s.part[i];
+  const Weigher weigh(top, set.temperature, sm.powers);
+  const Stay stay = set.ranked ? *x.s.stay : Stay{kKeyMinusInf, -1};
+  sm.powers.fill();
   __syncthreads();
-  int n_cand = 0;
-  bool overflow = false;
-  if (set.ranked) {
-    for (int w = 0; w < waves; ++w) {
-      const int n = (int)sm.cand_n[w];
-      if (n > kCandPerWave || n_cand + n > kCandSplit) {
-        overflow = true;
-        break;
-      }
-      if (w % kWaves == wave)
-        for (int i = lane; i < n; i += 64) sm.cand[n_cand + i] = s.cand[w * kCandPerWave + i];
-      n_cand += n;
-    }
-    __syncthreads();
-  }
-  draw_row(a, r, row, set, weigh, top, waves, overflow, n_cand, sm);
+  sum_range(x.row, x.w, set, weigh, stay, a.logp != nullptr, x.s.part, &x.s.sums[x.w]);
+  if (!last_of_row(&x.s.count[2], a.splits, sm)) return;
+  for (int i = threadIdx.x; i < x.waves; i += kThreads) sm.sums[i] = x.s.sums[i];
+  for (int i = threadIdx.x; i < x.row.parts; i += kThreads) sm.part[i] = x.s.part[i];
+  __syncthreads();
+  draw_row(a, x.r, x.row, set, weigh, stay, x.waves, sm);
 }
 
-// Workgroups per row: enough for two on every compute unit
+// Workgroups per row: enough for every compute unit to have two
 int splits_of(int64_t n_rows, int64_t V) {
   int64_t s = (512 + n_rows - 1) / n_rows;
-  const int64_t most = (V + 4095) / 4096;              // at least 512 elements for a wavefront
+  const int64_t most = (V + 4095) / 4096;              // 512 elements for a wavefront
   if (s > most) s = most;
   if (s > kMaxSplits) s = kMaxSplits;
   return (int)(s < 1 ? 1 : s);
@@ -760,8 +851,11 @@ void launch(const SampleArgs& a, int32_t n_rows, hipStream_t s) {
     return;
   }
   sample_top_kernel<T><<<n_rows * a.splits, kThreads, 0, s>>>(a);
-  sample_weigh_kernel<T><<<n_rows * a.splits, kThreads, 0, s>>>(a);
-  sample_draw_kernel<T><<<n_rows, kThreads, 0, s>>>(a);
+  if (a.top_k || a.top_p) {
+    sample_bins_kernel<T><<<n_rows * a.splits, kThreads, 0, s>>>(a);
+    sample_list_kernel<T><<<n_rows * a.splits, kThreads, 0, s>>>(a);
+  }
+  sample_sums_kernel<T><<<n_rows * a.splits, kThreads, 0, s>>>(a);
 }
 
 }  // namespace
