@@ -4,7 +4,7 @@
 // their order, so which tokens are kept and which one is drawn does not depend on how a row is dealt to wavefronts: an fp32 cumulative sum over a vocabulary
 // leaves the draw to its rounding near every boundary.  2^40 keeps tokens down to 2^-41 of the likeliest one, and 2^20 weights fit 60 bits.
 //
-// A row is cut into parts of 256 16-byte vectors, dealt to wavefronts in turn, 8 wavefronts per workgroup and 1 or more workgroups ("splits") per row.
+// A row is cut into parts of 128 16-byte vectors, dealt to wavefronts in turn, 8 wavefronts per workgroup and 1 or more workgroups ("splits") per row.
 //   top      the largest logit;
 //   bins     (rows with a top-k or top-p) a histogram of the exponents y, 1/16 apart: of tokens if the row has a top-k, else of their weight.  The bin in which
 //            the top-k ends, or the weight that the top-p asks for;
@@ -23,10 +23,10 @@ namespace {
 constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr int kMaxVocab = 1 << 20;
 constexpr int kMaxSplits = 32;
-constexpr int kUnroll = 4;                            // vectors per lane and step, and per part of a wavefront's range
+constexpr int kUnroll = 2;                            // vectors per lane and step, and per part of a wavefront's range
 constexpr int kBins = 1024, kBinBits = 10;
 constexpr float kBinsPerOctave = 16.f;                // of exponents: the last bin holds weights of 0 alone
-constexpr int kList = 6144;                           // tokens of a list: two workgroups share a compute unit's LDS
+constexpr int kList = 4096;                           // tokens of a list: two workgroups share a compute unit's LDS
 constexpr uint32_t kKeyMinusInf = 0x007fffffu;        // order of -inf, below all that can be drawn
 constexpr uint64_t kOne = 1ull << 40;
 constexpr float kLog2E = 1.44269504088896341f;
@@ -187,6 +187,7 @@ struct Row {
   }
 };
 
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 struct Listed { uint32_t key, index; };
 struct WaveSums { uint64_t all; double soft; };      // all weights; exponentials at temperature 1, where the weights are of another
 // The tokens that stay: keys above `least`, and those equal to it up to index `equal_end`
@@ -202,7 +203,7 @@ constexpr int kMaxParts = kMaxVocab / 4 / (64 * kUnroll) + kMaxSplits * kWaves +
 
 struct Shared {
   Powers powers;
-  uint64_t hist[kBins];
+  __attribute__((aligned(16))) uint64_t hist[kBins];
   uint64_t part[kMaxParts];
   union {
     Listed list[kList];
@@ -477,8 +478,51 @@ __device__ __forceinline__ void list_range(const Row<T>& row, int w, const Weigh
   });
 }
 
+// What stays, from a list of up to kThreads tokens in LDS (in no order): one token per thread, which counts those in front of it (larger, or equal with a
+// lower index).  Sorted, the last one that stays has the least logit and the last index among those equal to it.  all: the weight of the row
+__device__ __forceinline__ Stay threshold_of_short_list(const Settings& set, const Weigher& weigh, const Gather& g, int n, uint64_t all, Shared& sm) {
+  const int t = threadIdx.x;
+  uint64_t* order = sm.hist;                   // tokens as whole numbers in that order; then their weights, sorted
+  static_assert(kThreads + 2 <= kBins, "");
+  const Listed mine = t < n ? sm.list[t] : Listed{0, 0};
+  const uint64_t place = (uint64_t)mine.key << 32 | (uint32_t)~mine.index;
+  __syncthreads();                             // the histogram is done with
+  if (t < n) order[t] = place;
+  if (t < 2) order[n + t] = 0;
+  __syncthreads();
+  int rank = 0;
+  if ((t & ~63) < n) {
+    for (int i = 0; i < n; i += 2) {
+      const u64x2 x = *(const u64x2*)(order + i);
+      rank += (x[0] > place) + (x[1] > place);
+    }
+  }
+  __syncthreads();
+  if (t < n) {
+    order[rank] = weigh.of_key(mine.key);
+    sm.list[rank] = mine;
+  }
+  __syncthreads();
+  auto weight = [&](int i) { return order[i]; };
+  uint64_t before;
+  int end = n;                                 // tokens that stay
+  if (set.top_k > 0) {
+    end = set.top_k < n ? set.top_k : n;
+    if (set.top_p < 1.f) {
+      const uint64_t total = block_sum64(t < end ? order[t] : 0, sm);
+      const int last = block_find(weight, end, reach_of(set.top_p, total) - 1, &before, sm);
+      end = last < end ? last + 1 : end;
+    }
+  } else {
+    const int last = block_find(weight, n, reach_of(set.top_p, all) - 1 - g.above, &before, sm);
+    end = last < n ? last + 1 : n;
+  }
+  return Stay{sm.list[end - 1].key, (int)sm.list[end - 1].index};
+}
+
 // What stays, from the list in LDS (in no order); all: the weight of the row
 __device__ __forceinline__ Stay threshold_of_list(const Settings& set, const Weigher& weigh, uint32_t top, const Gather& g, int n, uint64_t all, Shared& sm) {
+  if (n <= kThreads) return threshold_of_short_list(set, weigh, g, n, all, sm);
   auto each = [&](auto f) {
     for (int i = threadIdx.x; i < n; i += kThreads) f(sm.list[i].key);
   };
