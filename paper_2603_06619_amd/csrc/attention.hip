@@ -115,40 +115,46 @@ unsigned grid_of(int heads, int64_t slots) {
   return (unsigned)((heads % 8 != 0 && 8 % heads == 0) ? (slots * heads + 7) / 8 * 8 : slots * heads);
 }
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-// kRows rows of D elements, staged through registers: fetched one step ahead, written to LDS when the step begins.  Loads go through a buffer descriptor
-// of the rows that there are: what lies behind them (behind a sequence's end) is read as zeros by the hardware's bounds check and never meets a product.
+// A tile of kRows rows of D elements, copied to LDS without passing registers: one instruction writes 1 KB, lane l's 16 bytes at 16 l, and every lane reads from
+// where its place of the permuted tile wants it.  The copies go through a buffer descriptor of the rows that there are: what lies behind them (behind a
+// sequence's end) arrives as zeros by the hardware's bounds check and never meets a product.
 template <int D, int kRows>
-struct RowLoader {
-  static constexpr int kLanes = D / 8, kLoads = kRows * kLanes / 256, kStep = 256 / kLanes;
-  u32x4 x[kLoads];
-  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const char* base, int bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000);
+struct TileCopy {
+  static constexpr int kLanes = D / 8, kRowsPerCopy = 64 / kLanes, kCopies = kRows / kRowsPerCopy / 4;      // per wavefront
+  static __device__ __forceinline__ int row_of(int lane, int wave, int i) { return (wave * kCopies + i) * kRowsPerCopy + lane / kLanes; }
+  static __device__ __forceinline__ int column_of(int lane, int row) { return ((lane % kLanes) ^ RowTile<D>::swizzle(row)) * 16; }
+  static __device__ __forceinline__ void copy(const char* base, int bytes, int offset, char* tile, int wave, int i) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000),
+                                             (__attribute__((address_space(3))) void*)(tile + (wave * kCopies + i) * 1024), 16, offset, 0, 0, 0);
   }
   // `rows` rows from `base` on (more than kRows: kRows), row_bytes apart
-  __device__ __forceinline__ void fetch(const char* base, int row_bytes, int rows) {
-    const auto r = rows_at(base, rows > 0 ? ((rows < kRows ? rows : kRows) - 1) * row_bytes + D * 2 : 0);
-    const int at = threadIdx.x / kLanes * row_bytes + threadIdx.x % kLanes * 16;
+  static __device__ __forceinline__ void fetch(const char* base, int row_bytes, int rows, char* tile, int lane, int wave) {
+    const int bytes = rows > 0 ? ((rows < kRows ? rows : kRows) - 1) * row_bytes + D * 2 : 0;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, at + i * kStep * row_bytes, 0, 0);
-  }
-  // rows of a group's matrix: `rows` of them from head `head` of the query at `base` on
-  __device__ __forceinline__ void fetch_grouped(const char* base, int row_bytes, int group, uint32_t group_inverse, int head, int rows) {
-    const int live = rows < kRows ? rows : kRows;
-    const auto r = rows_at(base, live > 0 ? small_quotient(head + live - 1, group, group_inverse) * row_bytes + group * D * 2 : 0);
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int row = threadIdx.x / kLanes + i * kStep, at = head + row, t = small_quotient(at, group, group_inverse);
-      const int offset = t * row_bytes + (at - t * group) * (D * 2) + threadIdx.x % kLanes * 16;
-      x[i] = __builtin_amdgcn_raw_buffer_load_b128(r, row < live ? offset : 0x80000000u, 0, 0);
+    for (int i = 0; i < kCopies; ++i) {
+      const int row = row_of(lane, wave, i);
+      copy(base, bytes, row * row_bytes + column_of(lane, row), tile, wave, i);
     }
   }
-  __device__ __forceinline__ void store(char* tile) const {
+  // rows of a group's matrix: `rows` of them from head `head` of the query at `base` on
+  static __device__ __forceinline__ void fetch_grouped(const char* base, int row_bytes, int group, uint32_t group_inverse, int head, int rows, char* tile, int lane,
+                                                       int wave) {
+    const int live = rows < kRows ? rows : kRows;
+    const int bytes = live > 0 ? small_quotient(head + live - 1, group, group_inverse) * row_bytes + group * D * 2 : 0;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) *(u32x4*)(tile + RowTile<D>::chunk_at(threadIdx.x / kLanes + i * kStep, threadIdx.x % kLanes)) = x[i];
+    for (int i = 0; i < kCopies; ++i) {
+      const int row = row_of(lane, wave, i), at = head + row, t = small_quotient(at, group, group_inverse);
+      const int offset = t * row_bytes + (at - t * group) * (D * 2) + column_of(lane, row);
+      copy(base, bytes, row < live ? offset : (int)0x80000000u, tile, wave, i);
+    }
   }
 };
+// The copies of this step have arrived, and all are done with the step's tiles.  (The compiler waits for copies in flight by itself in front of the first
+// transposing read: a step issues them at its beginning and does its other products first.)
+__device__ __forceinline__ void end_of_step() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0)
+  __syncthreads();
+}
 
 // Where a mask cuts through a tile, a product multiplies masked rows by 0, and infinities or NaN in them come through as NaN.  Results that are not finite
 // are therefore computed once more, carefully: at the mask's edge such a tile gets zeros in their places before it enters the product, and the columns
@@ -263,18 +269,14 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   float m, sum;
   const float slack = kSlack / to_log2;
   f32x16 acc[D / 32];
-  RowLoader<D, kKeyTile> kl, vl;
   const char *next_k, *next_v;
+  auto fetch = [&](int key0, char (&to)[2][kKeyTile * D * 2]) __attribute__((always_inline)) {
+    TileCopy<D, kKeyTile>::fetch(next_k, k_bytes, n_keys - key0, to[0], lane, wave);
+    TileCopy<D, kKeyTile>::fetch(next_v, v_bytes, n_keys - key0, to[1], lane, wave);
+    next_k += (int64_t)kKeyTile * k_bytes;
+    next_v += (int64_t)kKeyTile * v_bytes;
+  };
   auto step = [&](int key0, char* kt, char* vt, auto careful) __attribute__((always_inline)) {
-    kl.store(kt);
-    vl.store(vt);
-    __syncthreads();                         // the other buffer is read before this by all
-    if (key0 + kKeyTile < n_keys) {
-      next_k += (int64_t)kKeyTile * k_bytes;
-      next_v += (int64_t)kKeyTile * v_bytes;
-      kl.fetch(next_k, k_bytes, n_keys - key0 - kKeyTile);
-      vl.fetch(next_v, v_bytes, n_keys - key0 - kKeyTile);
-    }
     if constexpr (decltype(careful)::value) {
       if (key0 + kKeyTile - 1 > tile_least) take_out_not_finite<D, kKeyTile>(vt, acc, half, [&](int i) { return key0 + i <= last; });
     }
@@ -333,11 +335,16 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
     for (int db = 0; db < D / 32; ++db) acc[db] = f32x16{};
     next_k = k;
     next_v = v;
-    kl.fetch(k, k_bytes, n_keys);
-    vl.fetch(v, v_bytes, n_keys);
+    fetch(0, tiles[0]);
+    end_of_step();
     for (int key0 = 0; key0 < n_keys; key0 += 2 * kKeyTile) {
+      if (key0 + kKeyTile < n_keys) fetch(key0 + kKeyTile, tiles[1]);
       step(key0, tiles[0][0], tiles[0][1], careful);
-      if (key0 + kKeyTile < n_keys) step(key0 + kKeyTile, tiles[1][0], tiles[1][1], careful);
+      end_of_step();
+      if (key0 + kKeyTile >= n_keys) break;
+      if (key0 + 2 * kKeyTile < n_keys) fetch(key0 + 2 * kKeyTile, tiles[0]);
+      step(key0 + kKeyTile, tiles[1][0], tiles[1][1], careful);
+      end_of_step();
     }
   };
   pass(std::false_type{});
@@ -395,20 +402,16 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
   const float to_log2 = a.scale * kLog2E, lse = a.lse[qh * a.n_q + at], shift = lse == -INFINITY ? INFINITY : lse * kLog2E;
 
   f32x16 acc[D / 32];
-  RowLoader<D, kKeyTile> kl, vl;
   const char *next_k, *next_v;
+  auto fetch = [&](int key0, char (&to)[2][kKeyTile * D * 2]) __attribute__((always_inline)) {
+    TileCopy<D, kKeyTile>::fetch(next_k, k_bytes, n_keys - key0, to[0], lane, wave);
+    TileCopy<D, kKeyTile>::fetch(next_v, v_bytes, n_keys - key0, to[1], lane, wave);
+    next_k += (int64_t)kKeyTile * k_bytes;
+    next_v += (int64_t)kKeyTile * v_bytes;
+  };
   float p_sum = 0.f, p_dp = 0.f;
   auto step = [&](int key0, char* kt, char* vt, auto kind) __attribute__((always_inline)) {
     constexpr Pass kPass = decltype(kind)::value;
-    kl.store(kt);
-    vl.store(vt);
-    __syncthreads();
-    if (key0 + kKeyTile < n_keys) {
-      next_k += (int64_t)kKeyTile * k_bytes;
-      next_v += (int64_t)kKeyTile * v_bytes;
-      kl.fetch(next_k, k_bytes, n_keys - key0 - kKeyTile);
-      vl.fetch(next_v, v_bytes, n_keys - key0 - kKeyTile);
-    }
     if constexpr (kPass == Pass::kCareful) {
       if (key0 + kKeyTile - 1 > tile_least) take_out_not_finite<D, kKeyTile>(kt, acc, half, [&](int i) { return key0 + i <= last; });
     }
@@ -463,18 +466,22 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     for (int db = 0; db < D / 32; ++db) acc[db] = f32x16{};
     next_k = k;
     next_v = v;
-    kl.fetch(k, k_bytes, n_keys);
-    vl.fetch(v, v_bytes, n_keys);
+    fetch(0, tiles[0]);
+    end_of_step();
     for (int key0 = 0; key0 < n_keys; key0 += 2 * kKeyTile) {
+      if (key0 + kKeyTile < n_keys) fetch(key0 + kKeyTile, tiles[1]);
       step(key0, tiles[0][0], tiles[0][1], kind);
-      if (key0 + kKeyTile < n_keys) step(key0 + kKeyTile, tiles[1][0], tiles[1][1], kind);
+      end_of_step();
+      if (key0 + kKeyTile >= n_keys) break;
+      if (key0 + 2 * kKeyTile < n_keys) fetch(key0 + 2 * kKeyTile, tiles[0]);
+      step(key0 + kKeyTile, tiles[1][0], tiles[1][1], kind);
+      end_of_step();
     }
   };
   if (tile_least < kFewKeys - 1) {
     pass(std::integral_constant<Pass, Pass::kDelta>{});
     p_sum = sum_halves(p_sum);
     delta = p_sum > 0.f ? sum_halves(p_dp) / p_sum : 0.f;
-    __syncthreads();                         // before the first tile is overwritten
   }
   pass(std::integral_constant<Pass, Pass::kPlain>{});
   if (__syncthreads_or(not_finite<D>(acc))) pass(std::integral_constant<Pass, Pass::kCareful>{});
@@ -514,15 +521,14 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
   const float to_log2 = a.scale * kLog2E;
 
   f32x16 dk[D / 32], dv[D / 32];
-  RowLoader<D, kDkvRows> ql, dl;
   float row_shift = INFINITY, row_delta = 0.f;
   int row_last = -1;
-  // the rows from `row0` on; query and head of row0 are kept as they go
+  // the rows from `row0` on; their first query and head are kept as they go
   int next_query, next_head, query = 0, head_of_group = 0;
   const int query_step = kDkvRows / a.group, head_step = kDkvRows - query_step * a.group;
-  auto fetch = [&](int row0) __attribute__((always_inline)) {
-    ql.fetch_grouped(q + (int64_t)next_query * q_bytes, q_bytes, a.group, a.group_inverse, next_head, n_rows - row0);
-    dl.fetch_grouped(d + (int64_t)next_query * d_bytes, d_bytes, a.group, a.group_inverse, next_head, n_rows - row0);
+  auto fetch = [&](int row0, char (&to)[2][kDkvRows * D * 2]) __attribute__((always_inline)) {
+    TileCopy<D, kDkvRows>::fetch_grouped(q + (int64_t)next_query * q_bytes, q_bytes, a.group, a.group_inverse, next_head, n_rows - row0, to[0], lane, wave);
+    TileCopy<D, kDkvRows>::fetch_grouped(d + (int64_t)next_query * d_bytes, d_bytes, a.group, a.group_inverse, next_head, n_rows - row0, to[1], lane, wave);
     if (threadIdx.x < kDkvRows) {
       const int at = next_head + threadIdx.x, of = small_quotient(at, a.group, a.group_inverse), t = next_query + of;
       row_shift = INFINITY;                  // probability 0: rows past the end, and rows that see no key
@@ -537,15 +543,15 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
       }
     }
   };
-  auto step = [&](int row0, char* qt, char* dt, RowWords& w, auto careful) __attribute__((always_inline)) {
-    ql.store(qt);
-    dl.store(dt);
+  // what goes with the tile that was fetched last
+  auto store_words = [&](RowWords& w) __attribute__((always_inline)) {
     if (threadIdx.x < kDkvRows) {
       w.shift[threadIdx.x] = row_shift;
       w.delta[threadIdx.x] = row_delta;
       w.last[threadIdx.x] = row_last;
     }
-    __syncthreads();
+  };
+  auto advance = [&]() __attribute__((always_inline)) {
     query = next_query;
     head_of_group = next_head;
     next_query += query_step;
@@ -554,7 +560,8 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
       next_head -= a.group;
       ++next_query;
     }
-    if (row0 + kDkvRows < n_rows) fetch(row0 + kDkvRows);
+  };
+  auto step = [&](char* qt, char* dt, RowWords& w, auto careful) __attribute__((always_inline)) {
     if constexpr (decltype(careful)::value) {
       if (query < tile_all) {
         take_out_not_finite<D, kDkvRows>(qt, dk, half, [&](int i) { return key <= w.last[i]; });
@@ -610,10 +617,21 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
     for (int db = 0; db < D / 32; ++db) dk[db] = dv[db] = f32x16{};
     next_query = first_query;
     next_head = 0;
-    fetch(first_row);
+    fetch(first_row, tiles[0]);
+    store_words(words[0]);
+    end_of_step();
     for (int row0 = first_row; row0 < n_rows; row0 += 2 * kDkvRows) {
-      step(row0, tiles[0][0], tiles[0][1], words[0], careful);
-      if (row0 + kDkvRows < n_rows) step(row0 + kDkvRows, tiles[1][0], tiles[1][1], words[1], careful);
+      advance();
+      if (row0 + kDkvRows < n_rows) fetch(row0 + kDkvRows, tiles[1]);
+      step(tiles[0][0], tiles[0][1], words[0], careful);
+      store_words(words[1]);
+      end_of_step();
+      if (row0 + kDkvRows >= n_rows) break;
+      advance();
+      if (row0 + 2 * kDkvRows < n_rows) fetch(row0 + 2 * kDkvRows, tiles[0]);
+      step(tiles[1][0], tiles[1][1], words[1], careful);
+      store_words(words[0]);
+      end_of_step();
     }
   };
   pass(std::false_type{});
