@@ -44,8 +44,9 @@ struct AttnArgs {
   uint32_t group_inverse;        // see small_quotient
 };
 
-// x / group for 0 <= x < 2^13: inverse = floor(2^32 / group) + 1 is too large by less than 1 / group in 2^32 / x
-__device__ __forceinline__ int small_quotient(int x, int group, uint32_t inverse) { return group == 1 ? x : (int)__umulhi((uint32_t)x, inverse); }
+// x / group for 0 <= x < 2^13, group <= 2^12: floor((x + 1/2) / group), which lies 1 / (2 group) below the next whole number at least, and the inverse,
+// floor(2^31 / group) + 1, adds (x + 1/2) / 2^31 at most
+__device__ __forceinline__ int small_quotient(int x, uint32_t inverse) { return (int)__umulhi((uint32_t)(2 * x + 1), inverse); }
 
 // Offsets come from device memory: clamped to the arrays, and a sequence never has a negative length.
 __device__ __forceinline__ int64_t offset_at(const int32_t* cu, int i, int64_t n) {
@@ -118,39 +119,45 @@ unsigned grid_of(int heads, int64_t slots) {
 // A tile of kRows rows of D elements, copied to LDS without passing registers: one instruction writes 1 KB, lane l's 16 bytes at 16 l, and every lane reads from
 // where its place of the permuted tile wants it.  The copies go through a buffer descriptor of the rows that there are: what lies behind them (behind a
 // sequence's end) arrives as zeros by the hardware's bounds check and never meets a product.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 template <int D, int kRows>
 struct TileCopy {
-  static constexpr int kLanes = D / 8, kRowsPerCopy = 64 / kLanes, kCopies = kRows / kRowsPerCopy / 4;      // per wavefront
+  static constexpr int kLanes = D / 8, kRowsPerCopy = 64 / kLanes, kCopies = kRows / kRowsPerCopy / 4;      // per wavefront, of four
   static __device__ __forceinline__ int row_of(int lane, int wave, int i) { return (wave * kCopies + i) * kRowsPerCopy + lane / kLanes; }
   static __device__ __forceinline__ int column_of(int lane, int row) { return ((lane % kLanes) ^ RowTile<D>::swizzle(row)) * 16; }
-  static __device__ __forceinline__ void copy(const char* base, int bytes, int offset, char* tile, int wave, int i) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000),
-                                             (__attribute__((address_space(3))) void*)(tile + (wave * kCopies + i) * 1024), 16, offset, 0, 0, 0);
+  // As inline assembly, which the compiler's wait counts do not see: of copies that it knows of, it would wait for all in front of every transposing read,
+  // whatever either's place.  A copy has no result in registers; end_of_step() waits for them.  Nor does the compiler see what must lie in front of it: 5 wait
+  // states behind a vector instruction that wrote `rows` (a spilled scalar register comes back that way), 1 behind the write of m0
+  static __device__ __forceinline__ void copy(i32x4 rows, int offset, char* tile, int wave, int i) {
+    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(tile + (wave * kCopies + i) * 1024);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(rows) : "memory", "m0");
+  }
+  static __device__ __forceinline__ i32x4 rows_at(const char* base, int bytes) {
+    const uint64_t at = (uint64_t)(uintptr_t)base;
+    return i32x4{(int)(uint32_t)at, (int)((uint32_t)(at >> 32) & 0xffff), bytes, 0x00027000};
   }
   // `rows` rows from `base` on (more than kRows: kRows), row_bytes apart
   static __device__ __forceinline__ void fetch(const char* base, int row_bytes, int rows, char* tile, int lane, int wave) {
-    const int bytes = rows > 0 ? ((rows < kRows ? rows : kRows) - 1) * row_bytes + D * 2 : 0;
+    const i32x4 r = rows_at(base, rows > 0 ? ((rows < kRows ? rows : kRows) - 1) * row_bytes + D * 2 : 0);
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
       const int row = row_of(lane, wave, i);
-      copy(base, bytes, row * row_bytes + column_of(lane, row), tile, wave, i);
+      copy(r, row * row_bytes + column_of(lane, row), tile, wave, i);
     }
   }
-  // rows of a group's matrix: `rows` of them from head `head` of the query at `base` on
+  // rows of a group's matrix: `rows` of them (more than kRows: kRows; fewer: they end with a query) from head `head` of the query at `base` on
   static __device__ __forceinline__ void fetch_grouped(const char* base, int row_bytes, int group, uint32_t group_inverse, int head, int rows, char* tile, int lane,
                                                        int wave) {
     const int live = rows < kRows ? rows : kRows;
-    const int bytes = live > 0 ? small_quotient(head + live - 1, group, group_inverse) * row_bytes + group * D * 2 : 0;
+    const i32x4 r = rows_at(base, live > 0 ? small_quotient(head + live - 1, group_inverse) * row_bytes + group * D * 2 : 0);
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) {
-      const int row = row_of(lane, wave, i), at = head + row, t = small_quotient(at, group, group_inverse);
-      const int offset = t * row_bytes + (at - t * group) * (D * 2) + column_of(lane, row);
-      copy(base, bytes, row < live ? offset : (int)0x80000000u, tile, wave, i);
+      const int row = row_of(lane, wave, i), at = head + row, t = small_quotient(at, group_inverse);
+      copy(r, t * row_bytes + (at - t * group) * (D * 2) + column_of(lane, row), tile, wave, i);
     }
   }
 };
-// The copies of this step have arrived, and all are done with the step's tiles.  (The compiler waits for copies in flight by itself in front of the first
-// transposing read: a step issues them at its beginning and does its other products first.)
+// The copies of this step have arrived, and all are done with the step's tiles.
 __device__ __forceinline__ void end_of_step() {
   __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0)
   __syncthreads();
@@ -174,7 +181,7 @@ __device__ __forceinline__ void take_out_not_finite(char* tile, f32x16 (&acc)[D 
       }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < kRows * D; i += 256) {
+  for (int i = threadIdx.x; i < kRows * D; i += blockDim.x) {
     uint16_t* x = (uint16_t*)tile + i;
     if ((*x & 0x7f80) == 0x7f80) *x = 0;
   }
@@ -521,32 +528,31 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
   const float to_log2 = a.scale * kLog2E;
 
   f32x16 dk[D / 32], dv[D / 32];
-  float row_shift = INFINITY, row_delta = 0.f;
+  float row_lse = -INFINITY, row_delta = 0.f;
   int row_last = -1;
   // the rows from `row0` on; their first query and head are kept as they go
   int next_query, next_head, query = 0, head_of_group = 0;
   const int query_step = kDkvRows / a.group, head_step = kDkvRows - query_step * a.group;
   auto fetch = [&](int row0, char (&to)[2][kDkvRows * D * 2]) __attribute__((always_inline)) {
-    TileCopy<D, kDkvRows>::fetch_grouped(q + (int64_t)next_query * q_bytes, q_bytes, a.group, a.group_inverse, next_head, n_rows - row0, to[0], lane, wave);
-    TileCopy<D, kDkvRows>::fetch_grouped(d + (int64_t)next_query * d_bytes, d_bytes, a.group, a.group_inverse, next_head, n_rows - row0, to[1], lane, wave);
-    if (threadIdx.x < kDkvRows) {
-      const int at = next_head + threadIdx.x, of = small_quotient(at, a.group, a.group_inverse), t = next_query + of;
-      row_shift = INFINITY;                  // probability 0: rows past the end, and rows that see no key
+    if (threadIdx.x < kDkvRows) {            // in front of the copies: waiting for these loads must not wait for those
+      const int at = next_head + threadIdx.x, of = small_quotient(at, a.group_inverse), t = next_query + of;
+      row_lse = -INFINITY;                   // probability 0: rows past the end, and rows that see no key
       row_delta = 0.f;
       row_last = -1;
       if (row0 + (int)threadIdx.x < n_rows) {
         const int64_t w = (at - of * a.group) * a.n_q + t;
-        const float l = lse[w];
-        row_shift = l == -INFINITY ? INFINITY : l * kLog2E;
+        row_lse = lse[w];
         row_delta = delta[w];
         row_last = last_key(a, s, t);
       }
     }
+    TileCopy<D, kDkvRows>::fetch_grouped(q + (int64_t)next_query * q_bytes, q_bytes, a.group, a.group_inverse, next_head, n_rows - row0, to[0], lane, wave);
+    TileCopy<D, kDkvRows>::fetch_grouped(d + (int64_t)next_query * d_bytes, d_bytes, a.group, a.group_inverse, next_head, n_rows - row0, to[1], lane, wave);
   };
   // what goes with the tile that was fetched last
   auto store_words = [&](RowWords& w) __attribute__((always_inline)) {
     if (threadIdx.x < kDkvRows) {
-      w.shift[threadIdx.x] = row_shift;
+      w.shift[threadIdx.x] = row_lse == -INFINITY ? INFINITY : row_lse * kLog2E;
       w.delta[threadIdx.x] = row_delta;
       w.last[threadIdx.x] = row_last;
     }
@@ -568,7 +574,7 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
         take_out_not_finite<D, kDkvRows>(dt, dv, half, [&](int i) { return key <= w.last[i]; });
       }
     }
-    if (query + small_quotient(head_of_group + kDkvRows - 1, a.group, a.group_inverse) < wave_first) return;
+    if (query + small_quotient(head_of_group + kDkvRows - 1, a.group_inverse) < wave_first) return;
     f32x16 p[2] = {}, dp[2] = {};
     tile_times_columns<D>(qt, k.f, p, lane);
     tile_times_columns<D>(dt, v.f, dp, lane);
@@ -678,7 +684,7 @@ nat_status attn_args(const nat_attn_params* p, const void* d_q, const void* d_k,
   a->hq = p->n_q_heads;
   a->hkv = p->n_kv_heads;
   a->group = group;
-  a->group_inverse = (uint32_t)((1ull << 32) / group + 1);
+  a->group_inverse = (uint32_t)((1ull << 31) / group + 1);
   a->causal = p->causal;
   a->n_q = p->n_q;
   a->n_k = p->n_k;
@@ -707,11 +713,12 @@ extern "C" nat_status nat_attn_fwd(const nat_attn_params* params, const void* d_
   if (!d_out || !d_lse || misaligned(d_out)) return NAT_INVALID_ARG;
   a.out = (uint16_t*)d_out;
   a.lse = d_lse;
-  a.slots = (int)(a.n_q * a.group / kRowTile + a.n_seqs);
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_ATTN_FWD, s);
-  if (params->head_dim == 128) attn_fwd_kernel<128><<<grid_of(a.hkv, a.slots), 256, 0, s>>>(a);
-  else attn_fwd_kernel<64><<<grid_of(a.hkv, a.slots), 256, 0, s>>>(a);
+  a.slots = (int)(a.n_q * a.group / kRowTile + a.n_seqs);
+  const unsigned blocks = grid_of(a.hkv, a.slots);
+  if (params->head_dim == 128) attn_fwd_kernel<128><<<blocks, 256, 0, s>>>(a);
+  else attn_fwd_kernel<64><<<blocks, 256, 0, s>>>(a);
   NAT_LAUNCH_CHECK();
   return NAT_OK;
 }
