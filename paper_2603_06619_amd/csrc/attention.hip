@@ -208,9 +208,9 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[D / 32]) {
 }
 
 // C[32 rb ..][n] = rows of a tile of 64 rows times the columns b: fragments are read four at a time while the four before them are multiplied (the
-// compiler by itself reads one and waits for it).
-template <int D>
-__device__ __forceinline__ void tile_times_columns(const char* tile, const bf16x8 (&b)[D / 16], f32x16 (&c)[2], int lane) {
+// compiler by itself reads one and waits for it).  beside(i), i = 0 .. D / 32 - 1, is work to be done under the products.
+template <int D, class Beside>
+__device__ __forceinline__ void tile_times_columns(const char* tile, const bf16x8 (&b)[D / 16], f32x16 (&c)[2], int lane, const Beside& beside) {
   constexpr int kSteps = D / 16, kGroups = 2 * kSteps / 4;
   bf16x8 f[2][4];
 #pragma unroll
@@ -227,8 +227,14 @@ __device__ __forceinline__ void tile_times_columns(const char* tile, const bf16x
       const int at = 4 * g + i;
       c[at / kSteps] = mfma32(f[g & 1][i], b[at % kSteps], c[at / kSteps]);
     }
+    beside(g);
     __builtin_amdgcn_sched_barrier(0);
   }
+}
+
+template <int D>
+__device__ __forceinline__ void tile_times_columns(const char* tile, const bf16x8 (&b)[D / 16], f32x16 (&c)[2], int lane) {
+  tile_times_columns<D>(tile, b, c, lane, [](int) __attribute__((always_inline)) {});
 }
 
 // Columns of a result, 32 elements db of this lane's column n, as bf16 to its row
@@ -575,26 +581,54 @@ __global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
       }
     }
     if (query + small_quotient(head_of_group + kDkvRows - 1, a.group_inverse) < wave_first) return;
+    constexpr bool kCareful = decltype(careful)::value;
     f32x16 p[2] = {}, dp[2] = {};
     tile_times_columns<D>(qt, k.f, p, lane);
-    tile_times_columns<D>(dt, v.f, dp, lane);
-    const bool edge = query < wave_all;
+    // Probabilities of what is masked are 0, and so are its dS if all is finite (if not, NaN leads to the careful pass, which takes them out one by one).  The
+    // mask has its branch here: the exponentials run under the products of dP
+    if (!kCareful && query < wave_all) {
+#pragma unroll
+      for (int i4 = 0; i4 < 8; ++i4) {
+        const i32x4 last = *(const i32x4*)(w.last + 8 * i4 + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (key > last[e]) p[i4 >> 2][4 * (i4 & 3) + e] = -INFINITY;
+      }
+    }
+    tile_times_columns<D>(dt, v.f, dp, lane, [&](int part) __attribute__((always_inline)) {
+      constexpr int kFours = 8 / (D / 32);
+#pragma unroll
+      for (int i4 = kFours * part; i4 < kFours * part + kFours; ++i4) {
+        const f32x4 shift = *(const f32x4*)(w.shift + 8 * i4 + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 4 * (i4 & 3) + e;
+          p[i4 >> 2][i] = exp2_fast(fmaf(p[i4 >> 2][i], to_log2, -shift[e]));
+        }
+        if constexpr (kCareful) {
+          const i32x4 last = *(const i32x4*)(w.last + 8 * i4 + 4 * half);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (key > last[e]) p[i4 >> 2][4 * (i4 & 3) + e] = 0.f;
+        }
+      }
+    });
     bf16x8 pf[2], df[2], dof[2][D / 32], qf[2][D / 32];
     auto ready = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
       for (int i4 = 0; i4 < 2; ++i4) {
         const int row = 16 * g + 8 * i4 + 4 * half;
-        const f32x4 shift = *(const f32x4*)(w.shift + row), del = *(const f32x4*)(w.delta + row);
+        const f32x4 del = *(const f32x4*)(w.delta + row);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 8 * (g & 1) + 4 * i4 + e;
-          p[g >> 1][i] = exp2_fast(fmaf(p[g >> 1][i], to_log2, -shift[e]));
           dp[g >> 1][i] = p[g >> 1][i] * (dp[g >> 1][i] - del[e]);
         }
-        if (edge) {
+        if constexpr (kCareful) {
+          const i32x4 last = *(const i32x4*)(w.last + row);
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (key > w.last[row + e]) p[g >> 1][8 * (g & 1) + 4 * i4 + e] = dp[g >> 1][8 * (g & 1) + 4 * i4 + e] = 0.f;
+            if (key > last[e]) dp[g >> 1][8 * (g & 1) + 4 * i4 + e] = 0.f;
         }
       }
       pf[g & 1] = fragment_of_result(p[g >> 1], g & 1);

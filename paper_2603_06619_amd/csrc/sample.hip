@@ -10,7 +10,7 @@
 //            the top-k ends, or the weight that the top-p asks for;
 //   list     the tokens of that bin (with a top-k: of all bins down to it).  Among them the least logit that stays, and the last index that does of those
 //            equal to it;
-//   sums     weights of what stays, summed over parts of the ranges;
+//   sums     weights of what stays, summed part by part;
 //   draw     in order of index: by the sums of the parts, then by steps, lanes and elements.
 // A row with one workgroup goes through them in one kernel; with more, each of top, bins, list and sums is a kernel, and the workgroup that comes last in
 // a row does what follows from all (it knows by a counter; nobody waits).  If the list is longer than LDS has room for (very many equal logits), the row
@@ -23,7 +23,7 @@ namespace {
 constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr int kMaxVocab = 1 << 20;
 constexpr int kMaxSplits = 32;
-constexpr int kUnroll = 2;                            // vectors per lane and step, and per part of a wavefront's range
+constexpr int kUnroll = 2;                            // vectors per lane and step, and per part
 constexpr int kBins = 1024, kBinBits = 10;
 constexpr float kBinsPerOctave = 16.f;                // of exponents: the last bin holds weights of 0 alone
 constexpr int kList = 4096;                           // tokens of a list: two workgroups share a compute unit's LDS
@@ -78,7 +78,7 @@ struct Weigher {
   __device__ __forceinline__ float exponent(float z) const { return __builtin_amdgcn_fmed3f((z - max) * per_nat, -60.f, 0.f); }
   // 2^y = 2^n 2^(j / 64) 2^r, |r| <= 1/128; 2^r - 1 = r (c1 + r (c2 + r (c3 + r c4))) through the four Chebyshev points of (2^r - 1) / r, all but the last two
   // steps in fp32: error below 2^-40 of the weight.  Adding 2^52 rounds to a whole number, which then is the low 52 bits (kBias: those above).  In all 24
-  // instructions; a polynomial of degree 9 without a table took 38 (weights of 512 rows of 152064 logits XX us, then YY)
+  // instructions, six of them fp64; a polynomial of degree 9 without a table takes 38
   static constexpr uint64_t kBias = 0x433ull << 52;
   __device__ __forceinline__ uint64_t biased_weight(float y) const {
     constexpr float kWhole = 0x1.8p23f;              // adding it rounds to a whole number, the low bits of the sum
@@ -151,7 +151,7 @@ struct Row {
   // The parts of wavefront w: f(first vector, this lane's vector) for every 64 vectors of a part, then end(part).  A part's vectors are loaded together, a part
   // ahead, and used in a loop that stays a loop: unrolled, code that runs a few times spends longer being fetched than running.  kBack: the last part
   // first.  Passes over a row go to and fro, so that each begins with what the one before it left in the caches (512 rows of 608 KB, 1.2 times
-  // the Infinity Cache: XX us, all passes forward YY)
+  // the Infinity Cache: 143 us, all passes forward 150)
   template <bool kBack, class F, class End>
   __device__ __forceinline__ void each_part(int w, const F& f, const End& end) const {
     const int lane = threadIdx.x & 63;
@@ -406,7 +406,7 @@ __device__ __noinline__ Stay threshold_slowly(const SampleArgs& a, const Row<T>&
   return Stay{r.least, sm.equal_end};
 }
 
-// top: the largest key of wavefront w's range
+// top: the largest key of wavefront w's parts
 template <class T>
 __device__ __forceinline__ uint32_t largest_key(const Row<T>& row, int w) {
   float m = -INFINITY;                       // fmaxf passes NaN over
@@ -424,9 +424,9 @@ __device__ __forceinline__ int bin_of(float y) {
   return b < kBins ? b : kBins - 1;
 }
 
-// bins: the range's tokens or weights, added to the histogram in LDS
+// bins: tokens or weights of the wavefront's parts, added to the histogram in LDS
 template <class T>
-__device__ __forceinline__ void bin_range(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, uint64_t* hist) {
+__device__ __forceinline__ void bin_parts(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, uint64_t* hist) {
   row.template each_vector<true>(w, [&](int, const typename Row<T>::Vector& x) {
 #pragma unroll
     for (int i = 0; i < Row<T>::kE; ++i) {
@@ -452,9 +452,9 @@ __device__ __forceinline__ Gather choose_bins(const Settings& set, const uint64_
   return set.top_k > 0 ? Gather{0, bin, 0} : Gather{bin, bin, above};
 }
 
-// list: the range's tokens in those bins; *n counts on past the room
+// list: the tokens in those bins, of the wavefront's parts; *n counts on past the room
 template <class T>
-__device__ __forceinline__ void list_range(const Row<T>& row, int w, const Weigher& weigh, const Gather& g, Listed* list, uint32_t* n) {
+__device__ __forceinline__ void list_parts(const Row<T>& row, int w, const Weigher& weigh, const Gather& g, Listed* list, uint32_t* n) {
   constexpr int kE = Row<T>::kE;
   const int lane = threadIdx.x & 63;
   row.template each_vector<false>(w, [&](int j, const typename Row<T>::Vector& x) {
@@ -561,9 +561,9 @@ __device__ __forceinline__ Stay threshold_of_list(const Settings& set, const Wei
   return Stay{r.least, some ? (int)~key : kMaxVocab};
 }
 
-// sums: weights of what stays over the range's parts; of all the range's tokens, and their exponentials at temperature 1
+// sums: weights of what stays, of each of the wavefront's parts; of all their tokens, and their exponentials at temperature 1
 template <class T>
-__device__ __forceinline__ void sum_range(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, const Stay& stay, bool want_soft, uint64_t* part,
+__device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, const Stay& stay, bool want_soft, uint64_t* part,
                                           WaveSums* sums) {
   constexpr int kE = Row<T>::kE;
   using Vector = typename Row<T>::Vector;
@@ -708,18 +708,18 @@ __global__ void __launch_bounds__(kThreads, 4) sample_row_kernel(SampleArgs a) {
   const Weigher weigh(top, set.temperature, sm.powers);
   Stay stay{kKeyMinusInf, -1};
   if (set.ranked) {
-    bin_range(row, wave, set, weigh, sm.hist);
+    bin_parts(row, wave, set, weigh, sm.hist);
     __syncthreads();
     uint64_t all = 0;
     for (int i = threadIdx.x; i < kBins; i += kThreads) all += sm.hist[i];
     all = block_sum64(all, sm);
     const Gather g = choose_bins(set, sm.hist, sm);
-    list_range(row, wave, weigh, g, sm.list, &sm.list_n);
+    list_parts(row, wave, weigh, g, sm.list, &sm.list_n);
     __syncthreads();
     stay = sm.list_n > kList ? threshold_slowly(a, row, set, weigh, top, sm) : threshold_of_list(set, weigh, top, g, (int)sm.list_n, all, sm);
     __syncthreads();
   }
-  sum_range(row, wave, set, weigh, stay, a.logp != nullptr, sm.part, &sm.sums[wave]);
+  sum_parts(row, wave, set, weigh, stay, a.logp != nullptr, sm.part, &sm.sums[wave]);
   __syncthreads();
   draw_row(a, r, row, set, weigh, stay, kWaves, sm);
 }
@@ -762,9 +762,10 @@ __device__ __forceinline__ uint32_t top_of_waves(const uint32_t* tops, int waves
   return __builtin_amdgcn_readfirstlane(top);
 }
 
-// What this workgroup wrote is seen by the one for which this is true: the last of the row's `n`.  One thread's fences do for all, which its barriers order
-// with the others: at the scope of the whole GPU a fence writes an XCD's L2 back, or invalidates it.
+// What this workgroup wrote is seen by the one for which this is true: the last of the row's `n`.  Every wavefront waits until its own stores have arrived in
+// the L2, then one thread's fences do for all: at the scope of the whole GPU a fence writes an XCD's L2 back, or invalidates it.
 __device__ __forceinline__ bool last_of_row(uint32_t* count, int n, Shared& sm) {
+  __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0)
   __syncthreads();
   if (threadIdx.x == 0) {
     __threadfence();
@@ -811,7 +812,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_bins_kernel(SampleArgs a) 
   for (int i = threadIdx.x; i < kBins; i += kThreads) sm.hist[i] = 0;
   sm.powers.fill();
   __syncthreads();
-  bin_range(x.row, x.w, set, weigh, sm.hist);
+  bin_parts(x.row, x.w, set, weigh, sm.hist);
   __syncthreads();
   for (int i = threadIdx.x; i < kBins; i += kThreads)
     if (sm.hist[i]) atomicAdd((unsigned long long*)&x.s.hist[i], (unsigned long long)sm.hist[i]);
@@ -834,7 +835,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_list_kernel(SampleArgs a) 
   const Gather g = *x.s.gather;
   sm.powers.fill();
   __syncthreads();
-  list_range(x.row, x.w, weigh, g, x.s.list, &x.s.count[3]);
+  list_parts(x.row, x.w, weigh, g, x.s.list, &x.s.count[3]);
   if (!last_of_row(&x.s.count[1], a.splits, sm)) return;
   const uint32_t n = __hip_atomic_load(&x.s.count[3], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   Stay stay;
@@ -865,7 +866,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_sums_kernel(SampleArgs a) 
   const Stay stay = set.ranked ? *x.s.stay : Stay{kKeyMinusInf, -1};
   sm.powers.fill();
   __syncthreads();
-  sum_range(x.row, x.w, set, weigh, stay, a.logp != nullptr, x.s.part, &x.s.sums[x.w]);
+  sum_parts(x.row, x.w, set, weigh, stay, a.logp != nullptr, x.s.part, &x.s.sums[x.w]);
   if (!last_of_row(&x.s.count[2], a.splits, sm)) return;
   for (int i = threadIdx.x; i < x.waves; i += kThreads) sm.sums[i] = x.s.sums[i];
   for (int i = threadIdx.x; i < x.row.parts; i += kThreads) sm.part[i] = x.s.part[i];
