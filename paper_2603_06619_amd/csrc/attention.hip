@@ -504,7 +504,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(256) attn_dkv_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(256, D == 64 ? 2 : 1) attn_dkv_kernel(AttnArgs a) {
   struct RowWords { float shift[kDkvRows], delta[kDkvRows]; int last[kDkvRows]; };
   __shared__ __attribute__((aligned(16))) char tiles[2][2][kDkvRows * D * 2];
   __shared__ __attribute__((aligned(16))) RowWords words[2];
