@@ -196,8 +196,8 @@ struct Stay {
   int equal_end;
   __device__ __forceinline__ bool has(uint32_t key, int index) const { return key > least || (key == least && index <= equal_end); }
 };
-// What is listed: exponents' bins first .. last; what lies above bin `last`, in tokens or weight
-struct Gather { int first, last; uint64_t above; };
+// What is listed: exponents' bins first .. last; the weight above them and that of the row (rows without a top-k)
+struct Gather { int first, last; uint64_t above, all; };
 
 constexpr int kMaxParts = kMaxVocab / 4 / (64 * kUnroll) + kMaxSplits * kWaves + 2;
 
@@ -217,19 +217,27 @@ struct Shared {
   int equal_end, last_one;
 };
 
-__device__ __forceinline__ uint64_t wave_sum64(uint64_t x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor((unsigned long long)x, d, 64);
+// A value from another lane by way of the vector pipeline, 0 where the control has none: the sums below take a tenth of the time of their shuffles through LDS
+template <int kControl, int kRows>
+__device__ __forceinline__ uint64_t from_lane(uint64_t x) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, kControl, kRows, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), kControl, kRows, 0xf, false);
+  return (uint64_t)hi << 32 | lo;
+}
+// inclusive: within rows of 16 lanes by 1, 2, 4, 8, then the last lane of rows 0 and 2 to rows 1 and 3, then lane 31 to rows 2 and 3
+__device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {
+  x += from_lane<0x111, 0xf>(x);
+  x += from_lane<0x112, 0xf>(x);
+  x += from_lane<0x114, 0xf>(x);
+  x += from_lane<0x118, 0xf>(x);
+  x += from_lane<0x142, 0xa>(x);
+  x += from_lane<0x143, 0xc>(x);
   return x;
 }
-__device__ __forceinline__ uint64_t wave_scan64(uint64_t x) {       // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t y = __shfl_up((unsigned long long)x, d, 64);
-    if (lane >= d) x += y;
-  }
-  return x;
+__device__ __forceinline__ uint64_t wave_sum64(uint64_t x) {
+  x = wave_scan64(x);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, 63), hi = __builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), 63);
+  return (uint64_t)hi << 32 | lo;
 }
 
 // over the workgroup; every thread gets the result
@@ -243,10 +251,10 @@ __device__ __forceinline__ uint64_t block_sum64(uint64_t x, Shared& sm) {
   return s;
 }
 
-// The i in [0, n) at which the running sum of x(i) passes `target`, i.e. the first whose inclusive sum is > target, and the sum before it; n if
-// there is none.  What x reads has been written behind a barrier.
-template <class X>
-__device__ __forceinline__ int block_find(const X& x, int n, uint64_t target, uint64_t* before, Shared& sm) {
+// The i in [0, n) at which the running sum of x(i) passes target(sum of all), i.e. the first whose inclusive sum is greater, the sum before it, and that of all;
+// n if there is none.  What x reads has been written behind a barrier.
+template <class X, class Target>
+__device__ __forceinline__ int block_find(const X& x, int n, const Target& target_of, uint64_t* before, uint64_t* total, Shared& sm) {
   const int per = (n + kThreads - 1) / kThreads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int lo = threadIdx.x * per < n ? threadIdx.x * per : n, hi = lo + per < n ? lo + per : n;
   uint64_t mine = 0;
@@ -256,8 +264,14 @@ __device__ __forceinline__ int block_find(const X& x, int n, uint64_t target, ui
   if (lane == 63) sm.wave64[wave] = incl;
   if (threadIdx.x == 0) sm.found = (uint32_t)n;
   __syncthreads();
-  uint64_t at = incl - mine;
-  for (int w = 0; w < wave; ++w) at += sm.wave64[w];
+  uint64_t at = incl - mine, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const uint64_t sum = sm.wave64[w];
+    at += w < wave ? sum : 0;
+    all += sum;
+  }
+  const uint64_t target = target_of(all);
   if (at <= target && target < at + mine) {
     for (int i = lo; i < hi; ++i) {
       const uint64_t xi = x(i);
@@ -271,7 +285,13 @@ __device__ __forceinline__ int block_find(const X& x, int n, uint64_t target, ui
   }
   __syncthreads();
   *before = sm.found64;
+  *total = all;
   return (int)sm.found;
+}
+template <class X>
+__device__ __forceinline__ int block_find(const X& x, int n, uint64_t target, uint64_t* before, Shared& sm) {
+  uint64_t total;
+  return block_find(x, n, [&](uint64_t) { return target; }, before, &total, sm);
 }
 
 // The largest key whose elements, with all above it, have a weight (an element's: of(key)) over `target` in all: narrowed down by histograms of the keys from
@@ -440,16 +460,11 @@ __device__ __forceinline__ void bin_parts(const Row<T>& row, int w, const Settin
 
 // Which bins to list, from the row's histogram (all threads; behind a barrier)
 __device__ __forceinline__ Gather choose_bins(const Settings& set, const uint64_t* hist, Shared& sm) {
-  auto entry = [&](int i) { return hist[i]; };
-  uint64_t target = (uint64_t)set.top_k - 1, above = 0;
-  if (set.top_k <= 0) {
-    uint64_t total = 0;
-    for (int i = threadIdx.x; i < kBins; i += kThreads) total += hist[i];
-    target = reach_of(set.top_p, block_sum64(total, sm)) - 1;
-  }
-  const int bin = block_find(entry, kBins, target, &above, sm);
-  if (bin == kBins) return Gather{0, kBins - 1, 0};            // fewer tokens than the top-k: all of them
-  return set.top_k > 0 ? Gather{0, bin, 0} : Gather{bin, bin, above};
+  uint64_t above, all;
+  const int bin = block_find([&](int i) { return hist[i]; }, kBins,
+                             [&](uint64_t total) { return (set.top_k > 0 ? (uint64_t)set.top_k : reach_of(set.top_p, total)) - 1; }, &above, &all, sm);
+  if (bin == kBins) return Gather{0, kBins - 1, 0, all};       // fewer tokens than the top-k: all of them
+  return set.top_k > 0 ? Gather{0, bin, 0, all} : Gather{bin, bin, above, all};
 }
 
 // list: the tokens in those bins, of the wavefront's parts; *n counts on past the room
@@ -479,8 +494,8 @@ __device__ __forceinline__ void list_parts(const Row<T>& row, int w, const Weigh
 }
 
 // What stays, from a list of up to kThreads tokens in LDS (in no order): one token per thread, which counts those in front of it (larger, or equal with a
-// lower index).  Sorted, the last one that stays has the least logit and the last index among those equal to it.  all: the weight of the row
-__device__ __forceinline__ Stay threshold_of_short_list(const Settings& set, const Weigher& weigh, const Gather& g, int n, uint64_t all, Shared& sm) {
+// lower index).  Sorted, the last one that stays has the least logit and the last index among those equal to it.
+__device__ __forceinline__ Stay threshold_of_short_list(const Settings& set, const Weigher& weigh, const Gather& g, int n, Shared& sm) {
   const int t = threadIdx.x;
   uint64_t* order = sm.hist;                   // tokens as whole numbers in that order; then their weights, sorted
   static_assert(kThreads + 2 <= kBins, "");
@@ -503,26 +518,19 @@ __device__ __forceinline__ Stay threshold_of_short_list(const Settings& set, con
     sm.list[rank] = mine;
   }
   __syncthreads();
-  auto weight = [&](int i) { return order[i]; };
-  uint64_t before;
-  int end = n;                                 // tokens that stay
-  if (set.top_k > 0) {
-    end = set.top_k < n ? set.top_k : n;
-    if (set.top_p < 1.f) {
-      const uint64_t total = block_sum64(t < end ? order[t] : 0, sm);
-      const int last = block_find(weight, end, reach_of(set.top_p, total) - 1, &before, sm);
-      end = last < end ? last + 1 : end;
-    }
-  } else {
-    const int last = block_find(weight, n, reach_of(set.top_p, all) - 1 - g.above, &before, sm);
-    end = last < n ? last + 1 : n;
+  int end = set.top_k > 0 && set.top_k < n ? set.top_k : n;    // tokens that stay
+  if (set.top_k <= 0 || set.top_p < 1.f) {
+    uint64_t before, total;
+    const int last = block_find([&](int i) { return order[i]; }, end,
+                                [&](uint64_t of_top_k) { return reach_of(set.top_p, set.top_k > 0 ? of_top_k : g.all) - 1 - g.above; }, &before, &total, sm);
+    end = last < end ? last + 1 : end;
   }
   return Stay{sm.list[end - 1].key, (int)sm.list[end - 1].index};
 }
 
-// What stays, from the list in LDS (in no order); all: the weight of the row
-__device__ __forceinline__ Stay threshold_of_list(const Settings& set, const Weigher& weigh, uint32_t top, const Gather& g, int n, uint64_t all, Shared& sm) {
-  if (n <= kThreads) return threshold_of_short_list(set, weigh, g, n, all, sm);
+// What stays, from the list in LDS (in no order)
+__device__ __forceinline__ Stay threshold_of_list(const Settings& set, const Weigher& weigh, uint32_t top, const Gather& g, int n, Shared& sm) {
+  if (n <= kThreads) return threshold_of_short_list(set, weigh, g, n, sm);
   auto each = [&](auto f) {
     for (int i = threadIdx.x; i < n; i += kThreads) f(sm.list[i].key);
   };
@@ -545,7 +553,7 @@ __device__ __forceinline__ Stay threshold_of_list(const Settings& set, const Wei
     lo = x < lo ? x : lo;
     hi = y > hi ? y : hi;
   }
-  const Ranked r = rank_tokens(set, weigh, set.top_k > 0, lo, hi, all, g.above, each, [&](uint32_t least) {
+  const Ranked r = rank_tokens(set, weigh, set.top_k > 0, lo, hi, g.all, g.above, each, [&](uint32_t least) {
     uint64_t t = 0;
     each([&](uint32_t k) { t += k > least ? weigh.of_key(k) : 0; });
     return block_sum64(t, sm);
@@ -634,12 +642,10 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int64_t r, const R
                                          Shared& sm) {
   constexpr int kE = Row<T>::kE;
   const int lane = threadIdx.x & 63;
-  uint64_t total = 0;
-  for (int i = threadIdx.x; i < row.parts; i += kThreads) total += sm.part[i];
-  total = block_sum64(total, sm);
-  const uint64_t target = set.greedy ? 0 : share_of(a.random[r], total);
-  uint64_t before;
-  const int part = block_find([&](int i) { return sm.part[i]; }, row.parts, target, &before, sm);
+  uint64_t before, total;
+  auto target_of = [&](uint64_t sum) { return set.greedy ? 0 : share_of(a.random[r], sum); };
+  const int part = block_find([&](int i) { return sm.part[i]; }, row.parts, target_of, &before, &total, sm);
+  const uint64_t target = target_of(total);
   if (threadIdx.x >= 64) return;
   uint64_t all = 0;
   double soft = 0.0;
@@ -710,13 +716,10 @@ __global__ void __launch_bounds__(kThreads, 4) sample_row_kernel(SampleArgs a) {
   if (set.ranked) {
     bin_parts(row, wave, set, weigh, sm.hist);
     __syncthreads();
-    uint64_t all = 0;
-    for (int i = threadIdx.x; i < kBins; i += kThreads) all += sm.hist[i];
-    all = block_sum64(all, sm);
     const Gather g = choose_bins(set, sm.hist, sm);
     list_parts(row, wave, weigh, g, sm.list, &sm.list_n);
     __syncthreads();
-    stay = sm.list_n > kList ? threshold_slowly(a, row, set, weigh, top, sm) : threshold_of_list(set, weigh, top, g, (int)sm.list_n, all, sm);
+    stay = sm.list_n > kList ? threshold_slowly(a, row, set, weigh, top, sm) : threshold_of_list(set, weigh, top, g, (int)sm.list_n, sm);
     __syncthreads();
   }
   sum_parts(row, wave, set, weigh, stay, a.logp != nullptr, sm.part, &sm.sums[wave]);
@@ -833,22 +836,18 @@ __global__ void __launch_bounds__(kThreads, 4) sample_list_kernel(SampleArgs a) 
   if (top <= kKeyMinusInf) return;
   const Weigher weigh(top, set.temperature, sm.powers);
   const Gather g = *x.s.gather;
-  sm.powers.fill();
-  __syncthreads();
   list_parts(x.row, x.w, weigh, g, x.s.list, &x.s.count[3]);
   if (!last_of_row(&x.s.count[1], a.splits, sm)) return;
+  // loads of what a short list has, together with that of its length
+  const Listed mine = x.s.list[threadIdx.x];
   const uint32_t n = __hip_atomic_load(&x.s.count[3], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  Stay stay;
-  if (n > kList) {
-    stay = threshold_slowly(a, x.row, set, weigh, top, sm);
-  } else {
-    uint64_t all = 0;
-    for (int i = threadIdx.x; i < kBins; i += kThreads) all += x.s.hist[i];
-    all = block_sum64(all, sm);
-    for (int i = threadIdx.x; i < (int)n; i += kThreads) sm.list[i] = x.s.list[i];
-    __syncthreads();
-    stay = threshold_of_list(set, weigh, top, g, (int)n, all, sm);
+  sm.powers.fill();
+  sm.list[threadIdx.x] = mine;
+  if (n <= kList) {
+    for (int i = threadIdx.x + kThreads; i < (int)n; i += kThreads) sm.list[i] = x.s.list[i];
   }
+  __syncthreads();
+  const Stay stay = n > kList ? threshold_slowly(a, x.row, set, weigh, top, sm) : threshold_of_list(set, weigh, top, g, (int)n, sm);
   if (threadIdx.x == 0) *x.s.stay = stay;
 }
 
