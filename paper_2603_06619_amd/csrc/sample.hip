@@ -187,6 +187,13 @@ struct Row {
   }
 };
 
+// What other workgroups read is written past the L2 of this XCD: a fence then finds nothing there to write back (list kernel of four rows 14.9 -> XA us)
+template <bool kOthers>
+__device__ __forceinline__ void put(uint64_t* p, uint64_t x) {
+  if constexpr (kOthers) __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  else *p = x;
+}
+
 typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 struct Listed { uint32_t key, index; };
 struct WaveSums { uint64_t all; double soft; };      // all weights; exponentials at temperature 1, where the weights are of another
@@ -376,9 +383,10 @@ __device__ __forceinline__ Ranked rank_tokens(const Settings& set, const Weigher
   return r;
 }
 
-// A list that is too long: the least logit that stays from the row itself, in slices of one vector per thread.
+// A list that is too long: the least logit that stays from the row itself, in slices of one vector per thread.  Its arguments come by value: had it references,
+// the callers would keep theirs in memory from the start (5 us of the list kernel's 15).
 template <class T>
-__device__ __noinline__ Stay threshold_slowly(const SampleArgs& a, const Row<T>& row, const Settings& set, const Weigher& weigh, uint32_t top, Shared& sm) {
+__device__ __noinline__ Stay threshold_slowly(const Row<T> row, const Settings set, const Weigher weigh, uint32_t top, Shared& sm) {
   constexpr int kE = Row<T>::kE;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, slices = (row.vectors + kThreads - 1) / kThreads;
   auto each = [&](auto f) {
@@ -409,7 +417,7 @@ __device__ __noinline__ Stay threshold_slowly(const SampleArgs& a, const Row<T>&
   __syncthreads();
   uint64_t before;
   const int part = block_find([&](int i) { return sm.slice[i]; }, slices * kWaves, r.n_least - 1, &before, sm);
-  if (part == slices * kWaves) return Stay{r.least, a.vocab};
+  if (part == slices * kWaves) return Stay{r.least, row.vocab};
   const int j = part * 64 + lane;
   uint32_t k[kE];
   row.load(j, k);
@@ -570,7 +578,7 @@ __device__ __forceinline__ Stay threshold_of_list(const Settings& set, const Wei
 }
 
 // sums: weights of what stays, of each of the wavefront's parts; of all their tokens, and their exponentials at temperature 1
-template <class T>
+template <bool kOthers, class T>
 __device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, const Stay& stay, bool want_soft, uint64_t* part,
                                           WaveSums* sums) {
   constexpr int kE = Row<T>::kE;
@@ -580,7 +588,7 @@ __device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settin
   double soft = 0.0;
   auto end = [&](int id) {
     n = wave_sum64(n);
-    if (lane == 0) part[id] = n;
+    if (lane == 0) put<kOthers>(part + id, n);
     n = 0;
   };
   if (set.greedy) {
@@ -633,17 +641,20 @@ __device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settin
     for (int d = 1; d < 64; d <<= 1) soft += __shfl_xor(soft, d, 64);
   }
   all = wave_sum64(all);
-  if (lane == 0) *sums = WaveSums{all, soft};
+  if (lane == 0) {
+    put<kOthers>(&sums->all, all);
+    put<kOthers>((uint64_t*)&sums->soft, __builtin_bit_cast(uint64_t, soft));
+  }
 }
 
 // draw, from the parts' sums and the wavefronts' in LDS (behind a barrier)
 template <class T>
 __device__ __forceinline__ void draw_row(const SampleArgs& a, int64_t r, const Row<T>& row, const Settings& set, const Weigher& weigh, const Stay& stay, int waves,
-                                         Shared& sm) {
+                                         uint32_t word, Shared& sm) {
   constexpr int kE = Row<T>::kE;
   const int lane = threadIdx.x & 63;
   uint64_t before, total;
-  auto target_of = [&](uint64_t sum) { return set.greedy ? 0 : share_of(a.random[r], sum); };
+  auto target_of = [&](uint64_t sum) { return set.greedy ? 0 : share_of(word, sum); };
   const int part = block_find([&](int i) { return sm.part[i]; }, row.parts, target_of, &before, &total, sm);
   const uint64_t target = target_of(total);
   if (threadIdx.x >= 64) return;
@@ -719,12 +730,12 @@ __global__ void __launch_bounds__(kThreads, 4) sample_row_kernel(SampleArgs a) {
     const Gather g = choose_bins(set, sm.hist, sm);
     list_parts(row, wave, weigh, g, sm.list, &sm.list_n);
     __syncthreads();
-    stay = sm.list_n > kList ? threshold_slowly(a, row, set, weigh, top, sm) : threshold_of_list(set, weigh, top, g, (int)sm.list_n, sm);
+    stay = sm.list_n > kList ? threshold_slowly(row, set, weigh, top, sm) : threshold_of_list(set, weigh, top, g, (int)sm.list_n, sm);
     __syncthreads();
   }
-  sum_parts(row, wave, set, weigh, stay, a.logp != nullptr, sm.part, &sm.sums[wave]);
+  sum_parts<false>(row, wave, set, weigh, stay, a.logp != nullptr, sm.part, &sm.sums[wave]);
   __syncthreads();
-  draw_row(a, r, row, set, weigh, stay, kWaves, sm);
+  draw_row(a, r, row, set, weigh, stay, kWaves, a.random[r], sm);
 }
 
 // Several workgroups per row: what passes between them, in the workspace
@@ -807,10 +818,9 @@ template <class T>
 __global__ void __launch_bounds__(kThreads, 4) sample_bins_kernel(SampleArgs a) {
   __shared__ Shared sm;
   const SplitRow<T> x(a);
-  const Settings set(a, x.r);
-  if (!set.ranked) return;
   const uint32_t top = top_of_waves(x.s.top, x.waves);
-  if (top <= kKeyMinusInf) return;
+  const Settings set(a, x.r);
+  if (!set.ranked || top <= kKeyMinusInf) return;
   const Weigher weigh(top, set.temperature, sm.powers);
   for (int i = threadIdx.x; i < kBins; i += kThreads) sm.hist[i] = 0;
   sm.powers.fill();
@@ -830,13 +840,26 @@ template <class T>
 __global__ void __launch_bounds__(kThreads, 4) sample_list_kernel(SampleArgs a) {
   __shared__ Shared sm;
   const SplitRow<T> x(a);
-  const Settings set(a, x.r);
-  if (!set.ranked) return;
-  const uint32_t top = top_of_waves(x.s.top, x.waves);
-  if (top <= kKeyMinusInf) return;
-  const Weigher weigh(top, set.temperature, sm.powers);
+  // all loads at once, in front of the first that decides anything
   const Gather g = *x.s.gather;
-  list_parts(x.row, x.w, weigh, g, x.s.list, &x.s.count[3]);
+  const uint32_t top = top_of_waves(x.s.top, x.waves);
+  const Settings set(a, x.r);
+  if (threadIdx.x == 0) sm.list_n = 0;
+  if (!set.ranked || top <= kKeyMinusInf) return;
+  const Weigher weigh(top, set.temperature, sm.powers);
+  __syncthreads();
+  list_parts(x.row, x.w, weigh, g, sm.list, &sm.list_n);
+  __syncthreads();
+  // one place in the row's list for all of them: places of their own for every wavefront's tokens are atomics one after another
+  const int here = sm.list_n;
+  if (here > 0) {
+    if (threadIdx.x == 0) sm.found = atomicAdd(&x.s.count[3], (uint32_t)here);
+    __syncthreads();
+    for (int i = threadIdx.x; i < here && i < kList; i += kThreads) {
+      const uint32_t at = sm.found + i;
+      if (at < kList) put<true>((uint64_t*)&x.s.list[at], __builtin_bit_cast(uint64_t, sm.list[i]));
+    }
+  }
   if (!last_of_row(&x.s.count[1], a.splits, sm)) return;
   // loads of what a short list has, together with that of its length
   const Listed mine = x.s.list[threadIdx.x];
@@ -847,7 +870,7 @@ __global__ void __launch_bounds__(kThreads, 4) sample_list_kernel(SampleArgs a) 
     for (int i = threadIdx.x + kThreads; i < (int)n; i += kThreads) sm.list[i] = x.s.list[i];
   }
   __syncthreads();
-  const Stay stay = n > kList ? threshold_slowly(a, x.row, set, weigh, top, sm) : threshold_of_list(set, weigh, top, g, (int)n, sm);
+  const Stay stay = n > kList ? threshold_slowly(x.row, set, weigh, top, sm) : threshold_of_list(set, weigh, top, g, (int)n, sm);
   if (threadIdx.x == 0) *x.s.stay = stay;
 }
 
@@ -855,22 +878,23 @@ template <class T>
 __global__ void __launch_bounds__(kThreads, 4) sample_sums_kernel(SampleArgs a) {
   __shared__ Shared sm;
   const SplitRow<T> x(a);
+  const Stay ranked = *x.s.stay;             // of rows without a rank anything
+  const uint32_t top = top_of_waves(x.s.top, x.waves), word = a.random[x.r];
   const Settings set(a, x.r);
-  const uint32_t top = top_of_waves(x.s.top, x.waves);
   if (top <= kKeyMinusInf) {
     if (blockIdx.x % a.splits == 0 && threadIdx.x == 0) nothing_to_draw(a, x.r);
     return;
   }
   const Weigher weigh(top, set.temperature, sm.powers);
-  const Stay stay = set.ranked ? *x.s.stay : Stay{kKeyMinusInf, -1};
+  const Stay stay = set.ranked ? ranked : Stay{kKeyMinusInf, -1};
   sm.powers.fill();
   __syncthreads();
-  sum_parts(x.row, x.w, set, weigh, stay, a.logp != nullptr, x.s.part, &x.s.sums[x.w]);
+  sum_parts<true>(x.row, x.w, set, weigh, stay, a.logp != nullptr, x.s.part, &x.s.sums[x.w]);
   if (!last_of_row(&x.s.count[2], a.splits, sm)) return;
   for (int i = threadIdx.x; i < x.waves; i += kThreads) sm.sums[i] = x.s.sums[i];
   for (int i = threadIdx.x; i < x.row.parts; i += kThreads) sm.part[i] = x.s.part[i];
   __syncthreads();
-  draw_row(a, x.r, x.row, set, weigh, stay, x.waves, sm);
+  draw_row(a, x.r, x.row, set, weigh, stay, x.waves, word, sm);
 }
 
 // Workgroups per row: enough for every compute unit to have two
