@@ -336,10 +336,10 @@ __device__ __forceinline__ bool select_key(const Each& each, uint32_t lo, uint32
 
 struct Drawn { int index; uint32_t key; uint64_t weight, total; };
 
-__device__ __forceinline__ void write_out(const SampleArgs& a, int64_t r, const Drawn& d, const Weigher& weigh, double soft) {
+__device__ __forceinline__ void write_out(const SampleArgs& a, int64_t r, const Drawn& d, const Weigher& weigh, double log_soft) {
   const float z = fminf(logit_of(d.key), __FLT_MAX__);
   a.ids[r] = d.index;
-  if (a.logp) a.logp[r] = (float)((double)(z - weigh.max) - log(soft));
+  if (a.logp) a.logp[r] = (float)((double)(z - weigh.max) - log_soft);
   if (a.logq) a.logq[r] = (float)log((double)d.weight / (double)d.total);
 }
 __device__ __forceinline__ void nothing_to_draw(const SampleArgs& a, int64_t r) {
@@ -658,6 +658,10 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int64_t r, const R
   const int part = block_find([&](int i) { return sm.part[i]; }, row.parts, target_of, &before, &total, sm);
   const uint64_t target = target_of(total);
   if (threadIdx.x >= 64) return;
+  typename Row<T>::Vector x[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) row.load((part * kUnroll + u) * 64 + lane, x[u]);
+  // while they arrive
   uint64_t all = 0;
   double soft = 0.0;
   for (int w = lane; w < waves; w += 64) {
@@ -668,15 +672,14 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int64_t r, const R
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) soft += __shfl_xor(soft, d, 64);
   if (!set.greedy && set.temperature == 1.f) soft = (double)all * (1.0 / (double)kOne);
+  const double log_soft = a.logp ? log(soft) : 0.0;
 #pragma unroll 1
   for (int u = 0; u < kUnroll; ++u) {
     const int j = (part * kUnroll + u) * 64 + lane;
-    typename Row<T>::Vector x;
-    row.load(j, x);
     uint64_t w[kE], sum = 0;
 #pragma unroll
     for (int i = 0; i < kE; ++i) {
-      const float z = Row<T>::value(x.e[i]);
+      const float z = Row<T>::value(x[0].e[i]);
       if (set.greedy) {
         w[i] = z >= weigh.max;
       } else {
@@ -692,13 +695,15 @@ __device__ __forceinline__ void draw_row(const SampleArgs& a, int64_t r, const R
       Drawn d{-1, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < kE; ++i) {
-        if (d.index < 0 && target < at + w[i]) d = Drawn{j * kE - row.lead + i, key_of(Row<T>::value(x.e[i])), set.greedy ? 1 : w[i], set.greedy ? 1 : total};
+        if (d.index < 0 && target < at + w[i]) d = Drawn{j * kE - row.lead + i, key_of(Row<T>::value(x[0].e[i])), set.greedy ? 1 : w[i], set.greedy ? 1 : total};
         at += w[i];
       }
-      write_out(a, r, d, weigh, soft);
+      write_out(a, r, d, weigh, log_soft);
     }
     if (__any(mine)) return;
     before += __shfl((unsigned long long)incl, 63, 64);
+#pragma unroll
+    for (int v = 0; v + 1 < kUnroll; ++v) x[v].q = x[v + 1].q;
   }
 }
 
