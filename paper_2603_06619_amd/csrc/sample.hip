@@ -15,6 +15,10 @@
 // A row with one workgroup goes through them in one kernel; with more, each of top, bins, list and sums is a kernel, and the workgroup that comes last in
 // a row does what follows from all (it knows by a counter; nobody waits).  If the list is longer than LDS has room for (very many equal logits), the row
 // is gone over once more by one workgroup (threshold_slowly).
+//
+// 512 rows of 152064 fp32 logits, no filter: 109 us for 311 MB, read twice (5.7 TB/s; weights alone are 60 us of vector instructions).  Four rows of 151936 bf16 logits
+// with every filter: 39 us, all of it latency (top 3, bins 8.5, list 8.7, sums 13, and three gaps between launches of 2): each phase reads a megabyte in 2 to 3 us, and
+// its last workgroup then takes 3 to 5 for fences, loads of what the others wrote, and a search.
 #include "nat_internal.h"
 
 namespace nat {
@@ -187,7 +191,7 @@ struct Row {
   }
 };
 
-// What other workgroups read is written past the L2 of this XCD: a fence then finds nothing there to write back (list kernel of four rows 14.9 -> XA us)
+// What other workgroups read is written past the L2 of this XCD: a fence then finds nothing there to write back (1 us, else 4)
 template <bool kOthers>
 __device__ __forceinline__ void put(uint64_t* p, uint64_t x) {
   if constexpr (kOthers) __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
