@@ -581,15 +581,24 @@ __device__ __forceinline__ Stay threshold_of_list(const Settings& set, const Wei
   return Stay{r.least, some ? (int)~key : kMaxVocab};
 }
 
-// sums: weights of what stays, of each of the wavefront's parts; of all their tokens, and their exponentials at temperature 1
-template <bool kOthers, class T>
-__device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, const Stay& stay, bool want_soft, uint64_t* part,
+// sums: weights of what stays, of each of the wavefront's parts; of all their tokens, and (kSoft) their exponentials at temperature 1
+template <bool kOthers, bool kSoft, class T>
+__device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, const Stay& stay, bool want_all, uint64_t* part,
                                           WaveSums* sums) {
   constexpr int kE = Row<T>::kE;
   using Vector = typename Row<T>::Vector;
   const int lane = threadIdx.x & 63;
   uint64_t all = 0, n = 0;
   double soft = 0.0;
+  auto add_soft = [&](const Vector& x) {
+    if constexpr (kSoft) {
+#pragma unroll
+      for (int i = 0; i < kE; ++i) {
+        const float e = __builtin_amdgcn_fmed3f((Row<T>::value(x.e[i]) - weigh.max) * kLog2E, -200.f, 0.f);       // NaN: 0
+        soft += (double)__builtin_amdgcn_exp2f(e);
+      }
+    }
+  };
   auto end = [&](int id) {
     n = wave_sum64(n);
     if (lane == 0) put<kOthers>(part + id, n);
@@ -599,11 +608,13 @@ __device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settin
     row.template each_part<true>(w, [&](int, const Vector& x) {
 #pragma unroll
       for (int i = 0; i < kE; ++i) n += Row<T>::value(x.e[i]) >= weigh.max;
+      add_soft(x);
     }, end);
   } else if (!set.ranked && set.least <= 1) {
     row.template each_part<true>(w, [&](int, const Vector& x) {
 #pragma unroll
       for (int i = 0; i < kE; ++i) n += weigh.biased_weight(weigh.exponent(Row<T>::value(x.e[i])));
+      add_soft(x);
     }, [&](int id) {
       n -= (uint64_t)(kE * kUnroll) * Weigher::kBias;
       all += n;
@@ -617,9 +628,9 @@ __device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settin
         all += a;
         n += a >= set.least ? a : 0;
       }
+      add_soft(x);
     }, end);
   } else {
-    const bool want_all = want_soft && set.temperature == 1.f;
     row.template each_part<true>(w, [&](int j, const Vector& x) {
 #pragma unroll
       for (int i = 0; i < kE; ++i) {
@@ -631,16 +642,10 @@ __device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settin
           n += stays && a >= set.least ? a : 0;
         }
       }
+      add_soft(x);
     }, end);
   }
-  if (want_soft && (set.greedy || set.temperature != 1.f)) {
-    row.template each_vector<false>(w, [&](int, const Vector& x) {
-#pragma unroll
-      for (int i = 0; i < kE; ++i) {
-        const float e = __builtin_amdgcn_fmed3f((Row<T>::value(x.e[i]) - weigh.max) * kLog2E, -200.f, 0.f);       // NaN: 0
-        soft += (double)__builtin_amdgcn_exp2f(e);
-      }
-    });
+  if constexpr (kSoft) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) soft += __shfl_xor(soft, d, 64);
   }
@@ -649,6 +654,12 @@ __device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settin
     put<kOthers>(&sums->all, all);
     put<kOthers>((uint64_t*)&sums->soft, __builtin_bit_cast(uint64_t, soft));
   }
+}
+template <bool kOthers, class T>
+__device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settings& set, const Weigher& weigh, const Stay& stay, bool want_soft, uint64_t* part,
+                                          WaveSums* sums) {
+  if (want_soft && (set.greedy || set.temperature != 1.f)) sum_parts<kOthers, true>(row, w, set, weigh, stay, false, part, sums);
+  else sum_parts<kOthers, false>(row, w, set, weigh, stay, want_soft, part, sums);
 }
 
 // draw, from the parts' sums and the wavefronts' in LDS (behind a barrier)
