@@ -802,9 +802,9 @@ __device__ __forceinline__ bool last_of_row(uint32_t* count, int n, Shared& sm) 
   __builtin_amdgcn_s_waitcnt(0x0f70);        // vmcnt(0)
   __syncthreads();
   if (threadIdx.x == 0) {
-    __threadfence();
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
     sm.last_one = atomicAdd(count, 1u) == (uint32_t)n - 1;
-    if (sm.last_one) __threadfence();
+    if (sm.last_one) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   }
   __syncthreads();
   return sm.last_one;
@@ -917,13 +917,16 @@ __global__ void __launch_bounds__(kThreads, 4) sample_sums_kernel(SampleArgs a) 
   draw_row(a, x.r, x.row, set, weigh, stay, x.waves, word, sm);
 }
 
-// Workgroups per row: enough for every compute unit to have two
+// Workgroups per row: for every compute unit one in all, each with 4096 elements at least (one sweep of its loads), and only where that takes kWorthSplitting elements
+// off a workgroup: the further launches and fences take as long.  In us without and with top-k and top-p, bf16, one workgroup per row against several: 4 rows of 32000
+// 16, 29 against 19, 28 (8 each), of 50257 20, 43 against 17, 30 (12); of 152064 42, 91 against 17, 32 (32); 128 rows of 50257 21, 44 against 23, 51 (2), of 152064 46, 96 against
+// 37, 81.  Two workgroups per compute unit: 200 rows of 152064 60, 134, one per row 48, 101.
+constexpr int64_t kWorthSplitting = 40000;
 int splits_of(int64_t n_rows, int64_t V) {
-  int64_t s = (512 + n_rows - 1) / n_rows;
-  const int64_t most = (V + 4095) / 4096;              // 512 elements for a wavefront
-  if (s > most) s = most;
+  int64_t s = 256 / n_rows;
+  if (s > V / 4096) s = V / 4096;
   if (s > kMaxSplits) s = kMaxSplits;
-  return (int)(s < 1 ? 1 : s);
+  return s < 1 || V - V / s < kWorthSplitting ? 1 : (int)s;
 }
 // of a row that starts anywhere in its first vector
 size_t row_bytes_of(int32_t V, int elem, int splits) {
