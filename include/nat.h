@@ -436,11 +436,14 @@ nat_status nat_attn_fwd(const nat_attn_params* params, const void* d_q, const vo
  * the sums for dk, dv over all query heads that share the key head.
  *   d_out, d_lse from nat_attn_fwd;  d_dout [n_q, n_q_heads, head_dim] bf16;
  *   d_dq like d_q, d_dk, d_dv like d_k: bf16 out (rows of no sequence are not written);
- *   d_ws / ws_bytes: at least nat_attn_bwd_workspace_bytes, 256-byte aligned.
+ *   d_ws / ws_bytes: at least nat_attn_bwd_workspace_bytes, 256-byte aligned.  With
+ *                nat_attn_bwd_workspace_full_bytes (of params' counts, causal and head_dim; 0 if they are out of
+ *                range) the sums of dk, dv are shared by more workgroups where there are few keys.
  * P and dS are rounded to bf16 for the products that they enter.  No atomics: results do not change from
- * run to run.  Errors as nat_attn_fwd, plus NAT_WORKSPACE_TOO_SMALL.  With n_q = 0, dk and dv are zeros.
+ * run to run (with workspaces of other sizes the sums may be cut elsewhere).  Errors as nat_attn_fwd, plus NAT_WORKSPACE_TOO_SMALL.  With n_q = 0, dk and dv are zeros.
  */
 size_t nat_attn_bwd_workspace_bytes(int64_t n_q, int32_t n_q_heads);
+size_t nat_attn_bwd_workspace_full_bytes(const nat_attn_params* params);
 nat_status nat_attn_bwd(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v,
                         const void* d_out, const float* d_lse, const void* d_dout, const int32_t* d_cu_q,
                         const int32_t* d_cu_k, void* d_dq, void* d_dk, void* d_dv,

@@ -121,6 +121,8 @@ def load_library():
     lib.nat_attn_fwd.argtypes = [pa, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.nat_attn_bwd_workspace_bytes.restype = sz
     lib.nat_attn_bwd_workspace_bytes.argtypes = [i64, i32]
+    lib.nat_attn_bwd_workspace_full_bytes.restype = sz
+    lib.nat_attn_bwd_workspace_full_bytes.argtypes = [ctypes.POINTER(_CAttnParams)]
     lib.nat_attn_bwd.restype = i32
     lib.nat_attn_bwd.argtypes = [pa, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.nat_kv_write.restype = i32
@@ -379,6 +381,11 @@ def nat_attn_fwd(q, k, v, cu_q, cu_k, causal, scale, out, lse):
 
 def attn_bwd_workspace_bytes(n_q, n_q_heads):
     return int(load_library().nat_attn_bwd_workspace_bytes(int(n_q), int(n_q_heads)))
+
+
+def attn_bwd_workspace_full_bytes(n_q, n_k, n_seqs, n_q_heads, n_kv_heads, head_dim, causal):
+    p = _CAttnParams(int(n_seqs), int(n_q_heads), int(n_kv_heads), int(head_dim), DTYPE_BF16, int(causal), 1.0, int(n_q), int(n_k))
+    return int(load_library().nat_attn_bwd_workspace_full_bytes(ctypes.byref(p)))
 
 
 def nat_attn_bwd(q, k, v, out, lse, dout, cu_q, cu_k, causal, scale, dq, dk, dv, workspace):

@@ -46,6 +46,8 @@ struct AttnArgs {
   uint16_t *dq, *dk, *dv;
   int64_t dout_stride, dq_stride, dk_stride, dv_stride;
   int slots;                     // tile slots per key head
+  int row_parts;                 // dk, dv: workgroups that share a tile's rows
+  float* parts;                  // their sums [row_parts][n_k][hkv][dk, dv][D], if there are several
   uint32_t group_inverse;        // see small_quotient
 };
 
@@ -521,6 +523,8 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
 // SIMD, so the work under the products has to come from itself, and a step is one block but for the mask's edge (a branch among the exponentials: 1300 us
 // instead of 1140, for 8 rollouts of up to 4096 tokens; 750 TFLOP/s, this at 1.6 GHz).  At D = 64 two fit: 16 rollouts of up to 311 tokens 19.6 us, with one 27.0; 4 of 4096,
 // with dq, 554 and 645.
+// Where there are few tiles of keys for the chip their rows are cut into row_parts ranges, one workgroup each, whose sums go to memory in fp32 and are added in order by
+// attn_dkv_join_kernel (backward of 1024 tokens, 32 heads on 8: 172 us, then 94; of 2048, 2 heads on 1: 185, then 87).
 template <int D>
 __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) attn_dkv_kernel(AttnArgs a) {
   struct RowWords { float shift[kDkvRows], delta[kDkvRows]; int last[kDkvRows]; };
@@ -528,7 +532,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) attn_dkv_kernel(AttnArgs
   __shared__ __attribute__((aligned(16))) RowWords words[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   int head, slot;
-  head_and_slot(blockIdx.x, a.hkv, a.slots, head, slot);
+  head_and_slot(blockIdx.x, a.hkv, a.slots * a.row_parts, head, slot);
+  const int part = slot % a.row_parts;
+  slot /= a.row_parts;
   if (slot >= a.slots) return;
   int64_t first_slot;
   const Sequence s = sequence(a, sequence_of_slot(a.cu_k, a.n_seqs, a.n_k, 1, kDkvKeys, slot, &first_slot));
@@ -542,7 +548,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) attn_dkv_kernel(AttnArgs
   const int n_rows = s.n_q * a.group, wave_key = tile_key + wave * 32;
   // the first row that sees the tile's first key
   const int first_query = a.causal && tile_key > s.ahead ? tile_key - s.ahead : 0;
-  const int first_row = first_query < s.n_q ? first_query * a.group : n_rows;
+  const int seen_from = first_query < s.n_q ? first_query * a.group : n_rows;
+  const int part_steps = ((n_rows - seen_from + kDkvRows - 1) / kDkvRows + a.row_parts - 1) / a.row_parts;
+  const int first_row = seen_from + part * part_steps * kDkvRows, end_row = n_rows - first_row > part_steps * kDkvRows ? first_row + part_steps * kDkvRows : n_rows;
   const int wave_first = a.causal ? wave_key - s.ahead : 0;            // the first query that sees the wavefront's first key
   const int tile_all = a.causal ? tile_key + kDkvKeys - 1 - s.ahead : 0;
   const int wave_all = a.causal ? wave_key + 31 - s.ahead : 0;         // queries from here on see all its keys
@@ -673,20 +681,20 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) attn_dkv_kernel(AttnArgs
   auto pass = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) dk[db] = dv[db] = f32x16{};
-    next_query = first_query;
-    next_head = 0;
+    next_query = first_row / a.group;
+    next_head = first_row - next_query * a.group;
     fetch(first_row, tiles[0]);
     store_words(words[0]);
     end_of_step();
-    for (int row0 = first_row; row0 < n_rows; row0 += 2 * kDkvRows) {
+    for (int row0 = first_row; row0 < end_row; row0 += 2 * kDkvRows) {
       advance();
-      if (row0 + kDkvRows < n_rows) fetch(row0 + kDkvRows, tiles[1]);
+      if (row0 + kDkvRows < end_row) fetch(row0 + kDkvRows, tiles[1]);
       step(tiles[0][0], tiles[0][1], words[0], careful);
       store_words(words[1]);
       end_of_step();
-      if (row0 + kDkvRows >= n_rows) break;
+      if (row0 + kDkvRows >= end_row) break;
       advance();
-      if (row0 + 2 * kDkvRows < n_rows) fetch(row0 + 2 * kDkvRows, tiles[0]);
+      if (row0 + 2 * kDkvRows < end_row) fetch(row0 + 2 * kDkvRows, tiles[0]);
       step(tiles[1][0], tiles[1][1], words[1], careful);
       store_words(words[0]);
       end_of_step();
@@ -695,8 +703,47 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) attn_dkv_kernel(AttnArgs
   pass(std::false_type{});
   if (__syncthreads_or(not_finite<D>(dk) || not_finite<D>(dv))) pass(std::true_type{});
   if (key >= s.n_k) return;
+  if (a.row_parts > 1) {
+    float* row = a.parts + ((part * a.n_k + s.k0 + key) * a.hkv + head) * (2 * D) + 4 * half;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        *(f32x4*)(row + 32 * db + 8 * i) = f32x4{dk[db][4 * i], dk[db][4 * i + 1], dk[db][4 * i + 2], dk[db][4 * i + 3]};
+        *(f32x4*)(row + D + 32 * db + 8 * i) = f32x4{dv[db][4 * i], dv[db][4 * i + 1], dv[db][4 * i + 2], dv[db][4 * i + 3]};
+      }
+    return;
+  }
   store_columns<D>(a.dk + (s.k0 + key) * a.dk_stride + head * D, dk, a.scale, lane);
   store_columns<D>(a.dv + (s.k0 + key) * a.dv_stride + head * D, dv, 1.f, lane);
+}
+
+// dk, dv of a tile's keys from the sums of its row_parts workgroups; kJoinKeys keys per workgroup, all loads of a sum under way at once
+constexpr int kJoinKeys = 8, kMaxRowParts = 8;
+template <int D>
+__global__ void __launch_bounds__(256) attn_dkv_join_kernel(AttnArgs a) {
+  int head, slot;
+  head_and_slot(blockIdx.x, a.hkv, a.slots, head, slot);
+  if (slot >= a.slots) return;
+  int64_t first_slot;
+  const Sequence s = sequence(a, sequence_of_slot(a.cu_k, a.n_seqs, a.n_k, 1, kDkvKeys, slot, &first_slot));
+  const int tile_key = (int)(slot - first_slot) * kDkvKeys;
+  if (slot < first_slot || tile_key >= s.n_k) return;
+  constexpr int kFours = 2 * D / 4;              // of a key
+  const int key0 = tile_key + blockIdx.y * kJoinKeys, n = (s.n_k - key0 < kJoinKeys ? s.n_k - key0 : kJoinKeys) * kFours;
+  const int64_t part_stride = a.n_k * a.hkv * (2 * D);
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int64_t key = s.k0 + key0 + i / kFours;
+    const int at = i % kFours * 4;
+    const float* from = a.parts + (key * a.hkv + head) * (2 * D) + at;
+    f32x4 x[kMaxRowParts], sum = {};
+#pragma unroll
+    for (int p = 0; p < kMaxRowParts; ++p) x[p] = p < a.row_parts ? *(const f32x4*)(from + p * part_stride) : f32x4{};
+#pragma unroll
+    for (int p = 0; p < kMaxRowParts; ++p) sum += x[p];
+    if (at < D) *(bf16x4*)(a.dk + key * a.dk_stride + head * D + at) = __builtin_convertvector(sum * a.scale, bf16x4);
+    else *(bf16x4*)(a.dv + key * a.dv_stride + head * D + at - D) = __builtin_convertvector(sum, bf16x4);
+  }
 }
 
 bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
@@ -752,6 +799,18 @@ nat_status attn_args(const nat_attn_params* p, const void* d_q, const void* d_k,
   return NAT_OK;
 }
 
+// Workgroups per tile of keys: as many as make up for tiles of unequal length (causal) or fill the chip, with four steps each at least.  Backward in us, D = 128, 32 heads
+// on 8, causal: 2048 tokens 332 with one, 190 with 3, 213 with 7; 4096 tokens 720, 557 with 3; all keys seen: 912, 899, 939 with 3.  D = 64, two workgroups at a time on a compute
+// unit: 8192 tokens of 4 heads 271 with one, 203 with 3.
+int row_parts_of(int64_t n_q, int64_t n_k, int64_t n_seqs, int64_t hkv, int64_t group, int head_dim, bool causal) {
+  if (n_seqs <= 0 || n_q <= 0 || n_k <= 0) return 1;
+  const int64_t blocks = (n_k / kDkvKeys + n_seqs) * hkv, steps = n_q * group / n_seqs / kDkvRows / (causal ? 2 : 1);
+  int64_t p = (!causal ? 512 : head_dim == 128 ? 768 : 1024) / blocks;
+  if (p > steps / 4) p = steps / 4;
+  return (int)(p < 1 ? 1 : p > kMaxRowParts ? kMaxRowParts : p);
+}
+size_t row_part_bytes(int64_t n_k, int64_t hkv, int64_t head_dim) { return (size_t)n_k * hkv * head_dim * 8; }
+
 }  // namespace
 }  // namespace nat
 
@@ -778,6 +837,15 @@ extern "C" nat_status nat_attn_fwd(const nat_attn_params* params, const void* d_
 extern "C" size_t nat_attn_bwd_workspace_bytes(int64_t n_q, int32_t n_q_heads) {
   if (n_q <= 0 || n_q_heads <= 0 || n_q > INT32_MAX || n_q_heads > 4096) return 0;
   return ((size_t)n_q * (size_t)n_q_heads * 4 + 255) / 256 * 256;
+}
+
+extern "C" size_t nat_attn_bwd_workspace_full_bytes(const nat_attn_params* p) {
+  if (!p || p->n_kv_heads <= 0 || p->n_q_heads <= 0 || p->n_q_heads % p->n_kv_heads != 0 || p->n_q > INT32_MAX || p->n_k > INT32_MAX ||
+      (p->head_dim != 64 && p->head_dim != 128))
+    return 0;
+  const size_t least = nat_attn_bwd_workspace_bytes(p->n_q, p->n_q_heads);
+  const int parts = row_parts_of(p->n_q, p->n_k, p->n_seqs, p->n_kv_heads, p->n_q_heads / p->n_kv_heads, p->head_dim, p->causal != 0);
+  return parts > 1 ? least + parts * row_part_bytes(p->n_k, p->n_kv_heads, p->head_dim) : least;
 }
 
 extern "C" nat_status nat_attn_bwd(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v, const void* d_out,
@@ -809,9 +877,19 @@ extern "C" nat_status nat_attn_bwd(const nat_attn_params* params, const void* d_
   if (a.n_k > 0) {
     ProfScope prof(PC_ATTN_BWD, s);
     a.slots = (int)(a.n_k / kDkvKeys + a.n_seqs);
-    if (params->head_dim == 128) attn_dkv_kernel<128><<<grid_of(a.hkv, a.slots), 256, 0, s>>>(a);
-    else attn_dkv_kernel<64><<<grid_of(a.hkv, a.slots), 256, 0, s>>>(a);
+    a.row_parts = row_parts_of(a.n_q, a.n_k, a.n_seqs, a.hkv, a.group, params->head_dim, a.causal != 0);
+    const size_t least = nat_attn_bwd_workspace_bytes(a.n_q, a.hq), slab = row_part_bytes(a.n_k, a.hkv, params->head_dim);
+    while (a.row_parts > 1 && ws_bytes < least + a.row_parts * slab) --a.row_parts;
+    a.parts = (float*)((char*)d_ws + least);
+    const unsigned blocks = grid_of(a.hkv, (int64_t)a.slots * a.row_parts);
+    if (params->head_dim == 128) attn_dkv_kernel<128><<<blocks, 256, 0, s>>>(a);
+    else attn_dkv_kernel<64><<<blocks, 256, 0, s>>>(a);
     NAT_LAUNCH_CHECK();
+    if (a.row_parts > 1) {
+      if (params->head_dim == 128) attn_dkv_join_kernel<128><<<dim3(grid_of(a.hkv, a.slots), kDkvKeys / kJoinKeys), 256, 0, s>>>(a);
+      else attn_dkv_join_kernel<64><<<dim3(grid_of(a.hkv, a.slots), kDkvKeys / kJoinKeys), 256, 0, s>>>(a);
+      NAT_LAUNCH_CHECK();
+    }
   }
   return NAT_OK;
 }

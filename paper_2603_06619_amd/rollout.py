@@ -50,7 +50,7 @@ class RolloutStage:
     def attention_backward(self, dout, q, k, v, out, lse, cu_q, cu_k=None, causal=True, scale=None):
         """(dq, dk, dv) of attention(), with its results."""
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        ws = self._buf("attn_bwd", nb.attn_bwd_workspace_bytes(q.shape[0], q.shape[1]))
+        ws = self._buf("attn_bwd", nb.attn_bwd_workspace_full_bytes(q.shape[0], k.shape[0], cu_q.numel() - 1, q.shape[1], k.shape[1], q.shape[2], causal))
         nb.nat_attn_bwd(q, k, v, out, lse, dout, cu_q, cu_q if cu_k is None else cu_k, causal, self._scale(scale, q.shape[2]),
                         dq, dk, dv, ws)
         return dq, dk, dv

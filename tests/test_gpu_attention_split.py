@@ -1,0 +1,105 @@
+"""nat_attn_bwd where several workgroups share the rows that see a tile of keys (few keys, many rows): within the limits of test_gpu_attention.py, with every
+size of workspace."""
+import numpy as np
+import pytest
+import torch
+
+from nat_testlib import DEV
+from test_gpu_attention import check, host, make, run, stage  # noqa: F401 (stage is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def parts(c, causal=True):
+    import paper_2603_06619_amd as nat
+    (n_q, hq, D), (n_k, hkv, _) = c["q"].shape, c["k"].shape
+    full = nat.attn_bwd_workspace_full_bytes(n_q, n_k, c["cu_q"].numel() - 1, hq, hkv, D, causal)
+    return (full - nat.attn_bwd_workspace_bytes(n_q, hq)) // (n_k * hkv * D * 8)
+
+
+@pytest.mark.parametrize("lens_q,lens_k,hq,hkv,D,causal", [
+    ([700], [700], 8, 1, 64, True), ([700], [700], 8, 1, 128, True), ([513], [513], 14, 2, 128, True), ([601], [601], 2, 2, 64, False),
+    ([900], [33], 4, 2, 128, False), ([900], [33], 8, 1, 64, True), ([5, 1200, 0, 300], [5, 1200, 0, 300], 6, 2, 64, True), ([300, 900], [1000, 901], 7, 1, 128, True),
+    ([129], [129], 60, 1, 128, True),
+])
+def test_shared_rows(stage, lens_q, lens_k, hq, hkv, D, causal):  # noqa: F811
+    c = make(len(lens_q), lens_q, lens_k, hq, hkv, D)
+    assert parts(c, causal) > 1
+    check(c, run(stage, c, causal=causal), causal=causal)
+
+
+def test_every_workspace(stage):  # noqa: F811
+    """From the least on, the sums are cut as the workspace allows: each result within the limits, dq always the same; what lies behind the workspace and between the
+    rows of dk and dv stays."""
+    import paper_2603_06619_amd as nat
+    hq, hkv, D = 8, 1, 64
+    c = make(7, [640, 900], [640, 900], hq, hkv, D)
+    n = 1540
+    r = run(stage, c)
+    slab = n * hkv * D * 8
+    least, full = nat.attn_bwd_workspace_bytes(n, hq), nat.attn_bwd_workspace_full_bytes(n, n, 2, hq, hkv, D, True)
+    assert (full - least) // slab >= 3
+    for size in (least, least + slab, least + 2 * slab, full - slab, full, full + 1000):
+        ws = torch.full((size + 4096,), 0xaa, dtype=torch.uint8, device=DEV)
+        whole = torch.full((n, 2 * hkv * D + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+        dk, dv = (whole[:, at * D:(at + hkv) * D].unflatten(1, (hkv, D)) for at in (0, hkv))
+        dq = torch.empty_like(r["dq"])
+        nat.nat_attn_bwd(c["q"], c["k"], c["v"], r["out"], r["lse"], c["dout"], c["cu_q"], c["cu_k"], True, D ** -0.5, dq, dk, dv, ws[:size])
+        torch.cuda.synchronize()
+        assert torch.equal(dq, r["dq"]) and bool((ws[max(size, full):] == 0xaa).all()) and bool((whole[:, 2 * hkv * D:] == 7.0).all())
+        check(c, dict(r, dk=dk, dv=dv), names=("dk", "dv"))
+        if size >= full:
+            assert torch.equal(dk, r["dk"]) and torch.equal(dv, r["dv"])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_of_no_sequence_and_what_is_masked(stage, D):  # noqa: F811
+    """Offsets that leave rows out, and infinities and NaN where the mask hides them: later keys and values, and rows outside."""
+    import paper_2603_06619_amd as nat
+    hq, hkv, n = 8, 1, 1000
+    c = make(9, [n], [n], hq, hkv, D)
+    c["cu_q"] = c["cu_k"] = torch.tensor([40, 960], dtype=torch.int32, device=DEV)
+    assert parts(c) > 1
+    inner = {x: c[x][40:960].clone() for x in ("q", "k", "v", "dout")}
+    inner["cu_q"] = inner["cu_k"] = torch.tensor([0, 920], dtype=torch.int32, device=DEV)
+    ref = run(stage, inner)
+    for x in ("q", "k", "v", "dout"):
+        c[x][:40] = float("nan")
+        c[x][960:] = float("inf")
+    out, lse = stage.attention(c["q"], c["k"], c["v"], c["cu_q"], c["cu_k"])
+    dq, dk, dv = (torch.full_like(c[x], 9.0) for x in ("q", "k", "v"))
+    ws = torch.empty(nat.attn_bwd_workspace_full_bytes(n, n, 1, hq, hkv, D, True), dtype=torch.uint8, device=DEV)
+    nat.nat_attn_bwd(c["q"], c["k"], c["v"], out, lse, c["dout"], c["cu_q"], c["cu_k"], True, D ** -0.5, dq, dk, dv, ws)
+    for got, want in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+        assert bool((got[:40] == 9.0).all()) and bool((got[960:] == 9.0).all())
+        over = np.abs(host(got[40:960]) - host(ref[want]))
+        assert over.max() <= 2.0 ** -7 * np.abs(host(ref[want])).max()         # cut elsewhere: sums of other order, the rounding of the result
+    # values that only the last row sees, and that row takes no gradient: the others' gradients stay as they were
+    inner["dout"][919] = 0.0
+    ref = run(stage, inner)
+    inner["k"][919] = inner["v"][919] = 1e30
+    r = run(stage, inner)
+    assert torch.equal(r["dq"][:919], ref["dq"][:919])
+
+
+def test_graph(stage):  # noqa: F811
+    """Recorded once, replayed on new gradients with eager calls between."""
+    c = make(11, [800], [800], 8, 1, 64)
+    assert parts(c) > 1
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run(stage, c)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out, lse = stage.attention(c["q"], c["k"], c["v"], c["cu_q"], c["cu_k"])
+            got = stage.attention_backward(c["dout"], c["q"], c["k"], c["v"], out, lse, c["cu_q"], c["cu_k"])
+    for i in range(3):
+        c["dout"].copy_(torch.randn(c["dout"].shape, device=DEV))
+        want = run(stage, c)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            graph.replay()
+        torch.cuda.synchronize()
+        for g, n in zip(got, ("dq", "dk", "dv")):
+            assert torch.equal(g, want[n]), (i, n)
