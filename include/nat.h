@@ -431,6 +431,18 @@ nat_status nat_attn_fwd(const nat_attn_params* params, const void* d_q, const vo
                         const int32_t* d_cu_q, const int32_t* d_cu_k, void* d_out, float* d_lse, void* stream);
 
 /*
+ * The same with a workspace, in which several workgroups leave their results for the same rows where there are few rows
+ * and many keys (the keys' order of summation is then another).
+ *   d_ws / ws_bytes: nat_attn_fwd_workspace_bytes of params' counts, causal and head_dim (0: none is wanted, or they are
+ *                out of range), 256-byte aligned; with less the work is shared less, with none as by nat_attn_fwd.
+ * Errors as nat_attn_fwd, and d_ws not aligned -> NAT_INVALID_ARG.
+ */
+size_t nat_attn_fwd_workspace_bytes(const nat_attn_params* params);
+nat_status nat_attn_fwd_split(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v,
+                              const int32_t* d_cu_q, const int32_t* d_cu_k, void* d_out, float* d_lse,
+                              void* d_ws, size_t ws_bytes, void* stream);
+
+/*
  * Its gradients: with P_ij = exp(S_ij - lse_i), dS_ij = P_ij (dout_i . v_j - dout_i . out_i),
  *     dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i,
  * the sums for dk, dv over all query heads that share the key head.

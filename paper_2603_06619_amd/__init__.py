@@ -9,7 +9,7 @@ from .binding import (  # noqa: F401
     load_library, library_path, status_string, mask_words,
     nat_advantage, nat_select, nat_compact, nat_compact_static, nat_loss_fwd_bwd,
     nat_select_schedule, nat_select_poisson, nat_compact_pi, nat_prefix_pack, nat_loss_fwd_bwd_kl, nat_logp_fwd, logp_workspace_bytes, logp_workspace_min_bytes,
-    KV_BF16, KV_FP8, KvCache, nat_attn_fwd, nat_attn_bwd, attn_bwd_workspace_bytes, attn_bwd_workspace_full_bytes, nat_kv_write, nat_kv_read, nat_attn_decode,
+    KV_BF16, KV_FP8, KvCache, nat_attn_fwd, attn_fwd_workspace_bytes, nat_attn_bwd, attn_bwd_workspace_bytes, attn_bwd_workspace_full_bytes, nat_kv_write, nat_kv_read, nat_attn_decode,
     attn_decode_workspace_bytes, nat_sample, sample_workspace_bytes,
     compact_workspace_bytes, loss_workspace_bytes, loss_workspace_min_bytes,
     profile_enable, profile_collect, probe_mfma_scratch_bytes, nat_probe_mfma_bf16, nat_probe_copy,

@@ -1,5 +1,6 @@
 """ctypes binding of include/nat.h.  Argument marshalling only."""
 import ctypes
+import functools
 import os
 
 import torch
@@ -119,10 +120,14 @@ def load_library():
     pa, pc = ctypes.POINTER(_CAttnParams), ctypes.POINTER(_CKvCache)
     lib.nat_attn_fwd.restype = i32
     lib.nat_attn_fwd.argtypes = [pa, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.nat_attn_fwd_workspace_bytes.restype = sz
+    lib.nat_attn_fwd_workspace_bytes.argtypes = [pa]
+    lib.nat_attn_fwd_split.restype = i32
+    lib.nat_attn_fwd_split.argtypes = [pa, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.nat_attn_bwd_workspace_bytes.restype = sz
     lib.nat_attn_bwd_workspace_bytes.argtypes = [i64, i32]
     lib.nat_attn_bwd_workspace_full_bytes.restype = sz
-    lib.nat_attn_bwd_workspace_full_bytes.argtypes = [ctypes.POINTER(_CAttnParams)]
+    lib.nat_attn_bwd_workspace_full_bytes.argtypes = [pa]
     lib.nat_attn_bwd.restype = i32
     lib.nat_attn_bwd.argtypes = [pa, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.nat_kv_write.restype = i32
@@ -370,19 +375,29 @@ def _attn_params(q, k, v, cu_q, cu_k, causal, scale):
     return p
 
 
-def nat_attn_fwd(q, k, v, cu_q, cu_k, causal, scale, out, lse):
+@functools.lru_cache(maxsize=256)
+def attn_fwd_workspace_bytes(n_q, n_k, n_seqs, n_q_heads, n_kv_heads, head_dim, causal):
+    p = _CAttnParams(int(n_seqs), int(n_q_heads), int(n_kv_heads), int(head_dim), DTYPE_BF16, int(causal), 1.0, int(n_q), int(n_k))
+    return int(load_library().nat_attn_fwd_workspace_bytes(ctypes.byref(p)))
+
+
+def nat_attn_fwd(q, k, v, cu_q, cu_k, causal, scale, out, lse, workspace=None):
     """q [n_q, q heads, D], k, v [n_k, kv heads, D] bf16 (any row stride); cu_q, cu_k int32 [n_seqs + 1]; out like q, lse float32
-    [q heads, n_q]."""
+    [q heads, n_q].  With a workspace (attn_fwd_workspace_bytes) this is nat_attn_fwd_split."""
     p = _attn_params(q, k, v, cu_q, cu_k, causal, scale)
     p.out_stride = _rows(out, "out", q.shape)
-    _raise(load_library().nat_attn_fwd(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k), _ptr(out),
-                                       _vector(lse, torch.float32, p.n_q_heads * p.n_q, "lse"), _stream()), "nat_attn_fwd")
+    args = (ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k), _ptr(out), _vector(lse, torch.float32, p.n_q_heads * p.n_q, "lse"))
+    if workspace is None:
+        _raise(load_library().nat_attn_fwd(*args, _stream()), "nat_attn_fwd")
+    else:
+        _raise(load_library().nat_attn_fwd_split(*args, _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()), "nat_attn_fwd_split")
 
 
 def attn_bwd_workspace_bytes(n_q, n_q_heads):
     return int(load_library().nat_attn_bwd_workspace_bytes(int(n_q), int(n_q_heads)))
 
 
+@functools.lru_cache(maxsize=256)
 def attn_bwd_workspace_full_bytes(n_q, n_k, n_seqs, n_q_heads, n_kv_heads, head_dim, causal):
     p = _CAttnParams(int(n_seqs), int(n_q_heads), int(n_kv_heads), int(head_dim), DTYPE_BF16, int(causal), 1.0, int(n_q), int(n_k))
     return int(load_library().nat_attn_bwd_workspace_full_bytes(ctypes.byref(p)))

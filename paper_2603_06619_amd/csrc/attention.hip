@@ -47,7 +47,9 @@ struct AttnArgs {
   int64_t dout_stride, dq_stride, dk_stride, dv_stride;
   int slots;                     // tile slots per key head
   int row_parts;                 // dk, dv: workgroups that share a tile's rows
-  float* parts;                  // their sums [row_parts][n_k][hkv][dk, dv][D], if there are several
+  int key_parts;                 // forward: workgroups that share a tile's keys
+  float* parts;                  // what they leave if there are several: dk, dv [row_parts][n_k][hkv][2][D], or sums [key_parts][n_q][hq][D]
+  float* part_ml;                // and m, sum [key_parts][n_q][hq][2]
   uint32_t group_inverse;        // see small_quotient
 };
 
@@ -262,12 +264,17 @@ __device__ __forceinline__ void store_columns(uint16_t* row, const f32x16 (&acc)
 // 64 rows per wavefront with half the wavefronts 3.1, the next tile's products among this tile's exponentials 2.03, 8 wavefronts per workgroup 2.01 (701 tokens
 // behind 4093 cached ones 177 us instead of 147), copies three tiles ahead 2.07.  Calls of short prompts (48 of up to 193 tokens, 16 us) are a chain of loads: offsets,
 // the sequence's lengths, queries and first tile, then 1 to 4 steps.
-template <int D>
+// kSplit: key_parts workgroups share a tile's keys and leave their sums for attn_fwd_join_kernel (a kernel of its own: both in
+// one take 32 registers more).
+template <int D, bool kSplit>
 __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) char tiles[2][2][kKeyTile * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   int head, slot;
-  head_and_slot(blockIdx.x, a.hkv, a.slots, head, slot);
+  const int parts = kSplit ? a.key_parts : 1;
+  head_and_slot(blockIdx.x, a.hkv, a.slots * parts, head, slot);
+  const int part = slot % parts;
+  slot /= parts;
   if (slot >= a.slots) return;
   slot = a.slots - 1 - slot;                 // causal: the last tiles of a sequence have the most keys, and go first
   int64_t first_slot;
@@ -281,6 +288,12 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   q.load(a.q + (s.q0 + query) * a.q_stride + (head * a.group + of_group) * D, lane);
   const int tile_end = tile_row + kRowTile < n_rows ? tile_row + kRowTile : n_rows;
   const int n_keys = last_key(a, s, (tile_end - 1) / a.group) + 1;      // of the tile
+  int first_key = 0, end_key = n_keys;                                 // of this part
+  if (kSplit) {
+    const int steps = ((n_keys + kKeyTile - 1) / kKeyTile + parts - 1) / parts;
+    first_key = part * steps * kKeyTile;
+    end_key = n_keys - first_key > steps * kKeyTile ? first_key + steps * kKeyTile : n_keys;
+  }
   const int tile_least = last_key(a, s, tile_row / a.group);           // seen by all rows of the tile
   const int last = last_key(a, s, query);                              // of this lane's row
   const int wave_row = tile_row + wave * 32 < n_rows ? tile_row + wave * 32 : n_rows - 1, wave_end = wave_row + 32 < n_rows ? wave_row + 32 : n_rows;
@@ -359,16 +372,16 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
     sum = 0.f;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db) acc[db] = f32x16{};
-    next_k = k;
-    next_v = v;
-    fetch(0, tiles[0]);
+    next_k = k + (int64_t)first_key * k_bytes;
+    next_v = v + (int64_t)first_key * v_bytes;
+    fetch(first_key, tiles[0]);
     end_of_step();
-    for (int key0 = 0; key0 < n_keys; key0 += 2 * kKeyTile) {
-      if (key0 + kKeyTile < n_keys) fetch(key0 + kKeyTile, tiles[1]);
+    for (int key0 = first_key; key0 < end_key; key0 += 2 * kKeyTile) {
+      if (key0 + kKeyTile < end_key) fetch(key0 + kKeyTile, tiles[1]);
       step(key0, tiles[0][0], tiles[0][1], careful);
       end_of_step();
-      if (key0 + kKeyTile >= n_keys) break;
-      if (key0 + 2 * kKeyTile < n_keys) fetch(key0 + 2 * kKeyTile, tiles[0]);
+      if (key0 + kKeyTile >= end_key) break;
+      if (key0 + 2 * kKeyTile < end_key) fetch(key0 + 2 * kKeyTile, tiles[0]);
       step(key0 + kKeyTile, tiles[1][0], tiles[1][1], careful);
       end_of_step();
     }
@@ -379,8 +392,60 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   if (row >= n_rows) return;
   const int64_t at = s.q0 + query;
   const int qh = head * a.group + of_group;
+  if (kSplit) {
+    const int64_t of_part = (part * a.n_q + at) * a.hq + qh;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(a.parts + of_part * D + 32 * db + 8 * i + 4 * half) = f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]};
+    if (half == 0) *(f32x2*)(a.part_ml + of_part * 2) = f32x2{m, sum};
+    return;
+  }
   store_columns<D>(a.out + at * a.out_stride + qh * D, acc, sum == 0.f ? 0.f : 1.f / sum, lane);
   if (half == 0) a.lse[qh * a.n_q + at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, __logf(sum));
+}
+
+// Results of a tile's rows from those of its key_parts workgroups, scaled to their common maximum; two rows per wavefront, all loads of a row under way at once
+constexpr int kMaxKeyParts = 16, kJoinRows = 8;
+template <int D>
+__global__ void __launch_bounds__(256) attn_fwd_join_kernel(AttnArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int head, slot;
+  head_and_slot(blockIdx.x, a.hkv, a.slots, head, slot);
+  if (slot >= a.slots) return;
+  int64_t first_slot;
+  const Sequence s = sequence(a, sequence_of_slot(a.cu_q, a.n_seqs, a.n_q, a.group, kRowTile, slot, &first_slot));
+  const int n_rows = s.n_q * a.group, tile_row = (int)(slot - first_slot) * kRowTile;
+  if (slot < first_slot) return;
+  const float to_log2 = a.scale * kLog2E;
+  for (int row = tile_row + blockIdx.y * kJoinRows + wave; row < tile_row + (blockIdx.y + 1) * kJoinRows && row < n_rows; row += 4) {
+    const int query = row / a.group, qh = head * a.group + row - query * a.group;
+    const int64_t at = s.q0 + query, of = at * a.hq + qh, part_stride = a.n_q * a.hq;
+    f32x2 ml[kMaxKeyParts], y[kMaxKeyParts];
+#pragma unroll
+    for (int p = 0; p < kMaxKeyParts; ++p) {
+      ml[p] = f32x2{-INFINITY, 0.f};
+      y[p] = f32x2{};
+      if (p < a.key_parts) {
+        ml[p] = *(const f32x2*)(a.part_ml + (of + p * part_stride) * 2);
+        if (2 * lane < D) y[p] = *(const f32x2*)(a.parts + (of + p * part_stride) * D + 2 * lane);
+      }
+    }
+    float m = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int p = 0; p < kMaxKeyParts; ++p) m = fmaxf(m, ml[p][0]);
+    const float shift = m == -INFINITY ? 0.f : m;
+    f32x2 x = {};
+#pragma unroll
+    for (int p = 0; p < kMaxKeyParts; ++p) {
+      const float f = exp2_fast((ml[p][0] - shift) * to_log2);
+      sum = fmaf(ml[p][1], f, sum);
+      x += y[p] * f;
+    }
+    if (2 * lane < D) *(bf16x2*)(a.out + at * a.out_stride + qh * D + 2 * lane) = __builtin_convertvector(x * (sum == 0.f ? 0.f : 1.f / sum), bf16x2);
+    if (lane == 0) a.lse[qh * a.n_q + at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, __logf(sum));
+  }
 }
 
 enum class Pass { kDelta, kPlain, kCareful };
@@ -809,6 +874,24 @@ int row_parts_of(int64_t n_q, int64_t n_k, int64_t n_seqs, int64_t hkv, int64_t 
   if (p > steps / 4) p = steps / 4;
   return (int)(p < 1 ? 1 : p > kMaxRowParts ? kMaxRowParts : p);
 }
+// Workgroups per tile of rows: where the tiles do not fill the chip, or, of unequal length (as many queries as keys, causal), fill it less than twice; 256 keys each at
+// least, and more where there are many rows whose sums are written and read once more.  In us, D = 128, one workgroup per tile and so many: 16 rows behind 8000 (32 heads on 8) 147, 25 (15 parts); 8 x 5 behind 4000 77, 33; 256 behind 8000 152, 57; 8192 of 4 on 1
+// 149, 102 (3 parts).  Twice as many for 6 x 350 behind 2000 (28 on 4): 121 instead of 84; two of 256 keys on
+// average for 1024 (32 on 8): 43 instead of 29.
+int key_parts_of(int64_t n_q, int64_t n_k, int64_t n_seqs, int64_t hkv, int64_t group, int head_dim, bool causal) {
+  if (n_seqs <= 0 || n_q <= 0 || n_k <= 0) return 1;
+  const int64_t part_keys = 256 + n_q * hkv * group / 64;
+  const int64_t blocks = (n_q * group / kRowTile + n_seqs) * hkv, keys = (causal ? n_k - n_q / 2 : n_k) / n_seqs;
+  int64_t p = (head_dim == 128 ? 512 : 768) * (causal && 2 * n_q > n_k ? 2 : 1) / blocks;
+  if (p > keys / part_keys) p = keys / part_keys;
+  return (int)(p < 1 ? 1 : p > kMaxKeyParts ? kMaxKeyParts : p);
+}
+size_t key_part_bytes(int64_t n_q, int64_t hq, int64_t head_dim) { return (size_t)n_q * hq * (head_dim + 2) * 4; }
+// what the sizes of workspaces are computed from
+bool counts_ok(const nat_attn_params* p) {
+  return p && p->n_kv_heads > 0 && p->n_q_heads > 0 && p->n_q_heads <= 4096 && p->n_q_heads % p->n_kv_heads == 0 && p->n_q >= 0 && p->n_k >= 0 &&
+         p->n_q <= INT32_MAX && p->n_k <= INT32_MAX && (p->head_dim == 64 || p->head_dim == 128);
+}
 size_t row_part_bytes(int64_t n_k, int64_t hkv, int64_t head_dim) { return (size_t)n_k * hkv * head_dim * 8; }
 
 }  // namespace
@@ -816,22 +899,48 @@ size_t row_part_bytes(int64_t n_k, int64_t hkv, int64_t head_dim) { return (size
 
 using namespace nat;
 
-extern "C" nat_status nat_attn_fwd(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v, const int32_t* d_cu_q,
-                                   const int32_t* d_cu_k, void* d_out, float* d_lse, void* stream) {
+extern "C" size_t nat_attn_fwd_workspace_bytes(const nat_attn_params* p) {
+  if (!counts_ok(p)) return 0;
+  const int parts = key_parts_of(p->n_q, p->n_k, p->n_seqs, p->n_kv_heads, p->n_q_heads / p->n_kv_heads, p->head_dim, p->causal != 0);
+  return parts > 1 ? (parts * key_part_bytes(p->n_q, p->n_q_heads, p->head_dim) + 255) / 256 * 256 : 0;
+}
+
+extern "C" nat_status nat_attn_fwd_split(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v, const int32_t* d_cu_q,
+                                         const int32_t* d_cu_k, void* d_out, float* d_lse, void* d_ws, size_t ws_bytes, void* stream) {
   AttnArgs a;
   const nat_status st = attn_args(params, d_q, d_k, d_v, d_cu_q, d_cu_k, &a);
   if (st != NAT_OK || a.n_seqs == 0 || a.n_q == 0) return st;
-  if (!d_out || !d_lse || misaligned(d_out)) return NAT_INVALID_ARG;
+  if (!d_out || !d_lse || misaligned(d_out) || ((uintptr_t)d_ws & 255)) return NAT_INVALID_ARG;
   a.out = (uint16_t*)d_out;
   a.lse = d_lse;
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_ATTN_FWD, s);
   a.slots = (int)(a.n_q * a.group / kRowTile + a.n_seqs);
-  const unsigned blocks = grid_of(a.hkv, a.slots);
-  if (params->head_dim == 128) attn_fwd_kernel<128><<<blocks, 256, 0, s>>>(a);
-  else attn_fwd_kernel<64><<<blocks, 256, 0, s>>>(a);
-  NAT_LAUNCH_CHECK();
+  a.key_parts = key_parts_of(a.n_q, a.n_k, a.n_seqs, a.hkv, a.group, params->head_dim, a.causal != 0);
+  const size_t part_bytes = key_part_bytes(a.n_q, a.hq, params->head_dim);
+  while (a.key_parts > 1 && (!d_ws || ws_bytes < a.key_parts * part_bytes)) --a.key_parts;
+  a.parts = (float*)d_ws;
+  a.part_ml = a.parts + (size_t)a.key_parts * a.n_q * a.hq * params->head_dim;
+  const unsigned blocks = grid_of(a.hkv, (int64_t)a.slots * a.key_parts);
+  if (a.key_parts == 1) {
+    if (params->head_dim == 128) attn_fwd_kernel<128, false><<<blocks, 256, 0, s>>>(a);
+    else attn_fwd_kernel<64, false><<<blocks, 256, 0, s>>>(a);
+    NAT_LAUNCH_CHECK();
+  } else {
+    if (params->head_dim == 128) attn_fwd_kernel<128, true><<<blocks, 256, 0, s>>>(a);
+    else attn_fwd_kernel<64, true><<<blocks, 256, 0, s>>>(a);
+    NAT_LAUNCH_CHECK();
+    const dim3 joins(grid_of(a.hkv, a.slots), kRowTile / kJoinRows);
+    if (params->head_dim == 128) attn_fwd_join_kernel<128><<<joins, 256, 0, s>>>(a);
+    else attn_fwd_join_kernel<64><<<joins, 256, 0, s>>>(a);
+    NAT_LAUNCH_CHECK();
+  }
   return NAT_OK;
+}
+
+extern "C" nat_status nat_attn_fwd(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v, const int32_t* d_cu_q,
+                                   const int32_t* d_cu_k, void* d_out, float* d_lse, void* stream) {
+  return nat_attn_fwd_split(params, d_q, d_k, d_v, d_cu_q, d_cu_k, d_out, d_lse, nullptr, 0, stream);
 }
 
 extern "C" size_t nat_attn_bwd_workspace_bytes(int64_t n_q, int32_t n_q_heads) {
@@ -840,9 +949,7 @@ extern "C" size_t nat_attn_bwd_workspace_bytes(int64_t n_q, int32_t n_q_heads) {
 }
 
 extern "C" size_t nat_attn_bwd_workspace_full_bytes(const nat_attn_params* p) {
-  if (!p || p->n_kv_heads <= 0 || p->n_q_heads <= 0 || p->n_q_heads % p->n_kv_heads != 0 || p->n_q > INT32_MAX || p->n_k > INT32_MAX ||
-      (p->head_dim != 64 && p->head_dim != 128))
-    return 0;
+  if (!counts_ok(p)) return 0;
   const size_t least = nat_attn_bwd_workspace_bytes(p->n_q, p->n_q_heads);
   const int parts = row_parts_of(p->n_q, p->n_k, p->n_seqs, p->n_kv_heads, p->n_q_heads / p->n_kv_heads, p->head_dim, p->causal != 0);
   return parts > 1 ? least + parts * row_part_bytes(p->n_k, p->n_kv_heads, p->head_dim) : least;

@@ -44,7 +44,8 @@ class RolloutStage:
         Returns (out like q, log-sum-exp [q heads, n_q])."""
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-        nb.nat_attn_fwd(q, k, v, cu_q, cu_q if cu_k is None else cu_k, causal, self._scale(scale, q.shape[2]), out, lse)
+        ws = self._buf("attn_fwd", nb.attn_fwd_workspace_bytes(q.shape[0], k.shape[0], cu_q.numel() - 1, q.shape[1], k.shape[1], q.shape[2], causal))
+        nb.nat_attn_fwd(q, k, v, cu_q, cu_q if cu_k is None else cu_k, causal, self._scale(scale, q.shape[2]), out, lse, ws)
         return out, lse
 
     def attention_backward(self, dout, q, k, v, out, lse, cu_q, cu_k=None, causal=True, scale=None):

@@ -103,3 +103,54 @@ def test_graph(stage):  # noqa: F811
         torch.cuda.synchronize()
         for g, n in zip(got, ("dq", "dk", "dv")):
             assert torch.equal(g, want[n]), (i, n)
+
+
+def key_parts(c, causal=True):
+    import paper_2603_06619_amd as nat
+    (n_q, hq, D), (n_k, hkv, _) = c["q"].shape, c["k"].shape
+    return nat.attn_fwd_workspace_bytes(n_q, n_k, c["cu_q"].numel() - 1, hq, hkv, D, causal) // (n_q * hq * (D + 2) * 4)
+
+
+@pytest.mark.parametrize("lens_q,lens_k,hq,hkv,D,causal", [
+    ([1], [3001], 4, 4, 64, True), ([16], [8016], 8, 2, 128, True), ([70, 0, 3], [3000, 900, 1700], 7, 1, 128, True), ([5, 200], [4000, 1], 4, 2, 64, True),
+    ([700], [2100], 2, 1, 64, True), ([2100], [2100], 2, 1, 64, True), ([2100], [2100], 2, 1, 128, True), ([33], [1100], 60, 1, 64, False), ([65, 64], [4000, 20], 14, 2, 128, False),
+])
+def test_shared_keys(stage, lens_q, lens_k, hq, hkv, D, causal):  # noqa: F811
+    """The forward pass: rows whose keys lie in some parts only, sequences with few keys or none, rows that see nothing."""
+    c = make(len(lens_q), lens_q, lens_k, hq, hkv, D)
+    assert key_parts(c, causal) > 1
+    check(c, run(stage, c, causal=causal, backward=False), causal=causal, names=("out", "lse"))
+
+
+def test_every_forward_workspace(stage):  # noqa: F811
+    import paper_2603_06619_amd as nat
+    c = make(3, [40, 9], [4000, 2500], 8, 2, 64)
+    c["cu_q"] = torch.tensor([2, 40, 47], dtype=torch.int32, device=DEV)           # rows of no sequence on both sides
+    full, part = nat.attn_fwd_workspace_bytes(49, 6500, 2, 8, 2, 64, True), 49 * 8 * 66 * 4
+    assert full // part >= 4
+    want = None
+    for size in (0, part, 2 * part, full, full + 256):
+        ws = torch.full((size + 4096,), 0xaa, dtype=torch.uint8, device=DEV)
+        out, lse = torch.full_like(c["q"], 9.0), torch.full((8, 49), 9.0, device=DEV)
+        nat.nat_attn_fwd(c["q"], c["k"], c["v"], c["cu_q"], c["cu_k"], True, 0.125, out, lse, ws[:size])
+        torch.cuda.synchronize()
+        assert bool((ws[max(size, full):] == 0xaa).all())
+        assert bool((out[:2] == 9.0).all()) and bool((out[47:] == 9.0).all()) and bool((lse[:, :2] == 9.0).all()) and bool((lse[:, 47:] == 9.0).all())
+        inner = dict(q=c["q"][2:47], k=c["k"], v=c["v"], dout=c["dout"][2:47], cu_q=c["cu_q"] - 2, cu_k=c["cu_k"])
+        check(inner, dict(out=out[2:47], lse=lse[:, 2:47]), names=("out", "lse"))
+        if size >= full:
+            assert want is None or torch.equal(out, want)
+            want = out
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf"), 3e38])
+def test_what_shared_keys_hold_in_masked_places(stage, D, value):  # noqa: F811
+    """Keys and values behind a row's last one, in the same part and in later ones, whatever they hold."""
+    c = make(12, [20], [3000], 4, 2, D)
+    assert key_parts(c) > 1
+    ref = run(stage, c, backward=False)
+    c["k"][2990:] = value
+    c["v"][2990:] = value
+    r = run(stage, c, backward=False)
+    assert torch.equal(r["out"][:10], ref["out"][:10]) and torch.equal(r["lse"][:, :10], ref["lse"][:, :10])

@@ -21,3 +21,27 @@ def test_counts_out_of_range(kw):
     a.update(kw)
     size = nat.attn_bwd_workspace_full_bytes(a["n_q"], a["n_k"], a["n_seqs"], a["hq"], a["hkv"], a["D"], True)
     assert size in (0, nat.attn_bwd_workspace_bytes(1000, 8))
+
+
+def test_forward_workspace():
+    size = nat.attn_fwd_workspace_bytes
+    for n_q, n_k, hq, hkv, D in ((16, 8016, 32, 8, 128), (2048, 2048, 2, 1, 128), (1, 5000, 4, 4, 64)):
+        part = n_q * hq * (D + 2) * 4
+        assert any(size(n_q, n_k, 1, hq, hkv, D, True) == (p * part + 255) // 256 * 256 for p in range(2, 17))
+    assert size(32768, 32768, 8, 32, 8, 128, True) == 0                             # rows enough
+    assert size(16, 400, 1, 8, 8, 64, True) == 0                                    # too few keys to share
+    for a in ((16, 8016, 1, 3, 2, 64), (16, 8016, 1, 8, 0, 64), (16, 8016, 1, 8, 8, 96), (-1, 8016, 1, 8, 8, 64), (16, 1 << 40, 1, 8, 8, 64), (16, 8016, 0, 8, 8, 64)):
+        assert size(*a, True) == 0
+
+
+def test_forward_refusals():
+    import ctypes
+    from paper_2603_06619_amd import binding
+    lib, fake = nat.load_library(), 1 << 20
+    p = binding._CAttnParams(1, 8, 8, 64, nat.DTYPE_BF16, 1, 0.1, 16, 8016)
+    call = lambda **kw: lib.nat_attn_fwd_split(ctypes.byref(p), *(kw.get(n, fake) for n in ("q", "k", "v", "cu_q", "cu_k", "out", "lse", "ws")), 1 << 30, None)
+    invalid = lib.nat_attn_fwd(None, fake, fake, fake, fake, fake, fake, fake, None)
+    assert invalid != 0
+    for n in ("q", "k", "v", "cu_q", "cu_k", "out", "lse"):
+        assert call(**{n: None}) == invalid, n
+    assert call(ws=fake + 16) == invalid and call(out=fake + 8) == invalid
