@@ -419,18 +419,21 @@ class KvCache:
     k_exp, v_exp [n_pages, kv heads, page_size] uint8 (see nat_kv_cache in nat.h)."""
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
-        fp8 = k.dtype == torch.float8_e4m3fn
-        if k.dim() != 4 or not (fp8 or k.dtype == torch.bfloat16):
+        shape, dtype = k.shape, k.dtype
+        fp8 = dtype == torch.float8_e4m3fn
+        if len(shape) != 4 or not (fp8 or dtype == torch.bfloat16):
             raise TypeError("k: expected a bfloat16 or float8_e4m3fn tensor [n_pages, heads, page_size, head_dim]")
-        for name, t in (("k", k), ("v", v)):
-            if t.shape != k.shape or t.dtype != k.dtype or not t.is_contiguous() or not t.is_cuda:
-                raise TypeError(f"{name}: expected a contiguous {k.dtype} device tensor {tuple(k.shape)}")
+        if not (k.is_contiguous() and k.is_cuda):
+            raise TypeError(f"k: expected a contiguous {dtype} device tensor {tuple(shape)}")
+        if v.shape != shape or v.dtype != dtype or not v.is_contiguous() or not v.is_cuda:
+            raise TypeError(f"v: expected a contiguous {dtype} device tensor {tuple(shape)}")
         if fp8:
-            for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
-                if t is None or t.shape != k.shape[:3] or t.dtype != torch.uint8 or not t.is_contiguous() or not t.is_cuda:
-                    raise TypeError(f"{name}: expected a contiguous uint8 device tensor {tuple(k.shape[:3])}")
+            rows = shape[:3]
+            for t in (k_exp, v_exp):
+                if t is None or t.shape != rows or t.dtype != torch.uint8 or not t.is_contiguous() or not t.is_cuda:
+                    raise TypeError(f"{'k_exp' if t is k_exp else 'v_exp'}: expected a contiguous uint8 device tensor {tuple(rows)}")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
-        n_pages, heads, page_size, dim = k.shape
+        n_pages, heads, page_size, dim = shape
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = n_pages, heads, page_size, dim
         self._c = _CKvCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if fp8 else None, v_exp.data_ptr() if fp8 else None,
                             n_pages, heads, page_size, dim, KV_FP8 if fp8 else KV_BF16)
