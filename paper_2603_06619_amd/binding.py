@@ -347,6 +347,8 @@ def _rows(t, name, shape=None, dtype=torch.bfloat16):
         raise TypeError(f"{name}: expected a {dtype} device tensor [rows, heads, head_dim]")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return 0
     row, head, one = t.stride()
     n, heads, dim = t.shape
     if n == 0 or heads == 0 or dim == 0:
@@ -463,6 +465,7 @@ def nat_kv_read(cache, block_table, cu_k, k, v):
                                       k.shape[0], _ptr(k), _rows(k, "k", shape), _ptr(v), _rows(v, "v", shape), _stream()), "nat_kv_read")
 
 
+@functools.lru_cache(maxsize=256)
 def attn_decode_workspace_bytes(n_seqs, n_q_heads, n_kv_heads, head_dim, max_tokens):
     return int(load_library().nat_attn_decode_workspace_bytes(int(n_seqs), int(n_q_heads), int(n_kv_heads), int(head_dim), int(max_tokens)))
 
@@ -479,6 +482,7 @@ def nat_attn_decode(cache, q, block_table, seq_lens, scale, out, lse, workspace)
         workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_attn_decode")
 
 
+@functools.lru_cache(maxsize=256)
 def sample_workspace_bytes(n_rows, V, dtype):
     return int(load_library().nat_sample_workspace_bytes(int(n_rows), int(V), int(dtype)))
 

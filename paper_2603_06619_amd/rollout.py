@@ -42,15 +42,15 @@ class RolloutStage:
     def attention(self, q, k, v, cu_q, cu_k=None, causal=True, scale=None):
         """q [n_q, q heads, D], k, v [n_k, kv heads, D] bf16, packed by the int32 offsets cu_q, cu_k (None: the same).
         Returns (out like q, log-sum-exp [q heads, n_q])."""
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+        out = torch.empty_like(q)                    # (half the host time of torch.empty; rows back to back whatever those of q)
+        lse = q.new_empty((q.shape[1], q.shape[0]), dtype=torch.float32)
         ws = self._buf("attn_fwd", nb.attn_fwd_workspace_bytes(q.shape[0], k.shape[0], cu_q.numel() - 1, q.shape[1], k.shape[1], q.shape[2], causal))
         nb.nat_attn_fwd(q, k, v, cu_q, cu_q if cu_k is None else cu_k, causal, self._scale(scale, q.shape[2]), out, lse, ws)
         return out, lse
 
     def attention_backward(self, dout, q, k, v, out, lse, cu_q, cu_k=None, causal=True, scale=None):
         """(dq, dk, dv) of attention(), with its results."""
-        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
         ws = self._buf("attn_bwd", nb.attn_bwd_workspace_full_bytes(q.shape[0], k.shape[0], cu_q.numel() - 1, q.shape[1], k.shape[1], q.shape[2], causal))
         nb.nat_attn_bwd(q, k, v, out, lse, dout, cu_q, cu_q if cu_k is None else cu_k, causal, self._scale(scale, q.shape[2]),
                         dq, dk, dv, ws)
@@ -62,15 +62,15 @@ class RolloutStage:
     def read_cache(self, cache, block_table, cu_k, n_rows):
         """The first cu_k[b + 1] - cu_k[b] tokens of every sequence as packed bf16 rows: (k, v)."""
         shape = (n_rows, cache.n_kv_heads, cache.head_dim)
-        k, v = (torch.empty(shape, dtype=torch.bfloat16, device=cache.k.device) for _ in range(2))
+        k, v = cache.k.new_empty(shape, dtype=torch.bfloat16), cache.k.new_empty(shape, dtype=torch.bfloat16)
         nb.nat_kv_read(cache, block_table, cu_k, k, v)
         return k, v
 
     def decode(self, q, cache, block_table, seq_lens, scale=None):
         """Attention of one token per sequence, q [n_seqs, q heads, D], over its cached tokens: (out like q, log-sum-exp [n_seqs, q heads])."""
         n, hq, dim = q.shape
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((n, hq), dtype=torch.float32, device=q.device)
+        out = torch.empty_like(q)
+        lse = q.new_empty((n, hq), dtype=torch.float32)
         ws = self._buf("decode", nb.attn_decode_workspace_bytes(n, hq, cache.n_kv_heads, cache.head_dim,
                                                                block_table.shape[1] * cache.page_size))
         nb.nat_attn_decode(cache, q, block_table, seq_lens, self._scale(scale, dim), out, lse, ws)
@@ -80,7 +80,7 @@ class RolloutStage:
         """The next token of every row, its log-probability under the soft-max of the logits (the behaviour log-prob), and under
         the filtered distribution that it was drawn from: dict with ids, logp, logq."""
         n = logits.shape[0]
-        new = lambda dt: torch.empty(n, dtype=dt, device=logits.device)
+        new = lambda dt: logits.new_empty(n, dtype=dt)
         out = dict(ids=new(torch.int32), logp=new(torch.float32), logq=new(torch.float32))
         ws = self._buf("sample", nb.sample_workspace_bytes(n, logits.shape[1], nb._dtype_code(logits)))
         nb.nat_sample(logits, random, temperature, top_k, top_p, min_p, out["ids"], out["logp"], out["logq"], ws)
