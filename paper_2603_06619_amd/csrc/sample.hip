@@ -8,7 +8,7 @@
 //   top      the largest logit;
 //   bins     (rows with a top-k or top-p) a histogram of the exponents y, 1/16 apart: of tokens if the row has a top-k, else of their weight.  The bin in which
 //            the top-k ends, or the weight that the top-p asks for;
-//   list     the tokens of that bin (with a top-k: of all bins down to it).  Among them the least logit that stays, and the last index that does of those
+//   list     the tokens of that bin (with a top-k and a top-p: of all bins down to it).  Among them the least logit that stays, and the last index that does of those
 //            equal to it;
 //   sums     weights of what stays, summed part by part;
 //   draw     in order of index: by the sums of the parts, then by steps, lanes and elements.
@@ -207,7 +207,7 @@ struct Stay {
   int equal_end;
   __device__ __forceinline__ bool has(uint32_t key, int index) const { return key > least || (key == least && index <= equal_end); }
 };
-// What is listed: exponents' bins first .. last; the weight above them and that of the row (rows without a top-k)
+// What is listed: exponents' bins first .. last; what lies above them, tokens if the row has a top-k, else weight; the weight of the row (rows without a top-k)
 struct Gather { int first, last; uint64_t above, all; };
 
 constexpr int kMaxParts = kMaxVocab / 4 / (64 * kUnroll) + kMaxSplits * kWaves + 2;
@@ -360,7 +360,7 @@ __device__ __forceinline__ uint64_t reach_of(float top_p, uint64_t total) {
 }
 
 // Keys above `least` and the first n_least of those equal to it stay by rank, of elements that each(f) calls f(key) for.  over_top: the weight above all of
-// them, over(least): of them above a key; by_count: they begin with the row's largest and hold the whole top-k.
+// them, over(least): of them above a key; by_count: they hold the end of the top-k, over_top is the number of tokens above them, 0 if there is a top-p too.
 struct Ranked { uint32_t least; uint64_t n_least; };
 template <class Each, class Over>
 __device__ __forceinline__ Ranked rank_tokens(const Settings& set, const Weigher& weigh, bool by_count, uint32_t lo, uint32_t hi, uint64_t total, uint64_t over_top,
@@ -369,10 +369,10 @@ __device__ __forceinline__ Ranked rank_tokens(const Settings& set, const Weigher
   Ranked r{lo - 1, 0};
   uint64_t above, at_least = 0;
   if (by_count) {
-    if (select_key(each, lo, hi, (uint64_t)set.top_k - 1, [](uint32_t) -> uint64_t { return 1; }, &r.least, &above, sm)) r.n_least = set.top_k - above;
+    if (select_key(each, lo, hi, (uint64_t)set.top_k - over_top - 1, [](uint32_t) -> uint64_t { return 1; }, &r.least, &above, sm))
+      r.n_least = set.top_k - over_top - above;
     if (!(set.top_p < 1.f)) return r;
     at_least = weigh.of_key(r.least);
-    over_top = 0;
     total = over(r.least) + r.n_least * at_least;
   }
   const uint64_t reach = reach_of(set.top_p, total);
@@ -476,7 +476,7 @@ __device__ __forceinline__ Gather choose_bins(const Settings& set, const uint64_
   const int bin = block_find([&](int i) { return hist[i]; }, kBins,
                              [&](uint64_t total) { return (set.top_k > 0 ? (uint64_t)set.top_k : reach_of(set.top_p, total)) - 1; }, &above, &all, sm);
   if (bin == kBins) return Gather{0, kBins - 1, 0, all};       // fewer tokens than the top-k: all of them
-  return set.top_k > 0 ? Gather{0, bin, 0, all} : Gather{bin, bin, above, all};
+  return set.top_k > 0 && set.top_p < 1.f ? Gather{0, bin, 0, all} : Gather{bin, bin, above, all};
 }
 
 // list: the tokens in those bins, of the wavefront's parts; *n counts on past the room
@@ -530,11 +530,12 @@ __device__ __forceinline__ Stay threshold_of_short_list(const Settings& set, con
     sm.list[rank] = mine;
   }
   __syncthreads();
-  int end = set.top_k > 0 && set.top_k < n ? set.top_k : n;    // tokens that stay
+  int end = n;                                 // tokens that stay
+  if (set.top_k > 0 && set.top_k - (int)g.above < n) end = set.top_k - (int)g.above;
   if (set.top_k <= 0 || set.top_p < 1.f) {
     uint64_t before, total;
     const int last = block_find([&](int i) { return order[i]; }, end,
-                                [&](uint64_t of_top_k) { return reach_of(set.top_p, set.top_k > 0 ? of_top_k : g.all) - 1 - g.above; }, &before, &total, sm);
+                                [&](uint64_t of_top_k) { return set.top_k > 0 ? reach_of(set.top_p, of_top_k) - 1 : reach_of(set.top_p, g.all) - 1 - g.above; }, &before, &total, sm);
     end = last < end ? last + 1 : end;
   }
   return Stay{sm.list[end - 1].key, (int)sm.list[end - 1].index};
