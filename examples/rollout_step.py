@@ -130,8 +130,8 @@ def main(argv=None):
     ap.add_argument("--q-heads", type=int, default=16)
     ap.add_argument("--kv-heads", type=int, default=4)
     ap.add_argument("--head-dim", type=int, default=64)
-    ap.add_argument("--steps", type=int, default=3)
-    ap.add_argument("--lr", type=float, default=1.0)
+    ap.add_argument("--steps", type=int, default=12)
+    ap.add_argument("--lr", type=float, default=10.0)
     ap.add_argument("--fp8", action="store_true", help="the cache in 8 bits")
     a = ap.parse_args(argv)
     policy = Policy(a.vocab, a.hidden, a.q_heads, a.kv_heads, a.head_dim)

@@ -17,7 +17,7 @@
 // is gone over once more by one workgroup (threshold_slowly).
 //
 // 512 rows of 152064 fp32 logits, no filter: 109 us for 311 MB, read twice (5.7 TB/s; weights alone are 60 us of vector instructions).  Four rows of 151936 bf16 logits
-// with every filter: 36 to 41 us, all of it latency (top 3.3, bins 7.8, list 8.4, sums 11.5, and three gaps between launches of 2): each phase reads a megabyte in 2 to 3 us, and
+// with every filter: 33 us, all of it latency (top 3.3, bins 7.8, list 8.4, sums 11.5, and three gaps between launches of 2): each phase reads a megabyte in 2 to 3 us, and
 // its last workgroup then takes 3 to 5 for fences, loads of what the others wrote, and a search.
 #include "nat_internal.h"
 
