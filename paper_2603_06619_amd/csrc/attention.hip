@@ -259,8 +259,9 @@ __device__ __forceinline__ void store_columns(uint16_t* row, const f32x16 (&acc)
 }
 
 // out and lse.  A step takes 64 keys: with their values twice in LDS (64 KB at D = 128) two workgroups share a compute unit, and one's exponentials run beside
-// the other's products.  At D = 128 a step is 32 products (1024 cycles) and 32 exponentials with some 190 other vector instructions (about 1270 cycles) per
-// wavefront: both pipes would be full at twice the speed, the power limit comes first (matrix pipes 58 % busy).  For the prompt of 16384 tokens, this 2.0 ms:
+// the other's products.  At D = 128 a step is 32 products (1024 cycles) and 32 exponentials with some 120 other vector instructions (about 980 cycles) per
+// wavefront: either pipe would be full at 1.7 times the speed, the power limit comes first (matrix pipes 58 % busy).  At D = 64 the vector instructions are twice the
+// products: 4 x 4096 tokens of 16 heads 186 us, 740 TFLOP/s.  For the prompt of 16384 tokens, this 2.0 ms:
 // 64 rows per wavefront with half the wavefronts 3.1, the next tile's products among this tile's exponentials 2.03, 8 wavefronts per workgroup 2.01 (701 tokens
 // behind 4093 cached ones 177 us instead of 147), copies three tiles ahead 2.07.  Calls of short prompts (48 of up to 193 tokens, 16 us) are a chain of loads: offsets,
 // the sequence's lengths, queries and first tile, then 1 to 4 steps.

@@ -154,3 +154,28 @@ def test_what_shared_keys_hold_in_masked_places(stage, D, value):  # noqa: F811
     c["v"][2990:] = value
     r = run(stage, c, backward=False)
     assert torch.equal(r["out"][:10], ref["out"][:10]) and torch.equal(r["lse"][:, :10], ref["lse"][:, :10])
+
+
+def test_forward_graph_and_streams(stage):  # noqa: F811
+    """Recorded once and replayed on new queries while the same call runs eagerly on another stream, whose workspace is its own."""
+    c = make(13, [24, 7], [5000, 3000], 8, 2, 128)
+    assert key_parts(c) > 1
+    other = make(14, [24, 7], [5000, 3000], 8, 2, 128)
+    want_other = run(stage, other, backward=False)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run(stage, c, backward=False)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out, lse = stage.attention(c["q"], c["k"], c["v"], c["cu_q"], c["cu_k"])
+    for _ in range(4):
+        c["q"].copy_(torch.randn(c["q"].shape, device=DEV))
+        want = run(stage, c, backward=False)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            graph.replay()
+        beside = stage.attention(other["q"], other["k"], other["v"], other["cu_q"], other["cu_k"])
+        torch.cuda.synchronize()
+        assert torch.equal(out, want["out"]) and torch.equal(lse, want["lse"])
+        assert torch.equal(beside[0], want_other["out"]) and torch.equal(beside[1], want_other["lse"])
