@@ -206,6 +206,9 @@ struct RowFragments {            // 32 rows as an operand, one row per lane, in 
   }
 };
 
+// the same for all lanes: kept in a scalar register
+__device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
+
 template <int D>
 __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[D / 32]) {
   float x = 0.f;
@@ -263,12 +266,13 @@ __device__ __forceinline__ void store_columns(uint16_t* row, const f32x16 (&acc)
 // wavefront: either pipe would be full at 1.7 times the speed, the power limit comes first (matrix pipes 58 % busy).  At D = 64 the vector instructions are twice the
 // products: 4 x 4096 tokens of 16 heads 186 us, 740 TFLOP/s.  For the prompt of 16384 tokens, this 2.0 ms:
 // 64 rows per wavefront with half the wavefronts 3.1, the next tile's products among this tile's exponentials 2.03, 8 wavefronts per workgroup 2.01 (701 tokens
-// behind 4093 cached ones 177 us instead of 147), copies three tiles ahead 2.07.  Calls of short prompts (48 of up to 193 tokens, 16 us) are a chain of loads: offsets,
-// the sequence's lengths, queries and first tile, then 1 to 4 steps.
+// behind 4093 cached ones 177 us instead of 147), copies three tiles ahead 2.07.  Calls of short prompts (48 of up to 193 tokens, 16 heads on 8 of 64) are a chain of
+// loads, which four workgroups per compute unit share better than three: 14.4 us, 15.7 (and 128 registers suffice).  Of a
+// workgroup's 7 us 1.8 are offsets and lengths, 1.1 queries and first tile, 2.9 its 1 to 4 steps, 1.1 the stores.
 // kSplit: key_parts workgroups share a tile's keys and leave their sums for attn_fwd_join_kernel (a kernel of its own: both in
 // one take 32 registers more).
 template <int D, bool kSplit>
-__global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(256, D == 64 ? 4 : 2) attn_fwd_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) char tiles[2][2][kKeyTile * D * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   int head, slot;
@@ -303,11 +307,11 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   const char *k = (const char*)(a.k + s.k0 * a.k_stride + head * D), *v = (const char*)(a.v + s.k0 * a.v_stride + head * D);
   const int k_bytes = (int)a.k_stride * 2, v_bytes = (int)a.v_stride * 2;
 
-  const float to_log2 = a.scale * kLog2E;
+  const float to_log2 = uniform(a.scale * kLog2E);
   // What exponents are shifted by, and the sum (of this lane's half).  m follows the maximum of q.k only when that has grown by a factor of 2^kSlack in the
   // exponentials: they and their sums have room for it, and the results are seldom scaled
   float m, sum;
-  const float slack = kSlack / to_log2;
+  const float slack = uniform(kSlack / to_log2);
   f32x16 acc[D / 32];
   const char *next_k, *next_v;
   auto fetch = [&](int key0, char (&to)[2][kKeyTile * D * 2]) __attribute__((always_inline)) {
@@ -390,9 +394,12 @@ __global__ void __launch_bounds__(256, 2) attn_fwd_kernel(AttnArgs a) {
   pass(std::false_type{});
   if (__syncthreads_or(not_finite<D>(acc))) pass(std::true_type{});
   sum = sum_halves(sum);
-  if (row >= n_rows) return;
-  const int64_t at = s.q0 + query;
-  const int qh = head * a.group + of_group;
+  int thread = threadIdx.x;
+  if (D == 64) asm volatile("" : "+v"(thread));          // row, query and head anew, not kept in registers all the while
+  const int out_row = tile_row + (thread >> 6) * 32 + (thread & 31), out_query = out_row / a.group;
+  if (out_row >= n_rows) return;
+  const int64_t at = s.q0 + out_query;
+  const int qh = head * a.group + out_row - out_query * a.group;
   if (kSplit) {
     const int64_t of_part = (part * a.n_q + at) * a.hq + qh;
 #pragma unroll
