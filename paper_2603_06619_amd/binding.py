@@ -1,4 +1,4 @@
-"""ctypes binding of include/nat.h.  Argument marshalling only."""
+"""ctypes binding of include/nat.h.  Argument marshalling only (an input whose rows are one and the same in memory is copied, see _rows)."""
 import ctypes
 import functools
 import os
@@ -340,9 +340,13 @@ def nat_logp_fwd(hidden_k, W, ids_k, N_k, logp_out, entropy_out, workspace, diag
         "nat_logp_fwd")
 
 
-def _rows(t, name, shape=None, dtype=torch.bfloat16):
+_SHARED = -1
+
+
+def _rows(t, name, shape=None, dtype=torch.bfloat16, is_input=False):
     """A [rows, heads, head_dim] tensor whose heads lie back to back; returns its row stride.  What the kernels need and the
-    library cannot see (device, element type, extents) is checked here."""
+    library cannot see (device, element type, extents) is checked here.  A stride of 0 (a tensor expanded along its rows: a gradient that is equal for all of them, one
+    query for several sequences) would mean rows back to back to the library: _SHARED for an input, which the caller then gives rows of its own."""
     if t.dtype != dtype or t.dim() != 3 or not t.is_cuda:
         raise TypeError(f"{name}: expected a {dtype} device tensor [rows, heads, head_dim]")
     if shape is not None and t.shape != shape:
@@ -353,9 +357,20 @@ def _rows(t, name, shape=None, dtype=torch.bfloat16):
     n, heads, dim = t.shape
     if n == 0 or heads == 0 or dim == 0:
         return 0
+    if is_input and n > 1 and row == 0:
+        return _SHARED
     if (dim > 1 and one != 1) or (heads > 1 and head != dim):
         raise ValueError(f"{name}: the heads of a row must lie back to back")
+    if n > 1 and row < heads * dim:
+        raise ValueError(f"{name}: its rows overlap in memory")
     return row if n > 1 else 0
+
+
+def _own_rows(tensors, strides):
+    """Inputs and what _rows says of them, with rows of their own for those that share one."""
+    if _SHARED not in strides:
+        return tensors, strides
+    return [t.contiguous() if r == _SHARED else t for t, r in zip(tensors, strides)], [max(r, 0) for r in strides]
 
 
 def _vector(t, dtype, n, name):
@@ -372,9 +387,9 @@ def _attn_params(q, k, v, cu_q, cu_k, causal, scale):
     n_seqs = max(cu_q.numel() - 1, 0)
     _vector(cu_q, torch.int32, n_seqs + 1, "cu_q")
     _vector(cu_k, torch.int32, n_seqs + 1, "cu_k")
-    p = _CAttnParams(n_seqs, hq, hkv, dim, DTYPE_BF16, int(causal), float(scale), n_q, n_k, _rows(q, "q"), _rows(k, "k", (n_k, hkv, dim)),
-                     _rows(v, "v", (n_k, hkv, dim)))
-    return p
+    (q, k, v), strides = _own_rows((q, k, v), (_rows(q, "q", is_input=True), _rows(k, "k", (n_k, hkv, dim), is_input=True),
+                                               _rows(v, "v", (n_k, hkv, dim), is_input=True)))
+    return _CAttnParams(n_seqs, hq, hkv, dim, DTYPE_BF16, int(causal), float(scale), n_q, n_k, *strides), q, k, v
 
 
 @functools.lru_cache(maxsize=256)
@@ -386,7 +401,7 @@ def attn_fwd_workspace_bytes(n_q, n_k, n_seqs, n_q_heads, n_kv_heads, head_dim, 
 def nat_attn_fwd(q, k, v, cu_q, cu_k, causal, scale, out, lse, workspace=None):
     """q [n_q, q heads, D], k, v [n_k, kv heads, D] bf16 (any row stride); cu_q, cu_k int32 [n_seqs + 1]; out like q, lse float32
     [q heads, n_q].  With a workspace (attn_fwd_workspace_bytes) this is nat_attn_fwd_split."""
-    p = _attn_params(q, k, v, cu_q, cu_k, causal, scale)
+    p, q, k, v = _attn_params(q, k, v, cu_q, cu_k, causal, scale)
     p.out_stride = _rows(out, "out", q.shape)
     args = (ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k), _ptr(out), _vector(lse, torch.float32, p.n_q_heads * p.n_q, "lse"))
     if workspace is None:
@@ -407,8 +422,8 @@ def attn_bwd_workspace_full_bytes(n_q, n_k, n_seqs, n_q_heads, n_kv_heads, head_
 
 def nat_attn_bwd(q, k, v, out, lse, dout, cu_q, cu_k, causal, scale, dq, dk, dv, workspace):
     """The gradients of nat_attn_fwd; dq like q, dk and dv like k (any row stride)."""
-    p = _attn_params(q, k, v, cu_q, cu_k, causal, scale)
-    p.out_stride, p.dout_stride = _rows(out, "out", q.shape), _rows(dout, "dout", q.shape)
+    p, q, k, v = _attn_params(q, k, v, cu_q, cu_k, causal, scale)
+    (out, dout), (p.out_stride, p.dout_stride) = _own_rows((out, dout), (_rows(out, "out", q.shape, is_input=True), _rows(dout, "dout", q.shape, is_input=True)))
     p.dq_stride, p.dk_stride, p.dv_stride = _rows(dq, "dq", q.shape), _rows(dk, "dk", k.shape), _rows(dv, "dv", k.shape)
     _raise(load_library().nat_attn_bwd(
         ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _vector(lse, torch.float32, p.n_q_heads * p.n_q, "lse"), _ptr(dout),
@@ -445,7 +460,8 @@ def nat_kv_write(cache, k, v, slots):
     """k, v [rows, kv heads, D] bf16; slots int64 [rows], -1 for rows that are skipped."""
     n = k.shape[0]
     shape = (n, cache.n_kv_heads, cache.head_dim)
-    _raise(load_library().nat_kv_write(ctypes.byref(cache._c), _ptr(k), _rows(k, "k", shape), _ptr(v), _rows(v, "v", shape),
+    (k, v), (k_stride, v_stride) = _own_rows((k, v), (_rows(k, "k", shape, is_input=True), _rows(v, "v", shape, is_input=True)))
+    _raise(load_library().nat_kv_write(ctypes.byref(cache._c), _ptr(k), k_stride, _ptr(v), v_stride,
                                        _vector(slots, torch.int64, n, "slots"), n, _stream()), "nat_kv_write")
 
 
@@ -475,8 +491,9 @@ def nat_attn_decode(cache, q, block_table, seq_lens, scale, out, lse, workspace)
     n_seqs, hq, _ = q.shape
     width = _table(block_table, n_seqs)
     shape = (n_seqs, hq, cache.head_dim)
+    (q,), (q_stride,) = _own_rows((q,), (_rows(q, "q", shape, is_input=True),))
     _raise(load_library().nat_attn_decode(
-        ctypes.byref(cache._c), _ptr(q), _rows(q, "q", shape), n_seqs, hq, _ptr(block_table), width,
+        ctypes.byref(cache._c), _ptr(q), q_stride, n_seqs, hq, _ptr(block_table), width,
         _vector(seq_lens, torch.int32, n_seqs, "seq_lens"), float(scale), _ptr(out), _rows(out, "out", shape),
         _vector(lse, torch.float32, n_seqs * hq, "lse"), _ptr(workspace),
         workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_attn_decode")
@@ -495,8 +512,13 @@ def nat_sample(logits, random, temperature, top_k, top_p, min_p, ids_out, logp_o
     n, V = logits.shape
     if logits.dtype not in (torch.float32, torch.bfloat16):
         raise TypeError("logits must be float32 or bfloat16")
+    row = logits.stride(0) if n > 1 else V
+    if row < V:
+        if row > 0:
+            raise ValueError("logits: rows overlap in memory")
+        logits, row = logits.contiguous(), V             # one row for all, which the library would read as rows back to back
     _raise(load_library().nat_sample(
-        _ptr(logits), logits.stride(0) if n > 1 else 0, n, V, _dtype_code(logits), _vector(random, torch.int32, n, "random"),
+        _ptr(logits), row, n, V, _dtype_code(logits), _vector(random, torch.int32, n, "random"),
         _vector(temperature, torch.float32, n, "temperature"), _vector(top_k, torch.int32, n, "top_k"),
         _vector(top_p, torch.float32, n, "top_p"), _vector(min_p, torch.float32, n, "min_p"),
         _vector(ids_out, torch.int32, n, "ids_out"), _vector(logp_out, torch.float32, n, "logp_out"),

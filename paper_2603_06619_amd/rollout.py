@@ -21,6 +21,9 @@ class PagedCache(nb.KvCache):
 
 
 class RolloutStage:
+    """Inputs may have any row stride that the library takes, and may be expanded along their rows (a gradient that is equal for all rows, one prompt's logits for a
+    group of continuations): these are copied."""
+
     def __init__(self, device="cuda:0"):
         self.device = torch.device(device)
         self._ws = {}
