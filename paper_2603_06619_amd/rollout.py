@@ -29,9 +29,12 @@ class RolloutStage:
         self._ws = {}
 
     def _buf(self, key, nbytes):
-        """Workspace, kept per stream: calls on one stream follow one another, calls on different streams may overlap."""
+        """Workspace, kept per stream: calls on one stream follow one another, calls on different streams may overlap.  A call that is being recorded gets one of its
+        own, from the graph's memory: a graph keeps the address, and its replays follow neither the later calls of this stream nor other graphs recorded on it."""
         if nbytes == 0:
             return None
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(int(nbytes), dtype=torch.uint8, device=self.device)
         key = (key, nb._stream())
         t = self._ws.get(key)
         if t is None or t.numel() < nbytes:
