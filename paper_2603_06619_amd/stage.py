@@ -14,6 +14,10 @@ class LossStage:
         self.h_totals = torch.zeros(2, dtype=torch.int32).pin_memory()
 
     def _buf(self, key, nbytes):
+        """Workspace, kept for calls on one stream.  A call that is being recorded gets one of its own, from the graph's memory: a graph keeps the address, and a
+        larger call replaces the one that is kept."""
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(int(nbytes), dtype=torch.uint8, device=self.device)
         t = self._ws.get(key)
         if t is None or t.numel() < nbytes:
             t = torch.empty(int(nbytes), dtype=torch.uint8, device=self.device)

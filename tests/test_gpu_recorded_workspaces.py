@@ -108,3 +108,28 @@ def test_two_graphs_of_one_stream_side_by_side(kind):
                 assert torch.equal(a, b)
         for a, b in zip(eager, wants[0]):
             assert torch.equal(a, b)
+
+
+def test_a_larger_loss_call_after_recording():
+    """Log-probs of the loss stage, whose workspace a larger call replaces."""
+    from paper_2603_06619_amd.stage import LossStage
+    stage, fresh, side = LossStage(DEV), LossStage(DEV), torch.cuda.Stream()
+    g = torch.Generator(device=DEV).manual_seed(3)
+    W = rand(g, 5000, 256) * 0.1
+    hidden, ids = rand(g, 300, 256), torch.randint(0, 5000, (300,), generator=g, device=DEV).to(torch.int32)
+    more, more_ids = rand(g, 3000, 256), torch.randint(0, 5000, (3000,), generator=g, device=DEV).to(torch.int32)
+    graph, out = record(stage, side, lambda s: s.logp(hidden, W, ids, 300)["logp"])
+    size = stage._ws["loss"].numel()
+    with torch.cuda.stream(side):
+        stage.logp(more, W, more_ids, 3000)
+        assert stage._ws["loss"].numel() > size
+        theirs = [torch.full((size // 4,), 123456789, dtype=torch.int32, device=DEV) for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        hidden.copy_(torch.randn(hidden.shape, device=DEV))
+        want = fresh.logp(hidden, W, ids, 300)["logp"]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all(bool((t == 123456789).all()) for t in theirs)

@@ -40,3 +40,16 @@ def test_a_recorded_call_has_its_own(streams):
     assert stage._buf("z", 100) is new and stage._buf("x", 5000) is not kept
     held = [t for t in stage._ws.values() if t is first or t is second]
     assert not held
+
+
+def test_a_recorded_loss_call_has_its_own(streams):
+    from paper_2603_06619_amd.stage import LossStage
+    stage = LossStage.__new__(LossStage)                            # without the pinned words, which need a GPU
+    stage.device, stage._ws = torch.device("cpu"), {}
+    kept = stage._buf("loss", 1000)
+    assert stage._buf("loss", 700) is kept
+    streams["recording"] = True
+    first, second = stage._buf("loss", 1000), stage._buf("loss", 2000)
+    assert len({t.data_ptr() for t in (kept, first, second)}) == 3 and first.numel() >= 1000 and second.numel() >= 2000
+    streams["recording"] = False
+    assert stage._buf("loss", 1000) is kept
