@@ -173,10 +173,11 @@ __device__ __forceinline__ void end_of_step() {
 }
 
 // Where a mask cuts through a tile, a product multiplies masked rows by 0, and infinities or NaN in them come through as NaN.  Results that are not finite
-// are therefore computed once more, carefully: at the mask's edge such a tile gets zeros in their places before it enters the product, and the columns
-// that see them have them added by hand.
-template <int D, int kRows, class Sees>
-__device__ __forceinline__ void take_out_not_finite(char* tile, f32x16 (&acc)[D / 32], int half, const Sees& sees) {
+// are therefore computed once more, carefully: at the mask's edge the product with P or dS gets zeros in the places of such elements (the tile stays as it is: scores
+// and dP, whose masked elements are set, are made of it), and the columns that see them have them added by hand.  P has no sign: what it multiplies is
+// added itself.  An element of k or q that is not finite makes its scores infinite, and P 0 or NaN: what dS multiplies (kNan) gives NaN.
+template <int D, int kRows, bool kNan, class Sees>
+__device__ __forceinline__ void add_not_finite(const char* tile, f32x16 (&acc)[D / 32], int half, const Sees& sees) {
   for (int row = 0; row < kRows; ++row) {
     if (!sees(row)) continue;
 #pragma unroll
@@ -186,15 +187,22 @@ __device__ __forceinline__ void take_out_not_finite(char* tile, f32x16 (&acc)[D 
         const uint16_t* x = (const uint16_t*)(tile + RowTile<D>::chunk_at(row, 4 * db + i) + 8 * half);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if ((x[e] & 0x7f80) == 0x7f80) acc[db][4 * i + e] += __builtin_bit_cast(float, (uint32_t)x[e] << 16);
+          if ((x[e] & 0x7f80) == 0x7f80) acc[db][4 * i + e] += kNan ? NAN : __builtin_bit_cast(float, (uint32_t)x[e] << 16);
       }
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < kRows * D; i += blockDim.x) {
-    uint16_t* x = (uint16_t*)tile + i;
-    if ((*x & 0x7f80) == 0x7f80) *x = 0;
+}
+// transposed_fragment, with zeros in those places if `edge`
+template <int D>
+__device__ __forceinline__ bf16x8 finite_fragment(const char* tile, int lane, int db, int s, bool edge) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 x = __builtin_bit_cast(u32x4, transposed_fragment<D>(tile, lane, db, s));
+  const uint32_t keep = edge ? 0u : ~0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((x[i] & 0x7f80) == 0x7f80) x[i] &= 0xffff0000 | keep;
+    if ((x[i] & 0x7f800000) == 0x7f800000) x[i] &= 0xffff | keep;
   }
-  __syncthreads();
+  return __builtin_bit_cast(bf16x8, x);
 }
 
 template <int D>
@@ -299,7 +307,6 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) attn_fwd_kernel(AttnArgs
     first_key = part * steps * kKeyTile;
     end_key = n_keys - first_key > steps * kKeyTile ? first_key + steps * kKeyTile : n_keys;
   }
-  const int tile_least = last_key(a, s, tile_row / a.group);           // seen by all rows of the tile
   const int last = last_key(a, s, query);                              // of this lane's row
   const int wave_row = tile_row + wave * 32 < n_rows ? tile_row + wave * 32 : n_rows - 1, wave_end = wave_row + 32 < n_rows ? wave_row + 32 : n_rows;
   const int wave_least = last_key(a, s, wave_row / a.group);           // keys up to here are seen by all rows of the wavefront
@@ -321,10 +328,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) attn_fwd_kernel(AttnArgs
     next_v += (int64_t)kKeyTile * v_bytes;
   };
   auto step = [&](int key0, char* kt, char* vt, auto careful) __attribute__((always_inline)) {
-    if constexpr (decltype(careful)::value) {
-      if (key0 + kKeyTile - 1 > tile_least) take_out_not_finite<D, kKeyTile>(vt, acc, half, [&](int i) { return key0 + i <= last; });
-    }
+    constexpr bool kCareful = decltype(careful)::value;
+    const bool edge = kCareful && key0 + kKeyTile - 1 > wave_least;
     if (key0 > wave_last) return;
+    if (edge) add_not_finite<D, kKeyTile, false>(vt, acc, half, [&](int i) { return key0 + i <= last; });
     f32x16 st[2] = {};
     tile_times_columns<D>(kt, q.f, st, lane);
     if (key0 + kKeyTile - 1 > wave_least) {
@@ -360,7 +367,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) attn_fwd_kernel(AttnArgs
       }
       p[g & 1] = fragment_of_result(st[g >> 1], g & 1);
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) vf[g & 1][db] = transposed_fragment<D>(vt, lane, db, g);
+      for (int db = 0; db < D / 32; ++db)
+        if constexpr (!kCareful) vf[g & 1][db] = transposed_fragment<D>(vt, lane, db, g);
     };
     ready(0);
     __builtin_amdgcn_sched_barrier(0);
@@ -368,7 +376,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) attn_fwd_kernel(AttnArgs
     for (int g = 0; g < 4; ++g) {
       if (g < 3) ready(g + 1);
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(vf[g & 1][db], p[g & 1], acc[db]);
+      for (int db = 0; db < D / 32; ++db) {
+        if constexpr (kCareful) acc[db] = mfma32(finite_fragment<D>(vt, lane, db, g, edge), p[g & 1], acc[db]);
+        else acc[db] = mfma32(vf[g & 1][db], p[g & 1], acc[db]);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -513,10 +524,9 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
   float p_sum = 0.f, p_dp = 0.f;
   auto step = [&](int key0, char* kt, char* vt, auto kind) __attribute__((always_inline)) {
     constexpr Pass kPass = decltype(kind)::value;
-    if constexpr (kPass == Pass::kCareful) {
-      if (key0 + kKeyTile - 1 > tile_least) take_out_not_finite<D, kKeyTile>(kt, acc, half, [&](int i) { return key0 + i <= last; });
-    }
+    const bool edge = kPass == Pass::kCareful && key0 + kKeyTile - 1 > wave_least;
     if (key0 > wave_last) return;
+    if (edge) add_not_finite<D, kKeyTile, true>(kt, acc, half, [&](int i) { return key0 + i <= last; });
     f32x16 st[2] = {}, dp[2] = {};
     tile_times_columns<D>(kt, q.f, st, lane);
     tile_times_columns<D>(vt, d.f, dp, lane);
@@ -549,7 +559,8 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
         }
         p[g & 1] = fragment_of_result(st[g >> 1], g & 1);
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) kf[g & 1][db] = transposed_fragment<D>(kt, lane, db, g);
+        for (int db = 0; db < D / 32; ++db)
+          if constexpr (kPass != Pass::kCareful) kf[g & 1][db] = transposed_fragment<D>(kt, lane, db, g);
       };
       ready(0);
       __builtin_amdgcn_sched_barrier(0);
@@ -557,7 +568,10 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
       for (int g = 0; g < 4; ++g) {
         if (g < 3) ready(g + 1);
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(kf[g & 1][db], p[g & 1], acc[db]);
+        for (int db = 0; db < D / 32; ++db) {
+          if constexpr (kPass == Pass::kCareful) acc[db] = mfma32(finite_fragment<D>(kt, lane, db, g, edge), p[g & 1], acc[db]);
+          else acc[db] = mfma32(kf[g & 1][db], p[g & 1], acc[db]);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -625,7 +639,6 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) attn_dkv_kernel(AttnArgs
   const int part_steps = ((n_rows - seen_from + kDkvRows - 1) / kDkvRows + a.row_parts - 1) / a.row_parts;
   const int first_row = seen_from + part * part_steps * kDkvRows, end_row = n_rows - first_row > part_steps * kDkvRows ? first_row + part_steps * kDkvRows : n_rows;
   const int wave_first = a.causal ? wave_key - s.ahead : 0;            // the first query that sees the wavefront's first key
-  const int tile_all = a.causal ? tile_key + kDkvKeys - 1 - s.ahead : 0;
   const int wave_all = a.causal ? wave_key + 31 - s.ahead : 0;         // queries from here on see all its keys
   const char *q = (const char*)(a.q + s.q0 * a.q_stride + head * a.group * D), *d = (const char*)(a.dout + s.q0 * a.dout_stride + head * a.group * D);
   const int q_bytes = (int)a.q_stride * 2, d_bytes = (int)a.dout_stride * 2;
@@ -673,14 +686,13 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) attn_dkv_kernel(AttnArgs
     }
   };
   auto step = [&](char* qt, char* dt, RowWords& w, auto careful) __attribute__((always_inline)) {
-    if constexpr (decltype(careful)::value) {
-      if (query < tile_all) {
-        take_out_not_finite<D, kDkvRows>(qt, dk, half, [&](int i) { return key <= w.last[i]; });
-        take_out_not_finite<D, kDkvRows>(dt, dv, half, [&](int i) { return key <= w.last[i]; });
-      }
-    }
-    if (query + small_quotient(head_of_group + kDkvRows - 1, a.group_inverse) < wave_first) return;
     constexpr bool kCareful = decltype(careful)::value;
+    if (query + small_quotient(head_of_group + kDkvRows - 1, a.group_inverse) < wave_first) return;
+    const bool edge = kCareful && query < wave_all;
+    if (edge) {
+      add_not_finite<D, kDkvRows, true>(qt, dk, half, [&](int i) { return key <= w.last[i]; });
+      add_not_finite<D, kDkvRows, false>(dt, dv, half, [&](int i) { return key <= w.last[i]; });
+    }
     f32x16 p[2] = {}, dp[2] = {};
     tile_times_columns<D>(qt, k.f, p, lane);
     // Probabilities of what is masked are 0, and so are its dS if all is finite (if not, NaN leads to the careful pass, which takes them out one by one).  The
@@ -734,6 +746,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) attn_dkv_kernel(AttnArgs
       df[g & 1] = fragment_of_result(dp[g >> 1], g & 1);
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
+        if constexpr (kCareful) continue;
         dof[g & 1][db] = transposed_fragment<D>(dt, lane, db, g);
         qf[g & 1][db] = transposed_fragment<D>(qt, lane, db, g);
       }
@@ -745,8 +758,14 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) attn_dkv_kernel(AttnArgs
       if (g < 3) ready(g + 1);
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
-        dv[db] = mfma32(dof[g & 1][db], pf[g & 1], dv[db]);
-        dk[db] = mfma32(qf[g & 1][db], df[g & 1], dk[db]);
+        if constexpr (kCareful) {
+          dv[db] = mfma32(finite_fragment<D>(dt, lane, db, g, edge), pf[g & 1], dv[db]);
+          dk[db] = mfma32(finite_fragment<D>(qt, lane, db, g, edge), df[g & 1], dk[db]);
+          __builtin_amdgcn_sched_barrier(0);
+        } else {
+          dv[db] = mfma32(dof[g & 1][db], pf[g & 1], dv[db]);
+          dk[db] = mfma32(qf[g & 1][db], df[g & 1], dk[db]);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
