@@ -331,7 +331,6 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) attn_fwd_kernel(AttnArgs
     constexpr bool kCareful = decltype(careful)::value;
     const bool edge = kCareful && key0 + kKeyTile - 1 > wave_least;
     if (key0 > wave_last) return;
-    if (edge) add_not_finite<D, kKeyTile, false>(vt, acc, half, [&](int i) { return key0 + i <= last; });
     f32x16 st[2] = {};
     tile_times_columns<D>(kt, q.f, st, lane);
     if (key0 + kKeyTile - 1 > wave_least) {
@@ -382,6 +381,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) attn_fwd_kernel(AttnArgs
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    // behind the step's scaling of what was summed before: by 0 in the first tile
+    if (edge) add_not_finite<D, kKeyTile, false>(vt, acc, half, [&](int i) { return key0 + i <= last; });
   };
   auto pass = [&](auto careful) __attribute__((always_inline)) {
     m = -INFINITY;

@@ -67,3 +67,32 @@ def test_an_infinite_gradient(stage, D, at):  # noqa: F811
         got["dq"][at], got["dk"][:at + 1] = want["dq"][at], want["dk"][:at + 1]
         for name in want:
             assert torch.equal(got[name], want[name]), name
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("at", [0] + AT)
+def test_an_infinite_value(stage, D, at):  # noqa: F811
+    """Every row that sees it has its sign in that element; nothing else changes."""
+    n = 200
+    for value in (float("inf"), -float("inf")):
+        c = make(24, [n, 30], [n, 30], 4, 2, D)
+        want = run(stage, c, backward=False)
+        c["v"][at, :, 9] = value
+        got = run(stage, c, backward=False)
+        assert bool((got["out"][at:n, :, 9] == value).all())
+        got["out"][at:n, :, 9] = want["out"][at:n, :, 9]
+        assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_an_infinite_value_among_shared_keys(stage, D):  # noqa: F811
+    """Rows whose keys several workgroups share: seen by all rows, by some, in a part of its own."""
+    for at in (0, 1400, 2985, 2999):
+        c = make(25, [20], [3000], 4, 2, D)
+        want = run(stage, c, backward=False)
+        c["v"][at, :, 9] = float("inf")
+        got = run(stage, c, backward=False)
+        first = max(at - 2980, 0)
+        assert bool((got["out"][first:, :, 9] == float("inf")).all())
+        got["out"][first:, :, 9] = want["out"][first:, :, 9]
+        assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
