@@ -423,7 +423,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) attn_fwd_kernel(AttnArgs
     return;
   }
   store_columns<D>(a.out + at * a.out_stride + qh * D, acc, sum == 0.f ? 0.f : 1.f / sum, lane);
-  if (half == 0) a.lse[qh * a.n_q + at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, __logf(sum));
+  // a row that sees nothing has the sum 0; one of NaN scores, whose maximum is -inf as well, NaN
+  if (half == 0) a.lse[qh * a.n_q + at] = sum == 0.f ? -INFINITY : fmaf(m, a.scale, __logf(sum));
 }
 
 // Results of a tile's rows from those of its key_parts workgroups, scaled to their common maximum; two rows per wavefront, all loads of a row under way at once
@@ -464,7 +465,7 @@ __global__ void __launch_bounds__(256) attn_fwd_join_kernel(AttnArgs a) {
       x += y[p] * f;
     }
     if (2 * lane < D) *(bf16x2*)(a.out + at * a.out_stride + qh * D + 2 * lane) = __builtin_convertvector(x * (sum == 0.f ? 0.f : 1.f / sum), bf16x2);
-    if (lane == 0) a.lse[qh * a.n_q + at] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, __logf(sum));
+    if (lane == 0) a.lse[qh * a.n_q + at] = sum == 0.f ? -INFINITY : fmaf(m, a.scale, __logf(sum));
   }
 }
 

@@ -369,11 +369,10 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
   float all_m = -INFINITY, all_sum = 0.f;
 #pragma unroll
   for (int w = 0; w < 4; ++w) all_m = fmaxf(all_m, wave_m[w][n]);
-  if (all_m != -INFINITY) {
+  const float base = all_m == -INFINITY ? 0.f : all_m;       // (without any token, or if all scores are NaN: the sums then are 0, or NaN)
 #pragma unroll
-    for (int w = 0; w < 4; ++w) all_sum += wave_sum[w][n] * exp2_fast((wave_m[w][n] - all_m) * to_log2);
-  }
-  const float f = all_m == -INFINITY ? 0.f : exp2_fast((m - all_m) * to_log2);
+  for (int w = 0; w < 4; ++w) all_sum += wave_sum[w][n] * exp2_fast((wave_m[w][n] - base) * to_log2);
+  const float f = exp2_fast((m - base) * to_log2);
   float* mine = (float*)values[wave];
 #pragma unroll
   for (int db = 0; db < D / 16; ++db) *(f32x4*)(mine + n * D + 16 * db + 4 * g) = acc[db] * f;
@@ -394,7 +393,7 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
     } else {
       const float total = joined_sum[h];
       *(bf16x4*)(a.out + seq * a.out_stride + (head0 + h) * D + d) = __builtin_convertvector(x * (total == 0.f ? 0.f : 1.f / total), bf16x4);
-      if (d == 0) a.lse[row] = joined_m[h] == -INFINITY ? -INFINITY : fmaf(joined_m[h], a.scale, __logf(total));
+      if (d == 0) a.lse[row] = total == 0.f ? -INFINITY : fmaf(joined_m[h], a.scale, __logf(total));
     }
   }
 }
@@ -457,7 +456,7 @@ __global__ void __launch_bounds__(64 * kMaxJoinWaves) decode_join_kernel(DecodeA
     for (int w = 0; w < waves; ++w) z += *(const f32x4*)(part[w] + 4 * lane);
     *(bf16x4*)(a.out + seq * a.out_stride + qh * D + 4 * lane) = __builtin_convertvector(z * (sum == 0.f ? 0.f : 1.f / sum), bf16x4);
   }
-  if (lane == 0) a.lse[row] = m == -INFINITY ? -INFINITY : fmaf(m, a.scale, __logf(sum));
+  if (lane == 0) a.lse[row] = sum == 0.f ? -INFINITY : fmaf(m, a.scale, __logf(sum));
 }
 
 bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
