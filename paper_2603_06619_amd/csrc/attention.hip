@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 4 : 2) attn_fwd_kernel(AttnArgs
   // What exponents are shifted by, and the sum (of this lane's half).  m follows the maximum of q.k only when that has grown by a factor of 2^kSlack in the
   // exponentials: they and their sums have room for it, and the results are seldom scaled
   float m, sum;
-  const float slack = uniform(kSlack / to_log2);
+  const float slack = uniform(fminf(kSlack / to_log2, __FLT_MAX__));       // (finite: m leaves -inf whatever the scale)
   f32x16 acc[D / 32];
   const char *next_k, *next_v;
   auto fetch = [&](int key0, char (&to)[2][kKeyTile * D * 2]) __attribute__((always_inline)) {
