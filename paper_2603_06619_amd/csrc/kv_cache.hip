@@ -37,7 +37,7 @@ __device__ __forceinline__ u32x2 widen_fp8(uint32_t x) {
 struct WriteArgs {
   CacheArgs c;
   const uint16_t *k, *v;
-  int64_t k_stride, v_stride, n_rows;
+  int64_t k_stride, v_stride, n_rows, first;      // first: (row, head) pair that the launch begins with
   const int64_t* slots;
 };
 
@@ -85,7 +85,7 @@ template <int D, bool kFp8>
 __global__ void __launch_bounds__(256) kv_write_kernel(WriteArgs a) {
   constexpr int kLanes = D / 8;
   const int lane = threadIdx.x % kLanes;
-  const int64_t id = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, row = id / a.c.hkv;
+  const int64_t id = a.first + (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, row = id / a.c.hkv;
   if (row >= a.n_rows) return;
   const int head = (int)(id - row * a.c.hkv);
   const int64_t slot = a.slots[row];
@@ -99,7 +99,7 @@ struct ReadArgs {
   CacheArgs c;
   const int32_t *table, *cu;
   int table_width, n_seqs;
-  int64_t n_rows, k_stride, v_stride;
+  int64_t n_rows, k_stride, v_stride, first;      // first: as in WriteArgs
   uint16_t *k, *v;
 };
 
@@ -128,7 +128,7 @@ template <int D, bool kFp8>
 __global__ void __launch_bounds__(256) kv_read_kernel(ReadArgs a) {
   constexpr int kLanes = D / 8;
   const int lane = threadIdx.x % kLanes;
-  const int64_t id = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, row = id / a.c.hkv;
+  const int64_t id = a.first + (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, row = id / a.c.hkv;
   if (row >= a.n_rows || row < a.cu[0] || row >= a.cu[a.n_seqs]) return;
   const int head = (int)(id - row * a.c.hkv);
   const int seq = rollout_of_pos(a.cu, 0, a.n_seqs, row);
@@ -494,19 +494,23 @@ void by_shape(int head_dim, int format, Args... args) {
   if (head_dim == 128) format == NAT_KV_FP8 ? Launch<128, true>::go(args...) : Launch<128, false>::go(args...);
   else format == NAT_KV_FP8 ? Launch<64, true>::go(args...) : Launch<64, false>::go(args...);
 }
+// (row, head) pairs, `per` to a workgroup of 256, in as few launches as have room for them
+template <class Args>
+void launch_rows(void (*kernel)(Args), Args a, int64_t per, hipStream_t s) {
+  constexpr int64_t kMost = kMaxWorkItems / 256;
+  const int64_t pairs = a.n_rows * a.c.hkv;
+  for (a.first = 0; a.first < pairs; a.first += kMost * per) {
+    const int64_t blocks = (pairs - a.first + per - 1) / per;
+    kernel<<<(unsigned)(blocks < kMost ? blocks : kMost), 256, 0, s>>>(a);
+  }
+}
 template <int D, bool kFp8>
 struct LaunchWrite {
-  static void go(WriteArgs a, hipStream_t s) {
-    const int64_t per = 256 / (D / 8);
-    kv_write_kernel<D, kFp8><<<(unsigned)((a.n_rows * a.c.hkv + per - 1) / per), 256, 0, s>>>(a);
-  }
+  static void go(WriteArgs a, hipStream_t s) { launch_rows(kv_write_kernel<D, kFp8>, a, 256 / (D / 8), s); }
 };
 template <int D, bool kFp8>
 struct LaunchRead {
-  static void go(ReadArgs a, hipStream_t s) {
-    const int64_t per = 256 / (D / 8);
-    kv_read_kernel<D, kFp8><<<(unsigned)((a.n_rows * a.c.hkv + per - 1) / per), 256, 0, s>>>(a);
-  }
+  static void go(ReadArgs a, hipStream_t s) { launch_rows(kv_read_kernel<D, kFp8>, a, 256 / (D / 8), s); }
 };
 template <int D, bool kFp8>
 struct LaunchDecode {

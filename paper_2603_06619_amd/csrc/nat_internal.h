@@ -14,6 +14,9 @@ enum ProfClass : int {
   PC_ATTN_FWD, PC_ATTN_BWD, PC_KV_CACHE, PC_ATTN_DECODE, PC_SAMPLE, PC_NUM
 };
 
+// A launch has room for fewer than 2^32 work-items: of more, the rest is left out without an error.
+constexpr int64_t kMaxWorkItems = (int64_t{1} << 32) - 1;
+
 // Brackets the launches issued during its lifetime with two events when timing is on.
 struct ProfScope {
   ProfScope(int cls, hipStream_t s, bool enabled = true);
