@@ -937,10 +937,24 @@ size_t row_bytes_of(int32_t V, int elem, int splits) {
 }
 
 template <class T>
-void launch(const SampleArgs& a, int32_t n_rows, hipStream_t s) {
+void launch(SampleArgs a, int32_t n_rows, hipStream_t s) {
   if (a.splits == 1) {
-    sample_row_kernel<T><<<n_rows, kThreads, 0, s>>>(a);
-    return;
+    constexpr int32_t kMost = kMaxWorkItems / kThreads;          // rows of a launch
+    auto skip = [](auto*& p, int64_t n) { p = p ? p + n : p; };
+    for (;;) {
+      sample_row_kernel<T><<<n_rows < kMost ? n_rows : kMost, kThreads, 0, s>>>(a);
+      if (n_rows <= kMost) return;
+      n_rows -= kMost;
+      a.logits = (const T*)a.logits + kMost * a.row_stride;
+      skip(a.random, kMost);
+      skip(a.temperature, kMost);
+      skip(a.top_p, kMost);
+      skip(a.min_p, kMost);
+      skip(a.top_k, kMost);
+      skip(a.ids, kMost);
+      skip(a.logp, kMost);
+      skip(a.logq, kMost);
+    }
   }
   sample_top_kernel<T><<<n_rows * a.splits, kThreads, 0, s>>>(a);
   if (a.top_k || a.top_p) {
