@@ -423,8 +423,9 @@ typedef struct nat_attn_params {
  * Products of queries and keys and all sums are held in fp32; the probabilities are rounded to bf16 for
  * the product with the values.  Results do not change from run to run.
  * Errors: NULL pointer, negative count, causal not 0 / 1, scale out of range, a pointer (other than lse and
- * offsets) that is not 16-byte aligned -> NAT_INVALID_ARG; head counts, head_dim or a stride out of range, or
- * n_q * (n_q_heads / n_kv_heads) >= 2^30 -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE.
+ * offsets) that is not 16-byte aligned -> NAT_INVALID_ARG; head counts, head_dim or a stride out of range,
+ * n_q * (n_q_heads / n_kv_heads) >= 2^30, or more sequences than a launch has room for (n_seqs * n_kv_heads about
+ * 2^24: it takes fewer than 2^32 work-items) -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE.
  * n_seqs = 0 and n_q = 0 are valid and do nothing.
  */
 nat_status nat_attn_fwd(const nat_attn_params* params, const void* d_q, const void* d_k, const void* d_v,
@@ -511,7 +512,8 @@ nat_status nat_kv_read(const nat_kv_cache* cache, const int32_t* d_block_table, 
  *                short tables, which need none.
  * Long sequences are cut into chunks for different workgroups and joined by a second kernel; how depends on the sizes
  * alone, so results do not change from run to run.
- * Errors: as nat_kv_write, plus scale out of range -> NAT_INVALID_ARG, NAT_WORKSPACE_TOO_SMALL.
+ * Errors: as nat_kv_write, plus scale out of range -> NAT_INVALID_ARG, more chunks of sequences, or query heads, than a
+ * launch has room for (as in nat_attn_fwd) -> NAT_BAD_SHAPE, NAT_WORKSPACE_TOO_SMALL.
  */
 size_t nat_attn_decode_workspace_bytes(int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                        int64_t max_tokens);

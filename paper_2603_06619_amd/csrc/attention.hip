@@ -855,9 +855,10 @@ nat_status attn_args(const nat_attn_params* p, const void* d_q, const void* d_k,
     return NAT_BAD_SHAPE;
   const int64_t q_row = (int64_t)p->n_q_heads * p->head_dim, k_row = (int64_t)p->n_kv_heads * p->head_dim;
   const int group = p->n_q_heads / p->n_kv_heads;
-  // rows of a group's matrix and tile slots are counted in 32 bits
-  if (p->n_q * group > INT32_MAX / 2 || (p->n_q * group / kRowTile + p->n_seqs) * p->n_kv_heads > INT32_MAX / 2 ||
-      (p->n_k / kDkvKeys + p->n_seqs) * p->n_kv_heads > INT32_MAX / 2)
+  // rows of a group's matrix are counted in 32 bits, and a launch has to have room for the tile slots (grid_of adds up to 7 workgroups)
+  constexpr int64_t kMostSlots = kMaxWorkItems / 256 - 7;
+  if (p->n_q * group > INT32_MAX / 2 || (p->n_q * group / kRowTile + p->n_seqs) * p->n_kv_heads > kMostSlots ||
+      (p->n_k / kDkvKeys + p->n_seqs) * p->n_kv_heads > kMostSlots)
     return NAT_BAD_SHAPE;
   auto stride_ok = [](int64_t s, int64_t row) { return s == 0 || (s >= row && s % 8 == 0 && s < kMaxStride); };
   if (!stride_ok(p->q_stride, q_row) || !stride_ok(p->out_stride, q_row) || !stride_ok(p->dout_stride, q_row) || !stride_ok(p->dq_stride, q_row) ||

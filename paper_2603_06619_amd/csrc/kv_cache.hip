@@ -519,7 +519,7 @@ struct LaunchDecode {
   }
 };
 
-struct DecodePlan { int chunk, n_chunks, head_blocks; };
+struct DecodePlan { int chunk, n_chunks, head_blocks, join_waves; };
 bool decode_plan(int64_t n_seqs, int64_t hq, int64_t hkv, int64_t most, DecodePlan* p) {
   if (n_seqs * hq > INT32_MAX) return false;
   const int64_t group = hq / hkv;
@@ -527,7 +527,8 @@ bool decode_plan(int64_t n_seqs, int64_t hq, int64_t hkv, int64_t most, DecodePl
   p->chunk = chunk_of(n_seqs, hkv * p->head_blocks, most);
   const int64_t n = most > 0 ? (most + p->chunk - 1) / p->chunk : 1;
   p->n_chunks = (int)n;
-  return n_seqs * n * hkv * p->head_blocks <= INT32_MAX;
+  p->join_waves = (int)(n > kJoinChunks * kMaxJoinWaves ? kMaxJoinWaves : (n + kJoinChunks - 1) / kJoinChunks);
+  return n_seqs * n * hkv * p->head_blocks <= kMaxWorkItems / 256 && (n == 1 || n_seqs * hq <= kMaxWorkItems / (64 * p->join_waves));
 }
 bool decode_shape_ok(int32_t n_seqs, int32_t hq, int32_t hkv, int32_t head_dim, int64_t most) {
   return n_seqs >= 0 && (head_dim == 64 || head_dim == 128) && hkv > 0 && hkv <= 4096 && hq > 0 && hq <= 4096 && hq % hkv == 0 && most >= 0 &&
@@ -635,9 +636,8 @@ extern "C" nat_status nat_attn_decode(const nat_kv_cache* cache, const void* d_q
   by_shape<LaunchDecode>(cache->head_dim, cache->format, a, s);
   NAT_LAUNCH_CHECK();
   if (p.n_chunks == 1) return NAT_OK;
-  const int waves = p.n_chunks > kJoinChunks * kMaxJoinWaves ? kMaxJoinWaves : (p.n_chunks + kJoinChunks - 1) / kJoinChunks;
-  if (cache->head_dim == 128) decode_join_kernel<128><<<(unsigned)(n_seqs * n_q_heads), 64 * waves, 0, s>>>(a);
-  else decode_join_kernel<64><<<(unsigned)(n_seqs * n_q_heads), 64 * waves, 0, s>>>(a);
+  if (cache->head_dim == 128) decode_join_kernel<128><<<(unsigned)(n_seqs * n_q_heads), 64 * p.join_waves, 0, s>>>(a);
+  else decode_join_kernel<64><<<(unsigned)(n_seqs * n_q_heads), 64 * p.join_waves, 0, s>>>(a);
   NAT_LAUNCH_CHECK();
   return NAT_OK;
 }
