@@ -399,7 +399,8 @@ nat_status nat_loss_fwd_bwd_kl(const void* d_hidden_k, const void* d_W, const in
  * keys as queries its own and those before it; with more, queries behind a cached prefix; with fewer,
  * the first queries see none.  A query that sees no key has out = 0 and lse = -inf, and adds nothing to
  * any gradient.  What lies in masked places of keys, values, queries or gradients (infinities and NaN
- * too) has no influence.
+ * too) has no influence; what a query does see has the influence that the formulas give it (a value of
+ * infinity: out is infinite; scores of NaN: out and lse are NaN).
  *   n_seqs       sequences;  n_q, n_k: rows of the query and key arrays (at most 2^31 - 1);
  *   n_q_heads    a multiple of n_kv_heads; query head h reads key head h / (n_q_heads / n_kv_heads);
  *   head_dim     64 or 128;  dtype NAT_DTYPE_BF16;  causal 0 or 1;  scale > 0 and finite;
@@ -419,9 +420,11 @@ typedef struct nat_attn_params {
  *   d_cu_q, d_cu_k [n_seqs+1] int32: non-decreasing row offsets (d_cu_packed of nat_prefix_pack); values
  *                outside [0, n_q] / [0, n_k] are clamped;
  *   d_out [n_q, n_q_heads, head_dim] bf16 out;  d_lse [n_q_heads, n_q] float out.  Rows of no sequence
- *                are not written.
+ *                are not written: with arrays that are longer than their sequences, clear these rows, or cut
+ *                the arrays, before anything sums over all rows.
  * Products of queries and keys and all sums are held in fp32; the probabilities are rounded to bf16 for
- * the product with the values.  Results do not change from run to run.
+ * the product with the values (an error in the 2-norm of about 2e-3 with the rounding of out, which alone
+ * makes 1.6e-3).  Results do not change from run to run.
  * Errors: NULL pointer, negative count, causal not 0 / 1, scale out of range, a pointer (other than lse and
  * offsets) that is not 16-byte aligned -> NAT_INVALID_ARG; head counts, head_dim or a stride out of range,
  * n_q * (n_q_heads / n_kv_heads) >= 2^30, or more sequences than a launch has room for (n_seqs * n_kv_heads about
@@ -452,8 +455,10 @@ nat_status nat_attn_fwd_split(const nat_attn_params* params, const void* d_q, co
  *   d_ws / ws_bytes: at least nat_attn_bwd_workspace_bytes, 256-byte aligned.  With
  *                nat_attn_bwd_workspace_full_bytes (of params' counts, causal and head_dim; 0 if they are out of
  *                range) the sums of dk, dv are shared by more workgroups where there are few keys.
- * P and dS are rounded to bf16 for the products that they enter.  No atomics: results do not change from
- * run to run (with workspaces of other sizes the sums may be cut elsewhere).  Errors as nat_attn_fwd, plus NAT_WORKSPACE_TOO_SMALL.  With n_q = 0, dk and dv are zeros.
+ * P and dS are rounded to bf16 for the products that they enter, and dout_i . out_i takes out as it was stored where all
+ * queries of a tile see 64 keys or more (errors in the 2-norm of about 2.4e-3; 1.7e-3 with everything in fp32 and rounded
+ * once).  No atomics: results do not change from run to run (with workspaces of other sizes the sums may be cut
+ * elsewhere).  Errors as nat_attn_fwd, plus NAT_WORKSPACE_TOO_SMALL.  With n_q = 0, dk and dv are zeros.
  */
 size_t nat_attn_bwd_workspace_bytes(int64_t n_q, int32_t n_q_heads);
 size_t nat_attn_bwd_workspace_full_bytes(const nat_attn_params* params);
@@ -507,7 +512,8 @@ nat_status nat_kv_read(const nat_kv_cache* cache, const int32_t* d_block_table, 
  *   d_q          [n_seqs, n_q_heads, head_dim] bf16;  d_seq_lens [n_seqs] int32: cached tokens that count, the first ones
  *                (clamped to [0, table_width * page_size]); tokens whose page lies outside [0, n_pages) do not count;
  *   d_out        [n_seqs, n_q_heads, head_dim] bf16 out;  d_lse [n_seqs, n_q_heads] float out.  Without any token out = 0
- *                and lse = -inf.  What is stored in places beyond a sequence's length has no influence;
+ *                and lse = -inf.  What is stored in places beyond a sequence's length has no influence.  The probabilities
+ *                (of NAT_KV_FP8 with the value rows' powers of two) are rounded to bf16 for the product with the values;
  *   d_ws / ws_bytes: nat_attn_decode_workspace_bytes(.., max_tokens = table_width * page_size), 256-byte aligned; 0 for
  *                short tables, which need none.
  * Long sequences are cut into chunks for different workgroups and joined by a second kernel; how depends on the sizes
@@ -542,7 +548,11 @@ nat_status nat_attn_decode(const nat_kv_cache* cache, const void* d_q, int64_t q
  *                behaviour log-prob that nat_loss_fwd_bwd takes as d_old_logp;
  *   d_logq [n_rows] float out or NULL: log of the probability with which the token was drawn;
  *   d_ws / ws_bytes: at least nat_sample_workspace_bytes, 256-byte aligned; 0 for as many rows as fill the chip.
- * 2^y is taken to a relative error of 2^-40, i.e. weights are whole numbers within 2 of the exact ones.
+ * 2^y is taken to a relative error of 2^-40, i.e. weights are whole numbers within 2 of the exact ones.  At temperatures
+ * other than 1 the sum of d_logp is one of fp32 exponentials, in fp64.
+ * Rows with a top-k or top-p keep a list of the tokens among which it ends: those within 1/16 octave of weight, or, with both,
+ * all down to it.  With more than 4096 (a top-k above 4096 and a top-p, high temperatures, very many equal logits) one
+ * workgroup goes over the row several times more instead: the results are as exact, the time is 3 to 8 times as long.
  * Errors: NULL required pointer, n_rows < 0, logits not aligned to their element -> NAT_INVALID_ARG; V outside [1, 2^20],
  * 0 < row_stride < V -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE; NAT_WORKSPACE_TOO_SMALL.
  */

@@ -272,11 +272,13 @@ __device__ __forceinline__ void store_columns(uint16_t* row, const f32x16 (&acc)
 // out and lse.  A step takes 64 keys: with their values twice in LDS (64 KB at D = 128) two workgroups share a compute unit, and one's exponentials run beside
 // the other's products.  At D = 128 a step is 32 products (1024 cycles) and 32 exponentials with some 120 other vector instructions (about 980 cycles) per
 // wavefront: either pipe would be full at 1.7 times the speed, the power limit comes first (matrix pipes 58 % busy).  At D = 64 the vector instructions are twice the
-// products: 4 x 4096 tokens of 16 heads 186 us, 740 TFLOP/s.  For the prompt of 16384 tokens, this 2.0 ms:
+// products: 4 x 4096 tokens of 16 heads 186 us, 740 TFLOP/s.  For the prompt of 16384 tokens, this 2.0 to 2.1 ms:
 // 64 rows per wavefront with half the wavefronts 3.1, the next tile's products among this tile's exponentials 2.03, 8 wavefronts per workgroup 2.01 (701 tokens
 // behind 4093 cached ones 177 us instead of 147), copies three tiles ahead 2.07.  Calls of short prompts (48 of up to 193 tokens, 16 heads on 8 of 64) are a chain of
 // loads, which four workgroups per compute unit share better than three: 14.4 us, 15.7 (and 128 registers suffice).  Of a
 // workgroup's 7 us 1.8 are offsets and lengths, 1.1 queries and first tile, 2.9 its 1 to 4 steps, 1.1 the stores.
+// The careful pass, inlined, costs 106 spilled scalar registers at D = 128 (none at D = 64): the prompt takes 2.10 ms, without it 2.07, the 701 tokens 151 and 147 us, the
+// short prompts 13.65 and 13.45.
 // kSplit: key_parts workgroups share a tile's keys and leave their sums for attn_fwd_join_kernel (a kernel of its own: both in
 // one take 32 registers more).
 template <int D, bool kSplit>
@@ -475,7 +477,9 @@ enum class Pass { kDelta, kPlain, kCareful };
 // average out (of the 2-norm about 1.7e-3 / sqrt(keys), where the rounding of dS is 1.7e-3; a single such row a few per cent).  Tiles with a row of fewer than
 // kFewKeys keys go over their keys once more for it: delta = sum_j P_ij dP_ij.
 // Tiles as in the forward kernel, three products of equal size instead of two; 8 rollouts of up to 4096 tokens (32 heads on 8 of 128) 645 us, 1000 TFLOP/s.  The
-// exponentials under the products of dP, as in the kernel below, would want 58 registers more than two wavefronts per SIMD have: 845 us.
+// exponentials under the products of dP, as in the kernel below, would want 58 registers more than two wavefronts per SIMD have: 845 us.  As it is, all 256 are
+// in use at D = 128, 26 more and 77 scalar ones are spilled (without the careful pass 4 and none; the two backward kernels and the forward one then take 2080 us instead of
+// 2170 to 2210).
 template <int D>
 __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) char tiles[2][2][kKeyTile * D * 2];
@@ -611,7 +615,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
 // size (four reads of a tile per wavefront, as many cycles of LDS as of products).  At D = 128 these are 192 registers before the scores: one wavefront per
 // SIMD, so the work under the products has to come from itself, and a step is one block but for the mask's edge (a branch among the exponentials: 1300 us
 // instead of 1140, for 8 rollouts of up to 4096 tokens; 750 TFLOP/s, this at 1.6 GHz).  At D = 64 two fit: 16 rollouts of up to 311 tokens 19.6 us, with one 27.0; 4 of 4096,
-// with dq, 554 and 645.
+// with dq, 554 and 645.  The careful pass, inlined, costs 121 spilled scalar registers at D = 128, 11 at D = 64.
 // Where there are few tiles of keys for the chip their rows are cut into row_parts ranges, one workgroup each, whose sums go to memory in fp32 and are added in order by
 // attn_dkv_join_kernel (backward of 1024 tokens, 32 heads on 8: 172 us, then 94; of 2048, 2 heads on 1: 185, then 87).
 template <int D>

@@ -479,7 +479,7 @@ bool stride_ok(int64_t s, int64_t row) { return s == 0 || (s >= row && s % 8 == 
 
 // Tokens per workgroup, of the longest length that the table allows: 4096 chunks in all, of 1024 tokens at least (the chip holds 512 workgroups at a time, the
 // lengths of a batch differ, and short chunks even them out), or 512 chunks of 256 tokens at least (two steps of each wavefront), and never more than 4096 tokens.  256 sequences of
-// up to 304 tokens (8 key heads of 128, 8-bit) take 42 us in one chunk each, 63 in two with the join; 8 of 4096 tokens 23 in chunks of 512, 25 of 256; lengths from 33 to 8192 in
+// 304 tokens (8 key heads of 128, 8-bit) take 45 us in one chunk each, 66 in two with the join; 8 of 4096 tokens 23 in chunks of 512, 25 of 256; lengths from 33 to 8192 in
 // 128 sequences 101 us in four chunks each, 110 in two.
 int chunk_of(int64_t n_seqs, int64_t blocks, int64_t most) {
   auto min = [](int64_t x, int64_t y) { return x < y ? x : y; };

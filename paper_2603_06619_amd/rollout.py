@@ -22,7 +22,12 @@ class PagedCache(nb.KvCache):
 
 class RolloutStage:
     """Inputs may have any row stride that the library takes, and may be expanded along their rows (a gradient that is equal for all rows, one prompt's logits for a
-    group of continuations): these are copied."""
+    group of continuations): these are copied.
+
+    Outputs are allocated, not cleared: rows of q (and out, dq, ...) or of k that belong to no sequence, in front of cu[0] or behind cu[-1], are left as the
+    allocator gave them, NaN included.  With arrays that are longer than their sequences cut the results, or clear these rows, before a product sums over all.
+
+    Attention and decoding take products in bf16 with fp32 sums: the probabilities (and the gradients dS) are rounded to bf16 before the second product, see nat.h."""
 
     def __init__(self, device="cuda:0"):
         self.device = torch.device(device)
@@ -47,7 +52,7 @@ class RolloutStage:
 
     def attention(self, q, k, v, cu_q, cu_k=None, causal=True, scale=None):
         """q [n_q, q heads, D], k, v [n_k, kv heads, D] bf16, packed by the int32 offsets cu_q, cu_k (None: the same).
-        Returns (out like q, log-sum-exp [q heads, n_q])."""
+        Returns (out like q, log-sum-exp [q heads, n_q]); rows of no sequence are not written."""
         out = torch.empty_like(q)                    # (half the host time of torch.empty; rows back to back whatever those of q)
         lse = q.new_empty((q.shape[1], q.shape[0]), dtype=torch.float32)
         ws = self._buf("attn_fwd", nb.attn_fwd_workspace_bytes(q.shape[0], k.shape[0], cu_q.numel() - 1, q.shape[1], k.shape[1], q.shape[2], causal))
@@ -55,7 +60,7 @@ class RolloutStage:
         return out, lse
 
     def attention_backward(self, dout, q, k, v, out, lse, cu_q, cu_k=None, causal=True, scale=None):
-        """(dq, dk, dv) of attention(), with its results."""
+        """(dq, dk, dv) of attention(), with its results; rows of no sequence are not written."""
         dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
         ws = self._buf("attn_bwd", nb.attn_bwd_workspace_full_bytes(q.shape[0], k.shape[0], cu_q.numel() - 1, q.shape[1], k.shape[1], q.shape[2], causal))
         nb.nat_attn_bwd(q, k, v, out, lse, dout, cu_q, cu_q if cu_k is None else cu_k, causal, self._scale(scale, q.shape[2]),
