@@ -593,6 +593,8 @@ __device__ __forceinline__ void sum_parts(const Row<T>& row, int w, const Settin
   const int lane = threadIdx.x & 63;
   uint64_t all = 0, n = 0;
   double soft = 0.0;
+  // In fp32, summed in fp64: the exponent's rounding is an error of 2^-24 |exponent| of a term, of either sign, so log-probs have one of 3e-8 to 5e-8 (in the weights' 40
+  // bits, as at temperature 1, 2e-8, which is their own rounding; the weights would be computed twice)
   auto add_soft = [&](const Vector& x) {
     if constexpr (kSoft) {
 #pragma unroll
