@@ -15,7 +15,7 @@ def _visible(n_q, n_k, causal):
 
 
 def probabilities(q, k, scale, visible):
-    """P [a, b] and the log-sum-exp [a] of the visible scores; a row that sees nothing has P = 0 and -inf.  Masked places are
+    """P [a, b] and the log-sum-exp [a] of the visible scores; a row that sees nothing has P = 0 and -inf, one that sees a score of NaN has NaN.  Masked places are
     never touched by what q and k hold there."""
     with np.errstate(invalid="ignore", over="ignore"):
         s = np.where(visible, (q @ k.T) * scale, -np.inf)
@@ -24,8 +24,8 @@ def probabilities(q, k, scale, visible):
     e = np.where(visible, np.exp(s - safe[:, None]), 0.0)
     total = e.sum(axis=1)
     with np.errstate(divide="ignore"):
-        lse = np.where(total > 0, safe + np.log(total), -np.inf)
-    return e / np.where(total > 0, total, 1.0)[:, None], lse, s
+        lse = np.where(total == 0, -np.inf, safe + np.log(total))
+    return e / np.where(total == 0, 1.0, total)[:, None], lse, s
 
 
 def _masked_matmul(p, x, visible):
