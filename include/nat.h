@@ -10,7 +10,8 @@
  * In the model body: nat_attn_fwd / nat_attn_bwd (attention over the packed sequences of
  * nat_prefix_pack).  Where the rollouts are written: nat_sample (the next token and its
  * behaviour log-prob), nat_kv_write / nat_kv_read / nat_attn_decode (a paged key-value cache
- * and attention of one new token over it).
+ * and attention of one new token over it), nat_kv_reserve / nat_kv_release (its pages).  Between token ids and attention:
+ * nat_embed / nat_embed_bwd, nat_qk_norm_rope / nat_qk_norm_rope_bwd.
  *
  * Notation follows the paper: P prompts, G rollouts per prompt, B = P*G
  * rollouts, T_i response length of rollout i, t = 1..T_i token position,
@@ -470,13 +471,16 @@ nat_status nat_attn_bwd(const nat_attn_params* params, const void* d_q, const vo
 /*
  * A paged key-value cache, owned by the caller.  Token t of a sequence lies in page block_table[t / page_size]
  * at place t % page_size; slot = page * page_size + place.
- *   d_k, d_v     [n_pages, n_kv_heads, page_size, head_dim] in `format`: NAT_KV_BF16, or NAT_KV_FP8: 8 bits with 4
- *                exponent and 3 mantissa bits (largest value 448, no infinities);
- *   d_k_exp, d_v_exp [n_pages, n_kv_heads, page_size] uint8, NAT_KV_FP8 only: row (token, head) stands for its
- *                8-bit values times 2^(exp - 127);
+ *   d_k, d_v     [n_pages, n_kv_heads, page_size, head_dim] in `format`: NAT_KV_BF16, NAT_KV_FP8: 8 bits with 4
+ *                exponent and 3 mantissa bits (largest value 448, no infinities), or NAT_KV_FP4: 4 bits with 2 exponent
+ *                bits and 1 mantissa bit (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives as codes 0..7 and 8..15), two
+ *                elements to a byte, the first in its low half;
+ *   d_k_exp, d_v_exp NAT_KV_FP8: [n_pages, n_kv_heads, page_size] uint8, row (token, head) stands for its 8-bit values
+ *                times 2^(exp - 127);  NAT_KV_FP4: [n_pages, n_kv_heads, page_size, head_dim / 32] uint8, the same for each
+ *                group of 32 elements of a row (255: all of the group is NaN);  NAT_KV_BF16: not used;
  *   page_size    16, 32, 64, 128 or 256;  head_dim 64 or 128.  All four arrays 16-byte aligned.
  */
-enum { NAT_KV_BF16 = 0, NAT_KV_FP8 = 1 };
+enum { NAT_KV_BF16 = 0, NAT_KV_FP8 = 1, NAT_KV_FP4 = 4 };
 typedef struct nat_kv_cache {
   void *d_k, *d_v;
   uint8_t *d_k_exp, *d_v_exp;
@@ -490,6 +494,9 @@ typedef struct nat_kv_cache {
  *                of padding) are skipped; the other slots must differ from one another.
  * NAT_KV_FP8: the exponent of a row is the smallest e >= -126 with max |x| <= 448 * 2^e over its finite elements, and
  * its values are x / 2^e rounded to nearest, ties to even; elements that are not finite are stored as NaN.
+ * NAT_KV_FP4: the same for each group of 32 elements with the smallest e of -125 .. 125 for which max |x| <= 6 * 2^e (with 125 elements
+ * beyond it become +-6 * 2^125, which bf16 still holds); halfway the even code, and the sign stays where a value rounds to zero; a
+ * group with an element that is not finite is stored as exponent 255.
  * Errors: NULL or misaligned pointer, negative count, n_pages <= 0 -> NAT_INVALID_ARG; page_size, head_dim, heads or stride
  * out of range -> NAT_BAD_SHAPE; format -> NAT_UNSUPPORTED_DTYPE.
  */
@@ -501,7 +508,7 @@ nat_status nat_kv_write(const nat_kv_cache* cache, const void* d_k, int64_t k_st
  *   d_block_table [n_seqs, table_width] int32;  d_cu_k [n_seqs+1] int32 row offsets of the output;
  *   d_k, d_v     [n_rows, n_kv_heads, head_dim] out: row cu_k[b] + t is token t of sequence b.  Tokens beyond the
  *                table's width or with a page outside [0, n_pages) are zeros; rows of no sequence are not written.
- * Reading back is exact as far as bf16 goes: 3 mantissa bits and a power of two.  Errors as nat_kv_write.
+ * Reading back is exact as far as bf16 goes: 3 mantissa bits (or 1) and a power of two.  Errors as nat_kv_write.
  */
 nat_status nat_kv_read(const nat_kv_cache* cache, const int32_t* d_block_table, int32_t table_width,
                        const int32_t* d_cu_k, int32_t n_seqs, int64_t n_rows, void* d_k, int64_t k_stride,
@@ -526,6 +533,120 @@ size_t nat_attn_decode_workspace_bytes(int32_t n_seqs, int32_t n_q_heads, int32_
 nat_status nat_attn_decode(const nat_kv_cache* cache, const void* d_q, int64_t q_stride, int32_t n_seqs, int32_t n_q_heads,
                            const int32_t* d_block_table, int32_t table_width, const int32_t* d_seq_lens, float scale,
                            void* d_out, int64_t out_stride, float* d_lse, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Norms of queries and keys, head by head, and their rotation by position, in one pass: what a body does between its projections
+ * and nat_attn_fwd, nat_kv_write or nat_attn_decode.  For each row and head, with D = head_dim, R = rotary_dim, f_i = d_inv_freq[i]:
+ *     n_i = x_i w_i / sqrt(mean_j x_j^2 + eps)                                     (without a weight: n = x)
+ *     (n_a, n_b) -> (n_a cos t - n_b sin t, n_b cos t + n_a sin t),  t = position f_i,  for the R / 2 pairs of the first R elements:
+ *     a = i, b = i + R / 2, or (interleaved) a = 2 i, b = 2 i + 1.  The other elements stay n.
+ *   dtype        NAT_DTYPE_BF16 or NAT_DTYPE_F32, of rows, weights and results;  head_dim 64 or 128;
+ *   n_q_heads, n_kv_heads 1 .. 4096, in any ratio;  rotary_dim a multiple of 16 up to head_dim, or 0: no rotation;
+ *   interleaved  0 or 1;  eps > 0 and finite;  n_rows below 2^31;
+ *   *_stride     elements from row to row, a multiple of 8 (bf16) or 4 (f32), at least heads * head_dim; 0 = exactly that.
+ *   d_q [n_rows, n_q_heads, D], d_k [n_rows, n_kv_heads, D];  d_q_weight, d_k_weight [D], each NULL for no norm;
+ *   d_position_ids [n_rows] int32 (of nat_prefix_pack or nat_kv_reserve), NULL exactly if rotary_dim is 0;
+ *   d_inv_freq   [R / 2] double, angle per position in radians; the angle is formed in turns in 64 bits, so far positions
+ *                lose nothing;
+ *   d_q_out, d_k_out like d_q, d_k: may be the inputs themselves with the same stride, otherwise must not overlap them.
+ * Everything in between is held in fp32 and rounded once.  Errors: NULL pointer (but the optional ones), count, eps or flag out
+ * of range, pointers (of rows and weights) not 16-byte aligned -> NAT_INVALID_ARG; head counts, head_dim, rotary_dim or stride out
+ * of range -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE.  n_rows = 0 is valid.
+ */
+typedef struct nat_qk_params {
+  int32_t n_q_heads, n_kv_heads, head_dim, dtype, rotary_dim, interleaved;
+  float eps;
+  int64_t n_rows;
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+  int64_t dq_stride, dk_stride;                              /* nat_qk_norm_rope_bwd */
+} nat_qk_params;
+nat_status nat_qk_norm_rope(const nat_qk_params* params, const void* d_q, const void* d_k, const void* d_q_weight,
+                            const void* d_k_weight, const int32_t* d_position_ids, const double* d_inv_freq, void* d_q_out,
+                            void* d_k_out, void* stream);
+
+/*
+ * Its gradients, with dn the gradient at n (the results' gradient rotated by -t) and r = 1 / sqrt(mean x^2 + eps):
+ *     dw_i = sum over rows and heads of dn_i x_i r;   dx_i = r (dn_i w_i - x_i r^2 mean_j(dn_j w_j x_j)),  dx = dn without a weight.
+ *   d_q, d_k     the inputs of nat_qk_norm_rope (not its results);
+ *   d_dq_out, d_dk_out gradients of its results (strides q_out_stride, k_out_stride);
+ *   d_dq, d_dk   out (strides dq_stride, dk_stride); may be d_dq_out, d_dk_out with the same stride;
+ *   d_dq_weight, d_dk_weight [D] float out, NULL exactly if there is no such weight: overwritten, or added to when accumulate != 0;
+ *   d_ws / ws_bytes: at least nat_qk_norm_rope_bwd_workspace_bytes, 256-byte aligned (0 without weights).
+ * No atomics: results do not change from run to run.  With n_rows = 0 the weights' gradients are zeros (or stay).  Errors as
+ * nat_qk_norm_rope, plus NAT_WORKSPACE_TOO_SMALL.
+ */
+size_t nat_qk_norm_rope_bwd_workspace_bytes(int64_t n_rows, int32_t head_dim);
+nat_status nat_qk_norm_rope_bwd(const nat_qk_params* params, const void* d_q, const void* d_k, const void* d_q_weight,
+                                const void* d_k_weight, const int32_t* d_position_ids, const double* d_inv_freq,
+                                const void* d_dq_out, const void* d_dk_out, void* d_dq, void* d_dk, float* d_dq_weight,
+                                float* d_dk_weight, int32_t accumulate, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Token ids into rows of the body: out_r = scale * E[ids[r]], one rounding; an id outside [0, V) gives a row of zeros.
+ *   d_ids [n_rows] int32;  d_E [V, H] row-major, bf16 or f32;  d_out [n_rows, H], same dtype, out_stride elements from row to
+ *   row (0 = H).  E, out and out_stride in multiples of 16 bytes, as are rows.
+ * Errors: NULL or misaligned pointer, n_rows outside [0, 2^31), scale not finite -> NAT_INVALID_ARG; V <= 0, H <= 0, a row that is not a
+ * multiple of 16 bytes, a stride below H -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE.
+ */
+nat_status nat_embed(const int32_t* d_ids, int64_t n_rows, const void* d_E, int32_t V, int32_t H, int32_t dtype, float scale,
+                     void* d_out, int64_t out_stride, void* stream);
+
+/*
+ * Its gradient: dE_v = scale * sum over the rows r with ids[r] = v of dout_r.
+ *   d_dout [n_rows, H] in dtype (bf16 or f32), dout_stride elements from row to row (0 = H);
+ *   d_dE [V, H] float: overwritten (zeros where no row has the id), or added to when accumulate != 0, as d_dW of nat_loss_fwd_bwd: with
+ *                tied weights both go into one array.  Ids outside [0, V) add nothing.
+ *   d_ws / ws_bytes: at least nat_embed_bwd_workspace_bytes, 256-byte aligned.
+ * Ids are sorted on the device, rows of one id staying in order, and a row of dE is a sum in fp32 whose order depends on the ids
+ * alone: results do not change from run to run.  No atomics on floats.
+ * Errors as nat_embed, plus V > 2^30, n_rows >= 2^29 -> NAT_BAD_SHAPE, NAT_WORKSPACE_TOO_SMALL.  With n_rows = 0 dE is zeros, or stays.
+ */
+size_t nat_embed_bwd_workspace_bytes(int64_t n_rows, int32_t V, int32_t H);
+nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const void* d_dout, int64_t dout_stride, int32_t V, int32_t H,
+                         int32_t dtype, float scale, float* d_dE, int32_t accumulate, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Pages of a cache for new tokens, and where each of these goes.  Free pages are a stack: d_free_pages[0 .. n_free - 1], taken from
+ * the end.  Sequence i has len_i tokens (d_seq_lens) and wants new_i more; that takes need_i = ceil((len_i + new_i) / page_size)
+ * - ceil(len_i / page_size) pages.  A sequence is refused if its tokens do not fit its row of the table, its rows do not fit rows_cap,
+ * or need_i > 0 and the needs of the sequences 0 .. i together (without those of the sequences refused for the other reasons) are
+ * more than n_free.  The others get their pages in order of sequence and place: the next from the end of the stack into
+ * block_table[i][ceil(len_i / page_size)], and so on.
+ *   d_block_table [n_seqs, table_width] int32: only the new pages' places are written;
+ *   d_seq_lens, d_new_lens [n_seqs] int32 (lengths clamped to what the table holds, negative ones to 0);  page_size a power of two,
+ *                16 to 256;
+ *   d_free_pages [n_pages] int32, only read;  d_counts [1 or more] int32: n_free (clamped to [0, n_pages]);
+ *   d_counts_out [2] int32 out: pages that are left, sequences refused;  d_seq_lens_out [n_seqs] int32 out: len_i + new_i, or len_i if
+ *                refused.  Both may be the inputs themselves;
+ *   d_start      [n_seqs] int32 out: len_i, or -1 if refused;
+ *   d_cu_new     [n_seqs + 1] int32 out: offsets of the new tokens' rows, refused ones included (a step's rows keep their places; offsets
+ *                that do not fit 31 bits are 2^31 - 1);
+ *   d_slots      [rows_cap] int64 out: slot of row cu_new[i] + j, for nat_kv_write: -1 for refused sequences, for pages outside
+ *                [0, n_pages) and behind the last row;  d_position_ids [rows_cap] int32 out or NULL: len_i + j (0 behind the last row);
+ *   d_ws / ws_bytes: at least nat_kv_reserve_workspace_bytes, 256-byte aligned.
+ * Errors: NULL pointer, n_seqs < 0, rows_cap outside [0, 2^31), n_pages < 0, table_width < 0 -> NAT_INVALID_ARG; page_size, n_seqs > 2^24,
+ * table_width * page_size >= 2^31 -> NAT_BAD_SHAPE; NAT_WORKSPACE_TOO_SMALL.
+ */
+size_t nat_kv_reserve_workspace_bytes(int32_t n_seqs);
+nat_status nat_kv_reserve(int32_t* d_block_table, int32_t table_width, int32_t n_seqs, int32_t page_size, const int32_t* d_seq_lens,
+                          const int32_t* d_new_lens, const int32_t* d_free_pages, int32_t n_pages, const int32_t* d_counts,
+                          int64_t rows_cap, int32_t* d_counts_out, int32_t* d_seq_lens_out, int32_t* d_start, int32_t* d_cu_new,
+                          int64_t* d_slots, int32_t* d_position_ids, void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Pages back onto the stack: sequence i keeps its first min(len_i, keep_i) tokens (keep_i = 0: it has ended), and the pages at
+ * places ceil(kept / page_size) .. ceil(len_i / page_size) - 1 of its row go to d_free_pages[n_free], d_free_pages[n_free + 1], ... in order of
+ * sequence and place.  Entries outside [0, n_pages) do not go back, nor does what the stack has no room for (it holds n_pages).
+ * The table stays as it is: entries behind a sequence's length have no meaning.
+ *   d_keep_lens  [n_seqs] int32 (negative: 0);  d_counts_out [2] int32 out: free pages, and 0;  d_seq_lens_out [n_seqs] int32 out:
+ *                what is kept.  Both may be the inputs themselves.  d_ws: nat_kv_release_workspace_bytes, 256-byte aligned.
+ * Errors as nat_kv_reserve.
+ */
+size_t nat_kv_release_workspace_bytes(int32_t n_seqs);
+nat_status nat_kv_release(const int32_t* d_block_table, int32_t table_width, int32_t n_seqs, int32_t page_size,
+                          const int32_t* d_seq_lens, const int32_t* d_keep_lens, int32_t* d_free_pages, int32_t n_pages,
+                          const int32_t* d_counts, int32_t* d_counts_out, int32_t* d_seq_lens_out, void* d_ws, size_t ws_bytes,
+                          void* stream);
 
 /*
  * Draw the next token of every row from its logits (Sec. 2: the rollouts o_i ~ pi_theta_old).

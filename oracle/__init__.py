@@ -17,7 +17,10 @@ Modules
            (Eq. 3), sequence-mean objective (Eq. 5) and its gradient w.r.t.
            hidden states and the LM-head matrix (App. A)
   attention  attention over packed sequences, its gradients, attention of one token over a paged cache
-  kv_cache   the 8-bit format of cached rows
+  kv_cache   the 8-bit and 4-bit formats of cached rows
+  heads      norms and rotation of queries and keys, and their gradients
+  embedding  rows by token id, and the embedding's gradient
+  pages      block tables and slots of a paged cache
   sampling   temperature, top-k, top-p, min-p and the draw, in whole numbers
   drivers  exhaustive-enumeration and Monte-Carlo expectations of the masked
            estimator (Prop. 1), and the closed-form variances (App. B)

@@ -12,7 +12,7 @@ _lib = None
 FULL, URS, RPC, DET = 0, 1, 2, 3
 DTYPE_F32, DTYPE_BF16 = 0, 1
 KL_LOG_RATIO, KL_NONNEG = 0, 1
-KV_BF16, KV_FP8 = 0, 1
+KV_BF16, KV_FP8, KV_FP4 = 0, 1, 4
 DIAG_BAD_ID, DIAG_SHIFT_RANGE, DIAG_CLIPPED, DIAG_NONZERO_ADV, DIAG_WORDS = 0, 1, 2, 3, 4
 
 
@@ -39,6 +39,12 @@ class _CAttnParams(ctypes.Structure):
 class _CKvCache(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("d_k", "d_v", "d_k_exp", "d_v_exp")] + \
                [(n, ctypes.c_int32) for n in ("n_pages", "n_kv_heads", "page_size", "head_dim", "format")]
+
+
+class _CQkParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "dtype", "rotary_dim", "interleaved")] + \
+               [("eps", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("n_rows", "q_stride", "k_stride", "q_out_stride", "k_out_stride", "dq_stride", "dk_stride")]
 
 
 class SelectParams:
@@ -138,6 +144,26 @@ def load_library():
     lib.nat_attn_decode_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
     lib.nat_attn_decode.restype = i32
     lib.nat_attn_decode.argtypes = [pc, vp, i64, i32, i32, vp, i32, vp, f32, vp, i64, vp, vp, sz, vp]
+    pq = ctypes.POINTER(_CQkParams)
+    lib.nat_qk_norm_rope.restype = i32
+    lib.nat_qk_norm_rope.argtypes = [pq, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.nat_qk_norm_rope_bwd_workspace_bytes.restype = sz
+    lib.nat_qk_norm_rope_bwd_workspace_bytes.argtypes = [i64, i32]
+    lib.nat_qk_norm_rope_bwd.restype = i32
+    lib.nat_qk_norm_rope_bwd.argtypes = [pq, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+    lib.nat_embed.restype = i32
+    lib.nat_embed.argtypes = [vp, i64, vp, i32, i32, i32, f32, vp, i64, vp]
+    lib.nat_embed_bwd_workspace_bytes.restype = sz
+    lib.nat_embed_bwd_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.nat_embed_bwd.restype = i32
+    lib.nat_embed_bwd.argtypes = [vp, i64, vp, i64, i32, i32, i32, f32, vp, i32, vp, sz, vp]
+    for name in ("nat_kv_reserve_workspace_bytes", "nat_kv_release_workspace_bytes"):
+        getattr(lib, name).restype = sz
+        getattr(lib, name).argtypes = [i32]
+    lib.nat_kv_reserve.restype = i32
+    lib.nat_kv_reserve.argtypes = [vp, i32, i32, i32, vp, vp, vp, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.nat_kv_release.restype = i32
+    lib.nat_kv_release.argtypes = [vp, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     lib.nat_sample.restype = i32
     lib.nat_sample.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.nat_sample_workspace_bytes.restype = sz
@@ -433,27 +459,29 @@ def nat_attn_bwd(q, k, v, out, lse, dout, cu_q, cu_k, causal, scale, dq, dk, dv,
 
 class KvCache:
     """The arrays of a paged cache: k, v [n_pages, kv heads, page_size, D] in bfloat16, or in float8_e4m3fn with the exponents
-    k_exp, v_exp [n_pages, kv heads, page_size] uint8 (see nat_kv_cache in nat.h)."""
+    k_exp, v_exp [n_pages, kv heads, page_size] uint8, or, in 4 bits, k, v [.., page_size, D / 2] and k_exp, v_exp [.., page_size, D / 32] uint8
+    (see nat_kv_cache in nat.h)."""
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
         shape, dtype = k.shape, k.dtype
-        fp8 = dtype == torch.float8_e4m3fn
-        if len(shape) != 4 or not (fp8 or dtype == torch.bfloat16):
-            raise TypeError("k: expected a bfloat16 or float8_e4m3fn tensor [n_pages, heads, page_size, head_dim]")
+        fp8, fp4 = dtype == torch.float8_e4m3fn, dtype == torch.uint8
+        if len(shape) != 4 or not (fp8 or fp4 or dtype == torch.bfloat16):
+            raise TypeError("k: expected a bfloat16 or float8_e4m3fn tensor [n_pages, heads, page_size, head_dim], or a uint8 tensor [.., head_dim / 2]")
         if not (k.is_contiguous() and k.is_cuda):
             raise TypeError(f"k: expected a contiguous {dtype} device tensor {tuple(shape)}")
         if v.shape != shape or v.dtype != dtype or not v.is_contiguous() or not v.is_cuda:
             raise TypeError(f"v: expected a contiguous {dtype} device tensor {tuple(shape)}")
-        if fp8:
-            rows = shape[:3]
+        if fp8 or fp4:
+            rows = shape[:3] if fp8 else (*shape[:3], shape[3] // 16)
             for t in (k_exp, v_exp):
                 if t is None or t.shape != rows or t.dtype != torch.uint8 or not t.is_contiguous() or not t.is_cuda:
                     raise TypeError(f"{'k_exp' if t is k_exp else 'v_exp'}: expected a contiguous uint8 device tensor {tuple(rows)}")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         n_pages, heads, page_size, dim = shape
+        dim *= 2 if fp4 else 1
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = n_pages, heads, page_size, dim
-        self._c = _CKvCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if fp8 else None, v_exp.data_ptr() if fp8 else None,
-                            n_pages, heads, page_size, dim, KV_FP8 if fp8 else KV_BF16)
+        self._c = _CKvCache(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if fp8 or fp4 else None,
+                            v_exp.data_ptr() if fp8 or fp4 else None, n_pages, heads, page_size, dim, KV_FP8 if fp8 else KV_FP4 if fp4 else KV_BF16)
 
 
 def nat_kv_write(cache, k, v, slots):
@@ -524,6 +552,136 @@ def nat_sample(logits, random, temperature, top_k, top_p, min_p, ids_out, logp_o
         _vector(ids_out, torch.int32, n, "ids_out"), _vector(logp_out, torch.float32, n, "logp_out"),
         _vector(logq_out, torch.float32, n, "logq_out"), _ptr(workspace),
         workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_sample")
+
+
+def _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, q_name="q", k_name="k"):
+    if q.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{q_name} must be float32 or bfloat16")
+    n, hq, dim = q.shape
+    (q, k), (q_stride, k_stride) = _own_rows((q, k), (_rows(q, q_name, dtype=q.dtype, is_input=True), _rows(k, k_name, (n, k.shape[1], dim), q.dtype, True)))
+    rotary = 0
+    if (position_ids is None) != (inv_freq is None):
+        raise TypeError("position_ids and inv_freq go together")
+    if inv_freq is not None:
+        rotary = 2 * inv_freq.numel()
+        _vector(position_ids, torch.int32, n, "position_ids")
+        _vector(inv_freq, torch.float64, rotary // 2, "inv_freq")
+    _vector(q_weight, q.dtype, dim, "q_weight")
+    _vector(k_weight, q.dtype, dim, "k_weight")
+    return _CQkParams(hq, k.shape[1], dim, _dtype_code(q), rotary, int(interleaved), float(eps), n, q_stride, k_stride), q, k
+
+
+def nat_qk_norm_rope(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, q_out, k_out):
+    """q [rows, q heads, D], k [rows, kv heads, D] bfloat16 or float32 (any row stride); weights [D] of the same type, each or None; position_ids int32 [rows]
+    and inv_freq float64 [R / 2], or both None; q_out, k_out like q, k, or q, k themselves."""
+    p, q, k = _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
+    p.q_out_stride, p.k_out_stride = _rows(q_out, "q_out", q.shape, q.dtype), _rows(k_out, "k_out", k.shape, q.dtype)
+    _raise(load_library().nat_qk_norm_rope(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(position_ids), _ptr(inv_freq),
+                                           _ptr(q_out), _ptr(k_out), _stream()), "nat_qk_norm_rope")
+
+
+def qk_norm_rope_bwd_workspace_bytes(n_rows, head_dim):
+    return int(load_library().nat_qk_norm_rope_bwd_workspace_bytes(int(n_rows), int(head_dim)))
+
+
+def nat_qk_norm_rope_bwd(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, dq_out, dk_out, dq, dk, dq_weight, dk_weight, accumulate,
+                         workspace):
+    """The gradients of nat_qk_norm_rope: dq_out, dk_out of its results; dq, dk like q, k (or dq_out, dk_out themselves); dq_weight, dk_weight float32 [D], None
+    where there is no weight."""
+    p, q, k = _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
+    (dq_out, dk_out), (p.q_out_stride, p.k_out_stride) = _own_rows((dq_out, dk_out), (_rows(dq_out, "dq_out", q.shape, q.dtype, True),
+                                                                                      _rows(dk_out, "dk_out", k.shape, q.dtype, True)))
+    p.dq_stride, p.dk_stride = _rows(dq, "dq", q.shape, q.dtype), _rows(dk, "dk", k.shape, q.dtype)
+    _raise(load_library().nat_qk_norm_rope_bwd(
+        ctypes.byref(p), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(position_ids), _ptr(inv_freq), _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk),
+        _vector(dq_weight, torch.float32, p.head_dim, "dq_weight"), _vector(dk_weight, torch.float32, p.head_dim, "dk_weight"), int(bool(accumulate)),
+        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_qk_norm_rope_bwd")
+
+
+def _matrix(t, name, rows=None, cols=None, dtype=None, is_input=False):
+    """A [rows, H] tensor with contiguous rows; returns its row stride (0: back to back, _SHARED: an input with one row for all)."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in ((dtype,) if dtype else (torch.float32, torch.bfloat16)):
+        raise TypeError(f"{name}: expected a {dtype or 'float32 or bfloat16'} device tensor [rows, columns]")
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{name}: expected shape {(rows, cols)}, got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return 0
+    n, H = t.shape
+    row, one = t.stride()
+    if n == 0 or H == 0:
+        return 0
+    if is_input and n > 1 and row == 0:
+        return _SHARED
+    if H > 1 and one != 1:
+        raise ValueError(f"{name}: its rows must be contiguous")
+    if n > 1 and row < H:
+        raise ValueError(f"{name}: its rows overlap in memory")
+    return row if n > 1 else 0
+
+
+def nat_embed(ids, E, scale, out):
+    """ids int32 [rows], E [V, H] bfloat16 or float32, contiguous; out [rows, H] like E (any row stride)."""
+    if _matrix(E, "E") != 0:
+        raise ValueError("E: expected a contiguous tensor")
+    V, H = E.shape
+    n = ids.numel()
+    _raise(load_library().nat_embed(_vector(ids, torch.int32, n, "ids"), n, _ptr(E), V, H, _dtype_code(E), float(scale), _ptr(out),
+                                    _matrix(out, "out", n, H, E.dtype), _stream()), "nat_embed")
+
+
+@functools.lru_cache(maxsize=256)
+def embed_bwd_workspace_bytes(n_rows, V, H):
+    return int(load_library().nat_embed_bwd_workspace_bytes(int(n_rows), int(V), int(H)))
+
+
+def nat_embed_bwd(ids, dout, scale, dE, accumulate, workspace):
+    """ids int32 [rows], dout [rows, H] bfloat16 or float32 (any row stride); dE float32 [V, H], contiguous: overwritten, or added to."""
+    n = ids.numel()
+    if _matrix(dE, "dE", dtype=torch.float32) != 0:
+        raise ValueError("dE: expected a contiguous tensor")
+    V, H = dE.shape
+    (dout,), (stride,) = _own_rows((dout,), (_matrix(dout, "dout", n, H, is_input=True),))
+    _raise(load_library().nat_embed_bwd(_vector(ids, torch.int32, n, "ids"), n, _ptr(dout), stride, V, H, _dtype_code(dout), float(scale), _ptr(dE),
+                                        int(bool(accumulate)), _ptr(workspace),
+                                        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_embed_bwd")
+
+
+def kv_reserve_workspace_bytes(n_seqs):
+    return int(load_library().nat_kv_reserve_workspace_bytes(int(n_seqs)))
+
+
+def kv_release_workspace_bytes(n_seqs):
+    return int(load_library().nat_kv_release_workspace_bytes(int(n_seqs)))
+
+
+def _counts(t, name):
+    if t.dtype != torch.int32 or not t.is_cuda or t.numel() < 2 or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous int32 device tensor of 2 elements")
+    return t.data_ptr()
+
+
+def nat_kv_reserve(block_table, seq_lens, new_lens, free_pages, counts, page_size, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, workspace):
+    """block_table int32 [n_seqs, pages], free_pages int32 [n_pages], counts int32 [2] (free pages, sequences refused); seq_lens, new_lens int32 [n_seqs]. Out:
+    counts_out, seq_lens_out (may be counts, seq_lens), start int32 [n_seqs], cu_new int32 [n_seqs + 1], slots int64 and position_ids int32 (or None) [rows_cap]."""
+    n = seq_lens.numel()
+    width, i32, rows = _table(block_table, n), torch.int32, int(rows_cap)
+    _raise(load_library().nat_kv_reserve(
+        _ptr(block_table), width, n, int(page_size), _vector(seq_lens, i32, n, "seq_lens"), _vector(new_lens, i32, n, "new_lens"),
+        _vector(free_pages, i32, free_pages.numel(), "free_pages"), free_pages.numel(), _counts(counts, "counts"), rows, _counts(counts_out, "counts_out"),
+        _vector(seq_lens_out, i32, n, "seq_lens_out"), _vector(start, i32, n, "start"), _vector(cu_new, i32, n + 1, "cu_new"),
+        _vector(slots, torch.int64, rows, "slots"), _vector(position_ids, i32, rows, "position_ids"), _ptr(workspace),
+        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_kv_reserve")
+
+
+def nat_kv_release(block_table, seq_lens, keep_lens, free_pages, counts, page_size, counts_out, seq_lens_out, workspace):
+    """Arguments as nat_kv_reserve's; keep_lens int32 [n_seqs]: the tokens that stay.  free_pages is written behind its first counts[0] entries."""
+    n = seq_lens.numel()
+    width, i32 = _table(block_table, n), torch.int32
+    _raise(load_library().nat_kv_release(
+        _ptr(block_table), width, n, int(page_size), _vector(seq_lens, i32, n, "seq_lens"), _vector(keep_lens, i32, n, "keep_lens"),
+        _vector(free_pages, i32, free_pages.numel(), "free_pages"), free_pages.numel(), _counts(counts, "counts"), _counts(counts_out, "counts_out"),
+        _vector(seq_lens_out, i32, n, "seq_lens_out"), _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()),
+        "nat_kv_release")
 
 
 def probe_mfma_scratch_bytes():

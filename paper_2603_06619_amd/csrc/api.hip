@@ -15,7 +15,7 @@ std::vector<EventPair> g_prof_records;
 const char* const kClassNames[PC_NUM] = {
     "advantage", "select", "compact", "gather", "transpose", "logits_gemm", "token_stats",
     "dhidden_gemm", "dweight_gemm", "loss_reduce", "f32_path", "fill", "schedule", "prefix_pack",
-    "attn_fwd", "attn_bwd", "kv_cache", "attn_decode", "sample"};
+    "attn_fwd", "attn_bwd", "kv_cache", "attn_decode", "sample", "qk_norm_rope", "embed", "pages"};
 }  // namespace
 
 ProfScope::ProfScope(int cls, hipStream_t s, bool enabled) : cls_(cls), s_(s), rec_(nullptr) {

@@ -1,0 +1,431 @@
+// Norms of queries and keys, head by head, and their rotation by position, in one pass over the rows, and the gradients of both.
+//
+// A head's D elements lie in D / 16 lanes, two chunks of 8 elements each: of the R elements that turn, lane c has chunks c and c + R / 16, so that both elements
+// of a pair (i, i + R / 2) are its own, and pairs of neighbours are anyway.  The R / 2 sines and cosines of a row are formed by a lane each and go to all heads of the
+// row through LDS: a wavefront takes whole rows.
+#include "nat_internal.h"
+#include "mfma_tile.hip.h"
+
+#include <type_traits>
+
+namespace nat {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr int kWaves = 4;                 // per workgroup
+
+struct HeadsArgs {
+  const void *q, *k, *wq, *wk, *dq_out, *dk_out;
+  void *q_out, *k_out;                    // forward: results; backward: gradients
+  const int32_t* pos;
+  const double* freq;
+  float* part;                            // backward: [workgroups][2][D]
+  int hq, heads, turning, interleaved;    // heads: of queries and keys; turning: lanes of a head whose elements turn, R / 16
+  float eps;
+  int64_t n_rows, q_stride, k_stride, q_out_stride, k_out_stride, dq_stride, dk_stride;
+};
+
+// 8 elements as they lie in memory
+template <typename T> struct Chunk;
+template <>
+struct Chunk<uint16_t> {
+  u32x4 x;
+  __device__ __forceinline__ static Chunk load(const uint16_t* p) { return {*(const u32x4*)p}; }
+  __device__ __forceinline__ static Chunk all(float v) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, v) >> 16;
+    return {u32x4{1, 1, 1, 1} * (b | b << 16)};
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __builtin_bit_cast(float, x[i] << 16);
+      v[2 * i + 1] = __builtin_bit_cast(float, x[i] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ static void store(uint16_t* p, const float (&v)[8]) {
+    bf16x8 y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = (__bf16)v[i];
+    *(bf16x8*)p = y;
+  }
+  __device__ __forceinline__ static Chunk pick(bool a, const Chunk& p, const Chunk& q) {
+    Chunk r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.x[i] = a ? p.x[i] : q.x[i];
+    return r;
+  }
+};
+template <>
+struct Chunk<float> {
+  f32x4 x, y;
+  __device__ __forceinline__ static Chunk load(const float* p) { return {*(const f32x4*)p, *(const f32x4*)(p + 4)}; }
+  __device__ __forceinline__ static Chunk all(float v) { return {f32x4{v, v, v, v}, f32x4{v, v, v, v}}; }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = x[i];
+      v[4 + i] = y[i];
+    }
+  }
+  __device__ __forceinline__ static void store(float* p, const float (&v)[8]) {
+    *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+    *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+  }
+  __device__ __forceinline__ static Chunk pick(bool a, const Chunk& p, const Chunk& q) {
+    Chunk r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      r.x[i] = a ? p.x[i] : q.x[i];
+      r.y[i] = a ? p.y[i] : q.y[i];
+    }
+    return r;
+  }
+};
+
+// over the D / 16 lanes of a head (8 or 4, neighbours); all of them get it
+template <int D>
+__device__ __forceinline__ float sum_of_head(float x) {
+  auto dpp = [](float v, auto ctrl) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  x += dpp(x, std::integral_constant<int, 0xb1>{});           // lane ^ 1
+  x += dpp(x, std::integral_constant<int, 0x4e>{});           // lane ^ 2
+  if constexpr (D == 128) x += dpp(x, std::integral_constant<int, 0x141>{});      // lane ^ 7, of equal fours: as lane ^ 4
+  return x;
+}
+
+// What a lane is in its head, and the row's angles.
+template <int D>
+struct Lane {
+  static constexpr int kLanes = D / 16, kHeads = 64 / kLanes;         // lanes per head, heads per step of a wavefront
+  int head, at[2], angle[2];      // place of the first element of its two chunks; first angle of each (interleaved: 4 each, else 8 from angle[0])
+  bool turns;
+  __device__ __forceinline__ Lane(const HeadsArgs& a, int lane) {
+    const int c = lane % kLanes, n = a.turning;
+    head = lane / kLanes;
+    turns = c < n;
+    at[0] = 8 * (turns ? c : 2 * n + 2 * (c - n));
+    at[1] = 8 * (turns ? c + n : 2 * n + 2 * (c - n) + 1);
+    angle[0] = turns ? (a.interleaved ? 4 * c : 8 * c) : 0;
+    angle[1] = turns ? (a.interleaved ? 4 * (c + n) : 8 * c + 4) : 0;
+  }
+};
+
+// Sine and cosine of the row's angles, one per lane.  position * frequency / 2 pi in 64 bits: of the turns only the fraction counts, and for positions up to 2^31
+// it is exact to 2^-24 of a turn.
+__device__ __forceinline__ void form_angles(f32x2* angles, const double* freq, int n, int pos, int lane) {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  if (lane < n) {
+    const double t = (double)pos * (freq[lane] * 0.15915494309189533577);
+    float s, c;
+    sincospif(2.f * (float)(t - rint(t)), &s, &c);
+    angles[lane] = f32x2{c, s};
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+struct Turn { f32x4 cs[4]; };            // (cos, sin) of the lane's 8 angles
+template <int D>
+__device__ __forceinline__ Turn angles_of(const f32x2* angles, const Lane<D>& l) {
+  Turn t;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t.cs[i] = *(const f32x4*)(angles + l.angle[i >> 1] + 2 * (i & 1));
+  return t;
+}
+
+// The pairs of the two chunks by their angles, or (backward) by minus these.
+template <bool kBack>
+__device__ __forceinline__ void turn(float (&x)[8], float (&y)[8], const Turn& t, bool interleaved) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float c = t.cs[i >> 1][2 * (i & 1)], s = kBack ? -t.cs[i >> 1][2 * (i & 1) + 1] : t.cs[i >> 1][2 * (i & 1) + 1];
+    if (interleaved) {
+      float& a = i < 4 ? x[2 * i] : y[2 * i - 8];
+      float& b = i < 4 ? x[2 * i + 1] : y[2 * i - 7];
+      const float a0 = a;
+      a = a0 * c - b * s;
+      b = b * c + a0 * s;
+    } else {
+      const float a0 = x[i];
+      x[i] = a0 * c - y[i] * s;
+      y[i] = y[i] * c + a0 * s;
+    }
+  }
+}
+
+// 1 / sqrt(mean x^2 + eps) as a product r * s: where the squares pass fp32's range, x s with s = 2^-64 takes the place of x.
+template <int D>
+__device__ __forceinline__ void norm_of(const float (&x)[8], const float (&y)[8], float eps, float* r, float* s) {
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], fmaf(y[i], y[i], sum));
+  sum = sum_of_head<D>(sum);
+  *s = 1.f;
+  if (__any(sum == INFINITY)) {
+    const float z = sum == INFINITY ? 0x1p-64f : 1.f;
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t = fmaf(x[i] * z, x[i] * z, fmaf(y[i] * z, y[i] * z, t));
+    sum = sum_of_head<D>(t);
+    *s = z;
+    eps *= z * z;
+  }
+  *r = rsqrtf(fmaf(sum, 1.f / D, eps));
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(64 * kWaves) heads_fwd_kernel(HeadsArgs a) {
+  __shared__ __attribute__((aligned(16))) f32x2 angles[kWaves][D / 2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Lane<D> l(a, lane);
+  const Chunk<T> one = Chunk<T>::all(1.f);
+  Chunk<T> wq[2] = {one, one}, wk[2] = {one, one};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (a.wq) wq[i] = Chunk<T>::load((const T*)a.wq + l.at[i]);
+    if (a.wk) wk[i] = Chunk<T>::load((const T*)a.wk + l.at[i]);
+  }
+  for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.n_rows; row += (int64_t)gridDim.x * kWaves) {
+    Turn t = {};
+    if (a.turning) {
+      form_angles(angles[wave], a.freq, 8 * a.turning, a.pos[row], lane);
+      t = angles_of<D>(angles[wave], l);
+    }
+    for (int h = l.head; h < a.heads; h += Lane<D>::kHeads) {
+      const bool is_q = h < a.hq;
+      const T* from = is_q ? (const T*)a.q + row * a.q_stride + h * D : (const T*)a.k + row * a.k_stride + (h - a.hq) * D;
+      T* to = is_q ? (T*)a.q_out + row * a.q_out_stride + h * D : (T*)a.k_out + row * a.k_out_stride + (h - a.hq) * D;
+      float x[8], y[8], w[8];
+      Chunk<T>::load(from + l.at[0]).get(x);
+      Chunk<T>::load(from + l.at[1]).get(y);
+      if (is_q ? a.wq != nullptr : a.wk != nullptr) {
+        float r, s;
+        norm_of<D>(x, y, a.eps, &r, &s);
+        Chunk<T>::pick(is_q, wq[0], wk[0]).get(w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * s * r * w[i];
+        Chunk<T>::pick(is_q, wq[1], wk[1]).get(w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = y[i] * s * r * w[i];
+      }
+      if (l.turns) turn<false>(x, y, t, a.interleaved);
+      Chunk<T>::store(to + l.at[0], x);
+      Chunk<T>::store(to + l.at[1], y);
+    }
+  }
+}
+
+// A lane adds up the weights' gradients of its elements over its rows and heads; its workgroup's sums go to `part`.
+template <typename T, int D>
+__global__ void __launch_bounds__(64 * kWaves) heads_bwd_kernel(HeadsArgs a) {
+  __shared__ __attribute__((aligned(16))) f32x2 angles[kWaves][D / 2];
+  __shared__ __attribute__((aligned(16))) float sums[kWaves][2][D];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Lane<D> l(a, lane);
+  const Chunk<T> one = Chunk<T>::all(1.f);
+  Chunk<T> wq[2] = {one, one}, wk[2] = {one, one};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (a.wq) wq[i] = Chunk<T>::load((const T*)a.wq + l.at[i]);
+    if (a.wk) wk[i] = Chunk<T>::load((const T*)a.wk + l.at[i]);
+  }
+  float dw[2][16] = {};                  // of queries and keys
+  for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.n_rows; row += (int64_t)gridDim.x * kWaves) {
+    Turn t = {};
+    if (a.turning) {
+      form_angles(angles[wave], a.freq, 8 * a.turning, a.pos[row], lane);
+      t = angles_of<D>(angles[wave], l);
+    }
+    for (int h = l.head; h < a.heads; h += Lane<D>::kHeads) {
+      const bool is_q = h < a.hq;
+      const T* from = is_q ? (const T*)a.q + row * a.q_stride + h * D : (const T*)a.k + row * a.k_stride + (h - a.hq) * D;
+      const T* grad = is_q ? (const T*)a.dq_out + row * a.q_out_stride + h * D : (const T*)a.dk_out + row * a.k_out_stride + (h - a.hq) * D;
+      T* to = is_q ? (T*)a.q_out + row * a.dq_stride + h * D : (T*)a.k_out + row * a.dk_stride + (h - a.hq) * D;
+      float g0[8], g1[8];
+      Chunk<T>::load(grad + l.at[0]).get(g0);
+      Chunk<T>::load(grad + l.at[1]).get(g1);
+      if (l.turns) turn<true>(g0, g1, t, a.interleaved);
+      if (is_q ? a.wq != nullptr : a.wk != nullptr) {
+        float x[8], y[8], w[8], r, s, dot = 0.f;
+        Chunk<T>::load(from + l.at[0]).get(x);
+        Chunk<T>::load(from + l.at[1]).get(y);
+        norm_of<D>(x, y, a.eps, &r, &s);
+        auto half = [&](float (&v)[8], float (&g)[8], int part) __attribute__((always_inline)) {
+          Chunk<T>::pick(is_q, wq[part], wk[part]).get(w);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            v[i] = v[i] * s * r;                       // of norm sqrt(D), almost
+            const float d = g[i] * v[i];
+            if (is_q) dw[0][8 * part + i] += d;
+            else dw[1][8 * part + i] += d;
+            g[i] *= w[i];
+            dot = fmaf(g[i], v[i], dot);
+          }
+        };
+        half(x, g0, 0);
+        half(y, g1, 1);
+        dot = sum_of_head<D>(dot) * (1.f / D);
+        const float rs = r * s;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          g0[i] = rs * (g0[i] - x[i] * dot);
+          g1[i] = rs * (g1[i] - y[i] * dot);
+        }
+      }
+      Chunk<T>::store(to + l.at[0], g0);
+      Chunk<T>::store(to + l.at[1], g1);
+    }
+  }
+  if (!a.part) return;
+#pragma unroll
+  for (int side = 0; side < 2; ++side)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float x = dw[side][i];
+#pragma unroll
+      for (int d = Lane<D>::kLanes; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
+      if (l.head == 0) sums[wave][side][l.at[i >> 3] + (i & 7)] = x;
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * D; i += 64 * kWaves) {
+    float x = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) x += (&sums[w][0][0])[i];
+    a.part[(int64_t)blockIdx.x * 2 * D + i] = x;
+  }
+}
+
+// The workgroups' sums in order: one workgroup per 16 elements, 16 walkers each.
+__global__ void __launch_bounds__(256) heads_weights_kernel(const float* part, int n_parts, int D, float* dwq, float* dwk, int accumulate) {
+  __shared__ float sums[16][17];
+  const int e = blockIdx.x * 16 + (threadIdx.x & 15), walker = threadIdx.x >> 4;
+  float x = 0.f;
+  for (int i = walker; i < n_parts; i += 16) x += part[(int64_t)i * 2 * D + e];
+  sums[walker][threadIdx.x & 15] = x;
+  __syncthreads();
+  if (walker) return;
+  x = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) x += sums[w][threadIdx.x];
+  float* to = e < D ? dwq : dwk;
+  if (!to) return;
+  to += e < D ? e : e - D;
+  *to = accumulate ? *to + x : x;
+}
+
+bool misaligned(const void* p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+constexpr int kMostBlocks = 2048;
+int blocks_of(int64_t n_rows) {
+  const int64_t n = (n_rows + kWaves - 1) / kWaves;
+  return (int)(n < 1 ? 1 : n < kMostBlocks ? n : kMostBlocks);
+}
+
+nat_status heads_args(const nat_qk_params* p, const void* d_q, const void* d_k, const void* d_q_weight, const void* d_k_weight,
+                      const int32_t* d_position_ids, const double* d_inv_freq, HeadsArgs* a) {
+  if (!p || p->n_rows < 0 || p->n_rows > INT32_MAX || !(p->eps > 0.f) || !(p->eps < INFINITY) || (p->interleaved & ~1)) return NAT_INVALID_ARG;
+  if (p->dtype != NAT_DTYPE_BF16 && p->dtype != NAT_DTYPE_F32) return NAT_UNSUPPORTED_DTYPE;
+  const int D = p->head_dim;
+  if ((D != 64 && D != 128) || p->n_q_heads < 1 || p->n_q_heads > 4096 || p->n_kv_heads < 1 || p->n_kv_heads > 4096 || p->rotary_dim < 0 ||
+      p->rotary_dim > D || p->rotary_dim % 16)
+    return NAT_BAD_SHAPE;
+  const int64_t row[2] = {(int64_t)p->n_q_heads * D, (int64_t)p->n_kv_heads * D};
+  const int64_t* strides[6] = {&p->q_stride, &p->k_stride, &p->q_out_stride, &p->k_out_stride, &p->dq_stride, &p->dk_stride};
+  int64_t* to[6] = {&a->q_stride, &a->k_stride, &a->q_out_stride, &a->k_out_stride, &a->dq_stride, &a->dk_stride};
+  for (int i = 0; i < 6; ++i) {
+    const int64_t s = *strides[i];
+    if (s != 0 && (s < row[i & 1] || s % (p->dtype == NAT_DTYPE_BF16 ? 8 : 4) || s > INT32_MAX)) return NAT_BAD_SHAPE;
+    *to[i] = s ? s : row[i & 1];
+  }
+  if (misaligned(d_q) || misaligned(d_k) || misaligned(d_q_weight) || misaligned(d_k_weight) || misaligned(d_inv_freq, 8)) return NAT_INVALID_ARG;
+  if (p->n_rows > 0 && (!d_q || !d_k || (p->rotary_dim > 0) != (d_position_ids != nullptr) || (p->rotary_dim > 0 && !d_inv_freq))) return NAT_INVALID_ARG;
+  a->q = d_q;
+  a->k = d_k;
+  a->wq = d_q_weight;
+  a->wk = d_k_weight;
+  a->pos = d_position_ids;
+  a->freq = d_inv_freq;
+  a->hq = p->n_q_heads;
+  a->heads = p->n_q_heads + p->n_kv_heads;
+  a->turning = p->rotary_dim / 16;
+  a->interleaved = p->interleaved;
+  a->eps = p->eps;
+  a->n_rows = p->n_rows;
+  return NAT_OK;
+}
+
+}  // namespace
+}  // namespace nat
+
+using namespace nat;
+
+extern "C" nat_status nat_qk_norm_rope(const nat_qk_params* params, const void* d_q, const void* d_k, const void* d_q_weight, const void* d_k_weight,
+                                       const int32_t* d_position_ids, const double* d_inv_freq, void* d_q_out, void* d_k_out, void* stream) {
+  HeadsArgs a{};
+  const nat_status st = heads_args(params, d_q, d_k, d_q_weight, d_k_weight, d_position_ids, d_inv_freq, &a);
+  if (st != NAT_OK) return st;
+  if (misaligned(d_q_out) || misaligned(d_k_out)) return NAT_INVALID_ARG;
+  if (a.n_rows == 0) return NAT_OK;
+  if (!d_q_out || !d_k_out) return NAT_INVALID_ARG;
+  a.q_out = d_q_out;
+  a.k_out = d_k_out;
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope prof(PC_HEADS, s);
+  const int n = blocks_of(a.n_rows);
+  if (params->dtype == NAT_DTYPE_BF16) {
+    if (params->head_dim == 128) heads_fwd_kernel<uint16_t, 128><<<n, 64 * kWaves, 0, s>>>(a);
+    else heads_fwd_kernel<uint16_t, 64><<<n, 64 * kWaves, 0, s>>>(a);
+  } else {
+    if (params->head_dim == 128) heads_fwd_kernel<float, 128><<<n, 64 * kWaves, 0, s>>>(a);
+    else heads_fwd_kernel<float, 64><<<n, 64 * kWaves, 0, s>>>(a);
+  }
+  NAT_LAUNCH_CHECK();
+  return NAT_OK;
+}
+
+extern "C" size_t nat_qk_norm_rope_bwd_workspace_bytes(int64_t n_rows, int32_t head_dim) {
+  if (n_rows <= 0 || n_rows > INT32_MAX || (head_dim != 64 && head_dim != 128)) return 0;
+  return ((size_t)blocks_of(n_rows) * 2 * head_dim * 4 + 255) / 256 * 256;
+}
+
+extern "C" nat_status nat_qk_norm_rope_bwd(const nat_qk_params* params, const void* d_q, const void* d_k, const void* d_q_weight, const void* d_k_weight,
+                                           const int32_t* d_position_ids, const double* d_inv_freq, const void* d_dq_out, const void* d_dk_out,
+                                           void* d_dq, void* d_dk, float* d_dq_weight, float* d_dk_weight, int32_t accumulate, void* d_ws,
+                                           size_t ws_bytes, void* stream) {
+  HeadsArgs a{};
+  const nat_status st = heads_args(params, d_q, d_k, d_q_weight, d_k_weight, d_position_ids, d_inv_freq, &a);
+  if (st != NAT_OK) return st;
+  if (misaligned(d_dq_out) || misaligned(d_dk_out) || misaligned(d_dq) || misaligned(d_dk) || misaligned(d_dq_weight, 4) || misaligned(d_dk_weight, 4) ||
+      (d_q_weight != nullptr) != (d_dq_weight != nullptr) || (d_k_weight != nullptr) != (d_dk_weight != nullptr))
+    return NAT_INVALID_ARG;
+  const bool weights = d_q_weight || d_k_weight;
+  if (a.n_rows > 0 && (!d_dq_out || !d_dk_out || !d_dq || !d_dk)) return NAT_INVALID_ARG;
+  if (a.n_rows > 0 && weights && (!d_ws || ws_bytes < nat_qk_norm_rope_bwd_workspace_bytes(a.n_rows, params->head_dim))) return NAT_WORKSPACE_TOO_SMALL;
+  if (misaligned(d_ws, 256)) return NAT_INVALID_ARG;
+  a.dq_out = d_dq_out;
+  a.dk_out = d_dk_out;
+  a.q_out = d_dq;
+  a.k_out = d_dk;
+  a.part = weights ? (float*)d_ws : nullptr;
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope prof(PC_HEADS, s);
+  const int n = a.n_rows > 0 ? blocks_of(a.n_rows) : 0, D = params->head_dim;
+  if (n > 0) {
+    if (params->dtype == NAT_DTYPE_BF16) {
+      if (D == 128) heads_bwd_kernel<uint16_t, 128><<<n, 64 * kWaves, 0, s>>>(a);
+      else heads_bwd_kernel<uint16_t, 64><<<n, 64 * kWaves, 0, s>>>(a);
+    } else {
+      if (D == 128) heads_bwd_kernel<float, 128><<<n, 64 * kWaves, 0, s>>>(a);
+      else heads_bwd_kernel<float, 64><<<n, 64 * kWaves, 0, s>>>(a);
+    }
+    NAT_LAUNCH_CHECK();
+  }
+  if (weights && (n > 0 || !accumulate)) {
+    heads_weights_kernel<<<2 * D / 16, 256, 0, s>>>(a.part, n, D, d_dq_weight, d_dk_weight, accumulate);
+    NAT_LAUNCH_CHECK();
+  }
+  return NAT_OK;
+}

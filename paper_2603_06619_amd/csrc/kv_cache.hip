@@ -1,9 +1,12 @@
-// Paged key-value cache: writing rows into it (as they are, or in 8 bits), reading sequences back, and attention of one new token per sequence.
+// Paged key-value cache: writing rows into it (as they are, in 8 bits, or in 4), reading sequences back, and attention of one new token per sequence.
 //
 // A page holds page_size tokens of every key head, [head][token][head_dim], so that a head's tokens of a page are contiguous.  In the 8-bit format
 // (4 exponent bits, 3 mantissa bits, largest 448) a row (token, head) has one scale 2^e, the smallest power of two that brings its largest magnitude to 448 or
 // less: multiplying by a power of two rounds nothing, so the one rounding is that to 3 mantissa bits, and reading back is exact.  A power of two loses
 // no precision against a scale that reaches 448 exactly (the format is floating), and costs 1 byte per row.
+//
+// In the 4-bit format (2 exponent bits, 1 mantissa bit, largest 6) every group of 32 elements of a row has a scale of its own: with so few values one large element would
+// leave nothing of the others of a whole row.  The hardware's conversions take the scale along; every value is exact in bf16.
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
 
@@ -34,6 +37,14 @@ __device__ __forceinline__ u32x2 widen_fp8(uint32_t x) {
   return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 
+// Eight 4-bit values times 2^(exp - 127) to eight bf16, exactly (exp = 255: NaN)
+constexpr int kGroup = 32;                // elements that share a scale in 4 bits
+__device__ __forceinline__ u32x4 widen_fp4(uint32_t x, uint32_t exp) {
+  const float scale = power_of_two((int)exp);
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3))};
+}
+
 struct WriteArgs {
   CacheArgs c;
   const uint16_t *k, *v;
@@ -43,11 +54,40 @@ struct WriteArgs {
 
 // One row (token, head) per D / 8 lanes, 16 bytes of the input each.  32749 tokens of 8 heads of 128: 202 MB in 37 us, 5.5 TB/s (a copy: 4.9); 64 tokens 3.4 us,
 // the time of a launch.
-template <int D, bool kFp8>
+template <int D, int kFormat>
 __device__ __forceinline__ void write_row(const uint16_t* row, char* cache, uint8_t* exps, int64_t to, int lane) {
   const u32x4 x = *(const u32x4*)(row + 8 * lane);
-  if constexpr (!kFp8) {
+  if constexpr (kFormat == NAT_KV_BF16) {
     *(u32x4*)(cache + (to * D + 8 * lane) * 2) = x;
+  } else if constexpr (kFormat == NAT_KV_FP4) {
+    uint32_t largest = 0;                    // magnitude as bits of bf16, of the group that four lanes hold
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = x[i] & 0x7fff, hi = (x[i] >> 16) & 0x7fff;
+      if (lo > largest) largest = lo;
+      if (hi > largest) largest = hi;
+    }
+#pragma unroll
+    for (int d = 1; d < kGroup / 8; d <<= 1) {
+      const uint32_t other = __shfl_xor(largest, d, 64);
+      largest = other > largest ? other : largest;
+    }
+    // largest = 1.f 2^(E - 127) <= 1.5 2^(2 + e); at 2^125 values of 3.5 2^127 and more become 6 2^125, which bf16 still holds
+    int e = (int)(largest >> 7) - 2 + ((largest & 0x7f) > 0x40);
+    e = e < 2 ? 2 : e > 252 ? 252 : e;
+    const float scale = power_of_two(e);
+    const bool finite = largest < 0x7f80;
+    // (of an element of a vector as it stands, the cast takes the first one's bits)
+    auto pair = [&](int i) { const uint32_t two = x[i]; return __builtin_bit_cast(bf16x2, two); };
+    uint32_t out = 0;
+    if (finite) {
+      out = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(out, pair(0), scale, 0);
+      out = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(out, pair(1), scale, 1);
+      out = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(out, pair(2), scale, 2);
+      out = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(out, pair(3), scale, 3);
+    }
+    *(uint32_t*)(cache + to * (D / 2) + 4 * lane) = out;
+    if (lane % (kGroup / 8) == 0) exps[to * (D / kGroup) + lane / (kGroup / 8)] = (uint8_t)(finite ? e : 255);
   } else {
     uint32_t largest = 0;                    // of the finite magnitudes, as bits of bf16
 #pragma unroll
@@ -81,7 +121,7 @@ __device__ __forceinline__ void write_row(const uint16_t* row, char* cache, uint
   }
 }
 
-template <int D, bool kFp8>
+template <int D, int kFormat>
 __global__ void __launch_bounds__(256) kv_write_kernel(WriteArgs a) {
   constexpr int kLanes = D / 8;
   const int lane = threadIdx.x % kLanes;
@@ -91,8 +131,8 @@ __global__ void __launch_bounds__(256) kv_write_kernel(WriteArgs a) {
   const int64_t slot = a.slots[row];
   if (slot < 0 || (slot >> a.c.page_log2) >= a.c.n_pages) return;
   const int64_t to = cache_row(a.c, slot >> a.c.page_log2, head, (int)(slot & ((1 << a.c.page_log2) - 1)));
-  write_row<D, kFp8>(a.k + row * a.k_stride + head * D, a.c.k, a.c.k_exp, to, lane);
-  write_row<D, kFp8>(a.v + row * a.v_stride + head * D, a.c.v, a.c.v_exp, to, lane);
+  write_row<D, kFormat>(a.k + row * a.k_stride + head * D, a.c.k, a.c.k_exp, to, lane);
+  write_row<D, kFormat>(a.v + row * a.v_stride + head * D, a.c.v, a.c.v_exp, to, lane);
 }
 
 struct ReadArgs {
@@ -103,12 +143,14 @@ struct ReadArgs {
   uint16_t *k, *v;
 };
 
-template <int D, bool kFp8>
+template <int D, int kFormat>
 __device__ __forceinline__ void read_row(const char* cache, const uint8_t* exps, int64_t from, bool there, uint16_t* row, int lane) {
   u32x4 x = {0, 0, 0, 0};
   if (there) {
-    if constexpr (!kFp8) {
+    if constexpr (kFormat == NAT_KV_BF16) {
       x = *(const u32x4*)(cache + (from * D + 8 * lane) * 2);
+    } else if constexpr (kFormat == NAT_KV_FP4) {
+      x = widen_fp4(*(const uint32_t*)(cache + from * (D / 2) + 4 * lane), exps[from * (D / kGroup) + lane / (kGroup / 8)]);
     } else {
       const u32x2 y = *(const u32x2*)(cache + from * D + 8 * lane);
       const float scale = power_of_two(exps[from]);
@@ -124,7 +166,7 @@ __device__ __forceinline__ void read_row(const char* cache, const uint8_t* exps,
 }
 
 // The sequence of a packed row is searched for by the lanes that read it.  106 MB of 6 sequences in 20 us, 5.3 TB/s: most of it written, where a copy writes half.
-template <int D, bool kFp8>
+template <int D, int kFormat>
 __global__ void __launch_bounds__(256) kv_read_kernel(ReadArgs a) {
   constexpr int kLanes = D / 8;
   const int lane = threadIdx.x % kLanes;
@@ -136,8 +178,8 @@ __global__ void __launch_bounds__(256) kv_read_kernel(ReadArgs a) {
   const int page = place < a.table_width ? a.table[(int64_t)seq * a.table_width + place] : -1;
   const bool there = page >= 0 && page < a.c.n_pages;
   const int64_t from = there ? cache_row(a.c, page, head, (int)(at & ((1 << a.c.page_log2) - 1))) : 0;
-  read_row<D, kFp8>(a.c.k, a.c.k_exp, from, there, a.k + row * a.k_stride + head * D, lane);
-  read_row<D, kFp8>(a.c.v, a.c.v_exp, from, there, a.v + row * a.v_stride + head * D, lane);
+  read_row<D, kFormat>(a.c.k, a.c.k_exp, from, there, a.k + row * a.k_stride + head * D, lane);
+  read_row<D, kFormat>(a.c.v, a.c.v_exp, from, there, a.v + row * a.v_stride + head * D, lane);
 }
 
 // ------------------------------------------------------------------ one new token ----
@@ -186,25 +228,37 @@ __device__ __forceinline__ float sum_groups(float x) {
 
 // 32 tokens of keys and values in flight.  Keys are operands as they lie in memory (lane l: token l % 16 of a block of 16, elements by l / 16); the
 // order of the elements is the same in the query's fragments.
-template <int D, bool kFp8>
+template <int D, int kFormat>
 struct TokenTile {
-  static constexpr int kKeyLoads = kFp8 ? D / 64 : D / 32;            // 16-byte loads per block of 16 tokens
-  static constexpr int kRowLanes = kFp8 ? D / 16 : D / 8;             // lanes per row of values
+  static constexpr bool kFp4 = kFormat == NAT_KV_FP4;
+  static constexpr int kRowBytes = kFormat == NAT_KV_BF16 ? 2 * D : kFp4 ? D / 2 : D;
+  static constexpr int kKeyBytes = kRowBytes / 4 < 16 ? kRowBytes / 4 : 16;      // per load
+  static constexpr int kKeyLoads = kRowBytes / 4 / kKeyBytes;         // per block of 16 tokens
+  static constexpr int kRowLanes = kRowBytes / 16;                    // lanes per row of values
   static constexpr int kValueLoads = kTokens * kRowLanes / 64;
-  u32x4 k[2][kKeyLoads], v[kValueLoads];
-  uint32_t k_exp[2], v_exp[2];
+  typedef uint32_t Key __attribute__((ext_vector_type(kKeyBytes / 4)));
+  Key k[2][kKeyLoads];
+  u32x4 v[kValueLoads];
+  uint32_t k_exp[2], v_exp[kFp4 ? kValueLoads : 2];
+
+  // first of the eight elements of fragment s of a key that lane group g has
+  __device__ __forceinline__ static int element(int s, int g) {
+    if constexpr (kFp4) return D / 4 * g + 8 * s;
+    else if constexpr (kFormat == NAT_KV_FP8) return 64 * (s >> 1) + 16 * g + 8 * (s & 1);
+    else return 32 * s + 8 * g;
+  }
 
   // p0, p1: pages of the two blocks of 16 tokens, at: place of the first in its page
   __device__ __forceinline__ void load(const CacheArgs& c, int p0, int p1, int head, int t0, int lane) {
     const int mask = (1 << c.page_log2) - 1, n = lane & 15, g = lane >> 4;
     const int64_t r0 = cache_row(c, p0 < 0 ? 0 : p0, head, t0 & mask), r1 = cache_row(c, p1 < 0 ? 0 : p1, head, (t0 + 16) & mask);
-    constexpr int kRowBytes = kFp8 ? D : 2 * D;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const char* row = c.k + ((b ? r1 : r0) + n) * kRowBytes + 16 * g;
+      const char* row = c.k + ((b ? r1 : r0) + n) * kRowBytes + kKeyBytes * g;
 #pragma unroll
-      for (int i = 0; i < kKeyLoads; ++i) k[b][i] = *(const u32x4*)(row + 64 * i);
-      if constexpr (kFp8) {
+      for (int i = 0; i < kKeyLoads; ++i) k[b][i] = *(const Key*)(row + 64 * i);
+      if constexpr (kFp4) k_exp[b] = c.k_exp[((b ? r1 : r0) + n) * (D / kGroup) + D / 4 * g / kGroup];
+      if constexpr (kFormat == NAT_KV_FP8) {
         k_exp[b] = *(const uint32_t*)(c.k_exp + (b ? r1 : r0) + 4 * g);
         v_exp[b] = *(const uint32_t*)(c.v_exp + (b ? r1 : r0) + 4 * g);
       }
@@ -213,12 +267,15 @@ struct TokenTile {
     for (int i = 0; i < kValueLoads; ++i) {
       const int row = i * (64 / kRowLanes) + lane / kRowLanes;
       v[i] = *(const u32x4*)(c.v + ((row < 16 ? r0 : r1 - 16) + row) * kRowBytes + lane % kRowLanes * 16);
+      if constexpr (kFp4) v_exp[i] = c.v_exp[((row < 16 ? r0 : r1 - 16) + row) * (D / kGroup) + lane % kRowLanes];
     }
   }
 
   __device__ __forceinline__ bf16x8 key_fragment(int b, int s) const {
-    if constexpr (!kFp8) {
+    if constexpr (kFormat == NAT_KV_BF16) {
       return __builtin_bit_cast(bf16x8, k[b][s]);
+    } else if constexpr (kFp4) {
+      return __builtin_bit_cast(bf16x8, widen_fp4(k[b][0][s], k_exp[b]));
     } else {
       const u32x4 x = k[b][s >> 1];
       const u32x2 lo = widen_fp8(x[2 * (s & 1)]), hi = widen_fp8(x[2 * (s & 1) + 1]);
@@ -232,9 +289,14 @@ struct TokenTile {
     for (int i = 0; i < kValueLoads; ++i) {
       const int row = i * (64 / kRowLanes) + lane / kRowLanes, at = lane % kRowLanes;
       u32x4 x = v[i];
-      if (!whole && (row < first_live || row >= end_live)) x = u32x4{0, 0, 0, 0};
-      if constexpr (!kFp8) {
+      const bool dead = !whole && (row < first_live || row >= end_live);
+      if (dead) x = u32x4{0, 0, 0, 0};
+      if constexpr (kFormat == NAT_KV_BF16) {
         *(u32x4*)(tile + RowTile<D>::chunk_at(row, at)) = x;
+      } else if constexpr (kFp4) {
+        const uint32_t e = dead ? 127 : v_exp[i];            // (a place that is not there may hold 255)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *(u32x4*)(tile + RowTile<D>::chunk_at(row, 4 * at + j)) = widen_fp4(x[j], e);
       } else {
         const u32x2 a = widen_fp8(x[0]), b = widen_fp8(x[1]), c = widen_fp8(x[2]), d = widen_fp8(x[3]);
         *(u32x4*)(tile + RowTile<D>::chunk_at(row, 2 * at)) = u32x4{a[0], a[1], b[0], b[1]};
@@ -244,7 +306,7 @@ struct TokenTile {
   }
 };
 
-template <int D, bool kFp8>
+template <int D, int kFormat>
 __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
   __shared__ __attribute__((aligned(16))) char values[4][kTokens * D * 2];       // and, at the end, the wavefronts' results
   __shared__ int32_t pages[kMaxChunk / 16];
@@ -270,8 +332,7 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) {
     q[s] = bf16x8{};
-    const int at = kFp8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-    if (n < heads_here) q[s] = *(const bf16x8*)(a.q + seq * a.q_stride + (head0 + n) * D + at);
+    if (n < heads_here) q[s] = *(const bf16x8*)(a.q + seq * a.q_stride + (head0 + n) * D + TokenTile<D, kFormat>::element(s, g));
   }
   __syncthreads();
 
@@ -279,11 +340,11 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
   float m = -INFINITY, sum = 0.f;
   f32x4 acc[D / 16] = {};
   char* vt = values[wave];
-  auto load = [&](TokenTile<D, kFp8>& t, int t0) {
+  auto load = [&](TokenTile<D, kFormat>& t, int t0) {
     const int last = (end - 1) / 16, b = t0 / 16;
     t.load(a.c, __builtin_amdgcn_readfirstlane(pages[b]), __builtin_amdgcn_readfirstlane(pages[b < last ? b + 1 : last]), head, first + t0, lane);
   };
-  auto step = [&](const TokenTile<D, kFp8>& t, int t0) {
+  auto step = [&](const TokenTile<D, kFormat>& t, int t0) {
     const int last = (end - 1) / 16, b0 = t0 / 16;
     const bool there0 = pages[b0] >= 0, there1 = b0 < last && pages[b0 + 1] >= 0;
     const bool whole = t0 + kTokens <= end && there0 && there1;
@@ -294,7 +355,7 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) st[b] = mfma16x16(t.key_fragment(b, s), q[s], st[b]);
-    if constexpr (kFp8) {
+    if constexpr (kFormat == NAT_KV_FP8) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -330,7 +391,7 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
       for (int i = 0; i < 4; ++i) {
         float x = exp2_fast(fmaf(st[b][i], to_log2, -shift));
         sum += x;
-        if constexpr (kFp8) {
+        if constexpr (kFormat == NAT_KV_FP8) {
           const float scaled = x * power_of_two((t.v_exp[b] >> (8 * i)) & 0xff);
           x = whole || st[b][i] != -INFINITY ? scaled : 0.f;       // the scale of a token that is not there may be anything
         }
@@ -346,7 +407,7 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
       acc[db] = mfma16x16(__builtin_bit_cast(bf16x8, both), p, acc[db]);
     }
   };
-  TokenTile<D, kFp8> t0, t1;
+  TokenTile<D, kFormat> t0, t1;
   int at = wave * kTokens;
   if (at < end) load(t0, at);
   while (at < end) {
@@ -463,13 +524,13 @@ bool misaligned(const void* p) { return ((uintptr_t)p & 15) != 0; }
 
 nat_status cache_args(const nat_kv_cache* p, CacheArgs* c) {
   if (!p) return NAT_INVALID_ARG;
-  if (p->format != NAT_KV_BF16 && p->format != NAT_KV_FP8) return NAT_UNSUPPORTED_DTYPE;
+  if (p->format != NAT_KV_BF16 && p->format != NAT_KV_FP8 && p->format != NAT_KV_FP4) return NAT_UNSUPPORTED_DTYPE;
   if ((p->head_dim != 64 && p->head_dim != 128) || p->n_kv_heads <= 0 || p->n_kv_heads > 4096) return NAT_BAD_SHAPE;
   int log2 = 4;
   while (log2 < 8 && (1 << log2) != p->page_size) ++log2;
   if ((1 << log2) != p->page_size) return NAT_BAD_SHAPE;
   if (p->n_pages <= 0 || !p->d_k || !p->d_v || misaligned(p->d_k) || misaligned(p->d_v)) return NAT_INVALID_ARG;
-  if (p->format == NAT_KV_FP8 && (!p->d_k_exp || !p->d_v_exp || misaligned(p->d_k_exp) || misaligned(p->d_v_exp))) return NAT_INVALID_ARG;
+  if (p->format != NAT_KV_BF16 && (!p->d_k_exp || !p->d_v_exp || misaligned(p->d_k_exp) || misaligned(p->d_v_exp))) return NAT_INVALID_ARG;
   *c = CacheArgs{(char*)p->d_k, (char*)p->d_v, p->d_k_exp, p->d_v_exp, p->n_pages, p->n_kv_heads, log2};
   return NAT_OK;
 }
@@ -489,10 +550,16 @@ int chunk_of(int64_t n_seqs, int64_t blocks, int64_t most) {
   return (int)max(kMinChunk, ((most + n - 1) / n + 127) / 128 * 128);
 }
 
-template <template <int, bool> class Launch, class... Args>
+template <template <int, int> class Launch, int D, class... Args>
+void by_format(int format, Args... args) {
+  if (format == NAT_KV_FP8) Launch<D, NAT_KV_FP8>::go(args...);
+  else if (format == NAT_KV_FP4) Launch<D, NAT_KV_FP4>::go(args...);
+  else Launch<D, NAT_KV_BF16>::go(args...);
+}
+template <template <int, int> class Launch, class... Args>
 void by_shape(int head_dim, int format, Args... args) {
-  if (head_dim == 128) format == NAT_KV_FP8 ? Launch<128, true>::go(args...) : Launch<128, false>::go(args...);
-  else format == NAT_KV_FP8 ? Launch<64, true>::go(args...) : Launch<64, false>::go(args...);
+  if (head_dim == 128) by_format<Launch, 128>(format, args...);
+  else by_format<Launch, 64>(format, args...);
 }
 // (row, head) pairs, `per` to a workgroup of 256, in as few launches as have room for them
 template <class Args>
@@ -504,18 +571,18 @@ void launch_rows(void (*kernel)(Args), Args a, int64_t per, hipStream_t s) {
     kernel<<<(unsigned)(blocks < kMost ? blocks : kMost), 256, 0, s>>>(a);
   }
 }
-template <int D, bool kFp8>
+template <int D, int kFormat>
 struct LaunchWrite {
-  static void go(WriteArgs a, hipStream_t s) { launch_rows(kv_write_kernel<D, kFp8>, a, 256 / (D / 8), s); }
+  static void go(WriteArgs a, hipStream_t s) { launch_rows(kv_write_kernel<D, kFormat>, a, 256 / (D / 8), s); }
 };
-template <int D, bool kFp8>
+template <int D, int kFormat>
 struct LaunchRead {
-  static void go(ReadArgs a, hipStream_t s) { launch_rows(kv_read_kernel<D, kFp8>, a, 256 / (D / 8), s); }
+  static void go(ReadArgs a, hipStream_t s) { launch_rows(kv_read_kernel<D, kFormat>, a, 256 / (D / 8), s); }
 };
-template <int D, bool kFp8>
+template <int D, int kFormat>
 struct LaunchDecode {
   static void go(DecodeArgs a, hipStream_t s) {
-    decode_kernel<D, kFp8><<<(unsigned)((int64_t)a.n_seqs * a.n_chunks * a.c.hkv * a.head_blocks), 256, 0, s>>>(a);
+    decode_kernel<D, kFormat><<<(unsigned)((int64_t)a.n_seqs * a.n_chunks * a.c.hkv * a.head_blocks), 256, 0, s>>>(a);
   }
 };
 

@@ -11,7 +11,7 @@ namespace nat {
 enum ProfClass : int {
   PC_ADVANTAGE = 0, PC_SELECT, PC_COMPACT, PC_GATHER, PC_TRANSPOSE, PC_LOGITS, PC_TOKEN_STATS,
   PC_DHIDDEN, PC_DWEIGHT, PC_LOSS_REDUCE, PC_F32_PATH, PC_FILL, PC_SCHEDULE, PC_PREFIX_PACK,
-  PC_ATTN_FWD, PC_ATTN_BWD, PC_KV_CACHE, PC_ATTN_DECODE, PC_SAMPLE, PC_NUM
+  PC_ATTN_FWD, PC_ATTN_BWD, PC_KV_CACHE, PC_ATTN_DECODE, PC_SAMPLE, PC_HEADS, PC_EMBED, PC_PAGES, PC_NUM
 };
 
 // A launch has room for fewer than 2^32 work-items: of more, the rest is left out without an error.

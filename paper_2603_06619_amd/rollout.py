@@ -1,5 +1,5 @@
-"""Buffer plumbing around the operators of the model body and of the rollouts: attention over packed sequences and its
-gradients, a paged key-value cache, attention of one new token over it, sampling.  Outputs and workspaces come from torch;
+"""Buffer plumbing around the operators of the model body and of the rollouts: the embedding, norms and rotation of queries and keys, attention
+over packed sequences, and their gradients; a paged key-value cache, its pages, attention of one new token over it, sampling.  Outputs and workspaces come from torch;
 the work happens in the library, on the current stream."""
 import math
 
@@ -12,9 +12,14 @@ class PagedCache(nb.KvCache):
     """A KvCache that can allocate its arrays."""
 
     @classmethod
-    def empty(cls, n_pages, n_kv_heads, page_size, head_dim, fp8=False, device="cuda:0"):
+    def empty(cls, n_pages, n_kv_heads, page_size, head_dim, fp8=False, device="cuda:0", fp4=False):
         shape = (n_pages, n_kv_heads, page_size, head_dim)
         new = lambda s, dt: torch.empty(s, dtype=dt, device=device)
+        if fp8 and fp4:
+            raise ValueError("a cache is in 8 bits or in 4")
+        if fp4:
+            half, exps = (*shape[:3], head_dim // 2), (*shape[:3], head_dim // 32)
+            return cls(new(half, torch.uint8), new(half, torch.uint8), new(exps, torch.uint8), new(exps, torch.uint8))
         dt = torch.float8_e4m3fn if fp8 else torch.bfloat16
         exps = (new(shape[:3], torch.uint8), new(shape[:3], torch.uint8)) if fp8 else (None, None)
         return cls(new(shape, dt), new(shape, dt), *exps)
@@ -66,6 +71,59 @@ class RolloutStage:
         nb.nat_attn_bwd(q, k, v, out, lse, dout, cu_q, cu_q if cu_k is None else cu_k, causal, self._scale(scale, q.shape[2]),
                         dq, dk, dv, ws)
         return dq, dk, dv
+
+    def norm_rotate(self, q, k, position_ids, inv_freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
+        """Queries [n, q heads, D] and keys [n, kv heads, D], bf16 or float32, normed head by head (where there is a weight [D]) and rotated by position:
+        inv_freq float64 [R / 2], radians per position for the pairs of the first R elements; both None: no rotation.  Returns (q, k), new arrays."""
+        q_out, k_out = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
+        nb.nat_qk_norm_rope(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, q_out, k_out)
+        return q_out, k_out
+
+    def norm_rotate_backward(self, dq_out, dk_out, q, k, position_ids, inv_freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
+        """(dq, dk, dq_weight, dk_weight) of norm_rotate() with its inputs; the weights' in float32, None without a weight."""
+        dq, dk = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
+        dqw, dkw = (None if w is None else w.new_empty(w.shape, dtype=torch.float32) for w in (q_weight, k_weight))
+        ws = None
+        if dqw is not None or dkw is not None:
+            ws = self._buf("norm_rotate", nb.qk_norm_rope_bwd_workspace_bytes(q.shape[0], q.shape[2]))
+        nb.nat_qk_norm_rope_bwd(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, dq_out, dk_out, dq, dk, dqw, dkw, False, ws)
+        return dq, dk, dqw, dkw
+
+    def embed(self, ids, E, scale=1.0):
+        """Rows of E [V, H] (bf16 or float32) by int32 ids, times scale; zeros for ids outside [0, V)."""
+        out = E.new_empty((ids.numel(), E.shape[1]))
+        nb.nat_embed(ids, E, scale, out)
+        return out
+
+    def embed_backward(self, dout, ids, V, scale=1.0, dE=None, accumulate=False):
+        """The gradient [V, H] of embed(), float32; with accumulate it is added to dE (of tied weights: the head's dW)."""
+        if dE is None:
+            if accumulate:
+                raise ValueError("accumulate needs dE")
+            dE = dout.new_empty((V, dout.shape[1]), dtype=torch.float32)
+        elif dE.shape[0] != V:
+            raise ValueError(f"dE: expected {V} rows, got {dE.shape[0]}")
+        ws = self._buf("embed", nb.embed_bwd_workspace_bytes(ids.numel(), V, dout.shape[1]))
+        nb.nat_embed_bwd(ids, dout, scale, dE, accumulate, ws)
+        return dE
+
+    def reserve(self, block_table, seq_lens, new_lens, free_pages, counts, page_size, n_rows):
+        """Pages for new_lens more tokens of every sequence, from the end of the stack free_pages[:counts[0]] into block_table (in place), and the places of these tokens:
+        dict with slots (int64) and position_ids (int32) of the n_rows new rows, cu_new (their offsets), start (first position; -1: refused, no pages or no
+        room in the table), and seq_lens and counts (free pages, sequences refused) as they are now.  The free pages stay where they are, behind counts[0]."""
+        n = seq_lens.numel()
+        cu, start, lens, pos, left = torch.empty(3 * n + 3 + n_rows, dtype=torch.int32, device=seq_lens.device).split((n + 1, n, n, n_rows, 2))
+        slots = seq_lens.new_empty(n_rows, dtype=torch.int64)
+        nb.nat_kv_reserve(block_table, seq_lens, new_lens, free_pages, counts, page_size, n_rows, left, lens, start, cu, slots, pos,
+                          self._buf("pages", nb.kv_reserve_workspace_bytes(n)))
+        return dict(slots=slots, position_ids=pos, cu_new=cu, start=start, seq_lens=lens, counts=left)
+
+    def release(self, block_table, seq_lens, keep_lens, free_pages, counts, page_size):
+        """The pages behind the first keep_lens tokens of every sequence (0: it has ended) back to free_pages (in place): (seq_lens, counts) as they are now."""
+        n = seq_lens.numel()
+        lens, left = torch.empty(n + 2, dtype=torch.int32, device=seq_lens.device).split((n, 2))
+        nb.nat_kv_release(block_table, seq_lens, keep_lens, free_pages, counts, page_size, left, lens, self._buf("pages", nb.kv_release_workspace_bytes(n)))
+        return lens, left
 
     def write_cache(self, cache, k, v, slots):
         nb.nat_kv_write(cache, k, v, slots)

@@ -1,0 +1,220 @@
+"""The cache in 4 bits: written and read bit for bit as oracle/kv_cache.py says, attention of one token over it within the limits of bf16 probabilities and results."""
+import numpy as np
+import pytest
+import torch
+
+from nat_testlib import DEV
+from oracle import attention as oattn
+from oracle import kv_cache as okv
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def stage():
+    from paper_2603_06619_amd.rollout import RolloutStage
+    return RolloutStage(DEV)
+
+
+def new_cache(n_pages, heads, page, D, fill=None):
+    from paper_2603_06619_amd.rollout import PagedCache
+    c = PagedCache.empty(n_pages, heads, page, D, device=DEV, fp4=True)
+    assert c.head_dim == D
+    for x in (c.k, c.v, c.k_exp, c.v_exp):
+        if fill is not None:
+            x.fill_(fill)
+    return c
+
+
+def rows(seed, n, heads, D, pad=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn((n, heads * D + pad), generator=g, device=DEV) * torch.exp(4 * torch.randn((n, 1), generator=g, device=DEV))
+    return x.bfloat16()[:, :heads * D].unflatten(1, (heads, D))
+
+
+@pytest.mark.parametrize("heads,D,page,n", [(1, 64, 16, 1), (2, 128, 16, 50), (3, 64, 32, 333), (8, 128, 64, 1000), (5, 128, 256, 700)])
+def test_write_bit_for_bit(stage, heads, D, page, n):
+    n_pages = 2 * n // page + 3
+    cache = new_cache(n_pages, heads, page, D, 0x2a)
+    k, v = rows(1, n, heads, D), rows(2, n, heads, D, pad=16)
+    slots = np.random.default_rng(3).permutation(n_pages * page)[:n].astype(np.int64)
+    if n > 4:
+        slots[[1, n // 2]], slots[2], slots[3] = -1, n_pages * page, 2 ** 40            # padding, and outside the cache
+    stage.write_cache(cache, k, v, torch.from_numpy(slots).to(DEV))
+    live = (slots >= 0) & (slots < n_pages * page)
+    at = (slots[live] // page, slice(None), slots[live] % page)
+    for name, x in (("k", k), ("v", v)):
+        codes, exps = okv.quantise_groups(x.float().cpu().numpy())
+        for got, new in ((getattr(cache, name), codes), (getattr(cache, name + "_exp"), exps)):
+            want = np.full(got.shape, 0x2a, np.uint8)
+            want[at] = new[live]
+            assert np.array_equal(got.cpu().numpy(), want), name
+
+
+def test_write_of_every_bf16(stage):
+    """All 65536 of them, each as the largest of its group and beside one that is 1.5 to 48 times as large; zeros, the range's ends, and what is not finite."""
+    bits = torch.arange(65536, dtype=torch.int32, device=DEV).to(torch.int16).view(torch.bfloat16)
+    x = torch.zeros((6 * 65536 // 2, 2, 32), dtype=torch.bfloat16, device=DEV)
+    flat = x.view(6, 65536, 32)
+    for i, factor in enumerate((0, 1.5, 3, 6, 12, 48)):
+        flat[i, :, 5] = bits
+        if factor:
+            flat[i, :, 20] = (-bits.float() * factor).bfloat16()
+    x = x.view(-1, 1, 64)
+    n = x.shape[0]
+    cache = new_cache(n // 256, 1, 256, 64)
+    stage.write_cache(cache, x, x, torch.arange(n, device=DEV))
+    codes, exps = okv.quantise_groups(x.float().cpu().numpy())
+    assert np.array_equal(cache.k.view(n, 32).cpu().numpy(), codes[:, 0]) and np.array_equal(cache.k_exp.view(n, 2).cpu().numpy(), exps[:, 0])
+    table = torch.arange(n // 256, dtype=torch.int32, device=DEV)[None]
+    k, v = stage.read_cache(cache, table, torch.tensor([0, n], dtype=torch.int32, device=DEV), n)
+    want = okv.group_values(codes, exps)
+    for got in (k, v):
+        got = got.double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~np.isnan(want)], want[~np.isnan(want)])
+
+
+@pytest.mark.parametrize("heads,D,page", [(1, 64, 16), (3, 128, 64), (2, 64, 256)])
+def test_read_back(stage, heads, D, page):
+    import paper_2603_06619_amd as nat
+    lens = [1, page, 0, 3 * page + 5, page - 1]
+    n, need = sum(lens), [-(-l // page) for l in lens]
+    order = np.random.default_rng(4).permutation(sum(need) + 2)
+    table, at = np.full((len(lens), max(need) + 1), -1, np.int32), 0
+    for i, c in enumerate(need):
+        table[i, :c] = order[at:at + c]
+        at += c
+    cu = np.cumsum([0] + lens)
+    cache = new_cache(sum(need) + 2, heads, page, D, 0x55)
+    k, v = rows(5, n, heads, D), rows(6, n, heads, D)
+    slots = np.concatenate([table[i][np.arange(l) // page].astype(np.int64) * page + np.arange(l) % page for i, l in enumerate(lens)])
+    stage.write_cache(cache, k, v, torch.from_numpy(slots).to(DEV))
+    dev = lambda x: torch.from_numpy(x.astype(np.int32)).to(DEV)
+    gk, gv = stage.read_cache(cache, dev(table), dev(cu), n)
+    for got, x in ((gk, k), (gv, v)):
+        assert torch.equal(got.cpu(), torch.from_numpy(okv.group_values(*okv.quantise_groups(x.float().cpu().numpy()))).bfloat16())
+    table[3, 1] = 10 ** 6                                       # a page that is not there reads as zeros
+    whole = torch.full((n + 3, heads * D + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+    part = whole[:, :heads * D].unflatten(1, (heads, D))
+    part2 = part.clone()
+    nat.nat_kv_read(cache, dev(table), dev(cu), part, part2)
+    gone = slice(cu[3] + page, cu[3] + 2 * page)
+    assert bool((part[gone] == 0).all()) and torch.equal(part[:gone.start], gk[:gone.start]) and torch.equal(part[gone.stop:n], gk[gone.stop:])
+    assert bool((part[n:] == 7).all()) and bool((whole[:, heads * D:] == 7).all())
+
+
+def decode_case(seed, lens, hq, hkv, D, page, width=None, fill=0xff):
+    """A cache whose unwritten places hold NaN (exponents of 255) and a table with pages in no order."""
+    from paper_2603_06619_amd.rollout import RolloutStage
+    need = [-(-max(l, 0) // page) for l in lens]
+    n_pages = sum(need) + 1
+    order = np.random.default_rng(seed).permutation(n_pages)
+    table, at = np.full((len(lens), width or max(need + [1])), -1, np.int32), 0
+    for i, c in enumerate(need):
+        table[i, :c] = order[at:at + c]
+        at += c
+    cache, n = new_cache(n_pages, hkv, page, D, fill), sum(max(l, 0) for l in lens)
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    new = lambda r, h: torch.randn((r, h, D), generator=g, device=DEV, dtype=torch.bfloat16)
+    if n:
+        slots = np.concatenate([table[i][np.arange(l) // page].astype(np.int64) * page + np.arange(l) % page for i, l in enumerate(lens) if l > 0])
+        size = torch.exp(torch.randn((n, hkv, D // 32, 1), generator=g, device=DEV)).expand(-1, -1, -1, 32).reshape(n, hkv, D)        # groups of different size
+        RolloutStage(DEV).write_cache(cache, new(n, hkv), (new(n, hkv) * size).bfloat16(), torch.from_numpy(slots).to(DEV))
+    return dict(cache=cache, q=new(len(lens), hq), table=torch.from_numpy(table).to(DEV), lens=torch.tensor(lens, dtype=torch.int32, device=DEV))
+
+
+def check_decode(c, out, lse, scale=None):
+    k, v = (okv.group_values(getattr(c["cache"], n).cpu().numpy(), getattr(c["cache"], n + "_exp").cpu().numpy()) for n in ("k", "v"))
+    ref = oattn.decode(c["q"].double().cpu().numpy(), k, v, c["table"].cpu().numpy(), c["lens"].cpu().numpy(), scale, bounds=True)
+    got, l = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert np.isfinite(got).all() and np.array_equal(np.isneginf(l), np.isneginf(ref["lse"]))
+    assert np.all(np.abs(got - ref["out"]) <= ref["e_out"] + 1e-30)
+    fine = np.isfinite(ref["lse"])
+    assert np.all(np.abs(l[fine] - ref["lse"][fine]) <= ref["e_lse"][fine])
+    norm = np.linalg.norm(ref["out"])
+    assert norm == 0 or np.linalg.norm(got - ref["out"]) <= 4e-3 * norm
+
+
+@pytest.mark.parametrize("hq,hkv,D", [(1, 1, 64), (4, 4, 128), (8, 1, 64), (28, 4, 128), (16, 1, 128), (40, 2, 64), (17, 1, 128)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_decode(stage, hq, hkv, D, page):
+    c = decode_case(7, [1, 0, 15, 16, 17, 33, 257, 700, 31, 2000], hq, hkv, D, page)
+    check_decode(c, *stage.decode(c["q"], c["cache"], c["table"], c["lens"]))
+
+
+@pytest.mark.parametrize("page,width", [(16, 1), (32, 3), (256, 1), (128, 40), (16, 700)])
+def test_decode_short_tables_and_wide_ones(stage, page, width):
+    lens = [min(page * width, n) for n in (3, page, page * width, 1)]
+    c = decode_case(8, lens, 6, 2, 128, page, width=width)
+    check_decode(c, *stage.decode(c["q"], c["cache"], c["table"], c["lens"], scale=0.3), scale=0.3)
+
+
+def test_decode_lengths_are_clamped_and_missing_pages_do_not_count(stage):
+    for D in (64, 128):
+        c = decode_case(9, [64, 100, 300, 50], 4, 2, D, 16)
+        c["lens"] = torch.tensor([64, -7, 300, 50], dtype=torch.int32, device=DEV)
+        c["table"][2, 3], c["table"][2, 7], c["table"][2, 18] = -1, 1 << 20, -(1 << 31)
+        c["table"][3, 3] = 1 << 30                             # the last page of two places
+        check_decode(c, *stage.decode(c["q"], c["cache"], c["table"], c["lens"]))
+
+
+def test_decode_strides_streams_and_runs(stage):
+    c = decode_case(11, [5000, 40, 1234], 8, 2, 128, 64)
+    out, lse = stage.decode(c["q"], c["cache"], c["table"], c["lens"])
+    check_decode(c, out, lse)
+    wide = torch.full((3, 9 * 128 + 8), float("nan"), dtype=torch.bfloat16, device=DEV)
+    q = wide[:, 128:9 * 128].unflatten(1, (8, 128))
+    q.copy_(c["q"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = stage.decode(q, c["cache"], c["table"], c["lens"])
+    side.synchronize()
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+def test_decode_agrees_with_attention_over_the_rows_read_back(stage):
+    c = decode_case(12, [777, 64, 130], 12, 4, 128, 32)
+    out, lse = stage.decode(c["q"], c["cache"], c["table"], c["lens"])
+    cu_k = torch.tensor([0, 777, 841, 971], dtype=torch.int32, device=DEV)
+    k, v = stage.read_cache(c["cache"], c["table"], cu_k, 971)
+    ref, ref_lse = stage.attention(c["q"], k, v, torch.arange(4, dtype=torch.int32, device=DEV), cu_k)
+    assert float((out.float() - ref.float()).norm() / ref.float().norm()) <= 6e-3           # both within 4e-3, mostly the same roundings
+    assert float((lse - ref_lse.t()).abs().max()) <= 1e-4
+
+
+def test_a_value_group_and_a_key_group_that_are_not_finite(stage):
+    c = decode_case(14, [90, 90], 4, 2, 128, 16)
+    page, at = int(c["table"][0, 40 // 16]), 40 % 16
+    c["cache"].v_exp[page, 1, at, 2] = 255                      # elements 64 .. 95 of the second key head
+    out, lse = stage.decode(c["q"], c["cache"], c["table"], c["lens"])
+    hurt = torch.zeros((2, 4, 128), dtype=torch.bool, device=DEV)
+    hurt[0, 2:, 64:96] = True
+    assert torch.equal(out.isnan(), hurt) and bool(lse.isfinite().all())
+    c["cache"].v_exp[page, 1, at, 2] = 127
+    c["cache"].k_exp[page, 0, at, 3] = 255
+    out, lse = stage.decode(c["q"], c["cache"], c["table"], c["lens"])
+    hurt[:] = False
+    hurt[0, :2] = True
+    assert torch.equal(out.isnan(), hurt) and torch.equal(lse.isnan(), hurt[:, :, 0])
+
+
+def test_pages_beyond_32_bit_offsets(stage):
+    """The last pages of caches of 9 * 2^30 elements."""
+    D, page, hkv = 128, 256, 8
+    n_pages = 9 * 2 ** 30 // (D * page * hkv)
+    cache = new_cache(n_pages, hkv, page, D)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, v = (torch.randn((600, hkv, D), generator=g, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    pages = torch.tensor([[n_pages - 1, 0, n_pages - 2]], dtype=torch.int32, device=DEV)
+    t = torch.arange(600, device=DEV)
+    stage.write_cache(cache, k, v, pages[0].long()[t // page] * page + t % page)
+    small = new_cache(3, hkv, page, D)
+    order = torch.tensor([[0, 1, 2]], dtype=torch.int32, device=DEV)
+    stage.write_cache(small, k, v, t)
+    cu = torch.tensor([0, 600], dtype=torch.int32, device=DEV)
+    for a, b in zip(stage.read_cache(cache, pages, cu, 600), stage.read_cache(small, order, cu, 600)):
+        assert torch.equal(a, b)
+    q, lens = torch.randn((1, 16, D), generator=g, device=DEV, dtype=torch.bfloat16), torch.tensor([600], dtype=torch.int32, device=DEV)
+    for a, b in zip(stage.decode(q, cache, pages, lens), stage.decode(q, small, order, lens)):
+        assert torch.equal(a, b)
