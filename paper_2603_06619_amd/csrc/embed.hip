@@ -72,14 +72,59 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a) {
 }
 
 // ------------------------------------------------------------------ the sort ----
-// By digits from the lowest on, each pass stable.  A workgroup takes a tile of 1024 x kPer pairs; inside it, a wavefront ranks 64 pairs at a time by ballots
-// over the digit's bits.
-constexpr int kThreads = 1024, kSortWaves = kThreads / 64, kMostBits = 9, kMostBins = 1 << kMostBits;
-constexpr int kSmallPer = 8, kPer = 4;                     // pairs per thread: all of a small call in one workgroup; a tile of a larger one
-constexpr int kSmall = kThreads * kSmallPer, kTile = kThreads * kPer;
+struct SortArgs {
+  const int32_t *ids_in, *rows_in;      // rows_in NULL: the first pass, ids as the caller has them
+  int32_t *ids_out, *rows_out, *counts;
+  int64_t n;
+  int32_t V;
+  int shift, bits, tiles;
+  bool scanned;                         // counts hold places
+};
+
+__device__ __forceinline__ int32_t key_of(int32_t id, int32_t V) { return (uint32_t)id < (uint32_t)V ? id : V; }
+
+// Up to kRanked pairs: a pair's place is the number of pairs before it, counted outright, two instructions each.  64 pairs per workgroup, whose wavefronts share the others.
+constexpr int kRanked = 8192, kRankWaves = 16;
+__global__ void __launch_bounds__(64 * kRankWaves) rank_kernel(SortArgs a) {
+  __shared__ __attribute__((aligned(16))) int32_t keys[kRanked];
+  __shared__ int counts[kRankWaves][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)a.n, blocks = (n + 63) >> 6;
+  for (int i = threadIdx.x; i < 64 * blocks; i += 64 * kRankWaves) keys[i] = i < n ? key_of(a.ids_in[i], a.V) : INT32_MAX;
+  __syncthreads();
+  const int mine = blockIdx.x, it = keys[64 * mine + lane], key = it < INT32_MAX ? it : 0;       // (what a place without a pair counts is not used)
+  int before = 0;
+  for (int b = wave; b < blocks; b += kRankWaves) {
+    if (b == mine) {
+      for (int j = 0; j < 64; ++j) before += keys[64 * b + j] < key + (j < lane);      // (keys that are not there are never below)
+    } else {
+      const int limit = b < mine ? key + 1 : key;
+#pragma unroll
+      for (int j = 0; j < 64; j += 4) {
+        typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+        const i32x4 x = *(const i32x4*)(keys + 64 * b + j);
+        before += (x[0] < limit) + (x[1] < limit) + (x[2] < limit) + (x[3] < limit);
+      }
+    }
+  }
+  counts[wave][lane] = before;
+  __syncthreads();
+  if (wave || 64 * mine + lane >= n) return;
+  before = 0;
+#pragma unroll
+  for (int w = 0; w < kRankWaves; ++w) before += counts[w][lane];
+  a.ids_out[before] = key;
+  a.rows_out[before] = 64 * mine + lane;
+}
+
+// More pairs: by digits from the lowest on, each pass stable.  A workgroup of W wavefronts takes a tile of 64 W kPer pairs, each wavefront ranking 64 at a time by
+// ballots over the digit's bits.
+constexpr int kMostBits = 9, kMostBins = 1 << kMostBits;
+constexpr int kPer = 4;                                    // pairs per thread
+constexpr int kFewWaves = 4, kManyWaves = 16;              // of a tile: few, for the time that one takes; many for few tiles
 constexpr int kDirectTiles = 64;                           // up to so many tiles, each adds up the counts of those before it by itself
 
 // Exclusive prefix sum over the workgroup
+template <int W>
 __device__ __forceinline__ int block_scan(int x, int* wave_sums) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int sum = x;
@@ -92,25 +137,27 @@ __device__ __forceinline__ int block_scan(int x, int* wave_sums) {
   __syncthreads();
   int before = 0;
 #pragma unroll
-  for (int w = 0; w < kSortWaves; ++w) before += w < wave ? wave_sums[w] : 0;
+  for (int w = 0; w < W; ++w) before += w < wave ? wave_sums[w] : 0;
   __syncthreads();
   return before + sum - x;
 }
 
+template <int W>
 struct SortShared {
-  int counts[kSortWaves][kMostBins];      // of a wavefront and digit; then the place of its first pair
-  int wave_sums[kSortWaves];
+  int counts[W][kMostBins];               // of a wavefront and digit; then the place of its first pair
+  int wave_sums[W];
 };
 
-// place[e]: where pair e of this thread (number wave * 64 * P + 64 e + lane of the tile) lies in the tile sorted by its digit
-template <int P>
-__device__ __forceinline__ void rank_tile(SortShared& s, const int (&digit)[P], int bits, int (&place)[P]) {
+// place[e]: where pair e of this thread (number wave * 64 * kPer + 64 e + lane of the tile) lies in the tile sorted by its digit
+template <int W>
+__device__ __forceinline__ void rank_tile(SortShared<W>& s, const int (&digit)[kPer], int bits, int (&place)[kPer]) {
+  constexpr int kThreads = 64 * W;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << bits;
-  for (int i = threadIdx.x; i < kSortWaves * bins; i += kThreads) s.counts[i >> bits][i & (bins - 1)] = 0;
+  for (int i = threadIdx.x; i < W * bins; i += kThreads) s.counts[i >> bits][i & (bins - 1)] = 0;
   __syncthreads();
   volatile int* mine = s.counts[wave];
 #pragma unroll
-  for (int e = 0; e < P; ++e) {
+  for (int e = 0; e < kPer; ++e) {
     uint64_t same = ~uint64_t{0};
     for (int b = 0; b < bits; ++b) {
       const bool set = (digit[e] >> b) & 1;
@@ -125,98 +172,48 @@ __device__ __forceinline__ void rank_tile(SortShared& s, const int (&digit)[P], 
     __builtin_amdgcn_wave_barrier();
   }
   __syncthreads();
-  // digits in order, of each the wavefronts in order: bins * 16 entries, some per thread, or threads without any
-  const int total = bins * kSortWaves, per = total > kThreads ? total / kThreads : 1, first = threadIdx.x * per;
+  // digits in order, of each the wavefronts in order: some entries per thread, or threads without any
+  const int total = bins * W, per = total > kThreads ? total / kThreads : 1, first = threadIdx.x * per;
   int sum = 0;
-  for (int i = first; i < first + per && i < total; ++i) sum += s.counts[i % kSortWaves][i / kSortWaves];
-  sum = block_scan(sum, s.wave_sums);
+  for (int i = first; i < first + per && i < total; ++i) sum += s.counts[i % W][i / W];
+  sum = block_scan<W>(sum, s.wave_sums);
   for (int i = first; i < first + per && i < total; ++i) {
-    const int n = s.counts[i % kSortWaves][i / kSortWaves];
-    s.counts[i % kSortWaves][i / kSortWaves] = sum;
+    const int n = s.counts[i % W][i / W];
+    s.counts[i % W][i / W] = sum;
     sum += n;
   }
   __syncthreads();
 #pragma unroll
-  for (int e = 0; e < P; ++e) place[e] += s.counts[wave][digit[e]];
+  for (int e = 0; e < kPer; ++e) place[e] += s.counts[wave][digit[e]];
 }
 
-struct SortArgs {
-  const int32_t *ids_in, *rows_in;      // rows_in NULL: the first pass, ids as the caller has them
-  int32_t *ids_out, *rows_out, *counts;
-  int64_t n;
-  int32_t V;
-  int shift, bits, tiles, passes;
-  bool scanned;                         // counts hold places
-};
-
-__device__ __forceinline__ int32_t key_of(int32_t id, int32_t V) { return (uint32_t)id < (uint32_t)V ? id : V; }
-
-// All passes of a small call
-__global__ void __launch_bounds__(kThreads) sort_small_kernel(SortArgs a) {
-  __shared__ SortShared s;
-  __shared__ int32_t keys[kSmall];
-  __shared__ uint16_t rows[kSmall];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int key[kSmallPer], row[kSmallPer], digit[kSmallPer], place[kSmallPer];
-#pragma unroll
-  for (int e = 0; e < kSmallPer; ++e) {
-    const int i = wave * 64 * kSmallPer + 64 * e + lane;
-    key[e] = i < a.n ? key_of(a.ids_in[i], a.V) : INT32_MAX;       // behind all others, in every pass
-    row[e] = i;
-  }
-  for (int pass = 0; pass < a.passes; ++pass) {
-    const int shift = pass * a.bits, mask = (1 << a.bits) - 1;
-#pragma unroll
-    for (int e = 0; e < kSmallPer; ++e) digit[e] = (key[e] >> shift) & mask;
-    rank_tile<kSmallPer>(s, digit, a.bits, place);
-#pragma unroll
-    for (int e = 0; e < kSmallPer; ++e) {
-      keys[place[e]] = key[e];
-      rows[place[e]] = (uint16_t)row[e];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < kSmallPer; ++e) {
-      const int i = wave * 64 * kSmallPer + 64 * e + lane;
-      key[e] = keys[i];
-      row[e] = rows[i];
-    }
-    __syncthreads();
-  }
-#pragma unroll
-  for (int e = 0; e < kSmallPer; ++e) {
-    const int i = wave * 64 * kSmallPer + 64 * e + lane;
-    if (i < a.n) {
-      a.ids_out[i] = key[e];
-      a.rows_out[i] = row[e];
-    }
-  }
-}
-
-// counts[bin][tile]
-__global__ void __launch_bounds__(kThreads) sort_count_kernel(SortArgs a) {
+// counts[bin][tile] for the scan, else counts[tile][bin]
+template <int W>
+__global__ void __launch_bounds__(64 * W) sort_count_kernel(SortArgs a) {
+  constexpr int kThreads = 64 * W;
   __shared__ int bins[kMostBins];
   const int n_bins = 1 << a.bits;
-  if ((int)threadIdx.x < n_bins) bins[threadIdx.x] = 0;
+  for (int i = threadIdx.x; i < n_bins; i += kThreads) bins[i] = 0;
   __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * kTile;
+  const int64_t first = (int64_t)blockIdx.x * kThreads * kPer;
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
     const int64_t i = first + e * kThreads + threadIdx.x;
     if (i < a.n) atomicAdd(&bins[(key_of(a.ids_in[i], a.V) >> a.shift) & (n_bins - 1)], 1);
   }
   __syncthreads();
-  if ((int)threadIdx.x < n_bins) a.counts[(int64_t)threadIdx.x * a.tiles + blockIdx.x] = bins[threadIdx.x];
+  for (int i = threadIdx.x; i < n_bins; i += kThreads) a.counts[a.scanned ? (int64_t)i * a.tiles + blockIdx.x : (int64_t)blockIdx.x * n_bins + i] = bins[i];
 }
 
 // counts[bin][tile] -> those of the tiles before, and behind them all tiles' of the bin, in counts[bins * tiles + bin]
-__global__ void __launch_bounds__(kThreads) sort_scan_kernel(SortArgs a) {
-  __shared__ int wave_sums[kSortWaves], all;
+__global__ void __launch_bounds__(64 * kManyWaves) sort_scan_kernel(SortArgs a) {
+  constexpr int kThreads = 64 * kManyWaves;
+  __shared__ int wave_sums[kManyWaves], all;
   int32_t* of = a.counts + (int64_t)blockIdx.x * a.tiles;
   int before = 0;
   for (int first = 0; first < a.tiles; first += kThreads) {
     const int i = first + (int)threadIdx.x, x = i < a.tiles ? of[i] : 0;
-    const int sum = block_scan(x, wave_sums);
+    const int sum = block_scan<kManyWaves>(x, wave_sums);
     if (i < a.tiles) of[i] = before + sum;
     if (threadIdx.x == kThreads - 1) all = sum + x;
     __syncthreads();
@@ -226,35 +223,51 @@ __global__ void __launch_bounds__(kThreads) sort_scan_kernel(SortArgs a) {
   if (threadIdx.x == 0) a.counts[((int64_t)a.tiles << a.bits) + blockIdx.x] = before;
 }
 
-__global__ void __launch_bounds__(kThreads) sort_scatter_kernel(SortArgs a) {
-  __shared__ SortShared s;
+template <int W>
+__global__ void __launch_bounds__(64 * W) sort_scatter_kernel(SortArgs a) {
+  constexpr int kThreads = 64 * W, kTile = kThreads * kPer, kBins = (kMostBins + kThreads - 1) / kThreads;
+  __shared__ SortShared<W> s;
   __shared__ int to[kMostBins];           // place of the tile's first pair of a digit, minus its place inside the tile
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_bins = 1 << a.bits, tile = blockIdx.x;
-  int all = 0, before = 0;
-  if ((int)threadIdx.x < n_bins) {
-    const int32_t* of = a.counts + (int64_t)threadIdx.x * a.tiles;
+  // the thread's digits kBins * thread, ...: pairs of these in all tiles, and in those before this one
+  int all[kBins] = {}, before[kBins] = {}, sum = 0;
+#pragma unroll
+  for (int b = 0; b < kBins; ++b) {
+    const int bin = (int)threadIdx.x * kBins + b;
+    if (bin >= n_bins) continue;
     if (a.scanned) {
-      before = of[tile];
-      all = a.counts[((int64_t)a.tiles << a.bits) + threadIdx.x];
+      before[b] = a.counts[(int64_t)bin * a.tiles + tile];
+      all[b] = a.counts[((int64_t)a.tiles << a.bits) + bin];
     } else {
-      for (int t = 0; t < a.tiles; ++t) {
-        const int x = of[t];
-        all += x;
-        before += t < tile ? x : 0;
+      for (int t0 = 0; t0 < a.tiles; t0 += 16) {            // (in a row they would be a chain of loads)
+        int x[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) x[u] = t0 + u < a.tiles ? a.counts[(t0 + u) * n_bins + bin] : 0;
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+          all[b] += x[u];
+          before[b] += t0 + u < tile ? x[u] : 0;
+        }
       }
     }
+    sum += all[b];
   }
-  before += block_scan(all, s.wave_sums);
+  sum = block_scan<W>(sum, s.wave_sums);
   int key[kPer], row[kPer], digit[kPer], place[kPer];
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
     const int64_t i = (int64_t)tile * kTile + wave * 64 * kPer + 64 * e + lane;
-    key[e] = i < a.n ? key_of(a.ids_in[i], a.V) : INT32_MAX;
+    key[e] = i < a.n ? key_of(a.ids_in[i], a.V) : INT32_MAX;             // behind all others, in every pass
     row[e] = i < a.n ? a.rows_in ? a.rows_in[i] : (int32_t)i : -1;
     digit[e] = (key[e] >> a.shift) & (n_bins - 1);
   }
-  rank_tile<kPer>(s, digit, a.bits, place);
-  if ((int)threadIdx.x < n_bins) to[threadIdx.x] = before - s.counts[0][threadIdx.x];
+  rank_tile<W>(s, digit, a.bits, place);
+#pragma unroll
+  for (int b = 0; b < kBins; ++b) {
+    const int bin = (int)threadIdx.x * kBins + b;
+    if (bin < n_bins) to[bin] = sum + before[b] - s.counts[0][bin];
+    sum += all[b];
+  }
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
@@ -270,12 +283,13 @@ struct SumArgs {
   const int32_t *ids, *rows;            // sorted
   const char* dout;
   float *dE, *part;                     // part: [pieces][2][H], of the run that came in from the piece before, of the one that goes on behind
-  int64_t n, dout_bytes;
+  int64_t n, dout_bytes, sum_blocks;    // the other workgroups write zeros
   int32_t V, H;
-  int piece, slabs;                     // pairs per piece; groups of four 16-byte columns of 64 lanes
+  int piece, slabs, zero_rows;          // pairs per piece, at most 64; workgroups per row; rows of dE per workgroup that writes zeros
   float scale;
   int accumulate;
 };
+constexpr int kMostZeroRows = 2048;
 
 template <typename T>
 __device__ __forceinline__ void write_run(const SumArgs& a, int32_t id, int at, const float (&acc)[Piece<T>::kElements]) {
@@ -288,62 +302,145 @@ __device__ __forceinline__ void write_run(const SumArgs& a, int32_t id, int at, 
   }
 }
 
+// First place whose id is not below v, found by the whole wavefront: 64 probes per round
+__device__ __forceinline__ int64_t lower_bound(const int32_t* ids, int64_t n, int32_t v) {
+  const int lane = threadIdx.x & 63;
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t step = (hi - lo + 63) >> 6, probe = lo + lane * step;
+    const int below = __popcll(__ballot(probe < hi && ids[probe] < v));
+    if (below == 0) return lo;
+    const int64_t past = lo + below * step;
+    lo += (below - 1) * step + 1;
+    hi = step == 1 ? lo : past < hi ? past : hi;
+  }
+  return lo;
+}
+
+// Zeros into those of zero_rows rows that no pair has
+__device__ __forceinline__ void write_zeros(const SumArgs& a, int64_t block) {
+  __shared__ uint32_t used[kMostZeroRows / 32];
+  __shared__ int64_t range[2];
+  const int64_t v0 = block * a.zero_rows, v1 = v0 + a.zero_rows < a.V ? v0 + a.zero_rows : a.V;
+  for (int i = threadIdx.x; i < kMostZeroRows / 32; i += blockDim.x) used[i] = 0;
+  if (threadIdx.x < 64) {
+    const int64_t first = lower_bound(a.ids, a.n, (int32_t)v0), end = lower_bound(a.ids, a.n, (int32_t)v1);
+    if (threadIdx.x == 0) {
+      range[0] = first;
+      range[1] = end;
+    }
+  }
+  __syncthreads();
+  for (int64_t p = range[0] + threadIdx.x; p < range[1]; p += blockDim.x) {
+    const int i = (int)(a.ids[p] - v0);
+    atomicOr(&used[i >> 5], 1u << (i & 31));
+  }
+  __syncthreads();
+  const int chunks = a.H / 4;           // of 16 bytes
+  if (chunks >= (int)blockDim.x) {
+    for (int64_t v = v0; v < v1; ++v) {
+      if (used[(v - v0) >> 5] >> ((v - v0) & 31) & 1) continue;
+      f32x4* to = (f32x4*)(a.dE + v * a.H);
+      for (int i = threadIdx.x; i < chunks; i += blockDim.x) to[i] = f32x4{};
+    }
+  } else {
+    f32x4* to = (f32x4*)(a.dE + v0 * a.H);
+    for (int64_t i = threadIdx.x; i < (v1 - v0) * chunks; i += blockDim.x) {
+      const int v = (int)(i / chunks);
+      if (!(used[v >> 5] >> (v & 31) & 1)) to[i] = f32x4{};
+    }
+  }
+}
+
 template <typename T>
 __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a) {
-  constexpr int kE = Piece<T>::kElements;
-  const int slab = blockIdx.x % a.slabs;
-  const int64_t piece = blockIdx.x / a.slabs, p0 = piece * a.piece, p1 = p0 + a.piece < a.n ? p0 + a.piece : a.n;
-  const int at = (slab * 256 + (int)threadIdx.x) * kE;
-  if (at >= a.H) return;
-  const bool from_before = p0 > 0 && a.ids[p0 - 1] == a.ids[p0], goes_on = p1 < a.n && a.ids[p1 - 1] == a.ids[p1];
-  int32_t id = a.ids[p0];
-  bool first_run = true;
+  constexpr int kE = Piece<T>::kElements, kAhead = 8;
+  if (blockIdx.x >= a.sum_blocks) {
+    write_zeros(a, blockIdx.x - a.sum_blocks);
+    return;
+  }
+  const int slab = blockIdx.x % a.slabs, lane = threadIdx.x & 63;
+  const int64_t piece = blockIdx.x / a.slabs, p0 = piece * a.piece;
+  const int count = p0 + a.piece < a.n ? a.piece : (int)(a.n - p0), at = (slab * (int)blockDim.x + (int)threadIdx.x) * kE;
+  // the piece's pairs, one per lane, and the ids beside it
+  const int64_t p = p0 + (lane < count ? lane : count - 1);
+  const int ids = a.ids[p], rows = a.rows[p];
+  const int first = __builtin_amdgcn_readfirstlane(ids);
+  const bool from_before = p0 > 0 && a.ids[p0 - 1] == first, goes_on = p0 + count < a.n && a.ids[p0 + count] == __builtin_amdgcn_readlane(ids, count - 1);
+  const bool there = at < a.H;          // (all lanes stay: others read theirs)
+  const char* from = a.dout + (there ? at : 0) * (int64_t)sizeof(T);
   float acc[kE] = {};
-  auto flush = [&](bool last) {
-    if (id >= a.V) return;
-    const int side = first_run && from_before ? 0 : last && goes_on ? 1 : -1;
-    if (side < 0) {
-      write_run<T>(a, id, at, acc);
-    } else {
-      float* to = a.part + (piece * 2 + side) * a.H + at;
+  bool first_run = true;
+  for (int j0 = 0; j0 < count; j0 += kAhead) {
+    u32x4 x[kAhead];
 #pragma unroll
-      for (int i = 0; i < kE; i += 4) *(f32x4*)(to + i) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
-    }
-  };
-  for (int64_t p = p0; p < p1; ++p) {
-    const int32_t next = a.ids[p];
-    if (next != id) {
-      flush(false);
+    for (int u = 0; u < kAhead; ++u)
+      if (j0 + u < count) x[u] = *(const u32x4*)(from + __builtin_amdgcn_readlane(rows, j0 + u) * a.dout_bytes);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = j0 + u;
+      if (j >= count) continue;
+      Piece<T>::add(acc, x[u]);
+      const int id = __builtin_amdgcn_readlane(ids, j);
+      const bool last = j + 1 == count;
+      if (!last && __builtin_amdgcn_readlane(ids, j + 1) == id) continue;
+      if (id < a.V && there) {
+        const int side = first_run && from_before ? 0 : last && goes_on ? 1 : -1;
+        if (side < 0) {
+          write_run<T>(a, id, at, acc);
+        } else {
+          float* to = a.part + (piece * 2 + side) * a.H + at;
+#pragma unroll
+          for (int i = 0; i < kE; i += 4) *(f32x4*)(to + i) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+        }
+      }
       first_run = false;
-      id = next;
 #pragma unroll
       for (int i = 0; i < kE; ++i) acc[i] = 0.f;
     }
-    Piece<T>::add(acc, *(const u32x4*)(a.dout + a.rows[p] * a.dout_bytes + at * (int64_t)sizeof(T)));
   }
-  flush(true);
 }
 
 // The parts of a run that begins in this piece and goes on behind it
 template <typename T>
 __global__ void __launch_bounds__(256) embed_join_kernel(SumArgs a) {
-  constexpr int kE = Piece<T>::kElements;
-  const int slab = blockIdx.x % a.slabs;
+  constexpr int kE = Piece<T>::kElements, kAhead = 4;
+  const int slab = blockIdx.x % a.slabs, lane = threadIdx.x & 63;
   const int64_t piece = blockIdx.x / a.slabs, p0 = piece * a.piece, p1 = p0 + a.piece;
-  const int at = (slab * 256 + (int)threadIdx.x) * kE;
-  if (at >= a.H || p1 >= a.n) return;
-  const int32_t id = a.ids[p1];
-  if (id >= a.V || a.ids[p1 - 1] != id || (a.ids[p0] == id && p0 > 0 && a.ids[p0 - 1] == id)) return;
-  float acc[kE];
-  const float* from = a.part + (piece * 2 + 1) * a.H + at;
+  if (p1 >= a.n) return;
+  const int32_t id = a.ids[p1], behind = a.ids[p1 - 1], first = a.ids[p0], before = a.ids[p0 > 0 ? p0 - 1 : 0];
+  if (id >= a.V || behind != id || (first == id && p0 > 0 && before == id)) return;
+  const int at = (slab * (int)blockDim.x + (int)threadIdx.x) * kE;
+  const bool there = at < a.H;
+  float acc[kE] = {};
+  if (there) {
+    const float* from = a.part + (piece * 2 + 1) * a.H + at;
 #pragma unroll
-  for (int i = 0; i < kE; ++i) acc[i] = from[i];
-  for (int64_t c = piece + 1; c * a.piece < a.n && a.ids[c * a.piece] == id; ++c) {
-    from = a.part + c * 2 * a.H + at;
-#pragma unroll
-    for (int i = 0; i < kE; ++i) acc[i] += from[i];
+    for (int i = 0; i < kE; ++i) acc[i] = from[i];
   }
-  write_run<T>(a, id, at, acc);
+  // 64 pieces at a time: those that begin with the run
+  for (int64_t c0 = piece + 1;; c0 += 64) {
+    const int64_t q = (c0 + lane) * a.piece;
+    const uint64_t with = __ballot(q < a.n && a.ids[q < a.n ? q : 0] == id);
+    const int parts = with == ~uint64_t{0} ? 64 : __builtin_ctzll(~with);
+    if (there) {
+      const float* from = a.part + c0 * 2 * a.H + at;
+      for (int c = 0; c < parts; c += kAhead) {
+        f32x4 x[kAhead][kE / 4] = {};
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+          for (int i = 0; i < kE / 4; ++i)
+            if (c + u < parts) x[u][i] = *(const f32x4*)(from + (c + u) * (int64_t)2 * a.H + 4 * i);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+          for (int i = 0; i < kE; ++i) acc[i] += x[u][i >> 2][i & 3];
+      }
+    }
+    if (parts < 64) break;
+  }
+  if (there) write_run<T>(a, id, at, acc);
 }
 
 bool misaligned(const void* p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
@@ -357,7 +454,8 @@ nat_status embed_shape(int64_t n_rows, int32_t V, int32_t H, int32_t dtype, floa
 }
 
 struct SortPlan {
-  int passes, bits, tiles, piece, slabs;
+  int passes, bits, tiles, piece;
+  bool few;                             // tiles of kFewWaves wavefronts
   int64_t pieces;
   size_t pairs, counts, parts;          // bytes of each of four arrays of pairs, of the counts, of the parts
 };
@@ -366,16 +464,30 @@ SortPlan sort_plan(int64_t n, int32_t V, int32_t H) {
   const int bits = 32 - __builtin_clz((unsigned)V);
   p.passes = (bits + kMostBits - 1) / kMostBits;
   p.bits = (bits + p.passes - 1) / p.passes;
-  p.tiles = (int)((n + kTile - 1) / kTile);
-  p.slabs = (H + 1023) / 1024;          // of f32; bf16 has half as many
+  p.few = n <= kDirectTiles * 64 * kFewWaves * kPer;
+  const int64_t tile = 64 * (p.few ? kFewWaves : kManyWaves) * kPer;
+  p.tiles = (int)((n + tile - 1) / tile);
   p.piece = 8;
-  while (p.piece < 64 && n / p.piece * p.slabs > 2048) p.piece *= 2;
+  while (p.piece < 64 && n / p.piece * ((H + 1023) / 1024) > 2048) p.piece *= 2;
   p.pieces = (n + p.piece - 1) / p.piece;
   auto whole = [](size_t x) { return (x + 255) / 256 * 256; };
   p.pairs = whole((size_t)n * 4);
-  p.counts = n > kSmall ? whole((((size_t)p.tiles + 1) << p.bits) * 4) : 0;
+  p.counts = n > kRanked ? whole((((size_t)p.tiles + 1) << p.bits) * 4) : 0;
   p.parts = whole((size_t)p.pieces * 2 * H * 4);
   return p;
+}
+
+template <int W>
+nat_status sort_pass(const SortArgs& a, hipStream_t s) {
+  sort_count_kernel<W><<<a.tiles, 64 * W, 0, s>>>(a);
+  NAT_LAUNCH_CHECK();
+  if (a.scanned) {
+    sort_scan_kernel<<<1 << a.bits, 64 * kManyWaves, 0, s>>>(a);
+    NAT_LAUNCH_CHECK();
+  }
+  sort_scatter_kernel<W><<<a.tiles, 64 * W, 0, s>>>(a);
+  NAT_LAUNCH_CHECK();
+  return NAT_OK;
 }
 
 }  // namespace
@@ -417,52 +529,48 @@ extern "C" nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const 
   const nat_status st = embed_shape(n_rows, V, H, dtype, scale, dout_stride, &size);
   if (st != NAT_OK) return st;
   if (V > (1 << 30) || n_rows >= (int64_t{1} << 29)) return NAT_BAD_SHAPE;
-  const SortPlan p = sort_plan(n_rows, V, H);
-  const int slabs = dtype == NAT_DTYPE_BF16 ? (p.slabs + 1) / 2 : p.slabs;
-  if (p.pieces * slabs > kMaxWorkItems / 256) return NAT_BAD_SHAPE;
+  const SortPlan p = sort_plan(n_rows > 0 ? n_rows : 1, V, H);
+  // 16 bytes per thread, up to 256 threads
+  const int64_t lanes = (int64_t)H * size / 16;
+  const int threads = lanes >= 256 ? 256 : (int)((lanes + 63) / 64 * 64), slabs = (int)((lanes + threads - 1) / threads);
+  int zero_rows = 65536 / H < 1 ? 1 : 65536 / H > kMostZeroRows ? kMostZeroRows : 65536 / H;
+  if (zero_rows > V / 1024) zero_rows = V < 2048 ? 1 : V / 1024;
+  const int64_t zero_blocks = accumulate ? 0 : ((int64_t)V + zero_rows - 1) / zero_rows, sum_blocks = p.pieces * slabs;
+  if (sum_blocks + zero_blocks > kMaxWorkItems / threads) return NAT_BAD_SHAPE;
   if (!d_dE || misaligned(d_dE)) return NAT_INVALID_ARG;
   if (n_rows > 0 && (!d_ids || !d_dout || misaligned(d_dout))) return NAT_INVALID_ARG;
   if (n_rows > 0 && (!d_ws || ws_bytes < nat_embed_bwd_workspace_bytes(n_rows, V, H))) return NAT_WORKSPACE_TOO_SMALL;
   if (misaligned(d_ws, 256)) return NAT_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_EMBED, s);
-  if (!accumulate) {
-    const nat_status filled = fill_zero_f32(d_dE, (size_t)V * H, s);
-    if (filled != NAT_OK) return filled;
-  }
-  if (n_rows == 0) return NAT_OK;
+  if (n_rows == 0) return accumulate ? NAT_OK : fill_zero_f32(d_dE, (size_t)V * H, s);
   char* ws = (char*)d_ws;
   int32_t* pair[4];
   for (int i = 0; i < 4; ++i) pair[i] = (int32_t*)(ws + i * p.pairs);
-  SortArgs a{d_ids, nullptr, pair[0], pair[1], (int32_t*)(ws + 4 * p.pairs), n_rows, V, 0, p.bits, p.tiles, p.passes, p.tiles > kDirectTiles};
-  if (n_rows <= kSmall) {
-    sort_small_kernel<<<1, kThreads, 0, s>>>(a);
+  SortArgs a{d_ids, nullptr, pair[0], pair[1], (int32_t*)(ws + 4 * p.pairs), n_rows, V, 0, p.bits, p.tiles, p.tiles > kDirectTiles};
+  if (n_rows <= kRanked) {
+    rank_kernel<<<(unsigned)((n_rows + 63) / 64), 64 * kRankWaves, 0, s>>>(a);
     NAT_LAUNCH_CHECK();
   } else {
     for (int pass = 0; pass < p.passes; ++pass) {
       a.shift = pass * p.bits;
       a.ids_out = pair[pass & 1 ? 2 : 0];
       a.rows_out = pair[pass & 1 ? 3 : 1];
-      sort_count_kernel<<<p.tiles, kThreads, 0, s>>>(a);
-      NAT_LAUNCH_CHECK();
-      if (a.scanned) {
-        sort_scan_kernel<<<1 << p.bits, kThreads, 0, s>>>(a);
-        NAT_LAUNCH_CHECK();
-      }
-      sort_scatter_kernel<<<p.tiles, kThreads, 0, s>>>(a);
-      NAT_LAUNCH_CHECK();
+      const nat_status sorted = p.few ? sort_pass<kFewWaves>(a, s) : sort_pass<kManyWaves>(a, s);
+      if (sorted != NAT_OK) return sorted;
       a.ids_in = a.ids_out;
       a.rows_in = a.rows_out;
     }
   }
-  SumArgs b{a.ids_out, a.rows_out, (const char*)d_dout, d_dE, (float*)(ws + 4 * p.pairs + p.counts), n_rows, (dout_stride ? dout_stride : H) * size, V, H,
-            p.piece, slabs, scale, accumulate != 0};
-  const int64_t blocks = p.pieces * slabs;
-  if (dtype == NAT_DTYPE_BF16) embed_sum_kernel<uint16_t><<<(unsigned)blocks, 256, 0, s>>>(b);
-  else embed_sum_kernel<float><<<(unsigned)blocks, 256, 0, s>>>(b);
+  SumArgs b{a.ids_out, a.rows_out, (const char*)d_dout, d_dE, (float*)(ws + 4 * p.pairs + p.counts), n_rows, (dout_stride ? dout_stride : H) * size, sum_blocks,
+            V, H, p.piece, slabs, zero_rows, scale, accumulate != 0};
+  const unsigned all = (unsigned)(sum_blocks + zero_blocks);
+  if (dtype == NAT_DTYPE_BF16) embed_sum_kernel<uint16_t><<<all, threads, 0, s>>>(b);
+  else embed_sum_kernel<float><<<all, threads, 0, s>>>(b);
   NAT_LAUNCH_CHECK();
-  if (dtype == NAT_DTYPE_BF16) embed_join_kernel<uint16_t><<<(unsigned)blocks, 256, 0, s>>>(b);
-  else embed_join_kernel<float><<<(unsigned)blocks, 256, 0, s>>>(b);
+  if (p.pieces == 1) return NAT_OK;
+  if (dtype == NAT_DTYPE_BF16) embed_join_kernel<uint16_t><<<(unsigned)sum_blocks, threads, 0, s>>>(b);
+  else embed_join_kernel<float><<<(unsigned)sum_blocks, threads, 0, s>>>(b);
   NAT_LAUNCH_CHECK();
   return NAT_OK;
 }

@@ -298,18 +298,25 @@ __global__ void __launch_bounds__(64 * kWaves) heads_bwd_kernel(HeadsArgs a) {
   }
 }
 
-// The workgroups' sums in order: one workgroup per 16 elements, 16 walkers each.
+// The workgroups' sums in order: one workgroup per kColumns elements, every kWalkers-th part to each walker.
+constexpr int kColumns = 8, kWalkers = 256 / kColumns;
 __global__ void __launch_bounds__(256) heads_weights_kernel(const float* part, int n_parts, int D, float* dwq, float* dwk, int accumulate) {
-  __shared__ float sums[16][17];
-  const int e = blockIdx.x * 16 + (threadIdx.x & 15), walker = threadIdx.x >> 4;
+  __shared__ float sums[kWalkers][kColumns + 1];
+  const int column = threadIdx.x % kColumns, walker = threadIdx.x / kColumns, e = blockIdx.x * kColumns + column;
   float x = 0.f;
-  for (int i = walker; i < n_parts; i += 16) x += part[(int64_t)i * 2 * D + e];
-  sums[walker][threadIdx.x & 15] = x;
+  for (int i0 = walker; i0 < n_parts; i0 += 8 * kWalkers) {
+    float y[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) y[u] = i0 + u * kWalkers < n_parts ? part[(int64_t)(i0 + u * kWalkers) * 2 * D + e] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x += y[u];
+  }
+  sums[walker][column] = x;
   __syncthreads();
   if (walker) return;
   x = 0.f;
 #pragma unroll
-  for (int w = 0; w < 16; ++w) x += sums[w][threadIdx.x];
+  for (int w = 0; w < kWalkers; ++w) x += sums[w][column];
   float* to = e < D ? dwq : dwk;
   if (!to) return;
   to += e < D ? e : e - D;
@@ -318,10 +325,10 @@ __global__ void __launch_bounds__(256) heads_weights_kernel(const float* part, i
 
 bool misaligned(const void* p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
 
-constexpr int kMostBlocks = 2048;
-int blocks_of(int64_t n_rows) {
+constexpr int kMostBlocks = 2048, kMostSums = 768;       // backward: as many as fit at once, each leaves sums
+int blocks_of(int64_t n_rows, int most) {
   const int64_t n = (n_rows + kWaves - 1) / kWaves;
-  return (int)(n < 1 ? 1 : n < kMostBlocks ? n : kMostBlocks);
+  return (int)(n < 1 ? 1 : n < most ? n : most);
 }
 
 nat_status heads_args(const nat_qk_params* p, const void* d_q, const void* d_k, const void* d_q_weight, const void* d_k_weight,
@@ -374,7 +381,7 @@ extern "C" nat_status nat_qk_norm_rope(const nat_qk_params* params, const void* 
   a.k_out = d_k_out;
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_HEADS, s);
-  const int n = blocks_of(a.n_rows);
+  const int n = blocks_of(a.n_rows, kMostBlocks);
   if (params->dtype == NAT_DTYPE_BF16) {
     if (params->head_dim == 128) heads_fwd_kernel<uint16_t, 128><<<n, 64 * kWaves, 0, s>>>(a);
     else heads_fwd_kernel<uint16_t, 64><<<n, 64 * kWaves, 0, s>>>(a);
@@ -388,7 +395,7 @@ extern "C" nat_status nat_qk_norm_rope(const nat_qk_params* params, const void* 
 
 extern "C" size_t nat_qk_norm_rope_bwd_workspace_bytes(int64_t n_rows, int32_t head_dim) {
   if (n_rows <= 0 || n_rows > INT32_MAX || (head_dim != 64 && head_dim != 128)) return 0;
-  return ((size_t)blocks_of(n_rows) * 2 * head_dim * 4 + 255) / 256 * 256;
+  return ((size_t)blocks_of(n_rows, kMostSums) * 2 * head_dim * 4 + 255) / 256 * 256;
 }
 
 extern "C" nat_status nat_qk_norm_rope_bwd(const nat_qk_params* params, const void* d_q, const void* d_k, const void* d_q_weight, const void* d_k_weight,
@@ -412,7 +419,7 @@ extern "C" nat_status nat_qk_norm_rope_bwd(const nat_qk_params* params, const vo
   a.part = weights ? (float*)d_ws : nullptr;
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_HEADS, s);
-  const int n = a.n_rows > 0 ? blocks_of(a.n_rows) : 0, D = params->head_dim;
+  const int n = a.n_rows > 0 ? blocks_of(a.n_rows, kMostSums) : 0, D = params->head_dim;
   if (n > 0) {
     if (params->dtype == NAT_DTYPE_BF16) {
       if (D == 128) heads_bwd_kernel<uint16_t, 128><<<n, 64 * kWaves, 0, s>>>(a);
@@ -424,7 +431,7 @@ extern "C" nat_status nat_qk_norm_rope_bwd(const nat_qk_params* params, const vo
     NAT_LAUNCH_CHECK();
   }
   if (weights && (n > 0 || !accumulate)) {
-    heads_weights_kernel<<<2 * D / 16, 256, 0, s>>>(a.part, n, D, d_dq_weight, d_dk_weight, accumulate);
+    heads_weights_kernel<<<2 * D / kColumns, 256, 0, s>>>(a.part, n, D, d_dq_weight, d_dk_weight, accumulate);
     NAT_LAUNCH_CHECK();
   }
   return NAT_OK;

@@ -4,6 +4,8 @@
 // sequence's own numbers, for any number of workgroups.
 #include "nat_internal.h"
 
+#include <type_traits>
+
 namespace nat {
 namespace {
 
@@ -23,72 +25,97 @@ struct PageArgs {
 __device__ __forceinline__ int clamped(int x, int64_t most) { return x < 0 ? 0 : x < most ? x : (int)most; }
 __device__ __forceinline__ int64_t pages_of(int64_t tokens, int log2) { return (tokens + (1 << log2) - 1) >> log2; }
 
-// Inclusive prefix sum over the workgroup; *all: of all threads
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* wave_sums, int64_t* all) {
+// Sums of numbers that are not negative, at most 2^32 - 1: in any order the same
+__device__ __forceinline__ uint32_t add(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
+
+// Inclusive prefix sum over the wavefront, and over the workgroup: *all of all threads.  One barrier: `sums` may be used again behind the next one.
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
+  auto from = [](uint32_t v, auto ctrl, auto rows) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+  };
+  using std::integral_constant;
+  x = add(x, from(x, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{}));      // 1, 2, 4, 8 lanes on, inside rows of 16
+  x = add(x, from(x, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{}));
+  x = add(x, from(x, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{}));
+  x = add(x, from(x, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{}));
+  x = add(x, from(x, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{}));      // the last of a row to the next one, of two rows to the next two
+  x = add(x, from(x, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{}));
+  return x;
+}
+__device__ __forceinline__ uint32_t block_sum(uint32_t x, uint32_t* sums, uint32_t* all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
-  }
+  x = wave_sum(x);
+  if (lane == 63) sums[wave] = x;
   __syncthreads();
-  if (lane == 63) wave_sums[wave] = x;
-  __syncthreads();
-  int64_t before = 0, sum = 0;
+  uint32_t before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    before += w < wave ? wave_sums[w] : 0;
-    sum += wave_sums[w];
+    before = add(before, w < wave ? sums[w] : 0);
+    total = add(total, sums[w]);
   }
-  *all = sum;
-  return before + x;
+  *all = total;
+  return add(before, x);
 }
 
-// Sequence by sequence: where its rows begin, whether it is served, which pages it gets
-__device__ __forceinline__ void plan(const PageArgs& a, int64_t* wave_sums) {
+// What a sequence's rows are made from
+struct Served { int32_t *cu, *start, *len, *top; };      // offsets; first position, -1: refused; length afterwards; place on the stack of the first new page
+
+// Sequence by sequence: where its rows begin, whether it is served, which pages it gets.  The results go to `mine` where that is not the caller's arrays.
+__device__ __forceinline__ void plan(const PageArgs& a, uint32_t (*sums)[kWaves], const Served* mine) {
   const int64_t most = (int64_t)a.width << a.page_log2;
-  const int n_free = clamped(a.counts[0], a.n_pages);
-  int64_t rows = 0, asked = 0, given = 0;
-  int refused = 0;
-  if (threadIdx.x == 0) a.cu[0] = 0;
-  for (int first = 0; first < a.n_seqs; first += kThreads) {
+  const uint32_t n_free = clamped(a.counts[0], a.n_pages);
+  uint32_t rows = 0, asked = 0, given = 0, refused = 0;
+  for (int first = 0, turn = 0; first < a.n_seqs; first += kThreads, turn ^= 2) {
     const int i = first + (int)threadIdx.x;
     const bool there = i < a.n_seqs;
     const int len = there ? clamped(a.lens[i], most) : 0, more = there && a.change[i] > 0 ? a.change[i] : 0;
-    int64_t all;
-    const int64_t end = rows + block_sum(more, wave_sums, &all);
-    rows += all;
+    uint32_t all;
+    const uint32_t end = add(rows, block_sum(more, sums[turn], &all));
+    rows = add(rows, all);
     bool served = len + (int64_t)more <= most && (more == 0 || end <= a.rows_cap);
-    const int64_t need = served ? pages_of(len + (int64_t)more, a.page_log2) - pages_of(len, a.page_log2) : 0;
-    const int64_t upto = asked + block_sum(need, wave_sums, &all);
-    asked += all;
+    const uint32_t need = served ? (uint32_t)(pages_of(len + (int64_t)more, a.page_log2) - pages_of(len, a.page_log2)) : 0;
+    const uint32_t upto = add(asked, block_sum(need, sums[turn + 1], &all));
+    asked = add(asked, all);
     served = served && (need == 0 || upto <= n_free);
-    block_sum(served ? need : 0, wave_sums, &all);
-    given += all;
-    block_sum(there && !served, wave_sums, &all);
-    refused += (int)all;
+    given += served ? need : 0;
+    refused += there && !served;
     if (there) {
-      a.cu[i + 1] = end < INT32_MAX ? (int)end : INT32_MAX;
-      a.start[i] = served ? len : -1;
-      a.lens_out[i] = served ? len + more : len;
-      a.ws[i] = (int)(n_free - 1 - (upto - need));      // (unused by those that get none)
+      const int cu = end < INT32_MAX ? (int)end : INT32_MAX, start = served ? len : -1, now = served ? len + more : len;
+      const int top = (int)(n_free - 1 - (upto - need));      // (unused by those that get none)
+      a.cu[i + 1] = cu;
+      a.start[i] = start;
+      a.lens_out[i] = now;
+      if (mine) {
+        mine->cu[i + 1] = cu;
+        mine->start[i] = start;
+        mine->len[i] = now;
+        mine->top[i] = top;
+      } else {
+        a.ws[i] = top;
+      }
     }
   }
+  __syncthreads();
+  uint32_t all;
+  block_sum(given, sums[0], &all);
+  const uint32_t left = n_free - all;
+  block_sum(refused, sums[1], &all);
   if (threadIdx.x == 0) {
-    a.counts_out[0] = (int)(n_free - given);
-    a.counts_out[1] = refused;
+    a.cu[0] = 0;
+    if (mine) mine->cu[0] = 0;
+    a.counts_out[0] = (int)left;
+    a.counts_out[1] = (int)all;
   }
 }
 
-// Slots, positions and the table's new entries, a row per thread
-__device__ __forceinline__ void fill_row(const PageArgs& a, int64_t row) {
+// Slot, position and the table's new entry of a row
+__device__ __forceinline__ void fill_row(const PageArgs& a, const Served& s, int64_t row) {
   int64_t slot = -1;
   int pos = 0;
-  if (row < a.cu[a.n_seqs]) {
-    const int seq = rollout_of_pos(a.cu, 0, a.n_seqs, row), start = a.start[seq];
-    const int64_t most = (int64_t)a.width << a.page_log2;
-    const int at = (int)(row - a.cu[seq]);
-    const int64_t to = (int64_t)(start < 0 ? clamped(a.lens_out[seq], most) : start) + at;
+  if (row < s.cu[a.n_seqs]) {
+    const int seq = rollout_of_pos(s.cu, 0, a.n_seqs, row), start = s.start[seq];
+    const int at = (int)(row - s.cu[seq]);
+    const int64_t to = (int64_t)(start < 0 ? s.len[seq] : start) + at;
     pos = to < INT32_MAX ? (int)to : INT32_MAX;              // (a refused sequence may ask for anything)
     if (start >= 0) {
       const int place = pos >> a.page_log2, fresh = (int)pages_of(start, a.page_log2);
@@ -96,7 +123,7 @@ __device__ __forceinline__ void fill_row(const PageArgs& a, int64_t row) {
       if (place < fresh) {
         page = a.table[(int64_t)seq * a.width + place];
       } else {
-        page = a.free_pages[a.ws[seq] - (place - fresh)];
+        page = a.free_pages[s.top[seq] - (place - fresh)];
         if (at == 0 || (pos & ((1 << a.page_log2) - 1)) == 0) a.table[(int64_t)seq * a.width + place] = page;
       }
       if (page >= 0 && page < a.n_pages) slot = ((int64_t)page << a.page_log2) + (pos & ((1 << a.page_log2) - 1));
@@ -107,13 +134,24 @@ __device__ __forceinline__ void fill_row(const PageArgs& a, int64_t row) {
 }
 
 __global__ void __launch_bounds__(kThreads) reserve_plan_kernel(PageArgs a) {
-  __shared__ int64_t wave_sums[kWaves];
-  plan(a, wave_sums);
+  __shared__ uint32_t sums[4][kWaves];
+  plan(a, sums, nullptr);
 }
 
-__global__ void __launch_bounds__(256) reserve_fill_kernel(PageArgs a, int64_t first) {
-  const int64_t row = first + (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (row < a.rows_cap) fill_row(a, row);
+__global__ void __launch_bounds__(256) reserve_fill_kernel(PageArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (row < a.rows_cap) fill_row(a, Served{a.cu, a.start, a.lens_out, a.ws}, row);
+}
+
+// Both for few sequences and rows: one launch.
+constexpr int kFewRows = 4096;
+__global__ void __launch_bounds__(kThreads) reserve_small_kernel(PageArgs a) {
+  __shared__ uint32_t sums[4][kWaves];
+  __shared__ int32_t cu[kThreads + 1], start[kThreads], len[kThreads], top[kThreads];
+  const Served s{cu, start, len, top};
+  plan(a, sums, &s);
+  __syncthreads();
+  for (int64_t row = threadIdx.x; row < a.rows_cap; row += kThreads) fill_row(a, s, row);
 }
 
 // ------------------------------------------------------------------ back ----
@@ -144,14 +182,15 @@ __global__ void __launch_bounds__(256) release_count_kernel(PageArgs a) {
 
 // of many sequences: the pages of those before each
 __global__ void __launch_bounds__(kThreads) release_scan_kernel(PageArgs a) {
-  __shared__ int64_t wave_sums[kWaves];
-  int64_t before = 0;
-  for (int first = 0; first < a.n_seqs; first += kThreads) {
-    const int i = first + (int)threadIdx.x, n = i < a.n_seqs ? a.ws[i] : 0;
-    int64_t all;
-    const int64_t to = before + block_sum(n, wave_sums, &all) - n;
+  __shared__ uint32_t sums[2][kWaves];
+  uint32_t before = 0;
+  for (int first = 0, turn = 0; first < a.n_seqs; first += kThreads, turn ^= 1) {
+    const int i = first + (int)threadIdx.x;
+    const uint32_t n = i < a.n_seqs ? a.ws[i] : 0;
+    uint32_t all;
+    const uint32_t to = add(before, block_sum(n, sums[turn], &all) - n);
     if (i < a.n_seqs) a.ws[i] = to < INT32_MAX ? (int)to : INT32_MAX;
-    before += all;
+    before = add(before, all);
   }
 }
 
@@ -246,11 +285,15 @@ extern "C" nat_status nat_kv_reserve(int32_t* d_block_table, int32_t table_width
   a.rows_cap = rows_cap;
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_PAGES, s);
-  if (n_seqs > 0) reserve_plan_kernel<<<1, kThreads, 0, s>>>(a);
-  else pages_nothing_kernel<<<1, 1, 0, s>>>(a);
+  if (n_seqs <= kThreads && rows_cap <= kFewRows) {
+    reserve_small_kernel<<<1, kThreads, 0, s>>>(a);
+    NAT_LAUNCH_CHECK();
+    return NAT_OK;
+  }
+  reserve_plan_kernel<<<1, kThreads, 0, s>>>(a);
   NAT_LAUNCH_CHECK();
   if (rows_cap == 0) return NAT_OK;
-  reserve_fill_kernel<<<(unsigned)((rows_cap + 255) / 256), 256, 0, s>>>(a, 0);
+  reserve_fill_kernel<<<(unsigned)((rows_cap + 255) / 256), 256, 0, s>>>(a);
   NAT_LAUNCH_CHECK();
   return NAT_OK;
 }
