@@ -554,48 +554,66 @@ def nat_sample(logits, random, temperature, top_k, top_p, min_p, ids_out, logp_o
         workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_sample")
 
 
-def _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, q_name="q", k_name="k"):
-    if q.dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError(f"{q_name} must be float32 or bfloat16")
+def _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved):
+    """The parameters, q and k (with rows of their own), and the addresses of weights, positions and frequencies."""
+    dtype = q.dtype
+    code = _dtype_code(q)
     n, hq, dim = q.shape
-    (q, k), (q_stride, k_stride) = _own_rows((q, k), (_rows(q, q_name, dtype=q.dtype, is_input=True), _rows(k, k_name, (n, k.shape[1], dim), q.dtype, True)))
-    rotary = 0
-    if (position_ids is None) != (inv_freq is None):
+    hkv = k.shape[1]
+    q_stride, k_stride = _rows(q, "q", None, dtype, True), _rows(k, "k", (n, hkv, dim), dtype, True)
+    if q_stride < 0 or k_stride < 0:
+        (q, k), (q_stride, k_stride) = _own_rows((q, k), (q_stride, k_stride))
+    rotary, at = 0, [_vector(q_weight, dtype, dim, "q_weight"), _vector(k_weight, dtype, dim, "k_weight"), None, None]
+    if inv_freq is not None and position_ids is not None:
+        half = inv_freq.numel()
+        rotary, at[2], at[3] = 2 * half, _vector(position_ids, torch.int32, n, "position_ids"), _vector(inv_freq, torch.float64, half, "inv_freq")
+        if rotary == 0:
+            at[2] = at[3] = None
+    elif inv_freq is not None or position_ids is not None:
         raise TypeError("position_ids and inv_freq go together")
-    if inv_freq is not None:
-        rotary = 2 * inv_freq.numel()
-        _vector(position_ids, torch.int32, n, "position_ids")
-        _vector(inv_freq, torch.float64, rotary // 2, "inv_freq")
-    _vector(q_weight, q.dtype, dim, "q_weight")
-    _vector(k_weight, q.dtype, dim, "k_weight")
-    return _CQkParams(hq, k.shape[1], dim, _dtype_code(q), rotary, int(interleaved), float(eps), n, q_stride, k_stride), q, k
+    return _CQkParams(hq, hkv, dim, code, rotary, interleaved, eps, n, q_stride, k_stride), q, k, at
+
+
+def _qk_forward(p, q, k, at, q_out, k_out):
+    _raise(load_library().nat_qk_norm_rope(ctypes.byref(p), q.data_ptr(), k.data_ptr(), *at, q_out.data_ptr(), k_out.data_ptr(), _stream()), "nat_qk_norm_rope")
 
 
 def nat_qk_norm_rope(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, q_out, k_out):
     """q [rows, q heads, D], k [rows, kv heads, D] bfloat16 or float32 (any row stride); weights [D] of the same type, each or None; position_ids int32 [rows]
     and inv_freq float64 [R / 2], or both None; q_out, k_out like q, k, or q, k themselves."""
-    p, q, k = _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
+    p, q, k, at = _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
     p.q_out_stride, p.k_out_stride = _rows(q_out, "q_out", q.shape, q.dtype), _rows(k_out, "k_out", k.shape, q.dtype)
-    _raise(load_library().nat_qk_norm_rope(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(position_ids), _ptr(inv_freq),
-                                           _ptr(q_out), _ptr(k_out), _stream()), "nat_qk_norm_rope")
+    _qk_forward(p, q, k, at, q_out, k_out)
 
 
+@functools.lru_cache(maxsize=256)
 def qk_norm_rope_bwd_workspace_bytes(n_rows, head_dim):
     return int(load_library().nat_qk_norm_rope_bwd_workspace_bytes(int(n_rows), int(head_dim)))
+
+
+def _qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dq_weight, dk_weight, accumulate, workspace):
+    """dq, dk and the weights' gradients have been checked, or made."""
+    strides = _rows(dq_out, "dq_out", q.shape, q.dtype, True), _rows(dk_out, "dk_out", k.shape, q.dtype, True)
+    if strides != (0, 0):
+        (dq_out, dk_out), (p.q_out_stride, p.k_out_stride) = _own_rows((dq_out, dk_out), strides)
+    _raise(load_library().nat_qk_norm_rope_bwd(
+        ctypes.byref(p), q.data_ptr(), k.data_ptr(), *at, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), _ptr(dq_weight), _ptr(dk_weight),
+        accumulate, _ptr(workspace), _bytes(workspace), _stream()), "nat_qk_norm_rope_bwd")
 
 
 def nat_qk_norm_rope_bwd(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, dq_out, dk_out, dq, dk, dq_weight, dk_weight, accumulate,
                          workspace):
     """The gradients of nat_qk_norm_rope: dq_out, dk_out of its results; dq, dk like q, k (or dq_out, dk_out themselves); dq_weight, dk_weight float32 [D], None
     where there is no weight."""
-    p, q, k = _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
-    (dq_out, dk_out), (p.q_out_stride, p.k_out_stride) = _own_rows((dq_out, dk_out), (_rows(dq_out, "dq_out", q.shape, q.dtype, True),
-                                                                                      _rows(dk_out, "dk_out", k.shape, q.dtype, True)))
+    p, q, k, at = _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
     p.dq_stride, p.dk_stride = _rows(dq, "dq", q.shape, q.dtype), _rows(dk, "dk", k.shape, q.dtype)
-    _raise(load_library().nat_qk_norm_rope_bwd(
-        ctypes.byref(p), _ptr(q), _ptr(k), _ptr(q_weight), _ptr(k_weight), _ptr(position_ids), _ptr(inv_freq), _ptr(dq_out), _ptr(dk_out), _ptr(dq), _ptr(dk),
-        _vector(dq_weight, torch.float32, p.head_dim, "dq_weight"), _vector(dk_weight, torch.float32, p.head_dim, "dk_weight"), int(bool(accumulate)),
-        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_qk_norm_rope_bwd")
+    _vector(dq_weight, torch.float32, p.head_dim, "dq_weight")
+    _vector(dk_weight, torch.float32, p.head_dim, "dk_weight")
+    _qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dq_weight, dk_weight, int(bool(accumulate)), workspace)
+
+
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
 
 def _matrix(t, name, rows=None, cols=None, dtype=None, is_input=False):
@@ -646,10 +664,12 @@ def nat_embed_bwd(ids, dout, scale, dE, accumulate, workspace):
                                         workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_embed_bwd")
 
 
+@functools.lru_cache(maxsize=256)
 def kv_reserve_workspace_bytes(n_seqs):
     return int(load_library().nat_kv_reserve_workspace_bytes(int(n_seqs)))
 
 
+@functools.lru_cache(maxsize=256)
 def kv_release_workspace_bytes(n_seqs):
     return int(load_library().nat_kv_release_workspace_bytes(int(n_seqs)))
 
@@ -660,28 +680,37 @@ def _counts(t, name):
     return t.data_ptr()
 
 
+def _pages_args(block_table, seq_lens, change, change_name, free_pages, counts, page_size):
+    """The arguments that both calls have."""
+    n, n_pages, i32 = seq_lens.numel(), free_pages.numel(), torch.int32
+    width = _table(block_table, n)
+    return (block_table.data_ptr(), width, n, page_size, _vector(seq_lens, i32, n, "seq_lens"), _vector(change, i32, n, change_name),
+            _vector(free_pages, i32, n_pages, "free_pages"), n_pages, _counts(counts, "counts"))
+
+
+def _reserve(args, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, workspace):
+    """args: of _pages_args; the others are addresses."""
+    _raise(load_library().nat_kv_reserve(*args, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, _ptr(workspace), _bytes(workspace), _stream()),
+           "nat_kv_reserve")
+
+
 def nat_kv_reserve(block_table, seq_lens, new_lens, free_pages, counts, page_size, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, workspace):
     """block_table int32 [n_seqs, pages], free_pages int32 [n_pages], counts int32 [2] (free pages, sequences refused); seq_lens, new_lens int32 [n_seqs]. Out:
     counts_out, seq_lens_out (may be counts, seq_lens), start int32 [n_seqs], cu_new int32 [n_seqs + 1], slots int64 and position_ids int32 (or None) [rows_cap]."""
-    n = seq_lens.numel()
-    width, i32, rows = _table(block_table, n), torch.int32, int(rows_cap)
-    _raise(load_library().nat_kv_reserve(
-        _ptr(block_table), width, n, int(page_size), _vector(seq_lens, i32, n, "seq_lens"), _vector(new_lens, i32, n, "new_lens"),
-        _vector(free_pages, i32, free_pages.numel(), "free_pages"), free_pages.numel(), _counts(counts, "counts"), rows, _counts(counts_out, "counts_out"),
-        _vector(seq_lens_out, i32, n, "seq_lens_out"), _vector(start, i32, n, "start"), _vector(cu_new, i32, n + 1, "cu_new"),
-        _vector(slots, torch.int64, rows, "slots"), _vector(position_ids, i32, rows, "position_ids"), _ptr(workspace),
-        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_kv_reserve")
+    n, i32, rows = seq_lens.numel(), torch.int32, int(rows_cap)
+    _reserve(_pages_args(block_table, seq_lens, new_lens, "new_lens", free_pages, counts, int(page_size)), rows, _counts(counts_out, "counts_out"),
+             _vector(seq_lens_out, i32, n, "seq_lens_out"), _vector(start, i32, n, "start"), _vector(cu_new, i32, n + 1, "cu_new"),
+             _vector(slots, torch.int64, rows, "slots"), _vector(position_ids, i32, rows, "position_ids"), workspace)
+
+
+def _release(args, counts_out, seq_lens_out, workspace):
+    _raise(load_library().nat_kv_release(*args, counts_out, seq_lens_out, _ptr(workspace), _bytes(workspace), _stream()), "nat_kv_release")
 
 
 def nat_kv_release(block_table, seq_lens, keep_lens, free_pages, counts, page_size, counts_out, seq_lens_out, workspace):
     """Arguments as nat_kv_reserve's; keep_lens int32 [n_seqs]: the tokens that stay.  free_pages is written behind its first counts[0] entries."""
-    n = seq_lens.numel()
-    width, i32 = _table(block_table, n), torch.int32
-    _raise(load_library().nat_kv_release(
-        _ptr(block_table), width, n, int(page_size), _vector(seq_lens, i32, n, "seq_lens"), _vector(keep_lens, i32, n, "keep_lens"),
-        _vector(free_pages, i32, free_pages.numel(), "free_pages"), free_pages.numel(), _counts(counts, "counts"), _counts(counts_out, "counts_out"),
-        _vector(seq_lens_out, i32, n, "seq_lens_out"), _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()),
-        "nat_kv_release")
+    _release(_pages_args(block_table, seq_lens, keep_lens, "keep_lens", free_pages, counts, int(page_size)), _counts(counts_out, "counts_out"),
+             _vector(seq_lens_out, torch.int32, seq_lens.numel(), "seq_lens_out"), workspace)
 
 
 def probe_mfma_scratch_bytes():

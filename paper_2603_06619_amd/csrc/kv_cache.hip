@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(256) kv_read_kernel(ReadArgs a) {
 // where there is more than one.  Every cached byte is read once for all heads of the group; the products cost nothing beside that (a group of fewer than 16 heads
 // leaves columns of them empty).  The next 32 tokens are in registers while these are worked on: at two wavefronts per SIMD, 64 KB in flight per compute unit.
 // 128 sequences of up to 8192 tokens (32 heads on 8 of 128, 8-bit) 235 us, 5.3 TB/s; one of 32768 (28 on 4, bf16) 16.7 us, 4.0 TB/s: 256 tokens per
-// workgroup, of which the first loads are a third of the time.
+// workgroup, of which the first loads are a third of the time.  The first from 4 bits 136 us, 4.9 TB/s.
 // Rounded to fewer bits are the probabilities, to bf16 for the product (with an 8-bit row's power of two in them, which rounds nothing).
 constexpr int kTokens = 32;               // tokens per step of a wavefront
 constexpr int kHeads = 16;                // query heads per workgroup
@@ -241,6 +241,11 @@ struct TokenTile {
   u32x4 v[kValueLoads];
   uint32_t k_exp[2], v_exp[kFp4 ? kValueLoads : 2];
 
+  // row and 16 bytes of it that a lane has of load i of values.  In 4 bits a lane writes four chunks of LDS for its 16 bytes, and lanes next to each other take rows next to
+  // each other, whose chunks lie in different banks; four lanes to a row would meet in the same ones (two thirds of the LDS cycles of a decoding call were conflicts)
+  __device__ __forceinline__ static int value_row(int i, int lane) { return i * (64 / kRowLanes) + (kFp4 ? lane % (64 / kRowLanes) : lane / kRowLanes); }
+  __device__ __forceinline__ static int value_at(int lane) { return kFp4 ? lane / (64 / kRowLanes) : lane % kRowLanes; }
+
   // first of the eight elements of fragment s of a key that lane group g has
   __device__ __forceinline__ static int element(int s, int g) {
     if constexpr (kFp4) return D / 4 * g + 8 * s;
@@ -265,9 +270,9 @@ struct TokenTile {
     }
 #pragma unroll
     for (int i = 0; i < kValueLoads; ++i) {
-      const int row = i * (64 / kRowLanes) + lane / kRowLanes;
-      v[i] = *(const u32x4*)(c.v + ((row < 16 ? r0 : r1 - 16) + row) * kRowBytes + lane % kRowLanes * 16);
-      if constexpr (kFp4) v_exp[i] = c.v_exp[((row < 16 ? r0 : r1 - 16) + row) * (D / kGroup) + lane % kRowLanes];
+      const int row = value_row(i, lane);
+      v[i] = *(const u32x4*)(c.v + ((row < 16 ? r0 : r1 - 16) + row) * kRowBytes + value_at(lane) * 16);
+      if constexpr (kFp4) v_exp[i] = c.v_exp[((row < 16 ? r0 : r1 - 16) + row) * (D / kGroup) + value_at(lane)];
     }
   }
 
@@ -287,14 +292,13 @@ struct TokenTile {
   __device__ __forceinline__ void store_values(char* tile, bool whole, int first_live, int end_live, int lane) const {
 #pragma unroll
     for (int i = 0; i < kValueLoads; ++i) {
-      const int row = i * (64 / kRowLanes) + lane / kRowLanes, at = lane % kRowLanes;
+      const int row = value_row(i, lane), at = value_at(lane);
       u32x4 x = v[i];
-      const bool dead = !whole && (row < first_live || row >= end_live);
-      if (dead) x = u32x4{0, 0, 0, 0};
+      if (!whole && (row < first_live || row >= end_live)) x = u32x4{0, 0, 0, 0};
       if constexpr (kFormat == NAT_KV_BF16) {
         *(u32x4*)(tile + RowTile<D>::chunk_at(row, at)) = x;
       } else if constexpr (kFp4) {
-        const uint32_t e = dead ? 127 : v_exp[i];            // (a place that is not there may hold 255)
+        const uint32_t e = !whole && (row < first_live || row >= end_live) ? 127 : v_exp[i];            // (a place that is not there may hold 255)
 #pragma unroll
         for (int j = 0; j < 4; ++j) *(u32x4*)(tile + RowTile<D>::chunk_at(row, 4 * at + j)) = widen_fp4(x[j], e);
       } else {
@@ -311,7 +315,7 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
   __shared__ __attribute__((aligned(16))) char values[4][kTokens * D * 2];       // and, at the end, the wavefronts' results
   __shared__ int32_t pages[kMaxChunk / 16];
   __shared__ float wave_m[4][kHeads], wave_sum[4][kHeads], joined_m[kHeads], joined_sum[kHeads];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   int id = blockIdx.x;
   const int block = id % a.head_blocks;
   id /= a.head_blocks;
@@ -344,7 +348,10 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
     const int last = (end - 1) / 16, b = t0 / 16;
     t.load(a.c, __builtin_amdgcn_readfirstlane(pages[b]), __builtin_amdgcn_readfirstlane(pages[b < last ? b + 1 : last]), head, first + t0, lane);
   };
-  auto step = [&](const TokenTile<D, kFormat>& t, int t0) {
+  // In 4 bits one tile, loaded again as soon as its keys and values have been read: 124 registers, four workgroups per compute unit (the case of 128 sequences below 141 us;
+  // with a second tile 145, three workgroups; with a third 157).
+  constexpr int kTiles = kFormat == NAT_KV_FP4 ? 1 : 2;
+  auto step = [&](TokenTile<D, kFormat>& t, int t0, int ahead) {
     const int last = (end - 1) / 16, b0 = t0 / 16;
     const bool there0 = pages[b0] >= 0, there1 = b0 < last && pages[b0 + 1] >= 0;
     const bool whole = t0 + kTokens <= end && there0 && there1;
@@ -355,6 +362,9 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int s = 0; s < D / 32; ++s) st[b] = mfma16x16(t.key_fragment(b, s), q[s], st[b]);
+    if constexpr (kTiles == 1) {
+      if (ahead < end) load(t, ahead);
+    }
     if constexpr (kFormat == NAT_KV_FP8) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -407,17 +417,18 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
       acc[db] = mfma16x16(__builtin_bit_cast(bf16x8, both), p, acc[db]);
     }
   };
-  TokenTile<D, kFormat> t0, t1;
+  TokenTile<D, kFormat> tiles[kTiles];
   int at = wave * kTokens;
-  if (at < end) load(t0, at);
+  if (at < end) load(tiles[0], at);
   while (at < end) {
-    if (at + 4 * kTokens < end) load(t1, at + 4 * kTokens);
-    step(t0, at);
-    at += 4 * kTokens;
-    if (at >= end) break;
-    if (at + 4 * kTokens < end) load(t0, at + 4 * kTokens);
-    step(t1, at);
-    at += 4 * kTokens;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      if (at >= end) break;
+      const int ahead = at + 4 * kTokens;
+      if (kTiles > 1 && ahead < end) load(tiles[(i + 1) % kTiles], ahead);
+      step(tiles[i], at, ahead);
+      at += 4 * kTokens;
+    }
   }
 
   // join the wavefronts: every one scales its result by the chunk's maximum, the sum of the four leaves

@@ -75,18 +75,20 @@ class RolloutStage:
     def norm_rotate(self, q, k, position_ids, inv_freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
         """Queries [n, q heads, D] and keys [n, kv heads, D], bf16 or float32, normed head by head (where there is a weight [D]) and rotated by position:
         inv_freq float64 [R / 2], radians per position for the pairs of the first R elements; both None: no rotation.  Returns (q, k), new arrays."""
+        p, q, k, at = nb._qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
         q_out, k_out = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
-        nb.nat_qk_norm_rope(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, q_out, k_out)
+        nb._qk_forward(p, q, k, at, q_out, k_out)
         return q_out, k_out
 
     def norm_rotate_backward(self, dq_out, dk_out, q, k, position_ids, inv_freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
         """(dq, dk, dq_weight, dk_weight) of norm_rotate() with its inputs; the weights' in float32, None without a weight."""
+        p, q, k, at = nb._qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
         dq, dk = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
-        dqw, dkw = (None if w is None else w.new_empty(w.shape, dtype=torch.float32) for w in (q_weight, k_weight))
+        dqw, dkw = (None if w is None else torch.empty_like(w, dtype=torch.float32) for w in (q_weight, k_weight))
         ws = None
         if dqw is not None or dkw is not None:
-            ws = self._buf("norm_rotate", nb.qk_norm_rope_bwd_workspace_bytes(q.shape[0], q.shape[2]))
-        nb.nat_qk_norm_rope_bwd(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, dq_out, dk_out, dq, dk, dqw, dkw, False, ws)
+            ws = self._buf("norm_rotate", nb.qk_norm_rope_bwd_workspace_bytes(p.n_rows, p.head_dim))
+        nb._qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dqw, dkw, 0, ws)
         return dq, dk, dqw, dkw
 
     def embed(self, ids, E, scale=1.0):
@@ -111,18 +113,24 @@ class RolloutStage:
         """Pages for new_lens more tokens of every sequence, from the end of the stack free_pages[:counts[0]] into block_table (in place), and the places of these tokens:
         dict with slots (int64) and position_ids (int32) of the n_rows new rows, cu_new (their offsets), start (first position; -1: refused, no pages or no
         room in the table), and seq_lens and counts (free pages, sequences refused) as they are now.  The free pages stay where they are, behind counts[0]."""
-        n = seq_lens.numel()
-        cu, start, lens, pos, left = torch.empty(3 * n + 3 + n_rows, dtype=torch.int32, device=seq_lens.device).split((n + 1, n, n, n_rows, 2))
-        slots = seq_lens.new_empty(n_rows, dtype=torch.int64)
-        nb.nat_kv_reserve(block_table, seq_lens, new_lens, free_pages, counts, page_size, n_rows, left, lens, start, cu, slots, pos,
-                          self._buf("pages", nb.kv_reserve_workspace_bytes(n)))
+        args = nb._pages_args(block_table, seq_lens, new_lens, "new_lens", free_pages, counts, page_size)
+        n = args[2]
+        whole = torch.empty(3 * n + 3 + n_rows, dtype=torch.int32, device=seq_lens.device)
+        slots = torch.empty(n_rows, dtype=torch.int64, device=seq_lens.device)
+        at = whole.data_ptr()
+        cu, start, lens, pos = at + 8, at + 12 + 4 * n, at + 12 + 8 * n, at + 12 + 12 * n
+        nb._reserve(args, n_rows, at, lens, start, cu, slots.data_ptr(), pos, self._buf("pages", nb.kv_reserve_workspace_bytes(n)))
+        left, cu, start, lens, pos = whole.split((2, n + 1, n, n, n_rows))
         return dict(slots=slots, position_ids=pos, cu_new=cu, start=start, seq_lens=lens, counts=left)
 
     def release(self, block_table, seq_lens, keep_lens, free_pages, counts, page_size):
         """The pages behind the first keep_lens tokens of every sequence (0: it has ended) back to free_pages (in place): (seq_lens, counts) as they are now."""
-        n = seq_lens.numel()
-        lens, left = torch.empty(n + 2, dtype=torch.int32, device=seq_lens.device).split((n, 2))
-        nb.nat_kv_release(block_table, seq_lens, keep_lens, free_pages, counts, page_size, left, lens, self._buf("pages", nb.kv_release_workspace_bytes(n)))
+        args = nb._pages_args(block_table, seq_lens, keep_lens, "keep_lens", free_pages, counts, page_size)
+        n = args[2]
+        whole = torch.empty(n + 2, dtype=torch.int32, device=seq_lens.device)
+        at = whole.data_ptr()
+        nb._release(args, at, at + 8, self._buf("pages", nb.kv_release_workspace_bytes(n)))
+        left, lens = whole.split((2, n))
         return lens, left
 
     def write_cache(self, cache, k, v, slots):
