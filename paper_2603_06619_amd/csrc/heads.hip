@@ -82,16 +82,25 @@ struct Chunk<float> {
   }
 };
 
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), kCtrl, 0xf, 0xf, true));
+}
 // over the D / 16 lanes of a head (8 or 4, neighbours); all of them get it
 template <int D>
 __device__ __forceinline__ float sum_of_head(float x) {
-  auto dpp = [](float v, auto ctrl) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, true));
-  };
-  x += dpp(x, std::integral_constant<int, 0xb1>{});           // lane ^ 1
-  x += dpp(x, std::integral_constant<int, 0x4e>{});           // lane ^ 2
-  if constexpr (D == 128) x += dpp(x, std::integral_constant<int, 0x141>{});      // lane ^ 7, of equal fours: as lane ^ 4
+  x += dpp<0xb1>(x);                               // lane ^ 1
+  x += dpp<0x4e>(x);                               // lane ^ 2
+  if constexpr (D == 128) x += dpp<0x141>(x);      // lane ^ 7, of equal fours: as lane ^ 4
   return x;
+}
+// over the lanes that have the same place in their heads
+template <int D>
+__device__ __forceinline__ float sum_of_heads(float x) {
+  if constexpr (D == 64) x += dpp<0x124>(x);       // 4 and 8 lanes round in rows of 16
+  x += dpp<0x128>(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  return sum_halves(__builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]));
 }
 
 // What a lane is in its head, and the row's angles.
@@ -179,7 +188,7 @@ __device__ __forceinline__ void norm_of(const float (&x)[8], const float (&y)[8]
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kWaves) heads_fwd_kernel(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) f32x2 angles[kWaves][D / 2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Lane<D> l(a, lane);
   const Chunk<T> one = Chunk<T>::all(1.f);
   Chunk<T> wq[2] = {one, one}, wk[2] = {one, one};
@@ -218,76 +227,127 @@ __global__ void __launch_bounds__(64 * kWaves) heads_fwd_kernel(HeadsArgs a) {
   }
 }
 
+// Steps of a wavefront through a row: the queries' heads, then the keys', kHeads at a time.  What the next step needs is loaded before this one's is worked on, without a branch
+// around the loads (behind one the compiler waits for all of them): places that are not there are others of the same array, whose values go nowhere.
+struct Steps {
+  int q, all;                            // of queries, and of both
+  template <int D>
+  __device__ __forceinline__ static Steps of(const HeadsArgs& a) {
+    constexpr int n = Lane<D>::kHeads;
+    const int q = (a.hq + n - 1) / n;
+    return {q, q + (a.heads - a.hq + n - 1) / n};
+  }
+};
+template <typename T, int D>
+__device__ __forceinline__ const T* element_of(const HeadsArgs& a, const Steps& steps, int64_t row, int step, const Lane<D>& l, const void* q, const void* k, int64_t q_stride,
+                                               int64_t k_stride) {
+  const bool is_q = step < steps.q;
+  const int heads = is_q ? a.hq : a.heads - a.hq, h = (is_q ? step : step - steps.q) * Lane<D>::kHeads + l.head;
+  return (is_q ? (const T*)q + row * q_stride : (const T*)k + row * k_stride) + (h < heads ? h : heads - 1) * D;
+}
+
+template <typename T>
+struct Pair {
+  Chunk<T> x, y;
+  __device__ __forceinline__ static Pair load(const T* p, const int (&at)[2]) { return {Chunk<T>::load(p + at[0]), Chunk<T>::load(p + at[1])}; }
+};
+
 // A lane adds up the weights' gradients of its elements over its rows and heads; its workgroup's sums go to `part`.
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kWaves) heads_bwd_kernel(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) f32x2 angles[kWaves][D / 2];
   __shared__ __attribute__((aligned(16))) float sums[kWaves][2][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Lane<D> l(a, lane);
-  const Chunk<T> one = Chunk<T>::all(1.f);
-  Chunk<T> wq[2] = {one, one}, wk[2] = {one, one};
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if (a.wq) wq[i] = Chunk<T>::load((const T*)a.wq + l.at[i]);
-    if (a.wk) wk[i] = Chunk<T>::load((const T*)a.wk + l.at[i]);
-  }
+  const Steps steps = Steps::of<D>(a);
+  const int64_t stride = (int64_t)gridDim.x * kWaves, first = (int64_t)blockIdx.x * kWaves + wave;
   float dw[2][16] = {};                  // of queries and keys
-  for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.n_rows; row += (int64_t)gridDim.x * kWaves) {
-    Turn t = {};
-    if (a.turning) {
-      form_angles(angles[wave], a.freq, 8 * a.turning, a.pos[row], lane);
-      t = angles_of<D>(angles[wave], l);
-    }
-    for (int h = l.head; h < a.heads; h += Lane<D>::kHeads) {
-      const bool is_q = h < a.hq;
-      const T* from = is_q ? (const T*)a.q + row * a.q_stride + h * D : (const T*)a.k + row * a.k_stride + (h - a.hq) * D;
-      const T* grad = is_q ? (const T*)a.dq_out + row * a.q_out_stride + h * D : (const T*)a.dk_out + row * a.k_out_stride + (h - a.hq) * D;
-      T* to = is_q ? (T*)a.q_out + row * a.dq_stride + h * D : (T*)a.k_out + row * a.dk_stride + (h - a.hq) * D;
-      float g0[8], g1[8];
-      Chunk<T>::load(grad + l.at[0]).get(g0);
-      Chunk<T>::load(grad + l.at[1]).get(g1);
-      if (l.turns) turn<true>(g0, g1, t, a.interleaved);
-      if (is_q ? a.wq != nullptr : a.wk != nullptr) {
-        float x[8], y[8], w[8], r, s, dot = 0.f;
-        Chunk<T>::load(from + l.at[0]).get(x);
-        Chunk<T>::load(from + l.at[1]).get(y);
-        norm_of<D>(x, y, a.eps, &r, &s);
-        auto half = [&](float (&v)[8], float (&g)[8], int part) __attribute__((always_inline)) {
-          Chunk<T>::pick(is_q, wq[part], wk[part]).get(w);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            v[i] = v[i] * s * r;                       // of norm sqrt(D), almost
-            const float d = g[i] * v[i];
-            if (is_q) dw[0][8 * part + i] += d;
-            else dw[1][8 * part + i] += d;
-            g[i] *= w[i];
-            dot = fmaf(g[i], v[i], dot);
-          }
-        };
-        half(x, g0, 0);
-        half(y, g1, 1);
-        dot = sum_of_head<D>(dot) * (1.f / D);
-        const float rs = r * s;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          g0[i] = rs * (g0[i] - x[i] * dot);
-          g1[i] = rs * (g1[i] - y[i] * dot);
-        }
+  if (first < a.n_rows) {
+    struct Both { Pair<T> x, g; };
+    auto load = [&](int64_t row, int step) __attribute__((always_inline)) {
+      return Both{Pair<T>::load(element_of<T, D>(a, steps, row, step, l, a.q, a.k, a.q_stride, a.k_stride), l.at),
+                  Pair<T>::load(element_of<T, D>(a, steps, row, step, l, a.dq_out, a.dk_out, a.q_out_stride, a.k_out_stride), l.at)};
+    };
+    Both next = load(first, 0);
+    int next_pos = a.turning ? a.pos[first] : 0;
+    const Pair<T> one = {Chunk<T>::all(1.f), Chunk<T>::all(1.f)};
+    const Pair<T> weights[2] = {a.wq ? Pair<T>::load((const T*)a.wq, l.at) : one, a.wk ? Pair<T>::load((const T*)a.wk, l.at) : one};
+    for (int64_t row = first; row < a.n_rows; row += stride) {
+      const int64_t row1 = row + stride < a.n_rows ? row + stride : row;
+      Turn t = {};
+      if (a.turning) {
+        form_angles(angles[wave], a.freq, 8 * a.turning, next_pos, lane);
+        next_pos = a.pos[row1];
+        t = angles_of<D>(angles[wave], l);
       }
-      Chunk<T>::store(to + l.at[0], g0);
-      Chunk<T>::store(to + l.at[1], g1);
+      auto side = [&](auto is_k) __attribute__((always_inline)) {
+        constexpr bool kKeys = decltype(is_k)::value;
+        const bool norm = kKeys ? a.wk != nullptr : a.wq != nullptr;
+        const int begin = kKeys ? steps.q : 0, end = kKeys ? steps.all : steps.q, heads = kKeys ? a.heads - a.hq : a.hq;
+        T* out = kKeys ? (T*)a.k_out + row * a.dk_stride : (T*)a.q_out + row * a.dq_stride;
+        for (int step = begin; step < end; ++step) {
+          const Both raw = next;
+          const bool more = !kKeys || step + 1 < end;
+          next = load(more ? row : row1, more ? step + 1 : 0);
+          const int h = (step - begin) * Lane<D>::kHeads + l.head;
+          float g0[8], g1[8];
+          raw.g.x.get(g0);
+          raw.g.y.get(g1);
+          if (l.turns) turn<true>(g0, g1, t, a.interleaved);
+          if (norm) {
+            float x[8], y[8], w[8], r, s, dot = 0.f;
+            raw.x.x.get(x);
+            raw.x.y.get(y);
+            norm_of<D>(x, y, a.eps, &r, &s);
+            const float rs = r * s;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              x[i] = x[i] * s * r;               // of norm sqrt(D), almost
+              y[i] = y[i] * s * r;
+            }
+            if (h < heads) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                dw[kKeys][i] = fmaf(g0[i], x[i], dw[kKeys][i]);
+                dw[kKeys][8 + i] = fmaf(g1[i], y[i], dw[kKeys][8 + i]);
+              }
+            }
+            weights[kKeys].x.get(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              g0[i] *= w[i];
+              dot = fmaf(g0[i], x[i], dot);
+            }
+            weights[kKeys].y.get(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              g1[i] *= w[i];
+              dot = fmaf(g1[i], y[i], dot);
+            }
+            dot = sum_of_head<D>(dot) * (1.f / D);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              g0[i] = rs * (g0[i] - x[i] * dot);
+              g1[i] = rs * (g1[i] - y[i] * dot);
+            }
+          }
+          if (h < heads) {
+            Chunk<T>::store(out + h * D + l.at[0], g0);
+            Chunk<T>::store(out + h * D + l.at[1], g1);
+          }
+        }
+      };
+      side(std::false_type{});
+      side(std::true_type{});
     }
   }
   if (!a.part) return;
 #pragma unroll
-  for (int side = 0; side < 2; ++side)
+  for (int s = 0; s < 2; ++s)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float x = dw[side][i];
-#pragma unroll
-      for (int d = Lane<D>::kLanes; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
-      if (l.head == 0) sums[wave][side][l.at[i >> 3] + (i & 7)] = x;
+      const float x = sum_of_heads<D>(dw[s][i]);
+      if (l.head == 0) sums[wave][s][l.at[i >> 3] + (i & 7)] = x;
     }
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * D; i += 64 * kWaves) {
@@ -325,7 +385,7 @@ __global__ void __launch_bounds__(256) heads_weights_kernel(const float* part, i
 
 bool misaligned(const void* p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
 
-constexpr int kMostBlocks = 2048, kMostSums = 768;       // backward: as many as fit at once, each leaves sums
+constexpr int kMostBlocks = 1280, kMostSums = 768;       // as many as fit at once, or nearly; backward each leaves sums
 int blocks_of(int64_t n_rows, int most) {
   const int64_t n = (n_rows + kWaves - 1) / kWaves;
   return (int)(n < 1 ? 1 : n < most ? n : most);
