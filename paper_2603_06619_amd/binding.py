@@ -519,7 +519,9 @@ def nat_attn_decode(cache, q, block_table, seq_lens, scale, out, lse, workspace)
     n_seqs, hq, _ = q.shape
     width = _table(block_table, n_seqs)
     shape = (n_seqs, hq, cache.head_dim)
-    (q,), (q_stride,) = _own_rows((q,), (_rows(q, "q", shape, is_input=True),))
+    q_stride = _rows(q, "q", shape, is_input=True)
+    if q_stride == _SHARED:
+        q, q_stride = q.contiguous(), 0
     _raise(load_library().nat_attn_decode(
         ctypes.byref(cache._c), _ptr(q), q_stride, n_seqs, hq, _ptr(block_table), width,
         _vector(seq_lens, torch.int32, n_seqs, "seq_lens"), float(scale), _ptr(out), _rows(out, "out", shape),
