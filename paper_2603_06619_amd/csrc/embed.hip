@@ -84,42 +84,93 @@ struct SortArgs {
 __device__ __forceinline__ int32_t key_of(int32_t id, int32_t V) { return (uint32_t)id < (uint32_t)V ? id : V; }
 
 // Up to kRanked pairs: a pair's place is the number of pairs before it, counted outright, two instructions each.  A workgroup takes 16 pairs, each in four lanes of all its
-// wavefronts, which share the others in blocks of 64.  2897 pairs 5.3 us; sorted by digits in one workgroup they took 18.
-constexpr int kRanked = 8192, kRankWaves = 16, kRankPairs = 16;
+// wavefronts, which share the others in blocks of 64.  2897 pairs 5.3 us; sorted by digits in one workgroup they took 18.  Up to kMerged pairs are ranked in tiles of kMergeTile
+// first, 64 of them to a workgroup, which merge_kernel then joins.
+constexpr int kRanked = 8192, kRankWaves = 16, kRankPairs = 16, kTilePairs = 64;
+constexpr int kMergeTile = 4096, kMerged = 32768;
 constexpr int kBlock = 64, kBlockPitch = kBlock + 4;       // four lanes' blocks in different banks
+template <int kPairs, int kMost>
 __global__ void __launch_bounds__(64 * kRankWaves) rank_kernel(SortArgs a) {
   typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-  __shared__ __attribute__((aligned(16))) int32_t keys[kRanked / kBlock * kBlockPitch];
-  __shared__ int counts[kRankWaves][kRankPairs];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = (int)a.n, blocks = (n + kBlock - 1) / kBlock;
+  constexpr int kLanes = 64 / kPairs;                      // of a pair
+  __shared__ __attribute__((aligned(16))) int32_t keys[kMost / kBlock * kBlockPitch];
+  __shared__ int counts[kRankWaves][kPairs];
+  const int base = (int)(blockIdx.x / (kMost / kPairs)) * kMost;       // of the tile
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n - base < kMost ? (int)a.n - base : kMost, blocks = (n + kBlock - 1) / kBlock;
   for (int i = threadIdx.x; i < kBlock * blocks; i += 64 * kRankWaves)
-    keys[i / kBlock * kBlockPitch + i % kBlock] = i < n ? key_of(a.ids_in[i], a.V) : INT32_MAX;
+    keys[i / kBlock * kBlockPitch + i % kBlock] = i < n ? key_of(a.ids_in[base + i], a.V) : INT32_MAX;
   __syncthreads();
-  const int mine = blockIdx.x * kRankPairs + lane % kRankPairs, own = mine / kBlock, it = keys[own * kBlockPitch + mine % kBlock];
+  const int mine = (int)(blockIdx.x % (kMost / kPairs)) * kPairs + lane % kPairs, own = mine / kBlock, it = own < blocks ? keys[own * kBlockPitch + mine % kBlock] : 0;
   const int key = it < INT32_MAX ? it : 0;                 // (what a place without a pair counts is not used)
   int before = 0;
-  for (int b = wave * 4 + lane / kRankPairs; b < blocks; b += 4 * kRankWaves) {
+  for (int b = wave * kLanes + lane / kPairs; b < blocks; b += kLanes * kRankWaves) {
     const int32_t* block = keys + b * kBlockPitch;
     // keys that are not there are never below; of the own block those before this pair may be equal
-    const int limit = b < own ? key + 1 : key, equal = b == own ? mine % kBlock : 0;
+    if (b != own) {
+      const int limit = b < own ? key + 1 : key;
 #pragma unroll
-    for (int j = 0; j < kBlock; j += 4) {
-      const i32x4 x = *(const i32x4*)(block + j);
+      for (int j = 0; j < kBlock; j += 4) {
+        const i32x4 x = *(const i32x4*)(block + j);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) before += x[u] < limit;
+        for (int u = 0; u < 4; ++u) before += x[u] < limit;
+      }
+    } else {
+      const int at = mine % kBlock;
+#pragma unroll 2
+      for (int j = 0; j < kBlock; j += 4) {            // (unrolled all the way the limits of all places are kept in registers)
+        const i32x4 x = *(const i32x4*)(block + j);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) before += x[u] < key + (j + u < at);
+      }
     }
-    for (int j = 0; j < equal; ++j) before += block[j] == key;
   }
-  before += __shfl_xor(before, 16, 64);
-  before += __shfl_xor(before, 32, 64);
-  if (lane < kRankPairs) counts[wave][lane] = before;
+#pragma unroll
+  for (int d = kPairs; d < 64; d <<= 1) before += __shfl_xor(before, d, 64);
+  if (lane < kPairs) counts[wave][lane] = before;
   __syncthreads();
-  if (threadIdx.x >= kRankPairs || mine >= n) return;
+  if (threadIdx.x >= kPairs || mine >= n) return;
   before = 0;
 #pragma unroll
   for (int w = 0; w < kRankWaves; ++w) before += counts[w][lane];
-  a.ids_out[before] = key;
-  a.rows_out[before] = mine;
+  a.ids_out[base + before] = key;
+  a.rows_out[base + before] = base + mine;
+}
+
+// Sorted tiles into one: a pair's place is its place in its tile and, of each other tile, the number of pairs before it, which a search in LDS finds.  20483 pairs 7.6 us and
+// 12.9 for the ranks in the tiles; two passes by digits took 29.
+__global__ void __launch_bounds__(1024) merge_kernel(SortArgs a) {
+  typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+  extern __shared__ __attribute__((aligned(16))) int32_t keys[];
+  const int n = (int)a.n;
+  for (int i0 = 4 * threadIdx.x; i0 < n; i0 += 16384) {    // (the array is 256-byte aligned and has room for whole 16 bytes)
+    i32x4 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + 4096 * u < n) x[u] = *(const i32x4*)(a.ids_in + i0 + 4096 * u);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + 4096 * u < n) *(i32x4*)(keys + i0 + 4096 * u) = x[u];
+  }
+  __syncthreads();
+  const int i = blockIdx.x * 1024 + (int)threadIdx.x;
+  if (i >= n) return;
+  const int key = keys[i], tiles = (n + kMergeTile - 1) / kMergeTile, own = i / kMergeTile;
+  int place = i - own * kMergeTile;
+  for (int t = 0; t < tiles; ++t) {
+    if (t == own) continue;
+    const int32_t* tile = keys + t * kMergeTile;
+    const int limit = t < own ? key + 1 : key;             // equal ones of tiles before are before
+    int at = 0, len = n - t * kMergeTile < kMergeTile ? n - t * kMergeTile : kMergeTile;
+    while (len > 0) {
+      const int half = len >> 1;
+      const bool below = tile[at + half] < limit;
+      at = below ? at + half + 1 : at;
+      len = below ? len - half - 1 : half;
+    }
+    place += at;
+  }
+  a.ids_out[place] = key;
+  a.rows_out[place] = a.rows_in[i];
 }
 
 // More pairs: by digits from the lowest on, each pass stable.  A workgroup of W wavefronts takes a tile of 64 W kPer pairs, each wavefront ranking 64 at a time by
@@ -410,7 +461,7 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a) {
 // The parts of a run that begins in this piece and goes on behind it
 template <typename T>
 __global__ void __launch_bounds__(256) embed_join_kernel(SumArgs a) {
-  constexpr int kE = Piece<T>::kElements, kAhead = 4;
+  constexpr int kE = Piece<T>::kElements, kAhead = 16;
   const int slab = blockIdx.x % a.slabs, lane = threadIdx.x & 63;
   const int64_t piece = blockIdx.x / a.slabs, p0 = piece * a.piece, p1 = p0 + a.piece;
   if (p1 >= a.n) return;
@@ -478,7 +529,7 @@ SortPlan sort_plan(int64_t n, int32_t V, int32_t H) {
   p.pieces = (n + p.piece - 1) / p.piece;
   auto whole = [](size_t x) { return (x + 255) / 256 * 256; };
   p.pairs = whole((size_t)n * 4);
-  p.counts = n > kRanked ? whole((((size_t)p.tiles + 1) << p.bits) * 4) : 0;
+  p.counts = n > kMerged ? whole((((size_t)p.tiles + 1) << p.bits) * 4) : 0;
   p.parts = whole((size_t)p.pieces * 2 * H * 4);
   return p;
 }
@@ -555,7 +606,16 @@ extern "C" nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const 
   for (int i = 0; i < 4; ++i) pair[i] = (int32_t*)(ws + i * p.pairs);
   SortArgs a{d_ids, nullptr, pair[0], pair[1], (int32_t*)(ws + 4 * p.pairs), n_rows, V, 0, p.bits, p.tiles, p.tiles > kDirectTiles};
   if (n_rows <= kRanked) {
-    rank_kernel<<<(unsigned)((n_rows + kRankPairs - 1) / kRankPairs), 64 * kRankWaves, 0, s>>>(a);
+    rank_kernel<kRankPairs, kRanked><<<(unsigned)((n_rows + kRankPairs - 1) / kRankPairs), 64 * kRankWaves, 0, s>>>(a);
+    NAT_LAUNCH_CHECK();
+  } else if (n_rows <= kMerged) {
+    rank_kernel<kTilePairs, kMergeTile><<<(unsigned)((n_rows + kTilePairs - 1) / kTilePairs), 64 * kRankWaves, 0, s>>>(a);
+    NAT_LAUNCH_CHECK();
+    a.ids_in = pair[0];
+    a.rows_in = pair[1];
+    a.ids_out = pair[2];
+    a.rows_out = pair[3];
+    merge_kernel<<<(unsigned)((n_rows + 1023) / 1024), 1024, (size_t)(n_rows + 3) / 4 * 16, s>>>(a);
     NAT_LAUNCH_CHECK();
   } else {
     for (int pass = 0; pass < p.passes; ++pass) {

@@ -166,3 +166,13 @@ def test_other_streams_side_by_side(stage):
                 got[j] = stage.embed_backward(d, i, V)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("n", [4097, 8192, 12289, 16384, 32767, 32768, 32769, 65536, 65537])
+def test_gradient_where_the_sort_changes(stage, n):
+    """Ids of a small vocabulary, equal ones in every tile; and a run that is longer than 64 pieces of 64 rows."""
+    dout = normal(n, n, 16)
+    check(stage, ids_of(n, n, 37, "any"), dout, 37)
+    ids = ids_of(n, n, 5000, "text")
+    ids[n // 7: n // 7 + min(n // 2, 20000)] = 4999
+    check(stage, ids, dout, 5000, -1.5)
