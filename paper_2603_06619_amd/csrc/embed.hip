@@ -342,7 +342,7 @@ struct SumArgs {
   float *dE, *part;                     // part: [pieces][2][H], of the run that came in from the piece before, of the one that goes on behind
   int64_t n, dout_bytes, sum_blocks;    // the other workgroups write zeros
   int32_t V, H;
-  int piece, slabs, zero_rows;          // pairs per piece, at most 64; workgroups per row; rows of dE per workgroup that writes zeros
+  int piece, slabs, zero_rows;          // pairs per piece, at most 64; workgroups per row; rows of dE per workgroup that writes zeros (0: long ones)
   float scale;
   int accumulate;
 };
@@ -359,10 +359,9 @@ __device__ __forceinline__ void write_run(const SumArgs& a, int32_t id, int at, 
   }
 }
 
-// First place whose id is not below v, found by the whole wavefront: 64 probes per round
-__device__ __forceinline__ int64_t lower_bound(const int32_t* ids, int64_t n, int32_t v) {
+// First place of lo .. hi whose id is not below v, found by the whole wavefront: 64 probes per round
+__device__ __forceinline__ int64_t lower_bound(const int32_t* ids, int64_t lo, int64_t hi, int32_t v) {
   const int lane = threadIdx.x & 63;
-  int64_t lo = 0, hi = n;
   while (lo < hi) {
     const int64_t step = (hi - lo + 63) >> 6, probe = lo + lane * step;
     const int below = __popcll(__ballot(probe < hi && ids[probe] < v));
@@ -374,14 +373,45 @@ __device__ __forceinline__ int64_t lower_bound(const int32_t* ids, int64_t n, in
   return lo;
 }
 
-// Zeros into those of zero_rows rows that no pair has
+// Zeros into the rows that no pair has.
+//
+// Long rows: dE as a row of pieces of 4 KB, of which eight workgroups, one on each XCD, take 32, every eighth one each.  Stores alone reach 6.5 TB/s so, and 6.0 where a workgroup's four
+// pieces follow one another (2.49 GB in 381 and 417 us; a workgroup per piece 365, but each has to look for its rows first).  Every wavefront looks for itself.  A gradient that fits
+// the Infinity Cache is faster with fewer and longer workgroups, as short rows have them (20483 rows into 2.49 GB 525 -> 482 us, 5000 into 0.62 GB 135 -> 121, but 2897 into 0.13 GB 31.6 -> 38.9).
+constexpr int64_t kManyZeros = 256 << 20;                  // bytes
+constexpr int kLongRow = 1024, kZeroPiece = 1024, kZeroBlocks = 8, kZeroPieces = 4;       // elements, elements, workgroups, pieces of each
+__device__ __forceinline__ void write_long_zeros(const SumArgs& a, int64_t block) {
+  constexpr int kAll = kZeroPiece * kZeroBlocks * kZeroPieces;
+  const int lane = threadIdx.x & 63;
+  const int64_t base = block / kZeroBlocks * kAll, all = (int64_t)a.V * a.H;
+  const int32_t v0 = (int32_t)(base / a.H), rest = (int32_t)(base - (int64_t)v0 * a.H);
+  const int rows = (rest + kAll - 1) / a.H + 1;              // up to 33
+  uint64_t used = 0;
+  for (int64_t p = lower_bound(a.ids, 0, a.n, v0); p < a.n;) {
+    const int32_t id = p + lane < a.n ? a.ids[p + lane] : INT32_MAX;
+    for (int r = 0; r < rows; ++r) used |= (uint64_t)(__ballot(id == v0 + r) != 0) << r;
+    const int32_t last = __builtin_amdgcn_readlane(id, 63);
+    if (last >= v0 + rows - 1) break;
+    p = lower_bound(a.ids, p + 64, a.n, last + 1);         // (a long run is passed over)
+  }
+  f32x4* to = (f32x4*)(a.dE + base);
+  for (int t = threadIdx.x; t < kZeroPiece / 4; t += blockDim.x) {
+#pragma unroll
+    for (int i = 0; i < kZeroPieces; ++i) {
+      const int at = (i * kZeroBlocks + (int)(block % kZeroBlocks)) * kZeroPiece + 4 * t;
+      if (base + at < all && !(used >> ((uint32_t)(rest + at) / (uint32_t)a.H) & 1)) to[at / 4] = f32x4{};
+    }
+  }
+}
+
+// Otherwise: zero_rows of them to a workgroup, marked in LDS.
 __device__ __forceinline__ void write_zeros(const SumArgs& a, int64_t block) {
   __shared__ uint32_t used[kMostZeroRows / 32];
   __shared__ int64_t range[2];
   const int64_t v0 = block * a.zero_rows, v1 = v0 + a.zero_rows < a.V ? v0 + a.zero_rows : a.V;
   for (int i = threadIdx.x; i < kMostZeroRows / 32; i += blockDim.x) used[i] = 0;
   if (threadIdx.x < 64) {
-    const int64_t first = lower_bound(a.ids, a.n, (int32_t)v0), end = lower_bound(a.ids, a.n, (int32_t)v1);
+    const int64_t first = lower_bound(a.ids, 0, a.n, (int32_t)v0), end = lower_bound(a.ids, first, a.n, (int32_t)v1);
     if (threadIdx.x == 0) {
       range[0] = first;
       range[1] = end;
@@ -394,18 +424,10 @@ __device__ __forceinline__ void write_zeros(const SumArgs& a, int64_t block) {
   }
   __syncthreads();
   const int chunks = a.H / 4;           // of 16 bytes
-  if (chunks >= (int)blockDim.x) {
-    for (int64_t v = v0; v < v1; ++v) {
-      if (used[(v - v0) >> 5] >> ((v - v0) & 31) & 1) continue;
-      f32x4* to = (f32x4*)(a.dE + v * a.H);
-      for (int i = threadIdx.x; i < chunks; i += blockDim.x) to[i] = f32x4{};
-    }
-  } else {
-    f32x4* to = (f32x4*)(a.dE + v0 * a.H);
-    for (int64_t i = threadIdx.x; i < (v1 - v0) * chunks; i += blockDim.x) {
-      const int v = (int)(i / chunks);
-      if (!(used[v >> 5] >> (v & 31) & 1)) to[i] = f32x4{};
-    }
+  f32x4* to = (f32x4*)(a.dE + v0 * a.H);
+  for (int64_t i = threadIdx.x; i < (v1 - v0) * chunks; i += blockDim.x) {
+    const int v = (int)(i / chunks);
+    if (!(used[v >> 5] >> (v & 31) & 1)) to[i] = f32x4{};
   }
 }
 
@@ -413,7 +435,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a) {
   constexpr int kE = Piece<T>::kElements, kAhead = 8;
   if (blockIdx.x >= a.sum_blocks) {
-    write_zeros(a, blockIdx.x - a.sum_blocks);
+    if (a.zero_rows == 0) write_long_zeros(a, blockIdx.x - a.sum_blocks);
+    else write_zeros(a, blockIdx.x - a.sum_blocks);
     return;
   }
   const int slab = blockIdx.x % a.slabs, lane = threadIdx.x & 63;
@@ -590,9 +613,12 @@ extern "C" nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const 
   // 16 bytes per thread, up to 256 threads
   const int64_t lanes = (int64_t)H * size / 16;
   const int threads = lanes >= 256 ? 256 : (int)((lanes + 63) / 64 * 64), slabs = (int)((lanes + threads - 1) / threads);
-  int zero_rows = 65536 / H < 1 ? 1 : 65536 / H > kMostZeroRows ? kMostZeroRows : 65536 / H;
+  int zero_rows = 65536 / H > kMostZeroRows ? kMostZeroRows : 65536 / H < 1 ? 1 : 65536 / H;
   if (zero_rows > V / 1024) zero_rows = V < 2048 ? 1 : V / 1024;
-  const int64_t zero_blocks = accumulate ? 0 : ((int64_t)V + zero_rows - 1) / zero_rows, sum_blocks = p.pieces * slabs;
+  if (H >= kLongRow && (int64_t)V * H * 4 > kManyZeros) zero_rows = 0;
+  constexpr int64_t kZeros = (int64_t)kZeroPiece * kZeroPieces * kZeroBlocks;
+  const int64_t zero_blocks = accumulate ? 0 : zero_rows == 0 ? ((int64_t)V * H + kZeros - 1) / kZeros * kZeroBlocks : ((int64_t)V + zero_rows - 1) / zero_rows;
+  const int64_t sum_blocks = p.pieces * slabs;
   if (sum_blocks + zero_blocks > kMaxWorkItems / threads) return NAT_BAD_SHAPE;
   if (!d_dE || misaligned(d_dE)) return NAT_INVALID_ARG;
   if (n_rows > 0 && (!d_ids || !d_dout || misaligned(d_dout))) return NAT_INVALID_ARG;

@@ -176,3 +176,20 @@ def test_gradient_where_the_sort_changes(stage, n):
     ids = ids_of(n, n, 5000, "text")
     ids[n // 7: n // 7 + min(n // 2, 20000)] = 4999
     check(stage, ids, dout, 5000, -1.5)
+
+
+@pytest.mark.parametrize("V,H", [(70000, 1024), (60000, 1160), (30011, 2248), (66000, 1032)])
+@pytest.mark.parametrize("kind", ["text", "one", "any"])
+def test_gradient_of_a_large_vocabulary(stage, V, H, kind):
+    """Above 256 MB: rows that begin and end inside the pieces in which zeros are written; every second id, runs longer than a wavefront."""
+    n = 3000
+    ids = ids_of(V, n, V, kind)
+    ids[100:900:2] = np.arange(400) * 2 + V - 800            # (up to the last but one)
+    ids[1200:1500] = V // 2
+    at, dout = torch.from_numpy(ids).to(DEV), normal(V, n, H, dtype=torch.bfloat16)
+    got = stage.embed_backward(dout, at, V, dE=torch.full((V, H), float("nan"), device=DEV))
+    ok = (at >= 0) & (at < V)
+    want = torch.zeros((V, H), dtype=torch.float64, device=DEV).index_add_(0, at[ok].long(), dout[ok].double())
+    size = torch.zeros((V, H), dtype=torch.float64, device=DEV).index_add_(0, at[ok].long(), dout[ok].double().abs())
+    count = torch.zeros(V, dtype=torch.float64, device=DEV).index_add_(0, at[ok].long(), torch.ones(int(ok.sum()), dtype=torch.float64, device=DEV))
+    assert bool(((got.double() - want).abs() <= (count[:, None] + 1) * 2.0 ** -24 * size).all())
