@@ -548,7 +548,8 @@ nat_status nat_attn_decode(const nat_kv_cache* cache, const void* d_q, int64_t q
  *   d_position_ids [n_rows] int32 (of nat_prefix_pack or nat_kv_reserve), NULL exactly if rotary_dim is 0;
  *   d_inv_freq   [R / 2] double, angle per position in radians; the angle is formed in turns in 64 bits, so far positions
  *                lose nothing;
- *   d_q_out, d_k_out like d_q, d_k: may be the inputs themselves with the same stride, otherwise must not overlap them.
+ *   d_q_out, d_k_out like d_q, d_k: may be the inputs themselves with the same stride (with another one: NAT_INVALID_ARG), otherwise
+ *                must not overlap them.
  * Everything in between is held in fp32 and rounded once.  Errors: NULL pointer (but the optional ones), count, eps or flag out
  * of range, pointers (of rows and weights) not 16-byte aligned -> NAT_INVALID_ARG; head counts, head_dim, rotary_dim or stride out
  * of range -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE.  n_rows = 0 is valid.
@@ -599,7 +600,7 @@ nat_status nat_embed(const int32_t* d_ids, int64_t n_rows, const void* d_E, int3
  *   d_ws / ws_bytes: at least nat_embed_bwd_workspace_bytes, 256-byte aligned.
  * Ids are sorted on the device, rows of one id staying in order, and a row of dE is a sum in fp32 whose order depends on the ids
  * alone: results do not change from run to run.  No atomics on floats.
- * Errors as nat_embed, plus V > 2^30, n_rows >= 2^29 -> NAT_BAD_SHAPE, NAT_WORKSPACE_TOO_SMALL.  With n_rows = 0 dE is zeros, or stays.
+ * Errors as nat_embed, plus V > 2^30, n_rows >= 2^29 or more work than a launch has room for -> NAT_BAD_SHAPE, NAT_WORKSPACE_TOO_SMALL.  With n_rows = 0 dE is zeros, or stays.
  */
 size_t nat_embed_bwd_workspace_bytes(int64_t n_rows, int32_t V, int32_t H);
 nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const void* d_dout, int64_t dout_stride, int32_t V, int32_t H,

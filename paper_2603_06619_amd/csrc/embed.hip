@@ -3,6 +3,9 @@
 // The gradient sorts (id, row) pairs by id, rows of one id staying in order, and then walks the sorted pairs in pieces of equal length, whatever the ids: a token that
 // makes up a tenth of the batch is shared by many workgroups like any other rows.  A run of equal ids inside a piece is summed and written by its workgroup; of one that
 // crosses pieces each leaves its part, and a second kernel adds the parts in order.
+//
+// Bound by HBM.  The lookup of 16381 rows of 4096 in bf16, 268 MB (of which text repeats some), 34 us.  The gradient of 20483 such rows into a vocabulary of 151936, of which 2.49 GB
+// are written and 0.17 read, 481 us, 5.5 TB/s; of 2897 rows of 1024 in fp32 into 32000, 143 MB that the Infinity Cache holds, 31 us: ranks 5.5, sums and zeros 22.5, joining 4.
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
 
@@ -481,7 +484,7 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a) {
   }
 }
 
-// The parts of a run that begins in this piece and goes on behind it
+// The parts of a run that begins in this piece and goes on behind it, 16 loads ahead
 template <typename T>
 __global__ void __launch_bounds__(256) embed_join_kernel(SumArgs a) {
   constexpr int kE = Piece<T>::kElements, kAhead = 16;

@@ -2,7 +2,10 @@
 //
 // A head's D elements lie in D / 16 lanes, two chunks of 8 elements each: of the R elements that turn, lane c has chunks c and c + R / 16, so that both elements
 // of a pair (i, i + R / 2) are its own, and pairs of neighbours are anyway.  The R / 2 sines and cosines of a row are formed by a lane each and go to all heads of the
-// row through LDS: a wavefront takes whole rows.
+// row through LDS: a wavefront takes whole rows, of few rows parts of them.
+//
+// Bound by HBM: 14.4 thousand rows of 28 + 4 heads of 128 in bf16, 212 MB, take 38 us while half of them lie in the Infinity Cache, 44 (4.8 TB/s, a copy: 5.0) otherwise; 20.6 thousand of
+// 32 + 8 forward 66 us (377 MB), backward 117 (566 MB) and 5 for the weights' gradients.  64 rows of 32 + 8, the step of a decoding batch, 3.7 us (6.1 with a wavefront per row).
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
 
@@ -21,6 +24,7 @@ struct HeadsArgs {
   const double* freq;
   float* part;                            // backward: [workgroups][2][D]
   int hq, heads, turning, interleaved;    // heads: of queries and keys; turning: lanes of a head whose elements turn, R / 16
+  int parts;                              // forward: wavefronts per row
   float eps;
   int64_t n_rows, q_stride, k_stride, q_out_stride, k_out_stride, dq_stride, dk_stride;
 };
@@ -185,6 +189,7 @@ __device__ __forceinline__ void norm_of(const float (&x)[8], const float (&y)[8]
   *r = rsqrtf(fmaf(sum, 1.f / D, eps));
 }
 
+// Without loads ahead: 76 registers, six wavefronts per SIMD.  With them, as in the backward pass, 102 and four: 14.4 thousand rows of 28 + 4 heads 36 instead of 33 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kWaves) heads_fwd_kernel(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) f32x2 angles[kWaves][D / 2];
@@ -197,13 +202,15 @@ __global__ void __launch_bounds__(64 * kWaves) heads_fwd_kernel(HeadsArgs a) {
     if (a.wq) wq[i] = Chunk<T>::load((const T*)a.wq + l.at[i]);
     if (a.wk) wk[i] = Chunk<T>::load((const T*)a.wk + l.at[i]);
   }
-  for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.n_rows; row += (int64_t)gridDim.x * kWaves) {
+  for (int64_t unit = (int64_t)blockIdx.x * kWaves + wave; unit < a.n_rows * a.parts; unit += (int64_t)gridDim.x * kWaves) {
+    const int64_t row = a.parts == 1 ? unit : unit / a.parts;
+    const int part = (int)(unit - row * a.parts);
     Turn t = {};
     if (a.turning) {
       form_angles(angles[wave], a.freq, 8 * a.turning, a.pos[row], lane);
       t = angles_of<D>(angles[wave], l);
     }
-    for (int h = l.head; h < a.heads; h += Lane<D>::kHeads) {
+    for (int h = part * Lane<D>::kHeads + l.head; h < a.heads; h += a.parts * Lane<D>::kHeads) {
       const bool is_q = h < a.hq;
       const T* from = is_q ? (const T*)a.q + row * a.q_stride + h * D : (const T*)a.k + row * a.k_stride + (h - a.hq) * D;
       T* to = is_q ? (T*)a.q_out + row * a.q_out_stride + h * D : (T*)a.k_out + row * a.k_out_stride + (h - a.hq) * D;
@@ -252,7 +259,9 @@ struct Pair {
   __device__ __forceinline__ static Pair load(const T* p, const int (&at)[2]) { return {Chunk<T>::load(p + at[0]), Chunk<T>::load(p + at[1])}; }
 };
 
-// A lane adds up the weights' gradients of its elements over its rows and heads; its workgroup's sums go to `part`.
+// A lane adds up the weights' gradients of its elements over its rows and heads; its workgroup's sums go to `part`.  Three wavefronts per SIMD; loads a step ahead took 20.6 thousand
+// rows of 32 + 8 heads from 122 to 117 us, and 2940 of 16 + 16 heads of 64 in fp32, for which there is hardly a second row per wavefront, from 25.5 to 18.3 (with sums across
+// lanes by DPP and lane swaps).
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kWaves) heads_bwd_kernel(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) f32x2 angles[kWaves][D / 2];
@@ -358,7 +367,7 @@ __global__ void __launch_bounds__(64 * kWaves) heads_bwd_kernel(HeadsArgs a) {
   }
 }
 
-// The workgroups' sums in order: one workgroup per kColumns elements, every kWalkers-th part to each walker.
+// The workgroups' sums in order: one workgroup per kColumns elements, every kWalkers-th part to each walker, eight loads ahead (768 parts 4 us; one after the other 48).
 constexpr int kColumns = 8, kWalkers = 256 / kColumns;
 __global__ void __launch_bounds__(256) heads_weights_kernel(const float* part, int n_parts, int D, float* dwq, float* dwk, int accumulate) {
   __shared__ float sums[kWalkers][kColumns + 1];
@@ -384,6 +393,11 @@ __global__ void __launch_bounds__(256) heads_weights_kernel(const float* part, i
 }
 
 bool misaligned(const void* p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+// results in the place of the inputs, but in other rows
+bool other_rows(const void* in, int64_t in_stride, const void* out, int64_t out_stride, int64_t n_rows) {
+  return n_rows > 1 && in != nullptr && in == out && in_stride != out_stride;
+}
 
 constexpr int kMostBlocks = 1280, kMostSums = 768;       // as many as fit at once, or nearly; backward each leaves sums
 int blocks_of(int64_t n_rows, int most) {
@@ -434,14 +448,20 @@ extern "C" nat_status nat_qk_norm_rope(const nat_qk_params* params, const void* 
   HeadsArgs a{};
   const nat_status st = heads_args(params, d_q, d_k, d_q_weight, d_k_weight, d_position_ids, d_inv_freq, &a);
   if (st != NAT_OK) return st;
-  if (misaligned(d_q_out) || misaligned(d_k_out)) return NAT_INVALID_ARG;
+  if (misaligned(d_q_out) || misaligned(d_k_out) || other_rows(d_q, a.q_stride, d_q_out, a.q_out_stride, a.n_rows) ||
+      other_rows(d_k, a.k_stride, d_k_out, a.k_out_stride, a.n_rows))
+    return NAT_INVALID_ARG;
   if (a.n_rows == 0) return NAT_OK;
   if (!d_q_out || !d_k_out) return NAT_INVALID_ARG;
   a.q_out = d_q_out;
   a.k_out = d_k_out;
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_HEADS, s);
-  const int n = blocks_of(a.n_rows, kMostBlocks);
+  // of few rows each by several wavefronts, of up to as many steps as it has
+  const int steps = (a.heads * params->head_dim + 1023) / 1024;
+  const int64_t most = kMostBlocks * kWaves / a.n_rows;
+  a.parts = most < 1 ? 1 : most < steps ? (int)most : steps;
+  const int n = blocks_of(a.n_rows * a.parts, kMostBlocks);
   if (params->dtype == NAT_DTYPE_BF16) {
     if (params->head_dim == 128) heads_fwd_kernel<uint16_t, 128><<<n, 64 * kWaves, 0, s>>>(a);
     else heads_fwd_kernel<uint16_t, 64><<<n, 64 * kWaves, 0, s>>>(a);
@@ -466,7 +486,8 @@ extern "C" nat_status nat_qk_norm_rope_bwd(const nat_qk_params* params, const vo
   const nat_status st = heads_args(params, d_q, d_k, d_q_weight, d_k_weight, d_position_ids, d_inv_freq, &a);
   if (st != NAT_OK) return st;
   if (misaligned(d_dq_out) || misaligned(d_dk_out) || misaligned(d_dq) || misaligned(d_dk) || misaligned(d_dq_weight, 4) || misaligned(d_dk_weight, 4) ||
-      (d_q_weight != nullptr) != (d_dq_weight != nullptr) || (d_k_weight != nullptr) != (d_dk_weight != nullptr))
+      (d_q_weight != nullptr) != (d_dq_weight != nullptr) || (d_k_weight != nullptr) != (d_dk_weight != nullptr) ||
+      other_rows(d_dq_out, a.q_out_stride, d_dq, a.dq_stride, a.n_rows) || other_rows(d_dk_out, a.k_out_stride, d_dk, a.dk_stride, a.n_rows))
     return NAT_INVALID_ARG;
   const bool weights = d_q_weight || d_k_weight;
   if (a.n_rows > 0 && (!d_dq_out || !d_dk_out || !d_dq || !d_dk)) return NAT_INVALID_ARG;

@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(256) kv_read_kernel(ReadArgs a) {
 // four wavefronts take 32 tokens each in turn, with a running maximum and sum of their own, and join at the end; chunks are joined by a second kernel
 // where there is more than one.  Every cached byte is read once for all heads of the group; the products cost nothing beside that (a group of fewer than 16 heads
 // leaves columns of them empty).  The next 32 tokens are in registers while these are worked on: at two wavefronts per SIMD, 64 KB in flight per compute unit.
-// 128 sequences of up to 8192 tokens (32 heads on 8 of 128, 8-bit) 235 us, 5.3 TB/s; one of 32768 (28 on 4, bf16) 16.7 us, 4.0 TB/s: 256 tokens per
+// 128 sequences of up to 8192 tokens (32 heads on 8 of 128, 8-bit) 235 us, 5.3 TB/s; one of 32768 (28 on 4, bf16) 15.5 us, 4.3 TB/s: 256 tokens per
 // workgroup, of which the first loads are a third of the time.  The first from 4 bits 136 us, 4.9 TB/s.
 // Rounded to fewer bits are the probabilities, to bf16 for the product (with an 8-bit row's power of two in them, which rounds nothing).
 constexpr int kTokens = 32;               // tokens per step of a wavefront

@@ -42,6 +42,11 @@ def test_norm_and_rotation_refusals(nat, back):  # noqa: F811
     for name in ("q", "k", "qw", "kw", "qo", "ko") + (("dq", "dk") if back else ()):
         assert call(ptr={name: fake + 8}) == INVALID, name
     assert call(ptr=dict(freq=fake + 4)) == INVALID and call(rotary_dim=0) == INVALID              # positions without a rotation
+    ends = ("dq", "dk") if back else ("qo", "ko")                                                  # in the inputs' place, with other rows
+    apart = dict.fromkeys(("q", "k", "qo", "ko", "dq", "dk"), fake)
+    apart.update(dict(zip(ends, (2 * fake, 2 * fake))))
+    for stride, end, start in (("q_out_stride", ends[0], "qo" if back else "q"), ("k_out_stride", ends[1], "ko" if back else "k")):
+        assert call(ptr={**apart, end: apart[start]}, **{stride: 1024}) == INVALID, stride
     none = dict.fromkeys(("q", "k", "pos", "freq", "qo", "ko", "dq", "dk"))
     assert call(n_rows=0, ptr=none) == OK if not back else call(n_rows=0, ptr=none, accumulate=1, ws=(None, 0)) == OK
 
