@@ -586,8 +586,8 @@ nat_status nat_qk_norm_rope_bwd(const nat_qk_params* params, const void* d_q, co
  * Token ids into rows of the body: out_r = scale * E[ids[r]], one rounding; an id outside [0, V) gives a row of zeros.
  *   d_ids [n_rows] int32;  d_E [V, H] row-major, bf16 or f32;  d_out [n_rows, H], same dtype, out_stride elements from row to
  *   row (0 = H).  E, out and out_stride in multiples of 16 bytes, as are rows.
- * Errors: NULL or misaligned pointer, n_rows outside [0, 2^31), scale not finite -> NAT_INVALID_ARG; V <= 0, H <= 0, a row that is not a
- * multiple of 16 bytes, a stride below H -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE.
+ * Errors: NULL or misaligned pointer, n_rows outside [0, 2^31), scale not finite -> NAT_INVALID_ARG; V <= 0, H outside [1, 2^30], a row that is
+ * not a multiple of 16 bytes, a stride below H -> NAT_BAD_SHAPE; dtype -> NAT_UNSUPPORTED_DTYPE.
  */
 nat_status nat_embed(const int32_t* d_ids, int64_t n_rows, const void* d_E, int32_t V, int32_t H, int32_t dtype, float scale,
                      void* d_out, int64_t out_stride, void* stream);

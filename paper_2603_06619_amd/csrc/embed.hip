@@ -82,7 +82,23 @@ struct SortArgs {
   int32_t V;
   int shift, bits, tiles;
   bool scanned;                         // counts hold places
+  unsigned blocks;                      // the workgroups behind these write zeros
+  f32x4* zeros;
+  int64_t chunks;                       // of 16 bytes
 };
+
+// Zeros into the whole gradient, before the sums write the rows that have pairs.  Into the other rows alone, found in the sorted ids beside the sums, there are fewer, but short rows cost
+// more to look for than to write: 300000 pairs over 152064 ids, all of them random, 225 us at 128 elements (1000000 pairs) and 454, 234 and 301 at 512, 393 and 391 at 1024; long ones,
+// where so many random pairs leave few rows out, are slower by up to 8 percent (64000 pairs of 4096 over 32000 ids 319 us and 294).
+//
+// A gradient that the Infinity Cache holds for the most part: by workgroups of the sort's first launch, which leaves most of the chip idle.  2897 rows into 131 MB 28.6 us in all; beside
+// the sums, and only into the rows that no pair has, 32.1.
+__device__ __forceinline__ bool zero_block(const SortArgs& a) {
+  if (blockIdx.x < a.blocks) return false;
+  const int64_t i = (int64_t)(blockIdx.x - a.blocks) * blockDim.x + threadIdx.x;
+  if (i < a.chunks) a.zeros[i] = f32x4{};
+  return true;
+}
 
 __device__ __forceinline__ int32_t key_of(int32_t id, int32_t V) { return (uint32_t)id < (uint32_t)V ? id : V; }
 
@@ -98,6 +114,7 @@ __global__ void __launch_bounds__(64 * kRankWaves) rank_kernel(SortArgs a) {
   constexpr int kLanes = 64 / kPairs;                      // of a pair
   __shared__ __attribute__((aligned(16))) int32_t keys[kMost / kBlock * kBlockPitch];
   __shared__ int counts[kRankWaves][kPairs];
+  if (zero_block(a)) return;
   const int base = (int)(blockIdx.x / (kMost / kPairs)) * kMost;       // of the tile
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n - base < kMost ? (int)a.n - base : kMost, blocks = (n + kBlock - 1) / kBlock;
   for (int i = threadIdx.x; i < kBlock * blocks; i += 64 * kRankWaves)
@@ -252,6 +269,7 @@ template <int W>
 __global__ void __launch_bounds__(64 * W) sort_count_kernel(SortArgs a) {
   constexpr int kThreads = 64 * W;
   __shared__ int bins[kMostBins];
+  if (zero_block(a)) return;
   const int n_bins = 1 << a.bits;
   for (int i = threadIdx.x; i < n_bins; i += kThreads) bins[i] = 0;
   __syncthreads();
@@ -343,13 +361,12 @@ struct SumArgs {
   const int32_t *ids, *rows;            // sorted
   const char* dout;
   float *dE, *part;                     // part: [pieces][2][H], of the run that came in from the piece before, of the one that goes on behind
-  int64_t n, dout_bytes, sum_blocks;    // the other workgroups write zeros
+  int64_t n, dout_bytes;
   int32_t V, H;
-  int piece, slabs, zero_rows;          // pairs per piece, at most 64; workgroups per row; rows of dE per workgroup that writes zeros (0: long ones)
+  int piece, slabs;                     // pairs per piece, at most 64; workgroups per row
   float scale;
   int accumulate;
 };
-constexpr int kMostZeroRows = 2048;
 
 template <typename T>
 __device__ __forceinline__ void write_run(const SumArgs& a, int32_t id, int at, const float (&acc)[Piece<T>::kElements]) {
@@ -362,86 +379,9 @@ __device__ __forceinline__ void write_run(const SumArgs& a, int32_t id, int at, 
   }
 }
 
-// First place of lo .. hi whose id is not below v, found by the whole wavefront: 64 probes per round
-__device__ __forceinline__ int64_t lower_bound(const int32_t* ids, int64_t lo, int64_t hi, int32_t v) {
-  const int lane = threadIdx.x & 63;
-  while (lo < hi) {
-    const int64_t step = (hi - lo + 63) >> 6, probe = lo + lane * step;
-    const int below = __popcll(__ballot(probe < hi && ids[probe] < v));
-    if (below == 0) return lo;
-    const int64_t past = lo + below * step;
-    lo += (below - 1) * step + 1;
-    hi = step == 1 ? lo : past < hi ? past : hi;
-  }
-  return lo;
-}
-
-// Zeros into the rows that no pair has.
-//
-// Long rows: dE as a row of pieces of 4 KB, of which eight workgroups, one on each XCD, take 32, every eighth one each.  Stores alone reach 6.5 TB/s so, and 6.0 where a workgroup's four
-// pieces follow one another (2.49 GB in 381 and 417 us; a workgroup per piece 365, but each has to look for its rows first).  Every wavefront looks for itself.  A gradient that fits
-// the Infinity Cache is faster with fewer and longer workgroups, as short rows have them (20483 rows into 2.49 GB 525 -> 482 us, 5000 into 0.62 GB 135 -> 121, but 2897 into 0.13 GB 31.6 -> 38.9).
-constexpr int64_t kManyZeros = 256 << 20;                  // bytes
-constexpr int kLongRow = 1024, kZeroPiece = 1024, kZeroBlocks = 8, kZeroPieces = 4;       // elements, elements, workgroups, pieces of each
-__device__ __forceinline__ void write_long_zeros(const SumArgs& a, int64_t block) {
-  constexpr int kAll = kZeroPiece * kZeroBlocks * kZeroPieces;
-  const int lane = threadIdx.x & 63;
-  const int64_t base = block / kZeroBlocks * kAll, all = (int64_t)a.V * a.H;
-  const int32_t v0 = (int32_t)(base / a.H), rest = (int32_t)(base - (int64_t)v0 * a.H);
-  const int rows = (rest + kAll - 1) / a.H + 1;              // up to 33
-  uint64_t used = 0;
-  for (int64_t p = lower_bound(a.ids, 0, a.n, v0); p < a.n;) {
-    const int32_t id = p + lane < a.n ? a.ids[p + lane] : INT32_MAX;
-    for (int r = 0; r < rows; ++r) used |= (uint64_t)(__ballot(id == v0 + r) != 0) << r;
-    const int32_t last = __builtin_amdgcn_readlane(id, 63);
-    if (last >= v0 + rows - 1) break;
-    p = lower_bound(a.ids, p + 64, a.n, last + 1);         // (a long run is passed over)
-  }
-  f32x4* to = (f32x4*)(a.dE + base);
-  for (int t = threadIdx.x; t < kZeroPiece / 4; t += blockDim.x) {
-#pragma unroll
-    for (int i = 0; i < kZeroPieces; ++i) {
-      const int at = (i * kZeroBlocks + (int)(block % kZeroBlocks)) * kZeroPiece + 4 * t;
-      if (base + at < all && !(used >> ((uint32_t)(rest + at) / (uint32_t)a.H) & 1)) to[at / 4] = f32x4{};
-    }
-  }
-}
-
-// Otherwise: zero_rows of them to a workgroup, marked in LDS.
-__device__ __forceinline__ void write_zeros(const SumArgs& a, int64_t block) {
-  __shared__ uint32_t used[kMostZeroRows / 32];
-  __shared__ int64_t range[2];
-  const int64_t v0 = block * a.zero_rows, v1 = v0 + a.zero_rows < a.V ? v0 + a.zero_rows : a.V;
-  for (int i = threadIdx.x; i < kMostZeroRows / 32; i += blockDim.x) used[i] = 0;
-  if (threadIdx.x < 64) {
-    const int64_t first = lower_bound(a.ids, 0, a.n, (int32_t)v0), end = lower_bound(a.ids, first, a.n, (int32_t)v1);
-    if (threadIdx.x == 0) {
-      range[0] = first;
-      range[1] = end;
-    }
-  }
-  __syncthreads();
-  for (int64_t p = range[0] + threadIdx.x; p < range[1]; p += blockDim.x) {
-    const int i = (int)(a.ids[p] - v0);
-    atomicOr(&used[i >> 5], 1u << (i & 31));
-  }
-  __syncthreads();
-  const int chunks = a.H / 4;           // of 16 bytes
-  f32x4* to = (f32x4*)(a.dE + v0 * a.H);
-  for (int64_t i = threadIdx.x; i < (v1 - v0) * chunks; i += blockDim.x) {
-    const int v = (int)(i / chunks);
-    if (!(used[v >> 5] >> (v & 31) & 1)) to[i] = f32x4{};
-  }
-}
-
 template <typename T>
 __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a) {
   constexpr int kE = Piece<T>::kElements, kAhead = 8;
-  if (blockIdx.x >= a.sum_blocks) {
-    if (a.zero_rows == 0) write_long_zeros(a, blockIdx.x - a.sum_blocks);
-    else write_zeros(a, blockIdx.x - a.sum_blocks);
-    return;
-  }
   const int slab = blockIdx.x % a.slabs, lane = threadIdx.x & 63;
   const int64_t piece = blockIdx.x / a.slabs, p0 = piece * a.piece;
   const int count = p0 + a.piece < a.n ? a.piece : (int)(a.n - p0), at = (slab * (int)blockDim.x + (int)threadIdx.x) * kE;
@@ -532,7 +472,7 @@ nat_status embed_shape(int64_t n_rows, int32_t V, int32_t H, int32_t dtype, floa
   if (dtype != NAT_DTYPE_BF16 && dtype != NAT_DTYPE_F32) return NAT_UNSUPPORTED_DTYPE;
   *size = dtype == NAT_DTYPE_BF16 ? 2 : 4;
   if (n_rows < 0 || n_rows > INT32_MAX || !(scale > -INFINITY && scale < INFINITY)) return NAT_INVALID_ARG;
-  if (V <= 0 || H <= 0 || (int64_t)H * *size % 16 || (stride != 0 && (stride < H || stride * *size % 16 || stride > INT32_MAX))) return NAT_BAD_SHAPE;
+  if (V <= 0 || H <= 0 || H > (1 << 30) || (int64_t)H * *size % 16 || (stride != 0 && (stride < H || stride * *size % 16 || stride > INT32_MAX))) return NAT_BAD_SHAPE;
   return NAT_OK;
 }
 
@@ -560,9 +500,28 @@ SortPlan sort_plan(int64_t n, int32_t V, int32_t H) {
   return p;
 }
 
+// A larger one: in a launch of its own, 16 bytes per thread and 4 KB per workgroup, in order, of which LDS that nobody uses keeps three on a CU.  2.49 GB 340 us, 7.3 TB/s; with eight
+// on a CU 365, in workgroups of 1024 392, four pieces to a workgroup 381 to 417.  20483 rows of 4096 into 151936 then take 471 us in all, 506 beside the sort, and 482 beside the sums and
+// into the rows without a pair alone.  (311 MB 97.5 in a launch of its own and 92 beside the sort, 623 MB 114.4 and 119.5.)
+constexpr int64_t kManyZeros = 512 << 20;                  // bytes
+__global__ void __launch_bounds__(256) zero_kernel(f32x4* to, int64_t chunks) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < chunks) to[i] = f32x4{};
+}
+nat_status write_all_zeros(float* dE, int64_t chunks, hipStream_t s) {
+  constexpr int64_t most = kMaxWorkItems / 256;
+  for (int64_t at = 0; at < chunks; at += most * 256) {
+    const int64_t left = chunks - at, blocks = (left + 255) / 256;
+    zero_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 53000, s>>>((f32x4*)dE + at, left);
+    NAT_LAUNCH_CHECK();
+  }
+  return NAT_OK;
+}
+
 template <int W>
-nat_status sort_pass(const SortArgs& a, hipStream_t s) {
-  sort_count_kernel<W><<<a.tiles, 64 * W, 0, s>>>(a);
+nat_status sort_pass(SortArgs a, hipStream_t s) {
+  a.blocks = a.tiles;
+  sort_count_kernel<W><<<(unsigned)(a.tiles + (a.chunks + 64 * W - 1) / (64 * W)), 64 * W, 0, s>>>(a);
   NAT_LAUNCH_CHECK();
   if (a.scanned) {
     sort_scan_kernel<<<1 << a.bits, 64 * kManyWaves, 0, s>>>(a);
@@ -616,29 +575,35 @@ extern "C" nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const 
   // 16 bytes per thread, up to 256 threads
   const int64_t lanes = (int64_t)H * size / 16;
   const int threads = lanes >= 256 ? 256 : (int)((lanes + 63) / 64 * 64), slabs = (int)((lanes + threads - 1) / threads);
-  int zero_rows = 65536 / H > kMostZeroRows ? kMostZeroRows : 65536 / H < 1 ? 1 : 65536 / H;
-  if (zero_rows > V / 1024) zero_rows = V < 2048 ? 1 : V / 1024;
-  if (H >= kLongRow && (int64_t)V * H * 4 > kManyZeros) zero_rows = 0;
-  constexpr int64_t kZeros = (int64_t)kZeroPiece * kZeroPieces * kZeroBlocks;
-  const int64_t zero_blocks = accumulate ? 0 : zero_rows == 0 ? ((int64_t)V * H + kZeros - 1) / kZeros * kZeroBlocks : ((int64_t)V + zero_rows - 1) / zero_rows;
-  const int64_t sum_blocks = p.pieces * slabs;
-  if (sum_blocks + zero_blocks > kMaxWorkItems / threads) return NAT_BAD_SHAPE;
+  const int64_t chunks = (int64_t)V * H / 4, sum_blocks = p.pieces * slabs;
+  if (sum_blocks > kMaxWorkItems / threads) return NAT_BAD_SHAPE;
   if (!d_dE || misaligned(d_dE)) return NAT_INVALID_ARG;
   if (n_rows > 0 && (!d_ids || !d_dout || misaligned(d_dout))) return NAT_INVALID_ARG;
   if (n_rows > 0 && (!d_ws || ws_bytes < nat_embed_bwd_workspace_bytes(n_rows, V, H))) return NAT_WORKSPACE_TOO_SMALL;
   if (misaligned(d_ws, 256)) return NAT_INVALID_ARG;
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_EMBED, s);
-  if (n_rows == 0) return accumulate ? NAT_OK : fill_zero_f32(d_dE, (size_t)V * H, s);
+  if (n_rows == 0) return accumulate ? NAT_OK : write_all_zeros(d_dE, chunks, s);
   char* ws = (char*)d_ws;
   int32_t* pair[4];
   for (int i = 0; i < 4; ++i) pair[i] = (int32_t*)(ws + i * p.pairs);
-  SortArgs a{d_ids, nullptr, pair[0], pair[1], (int32_t*)(ws + 4 * p.pairs), n_rows, V, 0, p.bits, p.tiles, p.tiles > kDirectTiles};
+  SortArgs a{d_ids, nullptr, pair[0], pair[1], (int32_t*)(ws + 4 * p.pairs), n_rows, V, 0, p.bits, p.tiles, p.tiles > kDirectTiles,
+             0, (f32x4*)d_dE, !accumulate && chunks * 16 <= kManyZeros ? chunks : 0};
+  if (!accumulate && a.chunks == 0) {
+    const nat_status zeros = write_all_zeros(d_dE, chunks, s);
+    if (zeros != NAT_OK) return zeros;
+  }
+  auto grid = [&](int64_t blocks, int threads) {             // of the sort's first launch
+    a.blocks = (unsigned)blocks;
+    return (unsigned)(blocks + (a.chunks + threads - 1) / threads);
+  };
   if (n_rows <= kRanked) {
-    rank_kernel<kRankPairs, kRanked><<<(unsigned)((n_rows + kRankPairs - 1) / kRankPairs), 64 * kRankWaves, 0, s>>>(a);
+    const unsigned blocks = grid((n_rows + kRankPairs - 1) / kRankPairs, 64 * kRankWaves);
+    rank_kernel<kRankPairs, kRanked><<<blocks, 64 * kRankWaves, 0, s>>>(a);
     NAT_LAUNCH_CHECK();
   } else if (n_rows <= kMerged) {
-    rank_kernel<kTilePairs, kMergeTile><<<(unsigned)((n_rows + kTilePairs - 1) / kTilePairs), 64 * kRankWaves, 0, s>>>(a);
+    const unsigned blocks = grid((n_rows + kTilePairs - 1) / kTilePairs, 64 * kRankWaves);
+    rank_kernel<kTilePairs, kMergeTile><<<blocks, 64 * kRankWaves, 0, s>>>(a);
     NAT_LAUNCH_CHECK();
     a.ids_in = pair[0];
     a.rows_in = pair[1];
@@ -655,13 +620,13 @@ extern "C" nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const 
       if (sorted != NAT_OK) return sorted;
       a.ids_in = a.ids_out;
       a.rows_in = a.rows_out;
+      a.chunks = 0;
     }
   }
-  SumArgs b{a.ids_out, a.rows_out, (const char*)d_dout, d_dE, (float*)(ws + 4 * p.pairs + p.counts), n_rows, (dout_stride ? dout_stride : H) * size, sum_blocks,
-            V, H, p.piece, slabs, zero_rows, scale, accumulate != 0};
-  const unsigned all = (unsigned)(sum_blocks + zero_blocks);
-  if (dtype == NAT_DTYPE_BF16) embed_sum_kernel<uint16_t><<<all, threads, 0, s>>>(b);
-  else embed_sum_kernel<float><<<all, threads, 0, s>>>(b);
+  SumArgs b{a.ids_out, a.rows_out, (const char*)d_dout, d_dE, (float*)(ws + 4 * p.pairs + p.counts), n_rows, (dout_stride ? dout_stride : H) * size, V, H,
+            p.piece, slabs, scale, accumulate != 0};
+  if (dtype == NAT_DTYPE_BF16) embed_sum_kernel<uint16_t><<<(unsigned)sum_blocks, threads, 0, s>>>(b);
+  else embed_sum_kernel<float><<<(unsigned)sum_blocks, threads, 0, s>>>(b);
   NAT_LAUNCH_CHECK();
   if (p.pieces == 1) return NAT_OK;
   if (dtype == NAT_DTYPE_BF16) embed_join_kernel<uint16_t><<<(unsigned)sum_blocks, threads, 0, s>>>(b);

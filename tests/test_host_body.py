@@ -67,7 +67,7 @@ def test_embedding_refusals(nat):  # noqa: F811
     assert call(dtype=2) == DTYPE
     assert call(ids=None) == call(E=None) == call(out=None) == call(E=fake + 8) == call(out=fake + 4) == call(n=-1) == call(n=1 << 31) == INVALID
     assert call(scale=float("nan")) == call(scale=float("inf")) == INVALID
-    assert call(V=0) == call(V=-5) == call(H=0) == call(H=12) == call(H=2, dtype=0) == call(stride=56) == call(stride=68) == call(stride=-64) == SHAPE
+    assert call(V=0) == call(V=-5) == call(H=0) == call(H=(1 << 30) + 8) == call(H=12) == call(H=2, dtype=0) == call(stride=56) == call(stride=68) == call(stride=-64) == SHAPE
     assert call(n=0, ids=None, E=None, out=None) == OK
 
 
