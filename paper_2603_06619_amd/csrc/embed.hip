@@ -1,11 +1,12 @@
 // Rows of an embedding by token id, and the gradient of the embedding: for every token the sum of its rows' gradients.
 //
-// The gradient sorts (id, row) pairs by id, rows of one id staying in order, and then walks the sorted pairs in pieces of equal length, whatever the ids: a token that
+// The gradient of up to 1024 rows compares all ids with one another.  Otherwise it sorts (id, row) pairs by id, rows of one id staying in order, and then walks the sorted pairs in pieces of equal length, whatever the ids: a token that
 // makes up a tenth of the batch is shared by many workgroups like any other rows.  A run of equal ids inside a piece is summed and written by its workgroup; of one that
 // crosses pieces each leaves its part, and a second kernel adds the parts in order.
 //
 // Bound by HBM.  The lookup of 16381 rows of 4096 in bf16, 268 MB (of which text repeats some), 34 us.  The gradient of 20483 such rows into a vocabulary of 151936, of which 2.49 GB
-// are written and 0.17 read, 481 us, 5.5 TB/s; of 2897 rows of 1024 in fp32 into 32000, 143 MB that the Infinity Cache holds, 31 us: ranks 5.5, sums and zeros 22.5, joining 4.
+// are written and 0.17 read, 471 us, 5.6 TB/s: zeros 336, ranks 21, sums 107 (they write their rows again), joining 6; of 2897 rows of 1024 in fp32 into 32000, 143 MB that the Infinity
+// Cache holds, 28 us: ranks and zeros 18.8, sums 6, joining 3.
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
 
@@ -478,6 +479,86 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(SumArgs a, int
   write_run<T>(a, id, at, acc);
 }
 
+// Up to kFew pairs in one launch, without a sort: a workgroup per pair and 64 lanes, which compares its id with all of them, a wavefront with a quarter, and ends unless its pair is the
+// id's first.  Each wavefront adds up those of its quarter, the first wavefront their sums in order.
+//
+// Zeros by other workgroups, kFewSteps 16 bytes per thread, into the rows that no pair has, or none (chunks 0).  As each reads all ids, many pairs and many zeros are left to the sort:
+// 200 pairs over 131 MB 19 us, by the sort 26; 500 19.6 and 26; 1024 over 262 MB 45 and 42.  1000 pairs of 1024 over 8 MB 10.3 us and 15.5, of which the host takes ten.
+constexpr int kFew = 1024, kFewSteps = 4;
+constexpr int64_t kFewWork = int64_t{1} << 33;             // pairs times 16 bytes
+struct FewArgs : SumArgs {
+  unsigned sum_blocks;
+  int64_t chunks;                       // of 16 bytes
+};
+template <typename T>
+__global__ void __launch_bounds__(256) embed_few_kernel(FewArgs a) {
+  constexpr int kE = Piece<T>::kElements, kAhead = 8;
+  if (blockIdx.x >= a.sum_blocks) {
+    __shared__ uint32_t used[256 * kFewSteps / 32 + 1];    // a row has 16 bytes or more
+    const int64_t first = (int64_t)(blockIdx.x - a.sum_blocks) * 256 * kFewSteps;
+    const int row = a.H / 4, v0 = (int)(first / row);
+    const uint32_t rest = (uint32_t)(first - (int64_t)v0 * row);
+    for (int i = threadIdx.x; i < 256 * kFewSteps / 32 + 1; i += 256) used[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.n; i += 256) {
+      const int64_t r = (int64_t)a.ids[i] - v0;
+      if (r >= 0 && r <= 256 * kFewSteps) atomicOr(&used[r >> 5], 1u << (r & 31));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kFewSteps; ++u) {
+      const uint32_t at = u * 256 + threadIdx.x, r = (rest + at) / (uint32_t)row;
+      if (first + at < a.chunks && !(used[r >> 5] >> (r & 31) & 1)) ((f32x4*)a.dE)[first + at] = f32x4{};
+    }
+    return;
+  }
+  __shared__ uint64_t masks[kFew / 64];
+  __shared__ __attribute__((aligned(16))) float sums[4][64 * kE];
+  const int p = blockIdx.x / a.slabs, slab = blockIdx.x % a.slabs, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = (int)a.n;
+  const int blocks = (n + 63) / 64, each = (blocks + 3) / 4;           // of 64 pairs, per wavefront
+  const int id = a.ids[p];
+  for (int b = wave * each; b < (wave + 1) * each && b < blocks; ++b) {
+    const int q = 64 * b + lane;
+    const uint64_t same = __ballot(q < n && a.ids[q < n ? q : p] == id);
+    if (lane == 0) masks[b] = same;
+  }
+  __syncthreads();
+  const bool before = lane < blocks && 64 * lane < p && (masks[lane < blocks ? lane : 0] & (p - 64 * lane >= 64 ? ~uint64_t{0} : (uint64_t{1} << (p - 64 * lane)) - 1));
+  if ((uint32_t)id >= (uint32_t)a.V || __ballot(before)) return;       // the whole workgroup
+  const int at = (slab * 64 + lane) * kE;
+  const bool there = at < a.H;
+  const char* from = a.dout + (there ? at : 0) * (int64_t)sizeof(T);
+  float acc[kE] = {};
+  for (int b = wave * each; b < (wave + 1) * each && b < blocks; ++b) {
+    uint64_t same = masks[b];
+    while (same) {
+      u32x4 x[kAhead];
+      int rows[kAhead], with = 0;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        rows[u] = same ? 64 * b + __builtin_ctzll(same) : p;
+        with += same != 0;
+        same &= same - 1;
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (u < with) x[u] = *(const u32x4*)(from + rows[u] * a.dout_bytes);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (u < with) Piece<T>::add(acc, x[u]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kE; ++i) sums[wave][lane * kE + i] = acc[i];
+  __syncthreads();
+  if (wave || !there) return;
+#pragma unroll
+  for (int w = 1; w < 4; ++w)
+#pragma unroll
+    for (int i = 0; i < kE; ++i) acc[i] += sums[w][lane * kE + i];
+  write_run<T>(a, id, at, acc);
+}
+
 bool misaligned(const void* p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
 
 nat_status embed_shape(int64_t n_rows, int32_t V, int32_t H, int32_t dtype, float scale, int64_t stride, int* size) {
@@ -596,15 +677,38 @@ extern "C" nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const 
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_EMBED, s);
   if (n_rows == 0) return accumulate ? NAT_OK : write_all_zeros(d_dE, chunks, s);
+  // zeros in a launch of others, or in one of their own
+  const int64_t beside = !accumulate && chunks * 16 <= kManyZeros ? chunks : 0;
+  if (!accumulate && beside == 0) {
+    const nat_status zeros = write_all_zeros(d_dE, chunks, s);
+    if (zeros != NAT_OK) return zeros;
+  }
+  const int64_t few_slabs = (lanes + 63) / 64;
+  if (n_rows <= kFew && n_rows * beside <= kFewWork && few_slabs <= 1 << 13) {
+    FewArgs f{};
+    f.ids = d_ids;
+    f.dout = (const char*)d_dout;
+    f.dE = d_dE;
+    f.n = n_rows;
+    f.dout_bytes = (dout_stride ? dout_stride : H) * size;
+    f.V = V;
+    f.H = H;
+    f.slabs = (int)few_slabs;
+    f.scale = scale;
+    f.accumulate = accumulate != 0;
+    f.sum_blocks = (unsigned)(n_rows * few_slabs);
+    f.chunks = beside;
+    const unsigned blocks = f.sum_blocks + (unsigned)((beside + 256 * kFewSteps - 1) / (256 * kFewSteps));
+    if (dtype == NAT_DTYPE_BF16) embed_few_kernel<uint16_t><<<blocks, 256, 0, s>>>(f);
+    else embed_few_kernel<float><<<blocks, 256, 0, s>>>(f);
+    NAT_LAUNCH_CHECK();
+    return NAT_OK;
+  }
   char* ws = (char*)d_ws;
   int32_t* pair[4];
   for (int i = 0; i < 4; ++i) pair[i] = (int32_t*)(ws + i * p.pairs);
   SortArgs a{d_ids, nullptr, pair[0], pair[1], (int32_t*)(ws + 4 * p.pairs), n_rows, V, 0, p.bits, p.tiles, p.tiles > kDirectTiles,
-             0, (f32x4*)d_dE, !accumulate && chunks * 16 <= kManyZeros ? chunks : 0};
-  if (!accumulate && a.chunks == 0) {
-    const nat_status zeros = write_all_zeros(d_dE, chunks, s);
-    if (zeros != NAT_OK) return zeros;
-  }
+             0, (f32x4*)d_dE, beside};
   auto grid = [&](int64_t blocks, int threads) {             // of the sort's first launch
     a.blocks = (unsigned)blocks;
     return (unsigned)(blocks + (a.chunks + threads - 1) / threads);

@@ -193,3 +193,35 @@ def test_gradient_of_a_large_vocabulary(stage, V, H, kind):
     size = torch.zeros((V, H), dtype=torch.float64, device=DEV).index_add_(0, at[ok].long(), dout[ok].double().abs())
     count = torch.zeros(V, dtype=torch.float64, device=DEV).index_add_(0, at[ok].long(), torch.ones(int(ok.sum()), dtype=torch.float64, device=DEV))
     assert bool(((got.double() - want).abs() <= (count[:, None] + 1) * 2.0 ** -24 * size).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n", [255, 256, 1024, 1025])
+def test_gradient_of_few_rows(stage, n, dtype):
+    """Around the sizes at which there is no sort: runs over all 64s of the pairs, from the first pair and to the last; on top of what was there."""
+    V, H = 999, 520
+    ids = ids_of(n, n, V, "any")
+    ids[::7] = 5
+    ids[[0, n - 1]] = V - 1
+    dout, old = normal(n, n, H, dtype=dtype), normal(n + 1, V, H)
+    at, got = check(stage, ids, dout, V, -1.5)
+    assert torch.equal(stage.embed_backward(dout, at, V, -1.5, dE=old.clone(), accumulate=True), old + got)
+    check(stage, np.full(n, 7, np.int32), dout, 8)
+
+
+@pytest.mark.parametrize("n,V,H", [(300, 30011, 2248), (300, 300000, 8), (1024, 30011, 2248), (300, 140001, 1032), (2500, 140001, 1032), (40000, 140001, 1032)])
+def test_gradient_where_the_zeros_change(stage, n, V, H):
+    """Zeros beside the sums, beside the sort, and in a launch of their own."""
+    ids = ids_of(n, n, V, "any")
+    ids[20:30] = V - 1
+    ids[40:240:2] = np.arange(100) * 2 + V // 2
+    at, dout = torch.from_numpy(ids).to(DEV), normal(V, n, H, dtype=torch.bfloat16)
+    got = stage.embed_backward(dout, at, V, dE=torch.full((V, H), float("nan"), device=DEV))
+    ok = (at >= 0) & (at < V)
+    used, place = at[ok].unique(return_inverse=True)
+    total = lambda x: torch.zeros((used.numel(), x.shape[1]), dtype=torch.float64, device=DEV).index_add_(0, place, x)
+    rows = dout[ok].double()
+    limit = (total(torch.ones_like(rows[:, :1])) + 1) * 2.0 ** -24 * total(rows.abs())
+    assert bool(((got[used.long()].double() - total(rows)).abs() <= limit).all())
+    got[used.long()] = 0
+    assert bool((got == 0).all())
