@@ -205,6 +205,15 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _stream_of(*tensors):
+    """The current stream, for tensors (or None) that are all on the current device: a kernel launched there cannot reach others."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor of shape {tuple(t.shape)} is on {t.device}, but the current device is {device}")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def _raise(status, where):
     if status != 0:
         raise NatError(status, where)
@@ -576,8 +585,9 @@ def _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleave
     return _CQkParams(hq, hkv, dim, code, rotary, interleaved, eps, n, q_stride, k_stride), q, k, at
 
 
-def _qk_forward(p, q, k, at, q_out, k_out):
-    _raise(load_library().nat_qk_norm_rope(ctypes.byref(p), q.data_ptr(), k.data_ptr(), *at, q_out.data_ptr(), k_out.data_ptr(), _stream()), "nat_qk_norm_rope")
+def _qk_forward(p, q, k, at, q_out, k_out, others):
+    _raise(load_library().nat_qk_norm_rope(ctypes.byref(p), q.data_ptr(), k.data_ptr(), *at, q_out.data_ptr(), k_out.data_ptr(), _stream_of(q, k, q_out, k_out, *others)),
+           "nat_qk_norm_rope")
 
 
 def nat_qk_norm_rope(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, q_out, k_out):
@@ -585,7 +595,7 @@ def nat_qk_norm_rope(q, k, q_weight, k_weight, position_ids, inv_freq, eps, inte
     and inv_freq float64 [R / 2], or both None; q_out, k_out like q, k, or q, k themselves."""
     p, q, k, at = _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
     p.q_out_stride, p.k_out_stride = _rows(q_out, "q_out", q.shape, q.dtype), _rows(k_out, "k_out", k.shape, q.dtype)
-    _qk_forward(p, q, k, at, q_out, k_out)
+    _qk_forward(p, q, k, at, q_out, k_out, (q_weight, k_weight, position_ids, inv_freq))
 
 
 @functools.lru_cache(maxsize=256)
@@ -593,14 +603,14 @@ def qk_norm_rope_bwd_workspace_bytes(n_rows, head_dim):
     return int(load_library().nat_qk_norm_rope_bwd_workspace_bytes(int(n_rows), int(head_dim)))
 
 
-def _qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dq_weight, dk_weight, accumulate, workspace):
+def _qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dq_weight, dk_weight, accumulate, workspace, others):
     """dq, dk and the weights' gradients have been checked, or made."""
     strides = _rows(dq_out, "dq_out", q.shape, q.dtype, True), _rows(dk_out, "dk_out", k.shape, q.dtype, True)
     if strides != (0, 0):
         (dq_out, dk_out), (p.q_out_stride, p.k_out_stride) = _own_rows((dq_out, dk_out), strides)
     _raise(load_library().nat_qk_norm_rope_bwd(
         ctypes.byref(p), q.data_ptr(), k.data_ptr(), *at, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), _ptr(dq_weight), _ptr(dk_weight),
-        accumulate, _ptr(workspace), _bytes(workspace), _stream()), "nat_qk_norm_rope_bwd")
+        accumulate, _ptr(workspace), _bytes(workspace), _stream_of(q, k, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, *others)), "nat_qk_norm_rope_bwd")
 
 
 def nat_qk_norm_rope_bwd(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, dq_out, dk_out, dq, dk, dq_weight, dk_weight, accumulate,
@@ -611,7 +621,7 @@ def nat_qk_norm_rope_bwd(q, k, q_weight, k_weight, position_ids, inv_freq, eps, 
     p.dq_stride, p.dk_stride = _rows(dq, "dq", q.shape, q.dtype), _rows(dk, "dk", k.shape, q.dtype)
     _vector(dq_weight, torch.float32, p.head_dim, "dq_weight")
     _vector(dk_weight, torch.float32, p.head_dim, "dk_weight")
-    _qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dq_weight, dk_weight, int(bool(accumulate)), workspace)
+    _qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dq_weight, dk_weight, int(bool(accumulate)), workspace, (q_weight, k_weight, position_ids, inv_freq))
 
 
 def _bytes(workspace):
@@ -646,7 +656,7 @@ def nat_embed(ids, E, scale, out):
     V, H = E.shape
     n = ids.numel()
     _raise(load_library().nat_embed(_vector(ids, torch.int32, n, "ids"), n, _ptr(E), V, H, _dtype_code(E), float(scale), _ptr(out),
-                                    _matrix(out, "out", n, H, E.dtype), _stream()), "nat_embed")
+                                    _matrix(out, "out", n, H, E.dtype), _stream_of(ids, E, out)), "nat_embed")
 
 
 @functools.lru_cache(maxsize=256)
@@ -663,7 +673,7 @@ def nat_embed_bwd(ids, dout, scale, dE, accumulate, workspace):
     (dout,), (stride,) = _own_rows((dout,), (_matrix(dout, "dout", n, H, is_input=True),))
     _raise(load_library().nat_embed_bwd(_vector(ids, torch.int32, n, "ids"), n, _ptr(dout), stride, V, H, _dtype_code(dout), float(scale), _ptr(dE),
                                         int(bool(accumulate)), _ptr(workspace),
-                                        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_embed_bwd")
+                                        _bytes(workspace), _stream_of(ids, dout, dE, workspace)), "nat_embed_bwd")
 
 
 @functools.lru_cache(maxsize=256)
@@ -686,14 +696,16 @@ def _pages_args(block_table, seq_lens, change, change_name, free_pages, counts, 
     """The arguments that both calls have."""
     n, n_pages, i32 = seq_lens.numel(), free_pages.numel(), torch.int32
     width = _table(block_table, n)
-    return (block_table.data_ptr(), width, n, page_size, _vector(seq_lens, i32, n, "seq_lens"), _vector(change, i32, n, change_name),
+    args = (block_table.data_ptr(), width, n, page_size, _vector(seq_lens, i32, n, "seq_lens"), _vector(change, i32, n, change_name),
             _vector(free_pages, i32, n_pages, "free_pages"), n_pages, _counts(counts, "counts"))
+    _stream_of(block_table, seq_lens, change, free_pages, counts)
+    return args
 
 
-def _reserve(args, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, workspace):
-    """args: of _pages_args; the others are addresses."""
-    _raise(load_library().nat_kv_reserve(*args, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, _ptr(workspace), _bytes(workspace), _stream()),
-           "nat_kv_reserve")
+def _reserve(args, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, workspace, *others):
+    """args: of _pages_args; the results are addresses, others their tensors."""
+    _raise(load_library().nat_kv_reserve(*args, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, _ptr(workspace), _bytes(workspace),
+                                         _stream_of(workspace, *others)), "nat_kv_reserve")
 
 
 def nat_kv_reserve(block_table, seq_lens, new_lens, free_pages, counts, page_size, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, workspace):
@@ -702,17 +714,18 @@ def nat_kv_reserve(block_table, seq_lens, new_lens, free_pages, counts, page_siz
     n, i32, rows = seq_lens.numel(), torch.int32, int(rows_cap)
     _reserve(_pages_args(block_table, seq_lens, new_lens, "new_lens", free_pages, counts, int(page_size)), rows, _counts(counts_out, "counts_out"),
              _vector(seq_lens_out, i32, n, "seq_lens_out"), _vector(start, i32, n, "start"), _vector(cu_new, i32, n + 1, "cu_new"),
-             _vector(slots, torch.int64, rows, "slots"), _vector(position_ids, i32, rows, "position_ids"), workspace)
+             _vector(slots, torch.int64, rows, "slots"), _vector(position_ids, i32, rows, "position_ids"), workspace,
+             counts_out, seq_lens_out, start, cu_new, slots, position_ids)
 
 
-def _release(args, counts_out, seq_lens_out, workspace):
-    _raise(load_library().nat_kv_release(*args, counts_out, seq_lens_out, _ptr(workspace), _bytes(workspace), _stream()), "nat_kv_release")
+def _release(args, counts_out, seq_lens_out, workspace, *others):
+    _raise(load_library().nat_kv_release(*args, counts_out, seq_lens_out, _ptr(workspace), _bytes(workspace), _stream_of(workspace, *others)), "nat_kv_release")
 
 
 def nat_kv_release(block_table, seq_lens, keep_lens, free_pages, counts, page_size, counts_out, seq_lens_out, workspace):
     """Arguments as nat_kv_reserve's; keep_lens int32 [n_seqs]: the tokens that stay.  free_pages is written behind its first counts[0] entries."""
     _release(_pages_args(block_table, seq_lens, keep_lens, "keep_lens", free_pages, counts, int(page_size)), _counts(counts_out, "counts_out"),
-             _vector(seq_lens_out, torch.int32, seq_lens.numel(), "seq_lens_out"), workspace)
+             _vector(seq_lens_out, torch.int32, seq_lens.numel(), "seq_lens_out"), workspace, counts_out, seq_lens_out)
 
 
 def probe_mfma_scratch_bytes():

@@ -77,7 +77,7 @@ class RolloutStage:
         inv_freq float64 [R / 2], radians per position for the pairs of the first R elements; both None: no rotation.  Returns (q, k), new arrays."""
         p, q, k, at = nb._qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
         q_out, k_out = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
-        nb._qk_forward(p, q, k, at, q_out, k_out)
+        nb._qk_forward(p, q, k, at, q_out, k_out, (q_weight, k_weight, position_ids, inv_freq))
         return q_out, k_out
 
     def norm_rotate_backward(self, dq_out, dk_out, q, k, position_ids, inv_freq, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
@@ -88,7 +88,7 @@ class RolloutStage:
         ws = None
         if dqw is not None or dkw is not None:
             ws = self._buf("norm_rotate", nb.qk_norm_rope_bwd_workspace_bytes(p.n_rows, p.head_dim))
-        nb._qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dqw, dkw, 0, ws)
+        nb._qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dqw, dkw, 0, ws, (q_weight, k_weight, position_ids, inv_freq))
         return dq, dk, dqw, dkw
 
     def embed(self, ids, E, scale=1.0):

@@ -116,3 +116,16 @@ def test_two_graphs_and_an_eager_call_side_by_side(kind):
         torch.cuda.synchronize()
         for got, ref in zip((graphs[0][1], graphs[1][1], mine), want):
             assert all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=lambda f: f.__name__)
+def test_tensors_of_another_device_are_refused(kind, monkeypatch):
+    """A kernel is launched on the current device, which tensors elsewhere may not be reached from (the device is named here only)."""
+    from paper_2603_06619_amd.rollout import RolloutStage
+    stage = RolloutStage(DEV)
+    _, call = kind(gen(3), 20)
+    call(stage)
+    here = torch.cuda.current_device()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: here + 1)
+    with pytest.raises(ValueError, match="current device"):
+        call(stage)
