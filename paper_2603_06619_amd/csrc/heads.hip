@@ -29,12 +29,14 @@ struct HeadsArgs {
   int64_t n_rows, q_stride, k_stride, q_out_stride, k_out_stride, dq_stride, dk_stride;
 };
 
-// 8 elements as they lie in memory
+// 8 elements as they lie in memory.  kOnce: past the caches, for rows that nobody reads again soon.  Only where a load or store of a wavefront covers whole lines of 128 bytes, as the
+// two of a head of 128 elements in bf16 do; others (heads of 64, fp32) lose by it, up to a third.
 template <typename T> struct Chunk;
 template <>
 struct Chunk<uint16_t> {
   u32x4 x;
-  __device__ __forceinline__ static Chunk load(const uint16_t* p) { return {*(const u32x4*)p}; }
+  template <bool kOnce = false>
+  __device__ __forceinline__ static Chunk load(const uint16_t* p) { return {kOnce ? __builtin_nontemporal_load((const u32x4*)p) : *(const u32x4*)p}; }
   __device__ __forceinline__ static Chunk all(float v) {
     const uint32_t b = __builtin_bit_cast(uint32_t, v) >> 16;
     return {u32x4{1, 1, 1, 1} * (b | b << 16)};
@@ -46,11 +48,13 @@ struct Chunk<uint16_t> {
       v[2 * i + 1] = __builtin_bit_cast(float, x[i] & 0xffff0000u);
     }
   }
+  template <bool kOnce = false>
   __device__ __forceinline__ static void store(uint16_t* p, const float (&v)[8]) {
     bf16x8 y;
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = (__bf16)v[i];
-    *(bf16x8*)p = y;
+    if constexpr (kOnce) __builtin_nontemporal_store(y, (bf16x8*)p);
+    else *(bf16x8*)p = y;
   }
   __device__ __forceinline__ static Chunk pick(bool a, const Chunk& p, const Chunk& q) {
     Chunk r;
@@ -62,6 +66,7 @@ struct Chunk<uint16_t> {
 template <>
 struct Chunk<float> {
   f32x4 x, y;
+  template <bool kOnce = false>
   __device__ __forceinline__ static Chunk load(const float* p) { return {*(const f32x4*)p, *(const f32x4*)(p + 4)}; }
   __device__ __forceinline__ static Chunk all(float v) { return {f32x4{v, v, v, v}, f32x4{v, v, v, v}}; }
   __device__ __forceinline__ void get(float (&v)[8]) const {
@@ -71,6 +76,7 @@ struct Chunk<float> {
       v[4 + i] = y[i];
     }
   }
+  template <bool kOnce = false>
   __device__ __forceinline__ static void store(float* p, const float (&v)[8]) {
     *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
     *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
@@ -189,9 +195,12 @@ __device__ __forceinline__ void norm_of(const float (&x)[8], const float (&y)[8]
   *r = rsqrtf(fmaf(sum, 1.f / D, eps));
 }
 
+// Inputs are read past the caches, which the results fill for the next launch: 20.6 thousand rows of 32 + 8 heads 63 us, otherwise 77, between launches that write the inputs and read the
+// results 222 and 227, 14.4 thousand of 28 + 4 115 and 124.  (Results past the caches: 79 instead of 71 with the launch that reads them.)
 // Without loads ahead: 76 registers, six wavefronts per SIMD.  With them, as in the backward pass, 102 and four: 14.4 thousand rows of 28 + 4 heads 36 instead of 33 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kWaves) heads_fwd_kernel(HeadsArgs a) {
+  constexpr bool kOnce = D == 128 && sizeof(T) == 2;
   __shared__ __attribute__((aligned(16))) f32x2 angles[kWaves][D / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Lane<D> l(a, lane);
@@ -215,8 +224,8 @@ __global__ void __launch_bounds__(64 * kWaves) heads_fwd_kernel(HeadsArgs a) {
       const T* from = is_q ? (const T*)a.q + row * a.q_stride + h * D : (const T*)a.k + row * a.k_stride + (h - a.hq) * D;
       T* to = is_q ? (T*)a.q_out + row * a.q_out_stride + h * D : (T*)a.k_out + row * a.k_out_stride + (h - a.hq) * D;
       float x[8], y[8], w[8];
-      Chunk<T>::load(from + l.at[0]).get(x);
-      Chunk<T>::load(from + l.at[1]).get(y);
+      Chunk<T>::template load<kOnce>(from + l.at[0]).get(x);
+      Chunk<T>::template load<kOnce>(from + l.at[1]).get(y);
       if (is_q ? a.wq != nullptr : a.wk != nullptr) {
         float r, s;
         norm_of<D>(x, y, a.eps, &r, &s);
@@ -256,13 +265,16 @@ __device__ __forceinline__ const T* element_of(const HeadsArgs& a, const Steps& 
 template <typename T>
 struct Pair {
   Chunk<T> x, y;
-  __device__ __forceinline__ static Pair load(const T* p, const int (&at)[2]) { return {Chunk<T>::load(p + at[0]), Chunk<T>::load(p + at[1])}; }
+  template <bool kOnce = false>
+  __device__ __forceinline__ static Pair load(const T* p, const int (&at)[2]) {
+    return {Chunk<T>::template load<kOnce>(p + at[0]), Chunk<T>::template load<kOnce>(p + at[1])};
+  }
 };
 
 // A lane adds up the weights' gradients of its elements over its rows and heads; its workgroup's sums go to `part`.  Three wavefronts per SIMD; loads a step ahead took 20.6 thousand
 // rows of 32 + 8 heads from 122 to 117 us, and 2940 of 16 + 16 heads of 64 in fp32, for which there is hardly a second row per wavefront, from 25.5 to 18.3 (with sums across
 // lanes by DPP and lane swaps).
-template <typename T, int D>
+template <typename T, int D, bool kOnce>
 __global__ void __launch_bounds__(64 * kWaves) heads_bwd_kernel(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) f32x2 angles[kWaves][D / 2];
   __shared__ __attribute__((aligned(16))) float sums[kWaves][2][D];
@@ -274,8 +286,8 @@ __global__ void __launch_bounds__(64 * kWaves) heads_bwd_kernel(HeadsArgs a) {
   if (first < a.n_rows) {
     struct Both { Pair<T> x, g; };
     auto load = [&](int64_t row, int step) __attribute__((always_inline)) {
-      return Both{Pair<T>::load(element_of<T, D>(a, steps, row, step, l, a.q, a.k, a.q_stride, a.k_stride), l.at),
-                  Pair<T>::load(element_of<T, D>(a, steps, row, step, l, a.dq_out, a.dk_out, a.q_out_stride, a.k_out_stride), l.at)};
+      return Both{Pair<T>::template load<kOnce>(element_of<T, D>(a, steps, row, step, l, a.q, a.k, a.q_stride, a.k_stride), l.at),
+                  Pair<T>::template load<kOnce>(element_of<T, D>(a, steps, row, step, l, a.dq_out, a.dk_out, a.q_out_stride, a.k_out_stride), l.at)};
     };
     Both next = load(first, 0);
     int next_pos = a.turning ? a.pos[first] : 0;
@@ -341,8 +353,8 @@ __global__ void __launch_bounds__(64 * kWaves) heads_bwd_kernel(HeadsArgs a) {
             }
           }
           if (h < heads) {
-            Chunk<T>::store(out + h * D + l.at[0], g0);
-            Chunk<T>::store(out + h * D + l.at[1], g1);
+            Chunk<T>::template store<kOnce>(out + h * D + l.at[0], g0);
+            Chunk<T>::template store<kOnce>(out + h * D + l.at[1], g1);
           }
         }
       };
@@ -399,6 +411,9 @@ bool other_rows(const void* in, int64_t in_stride, const void* out, int64_t out_
   return n_rows > 1 && in != nullptr && in == out && in_stride != out_stride;
 }
 
+// Gradients of more than it holds go past the caches both ways: 20.6 thousand rows of 32 + 8 heads 97 us, kept 117, between launches that write the gradients and read the results 348 and
+// 363; 5.8 thousand, 177 MB, between such launches 193 and 190.
+constexpr int64_t kInfinityCache = 256 << 20;
 constexpr int kMostBlocks = 1280, kMostSums = 768;       // as many as fit at once, or nearly; backward each leaves sums
 int blocks_of(int64_t n_rows, int most) {
   const int64_t n = (n_rows + kWaves - 1) / kWaves;
@@ -503,11 +518,12 @@ extern "C" nat_status nat_qk_norm_rope_bwd(const nat_qk_params* params, const vo
   const int n = a.n_rows > 0 ? blocks_of(a.n_rows, kMostSums) : 0, D = params->head_dim;
   if (n > 0) {
     if (params->dtype == NAT_DTYPE_BF16) {
-      if (D == 128) heads_bwd_kernel<uint16_t, 128><<<n, 64 * kWaves, 0, s>>>(a);
-      else heads_bwd_kernel<uint16_t, 64><<<n, 64 * kWaves, 0, s>>>(a);
+      if (D == 128 && a.n_rows * a.heads * (D * 2 * 3) > kInfinityCache) heads_bwd_kernel<uint16_t, 128, true><<<n, 64 * kWaves, 0, s>>>(a);
+      else if (D == 128) heads_bwd_kernel<uint16_t, 128, false><<<n, 64 * kWaves, 0, s>>>(a);
+      else heads_bwd_kernel<uint16_t, 64, false><<<n, 64 * kWaves, 0, s>>>(a);
     } else {
-      if (D == 128) heads_bwd_kernel<float, 128><<<n, 64 * kWaves, 0, s>>>(a);
-      else heads_bwd_kernel<float, 64><<<n, 64 * kWaves, 0, s>>>(a);
+      if (D == 128) heads_bwd_kernel<float, 128, false><<<n, 64 * kWaves, 0, s>>>(a);
+      else heads_bwd_kernel<float, 64, false><<<n, 64 * kWaves, 0, s>>>(a);
     }
     NAT_LAUNCH_CHECK();
   }

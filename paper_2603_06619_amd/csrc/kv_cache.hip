@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(256) kv_read_kernel(ReadArgs a) {
 // where there is more than one.  Every cached byte is read once for all heads of the group; the products cost nothing beside that (a group of fewer than 16 heads
 // leaves columns of them empty).  The next 32 tokens are in registers while these are worked on: at two wavefronts per SIMD, 64 KB in flight per compute unit.
 // 128 sequences of up to 8192 tokens (32 heads on 8 of 128, 8-bit) 235 us, 5.3 TB/s; one of 32768 (28 on 4, bf16) 15.5 us, 4.3 TB/s: 256 tokens per
-// workgroup, of which the first loads are a third of the time.  The first from 4 bits 136 us, 4.9 TB/s.
+// workgroup, of which the first loads are a third of the time.  The first from 4 bits 125 us, 5.3 TB/s.
 // Rounded to fewer bits are the probabilities, to bf16 for the product (with an 8-bit row's power of two in them, which rounds nothing).
 constexpr int kTokens = 32;               // tokens per step of a wavefront
 constexpr int kHeads = 16;                // query heads per workgroup
@@ -253,6 +253,15 @@ struct TokenTile {
     else return 32 * s + 8 * g;
   }
 
+  // Of a cache in 4 bits past the chip's caches: nobody reads it again before the next token, and the other layers come in between.  128 sequences of up to 8192 tokens 128 us, otherwise
+  // 141; after a launch that has filled the Infinity Cache 16 sequences of up to 16384 50 and 60, one of 32768 17.4 and 21.4, 128 of up to 2048 with heads of 64 33.4 and 38.5 (which,
+  // called again and again, the cache holds: 31 and 29).
+  template <typename V>
+  __device__ __forceinline__ static V once(const V* p) {
+    if constexpr (kFp4) return __builtin_nontemporal_load(p);
+    else return *p;
+  }
+
   // p0, p1: pages of the two blocks of 16 tokens, at: place of the first in its page
   __device__ __forceinline__ void load(const CacheArgs& c, int p0, int p1, int head, int t0, int lane) {
     const int mask = (1 << c.page_log2) - 1, n = lane & 15, g = lane >> 4;
@@ -261,7 +270,7 @@ struct TokenTile {
     for (int b = 0; b < 2; ++b) {
       const char* row = c.k + ((b ? r1 : r0) + n) * kRowBytes + kKeyBytes * g;
 #pragma unroll
-      for (int i = 0; i < kKeyLoads; ++i) k[b][i] = *(const Key*)(row + 64 * i);
+      for (int i = 0; i < kKeyLoads; ++i) k[b][i] = once((const Key*)(row + 64 * i));
       if constexpr (kFp4) k_exp[b] = c.k_exp[((b ? r1 : r0) + n) * (D / kGroup) + D / 4 * g / kGroup];
       if constexpr (kFormat == NAT_KV_FP8) {
         k_exp[b] = *(const uint32_t*)(c.k_exp + (b ? r1 : r0) + 4 * g);
@@ -271,7 +280,7 @@ struct TokenTile {
 #pragma unroll
     for (int i = 0; i < kValueLoads; ++i) {
       const int row = value_row(i, lane);
-      v[i] = *(const u32x4*)(c.v + ((row < 16 ? r0 : r1 - 16) + row) * kRowBytes + value_at(lane) * 16);
+      v[i] = once((const u32x4*)(c.v + ((row < 16 ? r0 : r1 - 16) + row) * kRowBytes + value_at(lane) * 16));
       if constexpr (kFp4) v_exp[i] = c.v_exp[((row < 16 ? r0 : r1 - 16) + row) * (D / kGroup) + value_at(lane)];
     }
   }
@@ -348,8 +357,8 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
     const int last = (end - 1) / 16, b = t0 / 16;
     t.load(a.c, __builtin_amdgcn_readfirstlane(pages[b]), __builtin_amdgcn_readfirstlane(pages[b < last ? b + 1 : last]), head, first + t0, lane);
   };
-  // In 4 bits one tile, loaded again as soon as its keys and values have been read: 124 registers, four workgroups per compute unit (the case of 128 sequences below 141 us;
-  // with a second tile 145, three workgroups; with a third 157).
+  // In 4 bits one tile, loaded again as soon as its keys and values have been read: 124 registers, four workgroups per compute unit (128 sequences of up to 8192 tokens, loads
+  // through the caches: 141 us; with a second tile 145, three workgroups; with a third 157).
   constexpr int kTiles = kFormat == NAT_KV_FP4 ? 1 : 2;
   auto step = [&](TokenTile<D, kFormat>& t, int t0, int ahead) {
     const int last = (end - 1) / 16, b0 = t0 / 16;
