@@ -253,8 +253,8 @@ struct TokenTile {
     else return 32 * s + 8 * g;
   }
 
-  // Of a cache in 4 bits past the chip's caches: nobody reads it again before the next token, and the other layers come in between.  128 sequences of up to 8192 tokens 128 us, otherwise
-  // 141; after a launch that has filled the Infinity Cache 16 sequences of up to 16384 50 and 60, one of 32768 17.4 and 21.4, 128 of up to 2048 with heads of 64 33.4 and 38.5 (which,
+  // Of a cache in 4 bits past the chip's caches: nobody reads it again before the next token, and the other layers come in between.  128 sequences of up to 8192 tokens 126 us, otherwise
+  // 141; after a launch that has filled the Infinity Cache 126 and 174, 16 of up to 16384 46 and 60, one of 32768 16.5 and 21.4, 128 of up to 2048 with heads of 64 31.6 and 38.5 (which,
   // called again and again, the cache holds: 31 and 29).
   template <typename V>
   __device__ __forceinline__ static V once(const V* p) {
@@ -271,7 +271,7 @@ struct TokenTile {
       const char* row = c.k + ((b ? r1 : r0) + n) * kRowBytes + kKeyBytes * g;
 #pragma unroll
       for (int i = 0; i < kKeyLoads; ++i) k[b][i] = once((const Key*)(row + 64 * i));
-      if constexpr (kFp4) k_exp[b] = c.k_exp[((b ? r1 : r0) + n) * (D / kGroup) + D / 4 * g / kGroup];
+      if constexpr (kFp4) k_exp[b] = once(c.k_exp + ((b ? r1 : r0) + n) * (D / kGroup) + D / 4 * g / kGroup);
       if constexpr (kFormat == NAT_KV_FP8) {
         k_exp[b] = *(const uint32_t*)(c.k_exp + (b ? r1 : r0) + 4 * g);
         v_exp[b] = *(const uint32_t*)(c.v_exp + (b ? r1 : r0) + 4 * g);
@@ -281,7 +281,7 @@ struct TokenTile {
     for (int i = 0; i < kValueLoads; ++i) {
       const int row = value_row(i, lane);
       v[i] = once((const u32x4*)(c.v + ((row < 16 ? r0 : r1 - 16) + row) * kRowBytes + value_at(lane) * 16));
-      if constexpr (kFp4) v_exp[i] = c.v_exp[((row < 16 ? r0 : r1 - 16) + row) * (D / kGroup) + value_at(lane)];
+      if constexpr (kFp4) v_exp[i] = once(c.v_exp + ((row < 16 ? r0 : r1 - 16) + row) * (D / kGroup) + value_at(lane));
     }
   }
 
@@ -562,11 +562,14 @@ bool stride_ok(int64_t s, int64_t row) { return s == 0 || (s >= row && s % 8 == 
 // lengths of a batch differ, and short chunks even them out), or 512 chunks of 256 tokens at least (two steps of each wavefront), and never more than 4096 tokens.  256 sequences of
 // 304 tokens (8 key heads of 128, 8-bit) take 45 us in one chunk each, 66 in two with the join; 8 of 4096 tokens 23 in chunks of 512, 25 of 256; lengths from 33 to 8192 in
 // 128 sequences 101 us in four chunks each, 110 in two.
-int chunk_of(int64_t n_seqs, int64_t blocks, int64_t most) {
+// From 4 bits, where a token is half as many bytes, 2048 tokens take the place of 1024: 128 sequences of up to 2048 (8 key heads of 128) 39.4 us, in two chunks each 44.9; with heads of 64 25.8
+// and 31.2; 100 of up to 3000 54.9 and 52.5.
+constexpr int kFewTokens = 1024;
+int chunk_of(int64_t n_seqs, int64_t blocks, int64_t most, int64_t few) {
   auto min = [](int64_t x, int64_t y) { return x < y ? x : y; };
   auto max = [](int64_t x, int64_t y) { return x > y ? x : y; };
   const int64_t all = max(1, n_seqs * blocks), least = max(1, (most + kMaxChunk - 1) / kMaxChunk);
-  const int64_t n = max(least, max(min(4096 / all, most / 1024), min((512 + all - 1) / all, most / kMinChunk)));
+  const int64_t n = max(least, max(min(4096 / all, most / few), min((512 + all - 1) / all, most / kMinChunk)));
   return (int)max(kMinChunk, ((most + n - 1) / n + 127) / 128 * 128);
 }
 
@@ -607,11 +610,11 @@ struct LaunchDecode {
 };
 
 struct DecodePlan { int chunk, n_chunks, head_blocks, join_waves; };
-bool decode_plan(int64_t n_seqs, int64_t hq, int64_t hkv, int64_t most, DecodePlan* p) {
+bool decode_plan(int64_t n_seqs, int64_t hq, int64_t hkv, int64_t most, int64_t few, DecodePlan* p) {
   if (n_seqs * hq > INT32_MAX) return false;
   const int64_t group = hq / hkv;
   p->head_blocks = (int)((group + kHeads - 1) / kHeads);
-  p->chunk = chunk_of(n_seqs, hkv * p->head_blocks, most);
+  p->chunk = chunk_of(n_seqs, hkv * p->head_blocks, most, few);
   const int64_t n = most > 0 ? (most + p->chunk - 1) / p->chunk : 1;
   p->n_chunks = (int)n;
   p->join_waves = (int)(n > kJoinChunks * kMaxJoinWaves ? kMaxJoinWaves : (n + kJoinChunks - 1) / kJoinChunks);
@@ -679,7 +682,7 @@ extern "C" nat_status nat_kv_read(const nat_kv_cache* cache, const int32_t* d_bl
 extern "C" size_t nat_attn_decode_workspace_bytes(int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_tokens) {
   DecodePlan p;
   if (!decode_shape_ok(n_seqs, n_q_heads, n_kv_heads, head_dim, max_tokens) || n_seqs == 0 ||
-      !decode_plan(n_seqs, n_q_heads, n_kv_heads, max_tokens, &p) || p.n_chunks == 1)
+      !decode_plan(n_seqs, n_q_heads, n_kv_heads, max_tokens, kFewTokens, &p) || p.n_chunks == 1)
     return 0;
   return ((size_t)n_seqs * n_q_heads * p.n_chunks * (head_dim + 2) * 4 + 255) / 256 * 256;
 }
@@ -694,7 +697,7 @@ extern "C" nat_status nat_attn_decode(const nat_kv_cache* cache, const void* d_q
   const int64_t most = (int64_t)table_width * cache->page_size, row = (int64_t)n_q_heads * cache->head_dim;
   DecodePlan p;
   if (!decode_shape_ok(n_seqs, n_q_heads, cache->n_kv_heads, cache->head_dim, most) || !stride_ok(q_stride, row) || !stride_ok(out_stride, row) ||
-      !decode_plan(n_seqs, n_q_heads, cache->n_kv_heads, most, &p))
+      !decode_plan(n_seqs, n_q_heads, cache->n_kv_heads, most, cache->format == NAT_KV_FP4 ? 2 * kFewTokens : kFewTokens, &p))
     return NAT_BAD_SHAPE;
   if (n_seqs == 0) return NAT_OK;
   if (!d_q || (table_width > 0 && !d_block_table) || !d_seq_lens || !d_out || !d_lse || misaligned(d_q) || misaligned(d_out)) return NAT_INVALID_ARG;
