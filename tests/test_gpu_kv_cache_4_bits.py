@@ -218,3 +218,11 @@ def test_pages_beyond_32_bit_offsets(stage):
     q, lens = torch.randn((1, 16, D), generator=g, device=DEV, dtype=torch.bfloat16), torch.tensor([600], dtype=torch.int32, device=DEV)
     for a, b in zip(stage.decode(q, cache, pages, lens), stage.decode(q, small, order, lens)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("D,longest", [(64, 2048), (64, 4200), (128, 6150)])
+def test_decode_of_many_sequences_in_large_chunks(stage, D, longest):
+    """A chunk of 2048 tokens or a little more per workgroup: sequences that end at, before and behind one, and many short ones."""
+    lens = [longest, 0, 1, 2047, 2048, min(2049, longest), min(2176, longest), min(2177, longest), min(4100, longest)] + [7 * i % 50 for i in range(63)]
+    c = decode_case(15, lens, 8, 8, D, 16)
+    check_decode(c, *stage.decode(c["q"], c["cache"], c["table"], c["lens"]))
