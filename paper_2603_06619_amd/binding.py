@@ -207,7 +207,7 @@ def _stream():
 
 def _stream_of(*tensors):
     """The current stream, for tensors (or None) that are all on the current device: a kernel launched there cannot reach others."""
-    device = torch.cuda.current_device()
+    device = torch._C._cuda_getDevice()              # (tensors on a device: torch.cuda has been set up)
     for t in tensors:
         if t is not None and t.get_device() != device:
             raise ValueError(f"a tensor of shape {tuple(t.shape)} is on {t.device}, but the current device is {device}")
@@ -586,8 +586,7 @@ def _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleave
 
 
 def _qk_forward(p, q, k, at, q_out, k_out, others):
-    _raise(load_library().nat_qk_norm_rope(ctypes.byref(p), q.data_ptr(), k.data_ptr(), *at, q_out.data_ptr(), k_out.data_ptr(), _stream_of(q, k, q_out, k_out, *others)),
-           "nat_qk_norm_rope")
+    _raise(load_library().nat_qk_norm_rope(ctypes.byref(p), q.data_ptr(), k.data_ptr(), *at, q_out.data_ptr(), k_out.data_ptr(), _stream_of(q, k, *others)), "nat_qk_norm_rope")
 
 
 def nat_qk_norm_rope(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, q_out, k_out):
@@ -595,7 +594,7 @@ def nat_qk_norm_rope(q, k, q_weight, k_weight, position_ids, inv_freq, eps, inte
     and inv_freq float64 [R / 2], or both None; q_out, k_out like q, k, or q, k themselves."""
     p, q, k, at = _qk_params(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved)
     p.q_out_stride, p.k_out_stride = _rows(q_out, "q_out", q.shape, q.dtype), _rows(k_out, "k_out", k.shape, q.dtype)
-    _qk_forward(p, q, k, at, q_out, k_out, (q_weight, k_weight, position_ids, inv_freq))
+    _qk_forward(p, q, k, at, q_out, k_out, (q_out, k_out, q_weight, k_weight, position_ids, inv_freq))
 
 
 @functools.lru_cache(maxsize=256)
@@ -610,7 +609,7 @@ def _qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dq_weight, dk_weight, accu
         (dq_out, dk_out), (p.q_out_stride, p.k_out_stride) = _own_rows((dq_out, dk_out), strides)
     _raise(load_library().nat_qk_norm_rope_bwd(
         ctypes.byref(p), q.data_ptr(), k.data_ptr(), *at, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), _ptr(dq_weight), _ptr(dk_weight),
-        accumulate, _ptr(workspace), _bytes(workspace), _stream_of(q, k, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, *others)), "nat_qk_norm_rope_bwd")
+        accumulate, _ptr(workspace), _bytes(workspace), _stream_of(q, k, dq_out, dk_out, workspace, *others)), "nat_qk_norm_rope_bwd")
 
 
 def nat_qk_norm_rope_bwd(q, k, q_weight, k_weight, position_ids, inv_freq, eps, interleaved, dq_out, dk_out, dq, dk, dq_weight, dk_weight, accumulate,
@@ -621,7 +620,8 @@ def nat_qk_norm_rope_bwd(q, k, q_weight, k_weight, position_ids, inv_freq, eps, 
     p.dq_stride, p.dk_stride = _rows(dq, "dq", q.shape, q.dtype), _rows(dk, "dk", k.shape, q.dtype)
     _vector(dq_weight, torch.float32, p.head_dim, "dq_weight")
     _vector(dk_weight, torch.float32, p.head_dim, "dk_weight")
-    _qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dq_weight, dk_weight, int(bool(accumulate)), workspace, (q_weight, k_weight, position_ids, inv_freq))
+    _qk_backward(p, q, k, at, dq_out, dk_out, dq, dk, dq_weight, dk_weight, int(bool(accumulate)), workspace,
+                 (dq, dk, dq_weight, dk_weight, q_weight, k_weight, position_ids, inv_freq))
 
 
 def _bytes(workspace):

@@ -126,6 +126,6 @@ def test_tensors_of_another_device_are_refused(kind, monkeypatch):
     _, call = kind(gen(3), 20)
     call(stage)
     here = torch.cuda.current_device()
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: here + 1)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: here + 1)
     with pytest.raises(ValueError, match="current device"):
         call(stage)
