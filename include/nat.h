@@ -598,8 +598,8 @@ nat_status nat_embed(const int32_t* d_ids, int64_t n_rows, const void* d_E, int3
  *   d_dE [V, H] float: overwritten (zeros where no row has the id), or added to when accumulate != 0, as d_dW of nat_loss_fwd_bwd: with
  *                tied weights both go into one array.  Ids outside [0, V) add nothing.
  *   d_ws / ws_bytes: at least nat_embed_bwd_workspace_bytes, 256-byte aligned.
- * Ids are sorted on the device, rows of one id staying in order, and a row of dE is a sum in fp32 whose order depends on the ids
- * alone: results do not change from run to run.  No atomics on floats.
+ * A row of dE is a sum in fp32 whose order depends on the ids and the sizes alone: results do not change from run to run.  No atomics
+ * on floats.
  * Errors as nat_embed, plus V > 2^30, n_rows >= 2^29 or more work than a launch has room for -> NAT_BAD_SHAPE, NAT_WORKSPACE_TOO_SMALL.  With n_rows = 0 dE is zeros, or stays.
  */
 size_t nat_embed_bwd_workspace_bytes(int64_t n_rows, int32_t V, int32_t H);

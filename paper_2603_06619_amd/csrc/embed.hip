@@ -1,11 +1,11 @@
 // Rows of an embedding by token id, and the gradient of the embedding: for every token the sum of its rows' gradients.
 //
-// The gradient of up to 1024 rows compares all ids with one another.  Otherwise it sorts (id, row) pairs by id, rows of one id staying in order, and then walks the sorted pairs in pieces of equal length, whatever the ids: a token that
-// makes up a tenth of the batch is shared by many workgroups like any other rows.  A run of equal ids inside a piece is summed and written by its workgroup; of one that
-// crosses pieces each leaves its part, and a second kernel adds the parts in order.
+// The gradient of up to 1024 rows compares all ids with one another.  Otherwise it sorts (id, row) pairs by id, rows of one id staying in order, and then walks the sorted pairs in pieces of
+// equal length, whatever the ids: a token that makes up a tenth of the batch is shared by many workgroups like any other rows.  A run of equal ids inside a piece is summed and written by
+// its workgroup; of one that crosses pieces each leaves its part, and a second kernel adds the parts in order.
 //
 // Bound by HBM.  The lookup of 16381 rows of 4096 in bf16, 268 MB (of which text repeats some), 34 us.  The gradient of 20483 such rows into a vocabulary of 151936, of which 2.49 GB
-// are written and 0.17 read, 471 us, 5.6 TB/s: zeros 336, ranks 21, sums 107 (they write their rows again), joining 6; of 2897 rows of 1024 in fp32 into 32000, 143 MB that the Infinity
+// are written and 0.17 read, 457 us, 5.8 TB/s: zeros 340, ranks 21, sums 80 (they write their rows again), joining 6; of 2897 rows of 1024 in fp32 into 32000, 143 MB that the Infinity
 // Cache holds, 28 us: ranks and zeros 18.8, sums 6, joining 3.
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
@@ -597,8 +597,8 @@ SortPlan sort_plan(int64_t n, int32_t V, int32_t H) {
 }
 
 // A larger one: in a launch of its own, 16 bytes per thread and 4 KB per workgroup, in order, of which LDS that nobody uses keeps three on a CU.  2.49 GB 340 us, 7.3 TB/s; with eight
-// on a CU 365, in workgroups of 1024 392, four pieces to a workgroup 381 to 417.  20483 rows of 4096 into 151936 then take 471 us in all, 506 beside the sort, and 482 beside the sums and
-// into the rows without a pair alone.  (311 MB 97.5 in a launch of its own and 92 beside the sort, 623 MB 114.4 and 119.5.)
+// on a CU 365, in workgroups of 1024 392, four pieces to a workgroup 381 to 417.  20483 rows of 4096 into 151936 then took 471 us in all, 506 beside the sort, and 482 beside the sums and
+// into the rows without a pair alone (457 since rows are read past the caches).  (311 MB 97.5 in a launch of its own and 92 beside the sort, 623 MB 114.4 and 119.5.)
 constexpr int64_t kManyZeros = 512 << 20;                  // bytes
 __global__ void __launch_bounds__(256) zero_kernel(f32x4* to, int64_t chunks) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;

@@ -4,8 +4,8 @@
 // of a pair (i, i + R / 2) are its own, and pairs of neighbours are anyway.  The R / 2 sines and cosines of a row are formed by a lane each and go to all heads of the
 // row through LDS: a wavefront takes whole rows, of few rows parts of them.
 //
-// Bound by HBM: 14.4 thousand rows of 28 + 4 heads of 128 in bf16, 212 MB, take 38 us while half of them lie in the Infinity Cache, 44 (4.8 TB/s, a copy: 5.0) otherwise; 20.6 thousand of
-// 32 + 8 forward 66 us (377 MB), backward 117 (566 MB) and 5 for the weights' gradients.  64 rows of 32 + 8, the step of a decoding batch, 3.7 us (6.1 with a wavefront per row).
+// Bound by HBM: 14.4 thousand rows of 28 + 4 heads of 128 in bf16, 212 MB, take 37 us, 5.7 TB/s (a copy: 5.0); 20.6 thousand of 32 + 8 forward 63 us (377 MB), backward 105 (566 MB; 97 where
+// the forward pass has not just read the rows past the caches) and 5 for the weights' gradients.  64 rows of 32 + 8, the step of a decoding batch, 3.7 us (6.1 with a wavefront per row).
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
 
