@@ -10,6 +10,8 @@
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
 
+#include <type_traits>
+
 namespace nat {
 namespace {
 
@@ -143,43 +145,78 @@ struct ReadArgs {
   uint16_t *k, *v;
 };
 
+// 8 elements of a row as the cache has them
 template <int D, int kFormat>
-__device__ __forceinline__ void read_row(const char* cache, const uint8_t* exps, int64_t from, bool there, uint16_t* row, int lane) {
-  u32x4 x = {0, 0, 0, 0};
-  if (there) {
+struct Stored {
+  typedef uint32_t Bits __attribute__((ext_vector_type(kFormat == NAT_KV_BF16 ? 4 : 2)));
+  std::conditional_t<kFormat == NAT_KV_FP4, uint32_t, Bits> x;
+  uint8_t exp;
+  __device__ __forceinline__ void load(const char* cache, const uint8_t* exps, int64_t from, int lane) {
+    constexpr int kBytes = sizeof(x);
+    x = *(const decltype(x)*)(cache + (from * (D / 8) + lane) * kBytes);
+    if constexpr (kFormat == NAT_KV_FP4) exp = exps[from * (D / kGroup) + lane / (kGroup / 8)];
+    if constexpr (kFormat == NAT_KV_FP8) exp = exps[from];
+  }
+  __device__ __forceinline__ u32x4 bf16() const {
     if constexpr (kFormat == NAT_KV_BF16) {
-      x = *(const u32x4*)(cache + (from * D + 8 * lane) * 2);
+      return x;
     } else if constexpr (kFormat == NAT_KV_FP4) {
-      x = widen_fp4(*(const uint32_t*)(cache + from * (D / 2) + 4 * lane), exps[from * (D / kGroup) + lane / (kGroup / 8)]);
+      return widen_fp4(x, exp);
     } else {
-      const u32x2 y = *(const u32x2*)(cache + from * D + 8 * lane);
-      const float scale = power_of_two(exps[from]);
+      const float scale = power_of_two(exp);
+      u32x4 y;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], true);
-        x[2 * i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(lo * scale, bf16x2));
-        x[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(hi * scale, bf16x2));
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[i], true);
+        y[2 * i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(lo * scale, bf16x2));
+        y[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(hi * scale, bf16x2));
       }
+      return y;
     }
   }
-  *(u32x4*)(row + 8 * lane) = x;
-}
+};
 
-// The sequence of a packed row is searched for by the lanes that read it.  106 MB of 6 sequences in 20 us, 5.3 TB/s: most of it written, where a copy writes half.
+// The sequence of a packed row is searched for by the lanes that read it, once for the two rows that each of them reads: a chain of five or six loads, after which both rows of keys and of
+// values are under way.  106 MB of 6 sequences from 8 bits in 18.4 us, 5.8 TB/s, most of it written, where a copy writes half; 102 MB from 4 bits in 18.1, behind a launch that fills the
+// Infinity Cache and with one that reads the rows 56 (a row per lane 20.3, 20.9 and 64; four rows 19.2, 18.1 and 57).
+constexpr int kReadRows = 2;
 template <int D, int kFormat>
 __global__ void __launch_bounds__(256) kv_read_kernel(ReadArgs a) {
-  constexpr int kLanes = D / 8;
+  constexpr int kLanes = D / 8, kPairs = 256 / kLanes;
   const int lane = threadIdx.x % kLanes;
-  const int64_t id = a.first + (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, row = id / a.c.hkv;
-  if (row >= a.n_rows || row < a.cu[0] || row >= a.cu[a.n_seqs]) return;
-  const int head = (int)(id - row * a.c.hkv);
-  const int seq = rollout_of_pos(a.cu, 0, a.n_seqs, row);
-  const int64_t at = row - a.cu[seq], place = at >> a.c.page_log2;
-  const int page = place < a.table_width ? a.table[(int64_t)seq * a.table_width + place] : -1;
-  const bool there = page >= 0 && page < a.c.n_pages;
-  const int64_t from = there ? cache_row(a.c, page, head, (int)(at & ((1 << a.c.page_log2) - 1))) : 0;
-  read_row<D, kFormat>(a.c.k, a.c.k_exp, from, there, a.k + row * a.k_stride + head * D, lane);
-  read_row<D, kFormat>(a.c.v, a.c.v_exp, from, there, a.v + row * a.v_stride + head * D, lane);
+  const int64_t first = a.cu[0], last = a.cu[a.n_seqs] < a.n_rows ? a.cu[a.n_seqs] : a.n_rows;
+  int seq = 0, page[kReadRows], head[kReadRows];
+  int64_t begin = 0, end = 0, row[kReadRows], at[kReadRows];
+#pragma unroll
+  for (int u = 0; u < kReadRows; ++u) {
+    const int64_t id = a.first + ((int64_t)blockIdx.x * kReadRows + u) * kPairs + threadIdx.x / kLanes;
+    row[u] = id / a.c.hkv;
+    head[u] = (int)(id - row[u] * a.c.hkv);
+    if (row[u] < first || row[u] >= last) row[u] = -1;
+    if (row[u] >= end) {
+      seq = rollout_of_pos(a.cu, 0, a.n_seqs, row[u]);
+      begin = a.cu[seq];
+      end = a.cu[seq + 1];
+    }
+    at[u] = row[u] - begin;
+    const int64_t place = at[u] >> a.c.page_log2;
+    page[u] = -1;
+    if (row[u] >= 0 && place < a.table_width) page[u] = a.table[(int64_t)seq * a.table_width + place];
+  }
+  Stored<D, kFormat> k[kReadRows], v[kReadRows];
+#pragma unroll
+  for (int u = 0; u < kReadRows; ++u) {
+    if (page[u] >= a.c.n_pages) page[u] = -1;
+    const int64_t from = page[u] >= 0 ? cache_row(a.c, page[u], head[u], (int)(at[u] & ((1 << a.c.page_log2) - 1))) : 0;
+    k[u].load(a.c.k, a.c.k_exp, from, lane);
+    v[u].load(a.c.v, a.c.v_exp, from, lane);
+  }
+#pragma unroll
+  for (int u = 0; u < kReadRows; ++u) {
+    if (row[u] < 0) continue;
+    *(u32x4*)(a.k + row[u] * a.k_stride + head[u] * D + 8 * lane) = page[u] >= 0 ? k[u].bf16() : u32x4{0, 0, 0, 0};
+    *(u32x4*)(a.v + row[u] * a.v_stride + head[u] * D + 8 * lane) = page[u] >= 0 ? v[u].bf16() : u32x4{0, 0, 0, 0};
+  }
 }
 
 // ------------------------------------------------------------------ one new token ----
@@ -600,7 +637,7 @@ struct LaunchWrite {
 };
 template <int D, int kFormat>
 struct LaunchRead {
-  static void go(ReadArgs a, hipStream_t s) { launch_rows(kv_read_kernel<D, kFormat>, a, 256 / (D / 8), s); }
+  static void go(ReadArgs a, hipStream_t s) { launch_rows(kv_read_kernel<D, kFormat>, a, kReadRows * (256 / (D / 8)), s); }
 };
 template <int D, int kFormat>
 struct LaunchDecode {
