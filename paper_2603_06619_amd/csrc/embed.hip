@@ -5,10 +5,12 @@
 // its workgroup; of one that crosses pieces each leaves its part, and a second kernel adds the parts in order.
 //
 // Bound by HBM.  The lookup of 16381 rows of 4096 in bf16, 268 MB (of which text repeats some), 34 us.  The gradient of 20483 such rows into a vocabulary of 151936, of which 2.49 GB
-// are written and 0.17 read, 457 us, 5.8 TB/s: zeros 340, ranks 21, sums 80 (they write their rows again), joining 6; of 2897 rows of 1024 in fp32 into 32000, 143 MB that the Infinity
+// are written and 0.17 read, 449 us, 5.9 TB/s: zeros and ranks 345, merging 8, sums 80 (they write their rows again), joining 6; of 2897 rows of 1024 in fp32 into 32000, 143 MB that the Infinity
 // Cache holds, 28 us: ranks and zeros 18.8, sums 6, joining 3.
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
+
+#include <type_traits>
 
 namespace nat {
 namespace {
@@ -110,22 +112,22 @@ __device__ __forceinline__ int32_t key_of(int32_t id, int32_t V) { return (uint3
 constexpr int kRanked = 8192, kRankWaves = 16, kRankPairs = 16, kTilePairs = 64;
 constexpr int kMergeTile = 4096, kMerged = 32768;
 constexpr int kBlock = 64, kBlockPitch = kBlock + 4;       // four lanes' blocks in different banks
-template <int kPairs, int kMost>
-__global__ void __launch_bounds__(64 * kRankWaves) rank_kernel(SortArgs a) {
+template <int kPairs, int kMost, int W>
+__global__ void __launch_bounds__(64 * W) rank_kernel(SortArgs a) {
   typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
   constexpr int kLanes = 64 / kPairs;                      // of a pair
   __shared__ __attribute__((aligned(16))) int32_t keys[kMost / kBlock * kBlockPitch];
-  __shared__ int counts[kRankWaves][kPairs];
+  __shared__ int counts[W][kPairs];
   if (zero_block(a)) return;
   const int base = (int)(blockIdx.x / (kMost / kPairs)) * kMost;       // of the tile
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.n - base < kMost ? (int)a.n - base : kMost, blocks = (n + kBlock - 1) / kBlock;
-  for (int i = threadIdx.x; i < kBlock * blocks; i += 64 * kRankWaves)
+  for (int i = threadIdx.x; i < kBlock * blocks; i += 64 * W)
     keys[i / kBlock * kBlockPitch + i % kBlock] = i < n ? key_of(a.ids_in[base + i], a.V) : INT32_MAX;
   __syncthreads();
   const int mine = (int)(blockIdx.x % (kMost / kPairs)) * kPairs + lane % kPairs, own = mine / kBlock, it = own < blocks ? keys[own * kBlockPitch + mine % kBlock] : 0;
   const int key = it < INT32_MAX ? it : 0;                 // (what a place without a pair counts is not used)
   int before = 0;
-  for (int b = wave * kLanes + lane / kPairs; b < blocks; b += kLanes * kRankWaves) {
+  for (int b = wave * kLanes + lane / kPairs; b < blocks; b += kLanes * W) {
     const int32_t* block = keys + b * kBlockPitch;
     // keys that are not there are never below; of the own block those before this pair may be equal
     if (b != own) {
@@ -153,7 +155,7 @@ __global__ void __launch_bounds__(64 * kRankWaves) rank_kernel(SortArgs a) {
   if (threadIdx.x >= kPairs || mine >= n) return;
   before = 0;
 #pragma unroll
-  for (int w = 0; w < kRankWaves; ++w) before += counts[w][lane];
+  for (int w = 0; w < W; ++w) before += counts[w][lane];
   a.ids_out[base + before] = key;
   a.rows_out[base + before] = base + mine;
 }
@@ -381,7 +383,7 @@ __device__ __forceinline__ void write_run(const SumArgs& a, int32_t id, int at, 
   }
 }
 
-// Rows are read past the caches, which hold what is written (20483 of 4096 into 151936 in all 456 us, otherwise 471; 20000 into 20000 122 and 148, and 197 and 211 between the launches that
+// Rows are read past the caches, which hold what is written (20483 of 4096 into 151936, then, in all 456 us, otherwise 471; 20000 into 20000 122 and 148, and 197 and 211 between the launches that
 // write the rows and read the sums).
 template <typename T>
 __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a) {
@@ -596,10 +598,12 @@ SortPlan sort_plan(int64_t n, int32_t V, int32_t H) {
   return p;
 }
 
-// A larger one: in a launch of its own, 16 bytes per thread and 4 KB per workgroup, in order, of which LDS that nobody uses keeps three on a CU.  2.49 GB 340 us, 7.3 TB/s; with eight
-// on a CU 365, in workgroups of 1024 392, four pieces to a workgroup 381 to 417.  20483 rows of 4096 into 151936 then took 471 us in all, 506 beside the sort, and 482 beside the sums and
-// into the rows without a pair alone (457 since rows are read past the caches).  (311 MB 97.5 in a launch of its own and 92 beside the sort, 623 MB 114.4 and 119.5.)
+// A larger one: by workgroups of 256 threads, 16 bytes per thread and 4 KB per workgroup, in order, of which LDS that nobody uses keeps three on a CU.  2.49 GB 340 us, 7.3 TB/s; with eight
+// on a CU 365, in workgroups of 1024 392, four pieces to a workgroup 381 to 417.  Behind those of the sort's first launch, then of four wavefronts, or in a launch of their own where it is
+// another: 20483 rows of 4096 into 151936 449 us in all; a launch of their own 457, beside sixteen wavefronts 490, beside the sums and into the rows without a pair alone 470.
+// (311 MB 97.5 in a launch of their own and 92 beside sixteen wavefronts, 623 MB 122.5, or 120.5, and 125.)
 constexpr int64_t kManyZeros = 512 << 20;                  // bytes
+constexpr size_t kZeroLds = 52000;
 __global__ void __launch_bounds__(256) zero_kernel(f32x4* to, int64_t chunks) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i < chunks) to[i] = f32x4{};
@@ -608,7 +612,7 @@ nat_status write_all_zeros(float* dE, int64_t chunks, hipStream_t s) {
   constexpr int64_t most = kMaxWorkItems / 256;
   for (int64_t at = 0; at < chunks; at += most * 256) {
     const int64_t left = chunks - at, blocks = (left + 255) / 256;
-    zero_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 53000, s>>>((f32x4*)dE + at, left);
+    zero_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, kZeroLds, s>>>((f32x4*)dE + at, left);
     NAT_LAUNCH_CHECK();
   }
   return NAT_OK;
@@ -680,14 +684,16 @@ extern "C" nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const 
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_EMBED, s);
   if (n_rows == 0) return accumulate ? NAT_OK : write_all_zeros(d_dE, chunks, s);
-  // zeros in a launch of others, or in one of their own
+  // zeros beside others of the launch, or in a launch of their own
   const int64_t beside = !accumulate && chunks * 16 <= kManyZeros ? chunks : 0;
-  if (!accumulate && beside == 0) {
+  const bool many = !accumulate && beside == 0, by_ranks = n_rows <= kMerged && chunks <= kMaxWorkItems - (1 << 24);
+  const int64_t few_slabs = (lanes + 63) / 64;
+  const bool few = n_rows <= kFew && n_rows * beside <= kFewWork && few_slabs <= 1 << 13;
+  if (many && (few || !by_ranks)) {
     const nat_status zeros = write_all_zeros(d_dE, chunks, s);
     if (zeros != NAT_OK) return zeros;
   }
-  const int64_t few_slabs = (lanes + 63) / 64;
-  if (n_rows <= kFew && n_rows * beside <= kFewWork && few_slabs <= 1 << 13) {
+  if (few) {
     FewArgs f{};
     f.ids = d_ids;
     f.dout = (const char*)d_dout;
@@ -711,18 +717,20 @@ extern "C" nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const 
   int32_t* pair[4];
   for (int i = 0; i < 4; ++i) pair[i] = (int32_t*)(ws + i * p.pairs);
   SortArgs a{d_ids, nullptr, pair[0], pair[1], (int32_t*)(ws + 4 * p.pairs), n_rows, V, 0, p.bits, p.tiles, p.tiles > kDirectTiles,
-             0, (f32x4*)d_dE, beside};
-  auto grid = [&](int64_t blocks, int threads) {             // of the sort's first launch
-    a.blocks = (unsigned)blocks;
-    return (unsigned)(blocks + (a.chunks + threads - 1) / threads);
+             0, (f32x4*)d_dE, many && by_ranks ? chunks : beside};
+  auto rank = [&](auto pairs, auto most) {
+    constexpr int kPairs = decltype(pairs)::value, kMost = decltype(most)::value;
+    a.blocks = (unsigned)((n_rows + kPairs - 1) / kPairs);
+    const int threads = many ? 256 : 64 * kRankWaves;
+    const unsigned blocks = a.blocks + (unsigned)((a.chunks + threads - 1) / threads);
+    if (many) rank_kernel<kPairs, kMost, 4><<<blocks, threads, kZeroLds - kMost / kBlock * kBlockPitch * 4, s>>>(a);
+    else rank_kernel<kPairs, kMost, kRankWaves><<<blocks, threads, 0, s>>>(a);
   };
   if (n_rows <= kRanked) {
-    const unsigned blocks = grid((n_rows + kRankPairs - 1) / kRankPairs, 64 * kRankWaves);
-    rank_kernel<kRankPairs, kRanked><<<blocks, 64 * kRankWaves, 0, s>>>(a);
+    rank(std::integral_constant<int, kRankPairs>{}, std::integral_constant<int, kRanked>{});
     NAT_LAUNCH_CHECK();
   } else if (n_rows <= kMerged) {
-    const unsigned blocks = grid((n_rows + kTilePairs - 1) / kTilePairs, 64 * kRankWaves);
-    rank_kernel<kTilePairs, kMergeTile><<<blocks, 64 * kRankWaves, 0, s>>>(a);
+    rank(std::integral_constant<int, kTilePairs>{}, std::integral_constant<int, kMergeTile>{});
     NAT_LAUNCH_CHECK();
     a.ids_in = pair[0];
     a.rows_in = pair[1];
