@@ -226,3 +226,24 @@ def test_decode_of_many_sequences_in_large_chunks(stage, D, longest):
     lens = [longest, 0, 1, 2047, 2048, min(2049, longest), min(2176, longest), min(2177, longest), min(4100, longest)] + [7 * i % 50 for i in range(63)]
     c = decode_case(15, lens, 8, 8, D, 16)
     check_decode(c, *stage.decode(c["q"], c["cache"], c["table"], c["lens"]))
+
+
+@pytest.mark.parametrize("heads,D,page", [(1, 64, 16), (1, 128, 32), (3, 64, 16), (8, 128, 64)])
+def test_read_back_of_many_short_sequences(stage, heads, D, page):
+    """Rows of a lane that belong to different sequences, with empty ones between; a table that is too narrow for some; rows in front of the first and behind the last."""
+    lens = [(37 * i * i + 5 * i) % 71 if i % 4 else 0 for i in range(90)] + [0, 130, 1]
+    c = decode_case(16, lens, heads, heads, D, page)
+    width = 128 // page
+    table = c["table"][:, :width].contiguous()
+    cu = np.concatenate([[5], 5 + np.cumsum(lens)])
+    n = int(cu[-1]) + 40
+    out = torch.full((2, n, heads, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    import paper_2603_06619_amd as nat
+    nat.nat_kv_read(c["cache"], table, torch.from_numpy(cu.astype(np.int32)).to(DEV), out[0], out[1])
+    for side, name in enumerate(("k", "v")):
+        values = okv.group_values(getattr(c["cache"], name).cpu().numpy(), getattr(c["cache"], name + "_exp").cpu().numpy())         # [n_pages, heads, page, D]
+        want = np.full((n, heads, D), 7.0)
+        for i, length in enumerate(lens):
+            for t in range(length):
+                want[cu[i] + t] = values[int(table[i, t // page]), :, t % page] if t < page * width else 0.0
+        assert np.array_equal(out[side].double().cpu().numpy(), want)
