@@ -702,10 +702,10 @@ def _pages_args(block_table, seq_lens, change, change_name, free_pages, counts, 
     return args
 
 
-def _reserve(args, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, workspace, *others):
-    """args: of _pages_args; the results are addresses, others their tensors."""
-    _raise(load_library().nat_kv_reserve(*args, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, _ptr(workspace), _bytes(workspace),
-                                         _stream_of(workspace, *others)), "nat_kv_reserve")
+def _reserve(args, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, workspace, ws_bytes, *others):
+    """args: of _pages_args; the results and the workspace are addresses, others their tensors."""
+    _raise(load_library().nat_kv_reserve(*args, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, workspace, ws_bytes, _stream_of(*others)),
+           "nat_kv_reserve")
 
 
 def nat_kv_reserve(block_table, seq_lens, new_lens, free_pages, counts, page_size, rows_cap, counts_out, seq_lens_out, start, cu_new, slots, position_ids, workspace):
@@ -714,18 +714,18 @@ def nat_kv_reserve(block_table, seq_lens, new_lens, free_pages, counts, page_siz
     n, i32, rows = seq_lens.numel(), torch.int32, int(rows_cap)
     _reserve(_pages_args(block_table, seq_lens, new_lens, "new_lens", free_pages, counts, int(page_size)), rows, _counts(counts_out, "counts_out"),
              _vector(seq_lens_out, i32, n, "seq_lens_out"), _vector(start, i32, n, "start"), _vector(cu_new, i32, n + 1, "cu_new"),
-             _vector(slots, torch.int64, rows, "slots"), _vector(position_ids, i32, rows, "position_ids"), workspace,
-             counts_out, seq_lens_out, start, cu_new, slots, position_ids)
+             _vector(slots, torch.int64, rows, "slots"), _vector(position_ids, i32, rows, "position_ids"), _ptr(workspace), _bytes(workspace),
+             workspace, counts_out, seq_lens_out, start, cu_new, slots, position_ids)
 
 
-def _release(args, counts_out, seq_lens_out, workspace, *others):
-    _raise(load_library().nat_kv_release(*args, counts_out, seq_lens_out, _ptr(workspace), _bytes(workspace), _stream_of(workspace, *others)), "nat_kv_release")
+def _release(args, counts_out, seq_lens_out, workspace, ws_bytes, *others):
+    _raise(load_library().nat_kv_release(*args, counts_out, seq_lens_out, workspace, ws_bytes, _stream_of(*others)), "nat_kv_release")
 
 
 def nat_kv_release(block_table, seq_lens, keep_lens, free_pages, counts, page_size, counts_out, seq_lens_out, workspace):
     """Arguments as nat_kv_reserve's; keep_lens int32 [n_seqs]: the tokens that stay.  free_pages is written behind its first counts[0] entries."""
     _release(_pages_args(block_table, seq_lens, keep_lens, "keep_lens", free_pages, counts, int(page_size)), _counts(counts_out, "counts_out"),
-             _vector(seq_lens_out, torch.int32, seq_lens.numel(), "seq_lens_out"), workspace, counts_out, seq_lens_out)
+             _vector(seq_lens_out, torch.int32, seq_lens.numel(), "seq_lens_out"), _ptr(workspace), _bytes(workspace), workspace, counts_out, seq_lens_out)
 
 
 def probe_mfma_scratch_bytes():

@@ -115,22 +115,27 @@ class RolloutStage:
         room in the table), and seq_lens and counts (free pages, sequences refused) as they are now.  The free pages stay where they are, behind counts[0]."""
         args = nb._pages_args(block_table, seq_lens, new_lens, "new_lens", free_pages, counts, page_size)
         n = args[2]
-        whole = torch.empty(3 * n + 3 + n_rows, dtype=torch.int32, device=seq_lens.device)
+        ws_bytes = nb.kv_reserve_workspace_bytes(n)
+        used = 3 * n + 3 + n_rows
+        rest = -used % 64 + ws_bytes // 4                  # the workspace behind the results, at the next 256 bytes
+        whole = torch.empty(used + rest, dtype=torch.int32, device=seq_lens.device)
         slots = torch.empty(n_rows, dtype=torch.int64, device=seq_lens.device)
         at = whole.data_ptr()
         cu, start, lens, pos = at + 8, at + 12 + 4 * n, at + 12 + 8 * n, at + 12 + 12 * n
-        nb._reserve(args, n_rows, at, lens, start, cu, slots.data_ptr(), pos, self._buf("pages", nb.kv_reserve_workspace_bytes(n)))
-        left, cu, start, lens, pos = whole.split((2, n + 1, n, n, n_rows))
+        nb._reserve(args, n_rows, at, lens, start, cu, slots.data_ptr(), pos, at + 4 * (used + rest) - ws_bytes, ws_bytes)
+        left, cu, start, lens, pos, _ = whole.split((2, n + 1, n, n, n_rows, rest))
         return dict(slots=slots, position_ids=pos, cu_new=cu, start=start, seq_lens=lens, counts=left)
 
     def release(self, block_table, seq_lens, keep_lens, free_pages, counts, page_size):
         """The pages behind the first keep_lens tokens of every sequence (0: it has ended) back to free_pages (in place): (seq_lens, counts) as they are now."""
         args = nb._pages_args(block_table, seq_lens, keep_lens, "keep_lens", free_pages, counts, page_size)
         n = args[2]
-        whole = torch.empty(n + 2, dtype=torch.int32, device=seq_lens.device)
+        ws_bytes = nb.kv_release_workspace_bytes(n)
+        rest = -(n + 2) % 64 + ws_bytes // 4
+        whole = torch.empty(n + 2 + rest, dtype=torch.int32, device=seq_lens.device)
         at = whole.data_ptr()
-        nb._release(args, at, at + 8, self._buf("pages", nb.kv_release_workspace_bytes(n)))
-        left, lens = whole.split((2, n))
+        nb._release(args, at, at + 8, at + 4 * (n + 2 + rest) - ws_bytes, ws_bytes)
+        left, lens, _ = whole.split((2, n, rest))
         return lens, left
 
     def write_cache(self, cache, k, v, slots):
