@@ -49,8 +49,8 @@ def check(c, got, **kw):
 def check_backward(c, grads, got, **kw):
     for name, dout, dx, dw in zip("qk", grads, got[:2], got[2:]):
         n, heads = c[name].shape[:2]
-        # a lane: a row of 8192 rows at a time, 8 heads of these; then 3 steps across lanes, 4 wavefronts, 2048 workgroups by 16 walkers and their sum
-        chain = -(-n // 8192) * -(-heads // 8) + 4 + 4 + 128 + 16
+        # a lane: a row of 3072 rows at a time, 8 heads of these; then 4 steps across lanes, 4 wavefronts, 768 workgroups by 32 walkers and their sum
+        chain = -(-n // 3072) * -(-heads // 8) + 4 + 4 + 24 + 32
         ref = ohead.norm_rotate_backward(host(dout), host(c[name]), host(c[name + "_weight"]), host(c["position_ids"]), host(c["inv_freq"]),
                                          half=HALF[dout.dtype], chain=chain, **kw)
         close(dx, ref["dx"], ref["e_dx"])
@@ -193,3 +193,50 @@ def test_gradients_against_differences(stage):
         got = (f(dict(c, **{name: c[name] + h * u})) - f(dict(c, **{name: c[name] - h * u}))) / (2 * h)
         scale = float(grad.double().norm())
         assert abs(got - want) <= 2 * h * h * scale * 4 + 1e-4 * scale, (name, got, want, scale)
+
+
+@pytest.mark.parametrize("R", [0, 64, 128])
+def test_a_backward_pass_of_more_than_the_caches_hold(stage, R):
+    """Rows are independent, so halves, which are held, give the same rows; the weights' gradients against sums in 64 bits (R = 0: of dout_i x_i / sqrt(mean x^2 + eps), each term
+    off by 6 roundings)."""
+    import paper_2603_06619_amd as nat
+    n, hq, hkv, D = 4600, 64, 16, 128
+    assert n * (hq + hkv) * D * 2 * 3 > 1 << 28 > n // 2 * (hq + hkv) * D * 2 * 3
+    c, grads = case(14, n, hq, hkv, D, R, torch.bfloat16)
+    dq, dk, dqw, dkw = stage.norm_rotate_backward(*grads, **c)
+    for rows in (slice(0, n // 2), slice(n // 2, n)):
+        part = dict(c, q=c["q"][rows], k=c["k"][rows], position_ids=c["position_ids"][rows] if R else None)
+        a, b, _, _ = stage.norm_rotate_backward(*(x[rows] for x in grads), **part)
+        assert torch.equal(a, dq[rows]) and torch.equal(b, dk[rows])
+    if R == 0:
+        chain = -(-n // 3072) * -(-hq // 8) + 4 + 4 + 24 + 32 + 6
+        for x, g, got in ((c["q"], grads[0], dqw), (c["k"], grads[1], dkw)):
+            x = x.double()
+            terms = g.double() * x * (x.square().mean(-1, keepdim=True) + 1e-6).rsqrt()
+            assert bool(((got.double() - terms.sum((0, 1))).abs() <= chain * 2.0 ** -24 * terms.abs().sum((0, 1))).all())
+    ws = torch.empty(nat.qk_norm_rope_bwd_workspace_bytes(n, D), dtype=torch.uint8, device=DEV)
+    mine, dw = [g.clone() for g in grads], torch.empty((2, D), device=DEV)
+    nat.nat_qk_norm_rope_bwd(c["q"], c["k"], c["q_weight"], c["k_weight"], c["position_ids"], c["inv_freq"], 1e-6, False, *mine, *mine, dw[0], dw[1], False, ws)
+    assert torch.equal(mine[0], dq) and torch.equal(mine[1], dk) and torch.equal(dw[0], dqw) and torch.equal(dw[1], dkw)
+
+
+def test_rows_beyond_32_bit_offsets(stage):
+    """Rows 2^30 elements apart, of one array of 4.3 GB."""
+    import paper_2603_06619_amd as nat
+    n, hq, hkv, D = 3, 6, 2, 128
+    c, grads = case(15, n, hq, hkv, D, D, torch.bfloat16)
+    want, back = stage.norm_rotate(**c), stage.norm_rotate_backward(*grads, **c)
+    whole, at, apart = torch.empty(2 * 2 ** 30 + 8 * (hq + hkv) * D, dtype=torch.bfloat16, device=DEV), 0, []
+    for x in (c["q"], c["k"], *grads, *want, *back[:2]):
+        apart.append(whole.as_strided(x.shape, (2 ** 30, D, 1), at))
+        at += x.shape[1] * D
+    for x, y in zip(apart, (c["q"], c["k"], *grads)):
+        x.copy_(y)
+    q, k, dq_out, dk_out, q_out, k_out, dq, dk = apart
+    args = (q, k, c["q_weight"], c["k_weight"], c["position_ids"], c["inv_freq"], 1e-6, False)
+    nat.nat_qk_norm_rope(*args, q_out, k_out)
+    assert torch.equal(q_out, want[0]) and torch.equal(k_out, want[1])
+    ws = torch.empty(nat.qk_norm_rope_bwd_workspace_bytes(n, D), dtype=torch.uint8, device=DEV)
+    dw = torch.empty((2, D), device=DEV)
+    nat.nat_qk_norm_rope_bwd(*args, dq_out, dk_out, dq, dk, dw[0], dw[1], False, ws)
+    assert all(torch.equal(x, y) for x, y in zip((dq, dk, dw[0], dw[1]), back))
