@@ -292,7 +292,7 @@ struct TokenTile {
 
   // Of a cache in 4 bits past the chip's caches: nobody reads it again before the next token, and the other layers come in between.  128 sequences of up to 8192 tokens 126 us, otherwise
   // 141; after a launch that has filled the Infinity Cache 126 and 174, 16 of up to 16384 46 and 60, one of 32768 16.5 and 21.4, 128 of up to 2048 with heads of 64 31.6 and 38.5 (which,
-  // called again and again, the cache holds: 31 and 29).
+  // called again and again, the cache holds: 31 and 29).  Tables that name the same pages for two, four or eight sequences next to each other: 112, 105 and 100, otherwise 109, 99 and 98.
   template <typename V>
   __device__ __forceinline__ static V once(const V* p) {
     if constexpr (kFp4) return __builtin_nontemporal_load(p);
