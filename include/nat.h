@@ -520,7 +520,8 @@ nat_status nat_kv_read(const nat_kv_cache* cache, const int32_t* d_block_table, 
  *                (clamped to [0, table_width * page_size]); tokens whose page lies outside [0, n_pages) do not count;
  *   d_out        [n_seqs, n_q_heads, head_dim] bf16 out;  d_lse [n_seqs, n_q_heads] float out.  Without any token out = 0
  *                and lse = -inf.  What is stored in places beyond a sequence's length has no influence.  The probabilities
- *                (of NAT_KV_FP8 with the value rows' powers of two) are rounded to bf16 for the product with the values;
+ *                (of NAT_KV_FP8 with the value rows' powers of two) are rounded to bf16 for the product with the values, of
+ *                NAT_KV_FP4 to a sum of two bf16, which is good to 2^-16;
  *   d_ws / ws_bytes: nat_attn_decode_workspace_bytes(.., max_tokens = table_width * page_size), 256-byte aligned; 0 for
  *                short tables, which need none.
  * Long sequences are cut into chunks for different workgroups and joined by a second kernel; how depends on the sizes

@@ -228,7 +228,11 @@ __global__ void __launch_bounds__(256) kv_read_kernel(ReadArgs a) {
 // leaves columns of them empty).  The next 32 tokens are in registers while these are worked on: at two wavefronts per SIMD, 64 KB in flight per compute unit.
 // 128 sequences of up to 8192 tokens (32 heads on 8 of 128, 8-bit) 235 us, 5.3 TB/s; one of 32768 (28 on 4, bf16) 15.5 us, 4.3 TB/s: 256 tokens per
 // workgroup, of which the first loads are a third of the time.  The first from 4 bits 125 us, 5.3 TB/s.
-// Rounded to fewer bits are the probabilities, to bf16 for the product (with an 8-bit row's power of two in them, which rounds nothing).
+// Rounded to fewer bits are the probabilities, to bf16 for the product (with an 8-bit row's power of two in them, which rounds nothing).  From 4 bits, where values are exact in bf16, what
+// that rounding leaves is a second bf16, and both are multiplied: together good to 2^-16.  A group of up to 8 query heads leaves half of the columns empty; there these are kHalves, and the second
+// numbers take that half (lanes n >= 8, which hold the scores of head n - 8), so that there are no more products than before; larger groups have twice as many.  Error in the 2-norm 0.0017, the
+// result's rounding; with probabilities of 8 bits 0.0021.
+// 128 sequences of up to 8192 tokens (32 heads on 8 of 128) 127.6 us, rounded once 125.3; of up to 2048 39.9 and 39.5, with heads of 64 27.1 and 25.8 (with twice the products 41.8 and 28.7).
 constexpr int kTokens = 32;               // tokens per step of a wavefront
 constexpr int kHeads = 16;                // query heads per workgroup
 constexpr int kMaxChunk = 4096, kMinChunk = 256;
@@ -356,8 +360,8 @@ struct TokenTile {
   }
 };
 
-template <int D, int kFormat>
-__global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
+template <int D, int kFormat, bool kHalves>
+__global__ void __launch_bounds__(256, kFormat == NAT_KV_FP4 ? 4 : 2) decode_kernel(DecodeArgs a) {
   __shared__ __attribute__((aligned(16))) char values[4][kTokens * D * 2];       // and, at the end, the wavefronts' results
   __shared__ int32_t pages[kMaxChunk / 16];
   __shared__ float wave_m[4][kHeads], wave_sum[4][kHeads], joined_m[kHeads], joined_sum[kHeads];
@@ -372,7 +376,11 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
   if (first >= len && chunk > 0) return;
   const int end = len - first < a.chunk ? len - first : a.chunk;      // tokens of the chunk (0: an empty sequence)
   const int heads_here = a.group - block * kHeads < kHeads ? a.group - block * kHeads : kHeads;
-  const int head0 = head * a.group + block * kHeads;
+  const int head0 = head * a.group + block * kHeads, column = kHalves ? n % (kHeads / 2) : n;       // the lane's query head
+  // minus one for the lanes that take what rounding left, as either half of two bf16
+  uint32_t minus = kHalves && n < kHeads / 2 ? 0 : 0xbf80;
+  asm("" : "+v"(minus));                   // (as a constant the compiler writes it as -1 in 32 bits, which is the other half)
+  const bf16x2 of_low = __builtin_bit_cast(bf16x2, minus), of_high = __builtin_bit_cast(bf16x2, minus << 16);
 
   for (int i = threadIdx.x; i < (end + 15) / 16; i += 256) {
     const int p = a.table[(int64_t)seq * a.table_width + ((first + 16 * i) >> a.c.page_log2)];
@@ -382,7 +390,7 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
 #pragma unroll
   for (int s = 0; s < D / 32; ++s) {
     q[s] = bf16x8{};
-    if (n < heads_here) q[s] = *(const bf16x8*)(a.q + seq * a.q_stride + (head0 + n) * D + TokenTile<D, kFormat>::element(s, g));
+    if (column < heads_here) q[s] = *(const bf16x8*)(a.q + seq * a.q_stride + (head0 + column) * D + TokenTile<D, kFormat>::element(s, g));
   }
   __syncthreads();
 
@@ -440,18 +448,31 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
       m = top;
     }
     const float shift = m == -INFINITY ? 0.f : m * to_log2;
-    bf16x8 p;
+    bf16x8 p, rest;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float x = exp2_fast(fmaf(st[b][i], to_log2, -shift));
-        sum += x;
-        if constexpr (kFormat == NAT_KV_FP8) {
-          const float scaled = x * power_of_two((t.v_exp[b] >> (8 * i)) & 0xff);
-          x = whole || st[b][i] != -INFINITY ? scaled : 0.f;       // the scale of a token that is not there may be anything
+      for (int i = 0; i < 4; i += 2) {
+        f32x2 x;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          x[u] = exp2_fast(fmaf(st[b][i + u], to_log2, -shift));
+          sum += x[u];
+          if constexpr (kFormat == NAT_KV_FP8) {
+            const float scaled = x[u] * power_of_two((t.v_exp[b] >> (8 * (i + u))) & 0xff);
+            x[u] = whole || st[b][i + u] != -INFINITY ? scaled : 0.f;       // the scale of a token that is not there may be anything
+          }
         }
-        p[4 * b + i] = (__bf16)x;
+        const bf16x2 rounded = __builtin_convertvector(x, bf16x2);
+        p[4 * b + i] = rounded[0];
+        p[4 * b + i + 1] = rounded[1];
+        if constexpr (kFormat == NAT_KV_FP4) {
+          x[0] = __builtin_amdgcn_fdot2_f32_bf16(rounded, of_low, x[0], false);
+          x[1] = __builtin_amdgcn_fdot2_f32_bf16(rounded, of_high, x[1], false);
+          const bf16x2 left = __builtin_convertvector(x, bf16x2);
+          (kHalves ? p : rest)[4 * b + i] = left[0];
+          (kHalves ? p : rest)[4 * b + i + 1] = left[1];
+        }
       }
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) {
@@ -461,6 +482,7 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
       const s16x4 y = lds_transposed(vt + RowTile<D>::chunk_at(16 + 4 * g + (i >> 2), 2 * db + ((i & 3) >> 1)) + 8 * (i & 1));
       const s16x8 both = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
       acc[db] = mfma16x16(__builtin_bit_cast(bf16x8, both), p, acc[db]);
+      if constexpr (kFormat == NAT_KV_FP4 && !kHalves) acc[db] = mfma16x16(__builtin_bit_cast(bf16x8, both), rest, acc[db]);
     }
   };
   TokenTile<D, kFormat> tiles[kTiles];
@@ -503,7 +525,10 @@ __global__ void __launch_bounds__(256, 2) decode_kernel(DecodeArgs a) {
     const int h = i / (D / 4), d = i % (D / 4) * 4;
     f32x4 x = {};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) x += *(const f32x4*)((const float*)values[w] + h * D + d);
+    for (int w = 0; w < 4; ++w) {
+      x += *(const f32x4*)((const float*)values[w] + h * D + d);
+      if constexpr (kHalves) x += *(const f32x4*)((const float*)values[w] + (h + kHeads / 2) * D + d);
+    }
     const int64_t row = (int64_t)seq * a.hq + head0 + h;
     if (a.n_chunks > 1) {
       *(f32x4*)(a.part_out + (row * a.n_chunks + chunk) * D + d) = x;
@@ -642,7 +667,9 @@ struct LaunchRead {
 template <int D, int kFormat>
 struct LaunchDecode {
   static void go(DecodeArgs a, hipStream_t s) {
-    decode_kernel<D, kFormat><<<(unsigned)((int64_t)a.n_seqs * a.n_chunks * a.c.hkv * a.head_blocks), 256, 0, s>>>(a);
+    const unsigned blocks = (unsigned)((int64_t)a.n_seqs * a.n_chunks * a.c.hkv * a.head_blocks);
+    if (kFormat == NAT_KV_FP4 && a.group <= kHeads / 2) decode_kernel<D, kFormat, kFormat == NAT_KV_FP4><<<blocks, 256, 0, s>>>(a);
+    else decode_kernel<D, kFormat, false><<<blocks, 256, 0, s>>>(a);
   }
 };
 

@@ -32,7 +32,8 @@ class RolloutStage:
     Outputs are allocated, not cleared: rows of q (and out, dq, ...) or of k that belong to no sequence, in front of cu[0] or behind cu[-1], are left as the
     allocator gave them, NaN included.  With arrays that are longer than their sequences cut the results, or clear these rows, before a product sums over all.
 
-    Attention and decoding take products in bf16 with fp32 sums: the probabilities (and the gradients dS) are rounded to bf16 before the second product, see nat.h."""
+    Attention and decoding take products in bf16 with fp32 sums: the probabilities (and the gradients dS) are rounded to bf16 before the second product (from a cache in 4 bits to
+    16 bits), see nat.h."""
 
     def __init__(self, device="cuda:0"):
         self.device = torch.device(device)
