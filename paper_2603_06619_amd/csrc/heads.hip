@@ -175,24 +175,24 @@ __device__ __forceinline__ void turn(float (&x)[8], float (&y)[8], const Turn& t
   }
 }
 
-// 1 / sqrt(mean x^2 + eps) as a product r * s: where the squares pass fp32's range, x s with s = 2^-64 takes the place of x.
+// 1 / sqrt(mean x^2 + eps) as a product r * s: where the root's argument passes fp32's range, x s with s = 2^-80 takes the place of x.  The sum of 128 squares of elements below 2^128 then stays below
+// 2^103; as it comes from a mean of 2^103 on, what falls out of the range below has no weight.
 template <int D>
 __device__ __forceinline__ void norm_of(const float (&x)[8], const float (&y)[8], float eps, float* r, float* s) {
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], fmaf(y[i], y[i], sum));
-  sum = sum_of_head<D>(sum);
+  float mean = fmaf(sum_of_head<D>(sum), 1.f / D, eps);
   *s = 1.f;
-  if (__any(sum == INFINITY)) {
-    const float z = sum == INFINITY ? 0x1p-64f : 1.f;
+  if (__any(mean == INFINITY)) {
+    const float z = mean == INFINITY ? 0x1p-80f : 1.f;
     float t = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t = fmaf(x[i] * z, x[i] * z, fmaf(y[i] * z, y[i] * z, t));
-    sum = sum_of_head<D>(t);
+    mean = fmaf(sum_of_head<D>(t), 1.f / D, eps * z * z);          // (z * z alone would be zero)
     *s = z;
-    eps *= z * z;
   }
-  *r = rsqrtf(fmaf(sum, 1.f / D, eps));
+  *r = rsqrtf(mean);
 }
 
 // Inputs are read past the caches, which the results fill for the next launch: 20.6 thousand rows of 32 + 8 heads 63 us, otherwise 77, between launches that write the inputs and read the
