@@ -547,8 +547,8 @@ nat_status nat_attn_decode(const nat_kv_cache* cache, const void* d_q, int64_t q
  *   *_stride     elements from row to row, a multiple of 8 (bf16) or 4 (f32), at least heads * head_dim; 0 = exactly that.
  *   d_q [n_rows, n_q_heads, D], d_k [n_rows, n_kv_heads, D];  d_q_weight, d_k_weight [D], each NULL for no norm;
  *   d_position_ids [n_rows] int32 (of nat_prefix_pack or nat_kv_reserve), NULL exactly if rotary_dim is 0;
- *   d_inv_freq   [R / 2] double, angle per position in radians; the angle is formed in turns in 64 bits, so far positions
- *                lose nothing;
+ *   d_inv_freq   [R / 2] double, angle per position in radians, of any sign and size: of angles below 2^52 turns the fraction of a
+ *                turn is good to 2^-52, and then rounded to fp32 for sine and cosine;
  *   d_q_out, d_k_out like d_q, d_k: may be the inputs themselves with the same stride (with another one: NAT_INVALID_ARG), otherwise
  *                must not overlap them.
  * Everything in between is held in fp32 and rounded once.  Errors: NULL pointer (but the optional ones), count, eps or flag out

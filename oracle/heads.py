@@ -29,10 +29,16 @@ def _turn(x, angle, rotary, interleaved):
     return y, size
 
 
+TURN = 159154943091895335768883763372514362034459645740456448747667344058896797634226535        # 10^81 / (2 pi)
+
+
 def _angle(positions, inv_freq):
-    """In turns, so that far positions lose no more than the product does."""
-    t = np.asarray(positions, np.float64)[:, None] * (np.asarray(inv_freq, np.float64) / (2 * np.pi))
-    return 2 * np.pi * (t - np.rint(t))
+    """In whole numbers: the turns, of which a position has 2^200 f / (2 pi) parts of 2^-200, lose their whole ones, and what is left is a number of 64 bits."""
+    ratios = [float(f).as_integer_ratio() for f in np.asarray(inv_freq)]
+    per = np.array([(a * TURN << 200) // (b * 10 ** 81) for a, b in ratios], dtype=object)
+    half = np.array([1 << 199], dtype=object)
+    parts = (np.asarray(positions).astype(np.int64).astype(object)[:, None] * per + half) % (2 * half) - half
+    return 2 * np.pi * ((parts // 2 ** 137).astype(np.float64) * 2.0 ** -63)
 
 
 def norm_rotate(x, w=None, positions=None, inv_freq=None, eps=1e-6, interleaved=False, half=0.0):

@@ -130,15 +130,19 @@ struct Lane {
   }
 };
 
-// Sine and cosine of the row's angles, one per lane.  position * frequency / 2 pi in 64 bits: of the turns only the fraction counts, and for positions up to 2^31
-// it is exact to 2^-24 of a turn.
+// Sine and cosine of the row's angles, one per lane.  Of the turns, position * frequency / 2 pi, only the fraction counts: turns per position are taken as a sum of two numbers of 64 bits, good to 2^-105,
+// and the product's whole turns leave it before it is rounded, so that the fraction is good to 2^-52 as long as there are fewer than 2^52 turns.  To fp32, for the functions, it is rounded by up to
+// 2^-26 of a turn.
 __device__ __forceinline__ void form_angles(f32x2* angles, const double* freq, int n, int pos, int lane) {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   if (lane < n) {
-    const double t = (double)pos * (freq[lane] * 0.15915494309189533577);
+    constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;         // 1 / 2 pi
+    const double f = freq[lane], per = f * kTurn, rest = fma(f, kTurnRest, fma(f, kTurn, -per));
+    const double whole = rint((double)pos * per);
+    const float t = (float)fma((double)pos, rest, fma((double)pos, per, -whole));
     float s, c;
-    sincospif(2.f * (float)(t - rint(t)), &s, &c);
+    sincospif(2.f * t, &s, &c);
     angles[lane] = f32x2{c, s};
   }
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
