@@ -210,7 +210,24 @@ def _stream_of(*tensors):
     device = torch._C._cuda_getDevice()              # (tensors on a device: torch.cuda has been set up)
     for t in tensors:
         if t is not None and t.get_device() != device:
-            raise ValueError(f"a tensor of shape {tuple(t.shape)} is on {t.device}, but the current device is {device}")
+            raise _elsewhere(t, device)
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _elsewhere(t, device):
+    return ValueError(f"a tensor of shape {tuple(t.shape)} is on {t.device}, but the current device is {device}")
+
+
+def _stream_for(cache, *tensors):
+    """As _stream_of(), for a cache, whose arrays are all on one device, and tensors."""
+    device = cache._device
+    if device < 0:                                   # host tensors that pass for others, where only the binding is looked at
+        return _stream()
+    if device != torch._C._cuda_getDevice():
+        raise _elsewhere(cache.k, torch._C._cuda_getDevice())
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise _elsewhere(t, device)
     return torch._C._cuda_getCurrentRawStream(device)
 
 
@@ -486,6 +503,10 @@ class KvCache:
                 if t is None or t.shape != rows or t.dtype != torch.uint8 or not t.is_contiguous() or not t.is_cuda:
                     raise TypeError(f"{'k_exp' if t is k_exp else 'v_exp'}: expected a contiguous uint8 device tensor {tuple(rows)}")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self._device = k.get_device()
+        for t in (v, k_exp, v_exp) if fp8 or fp4 else (v,):
+            if t.get_device() != self._device:
+                raise ValueError(f"arrays of a cache are on {k.device} and on {t.device}")
         n_pages, heads, page_size, dim = shape
         dim *= 2 if fp4 else 1
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = n_pages, heads, page_size, dim
@@ -499,7 +520,7 @@ def nat_kv_write(cache, k, v, slots):
     shape = (n, cache.n_kv_heads, cache.head_dim)
     (k, v), (k_stride, v_stride) = _own_rows((k, v), (_rows(k, "k", shape, is_input=True), _rows(v, "v", shape, is_input=True)))
     _raise(load_library().nat_kv_write(ctypes.byref(cache._c), _ptr(k), k_stride, _ptr(v), v_stride,
-                                       _vector(slots, torch.int64, n, "slots"), n, _stream()), "nat_kv_write")
+                                       _vector(slots, torch.int64, n, "slots"), n, _stream_for(cache, k, v, slots)), "nat_kv_write")
 
 
 def _table(block_table, n_seqs):
@@ -515,7 +536,8 @@ def nat_kv_read(cache, block_table, cu_k, k, v):
     shape = (k.shape[0], cache.n_kv_heads, cache.head_dim)
     width = _table(block_table, n_seqs)
     _raise(load_library().nat_kv_read(ctypes.byref(cache._c), _ptr(block_table), width, _vector(cu_k, torch.int32, n_seqs + 1, "cu_k"), n_seqs,
-                                      k.shape[0], _ptr(k), _rows(k, "k", shape), _ptr(v), _rows(v, "v", shape), _stream()), "nat_kv_read")
+                                      k.shape[0], _ptr(k), _rows(k, "k", shape), _ptr(v), _rows(v, "v", shape),
+                                      _stream_for(cache, block_table, cu_k, k, v)), "nat_kv_read")
 
 
 @functools.lru_cache(maxsize=256)
@@ -534,8 +556,8 @@ def nat_attn_decode(cache, q, block_table, seq_lens, scale, out, lse, workspace)
     _raise(load_library().nat_attn_decode(
         ctypes.byref(cache._c), _ptr(q), q_stride, n_seqs, hq, _ptr(block_table), width,
         _vector(seq_lens, torch.int32, n_seqs, "seq_lens"), float(scale), _ptr(out), _rows(out, "out", shape),
-        _vector(lse, torch.float32, n_seqs * hq, "lse"), _ptr(workspace),
-        workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()), "nat_attn_decode")
+        _vector(lse, torch.float32, n_seqs * hq, "lse"), _ptr(workspace), _bytes(workspace),
+        _stream_for(cache, q, block_table, seq_lens, out, lse, workspace)), "nat_attn_decode")
 
 
 @functools.lru_cache(maxsize=256)
