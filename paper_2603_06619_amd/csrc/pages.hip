@@ -149,9 +149,11 @@ __global__ void __launch_bounds__(256) reserve_fill_kernel(PageArgs a) {
 }
 
 // Both in one launch for up to kThreads sequences: every workgroup plans for itself, which takes less than a launch (a batch of 192 sequences and 162 thousand rows 8.4 us and a
-// second launch's host time in two, 5.6 in one; a step of 512 sequences 7.1 and 4.5).  With results in the place of inputs, which another workgroup may have yet to read, one
-// workgroup takes all rows, up to kFewRows.
+// second launch's host time in two, 5.6 in one; a step of 512 sequences 7.1 and 4.5).  Of many rows a workgroup takes one 1024 after another, so that each compute unit plans once: a million rows
+// of 192 sequences 10.1 us, 4 million 27, room for as many of which a thousand are used 11.5 (with 512 workgroups 11.6, 27, 11.6; with one per 1024 rows 15, 52, 36; in two launches 13, 32, 13).
+// With results in the place of inputs, which another workgroup may have yet to read, one workgroup takes all rows, up to kFewRows.
 constexpr int kFewRows = 4096;
+constexpr int64_t kPlans = 256;
 __global__ void __launch_bounds__(kThreads) reserve_kernel(PageArgs a) {
   __shared__ uint32_t sums[4][kWaves];
   __shared__ int32_t cu[kThreads + 1], start[kThreads], len[kThreads], top[kThreads];
@@ -295,7 +297,7 @@ extern "C" nat_status nat_kv_reserve(int32_t* d_block_table, int32_t table_width
   const bool in_place = d_counts_out == d_counts || d_seq_lens_out == d_seq_lens;
   if (n_seqs <= kThreads && (!in_place || rows_cap <= kFewRows)) {
     const int64_t blocks = in_place || rows_cap == 0 ? 1 : (rows_cap + kThreads - 1) / kThreads;
-    reserve_kernel<<<(unsigned)blocks, kThreads, 0, s>>>(a);
+    reserve_kernel<<<(unsigned)(blocks < kPlans ? blocks : kPlans), kThreads, 0, s>>>(a);
     NAT_LAUNCH_CHECK();
     return NAT_OK;
   }
