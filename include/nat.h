@@ -614,12 +614,15 @@ nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const void* d_dou
  * or need_i > 0 and the needs of the sequences 0 .. i together (without those of the sequences refused for the other reasons) are
  * more than n_free.  The others get their pages in order of sequence and place: the next from the end of the stack into
  * block_table[i][ceil(len_i / page_size)], and so on.
+ * A page belongs to one place of the table or to the stack, never to two: the calls do not look for pages that are named twice.  Several rows may
+ * name the same pages where these are only read (nat_attn_decode, nat_kv_read: full pages of a prompt in front of several rollouts); a page that
+ * new tokens go into, which is a sequence's last one unless that is full, must be its own, and see nat_kv_release.
  *   d_block_table [n_seqs, table_width] int32: only the new pages' places are written;
  *   d_seq_lens, d_new_lens [n_seqs] int32 (lengths clamped to what the table holds, negative ones to 0);  page_size a power of two,
  *                16 to 256;
  *   d_free_pages [n_pages] int32, only read;  d_counts [1 or more] int32: n_free (clamped to [0, n_pages]);
  *   d_counts_out [2] int32 out: pages that are left, sequences refused;  d_seq_lens_out [n_seqs] int32 out: len_i + new_i, or len_i if
- *                refused.  Both may be the inputs themselves;
+ *                refused.  d_counts_out may be d_counts, and d_seq_lens_out d_seq_lens; no other results may overlap inputs or one another;
  *   d_start      [n_seqs] int32 out: len_i, or -1 if refused;
  *   d_cu_new     [n_seqs + 1] int32 out: offsets of the new tokens' rows, refused ones included (a step's rows keep their places; offsets
  *                that do not fit 31 bits are 2^31 - 1);
@@ -640,8 +643,10 @@ nat_status nat_kv_reserve(int32_t* d_block_table, int32_t table_width, int32_t n
  * places ceil(kept / page_size) .. ceil(len_i / page_size) - 1 of its row go to d_free_pages[n_free], d_free_pages[n_free + 1], ... in order of
  * sequence and place.  Entries outside [0, n_pages) do not go back, nor does what the stack has no room for (it holds n_pages).
  * The table stays as it is: entries behind a sequence's length have no meaning.
+ * A page that is named at several of these places, or is on the stack already, goes back once more for each, and would then be given to several
+ * sequences: of rows that name the same pages one alone has them here, and only when the others no longer read them, the other rows have -1 in these places.
  *   d_keep_lens  [n_seqs] int32 (negative: 0);  d_counts_out [2] int32 out: free pages, and 0;  d_seq_lens_out [n_seqs] int32 out:
- *                what is kept.  Both may be the inputs themselves.  d_ws: nat_kv_release_workspace_bytes, 256-byte aligned.
+ *                what is kept.  d_counts_out may be d_counts, and d_seq_lens_out d_seq_lens; no other arrays may overlap.  d_ws: nat_kv_release_workspace_bytes, 256-byte aligned.
  * Errors as nat_kv_reserve.
  */
 size_t nat_kv_release_workspace_bytes(int32_t n_seqs);

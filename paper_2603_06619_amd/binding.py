@@ -745,7 +745,8 @@ def _release(args, counts_out, seq_lens_out, workspace, ws_bytes, *others):
 
 
 def nat_kv_release(block_table, seq_lens, keep_lens, free_pages, counts, page_size, counts_out, seq_lens_out, workspace):
-    """Arguments as nat_kv_reserve's; keep_lens int32 [n_seqs]: the tokens that stay.  free_pages is written behind its first counts[0] entries."""
+    """Arguments as nat_kv_reserve's; keep_lens int32 [n_seqs]: the tokens that stay.  free_pages is written behind its first counts[0] entries.
+    Pages that several rows name go back several times: all but one of these rows must have -1 there (see nat.h)."""
     _release(_pages_args(block_table, seq_lens, keep_lens, "keep_lens", free_pages, counts, int(page_size)), _counts(counts_out, "counts_out"),
              _vector(seq_lens_out, torch.int32, seq_lens.numel(), "seq_lens_out"), _ptr(workspace), _bytes(workspace), workspace, counts_out, seq_lens_out)
 

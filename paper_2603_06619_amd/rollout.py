@@ -128,7 +128,8 @@ class RolloutStage:
         return dict(slots=slots, position_ids=pos, cu_new=cu, start=start, seq_lens=lens, counts=left)
 
     def release(self, block_table, seq_lens, keep_lens, free_pages, counts, page_size):
-        """The pages behind the first keep_lens tokens of every sequence (0: it has ended) back to free_pages (in place): (seq_lens, counts) as they are now."""
+        """The pages behind the first keep_lens tokens of every sequence (0: it has ended) back to free_pages (in place): (seq_lens, counts) as they are now.
+        A page goes back once for each row that has it there: of rows that share pages all but one must have -1 in their places."""
         args = nb._pages_args(block_table, seq_lens, keep_lens, "keep_lens", free_pages, counts, page_size)
         n = args[2]
         ws_bytes = nb.kv_release_workspace_bytes(n)
