@@ -5,8 +5,8 @@
 // its workgroup; of one that crosses pieces each leaves its part, and a second kernel adds the parts in order.
 //
 // Bound by HBM.  The lookup of 16381 rows of 4096 in bf16, 268 MB (of which text repeats some), 34 us.  The gradient of 20483 such rows into a vocabulary of 151936, of which 2.49 GB
-// are written and 0.17 read, 449 us, 5.9 TB/s: zeros and ranks 345, merging 8, sums 80 (they write their rows again), joining 6; of 2897 rows of 1024 in fp32 into 32000, 143 MB that the Infinity
-// Cache holds, 28 us: ranks and zeros 18.8, sums 6, joining 3.
+// are written and 0.17 read, 450 us, 5.9 TB/s: zeros and ranks 356, merging 9, sums 81 (they write their rows again), joining 6; of 2897 rows of 1024 in fp32 into 32000, 143 MB that the Infinity
+// Cache holds, 28 us: ranks and zeros 19.2, sums 6.5, joining 3.8.  Added to a gradient that is there (tied weights), the first 120 us: 0.44 GB, rows once and the 8422 ids' rows of the gradient twice.
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
 
@@ -600,9 +600,11 @@ SortPlan sort_plan(int64_t n, int32_t V, int32_t H) {
 
 // A larger one: by workgroups of 256 threads, 16 bytes per thread and 4 KB per workgroup, in order, of which LDS that nobody uses keeps three on a CU.  2.49 GB 340 us, 7.3 TB/s; with eight
 // on a CU 365, in workgroups of 1024 392, four pieces to a workgroup 381 to 417.  Behind those of the sort's first launch, then of four wavefronts, or in a launch of their own where it is
-// another: 20483 rows of 4096 into 151936 449 us in all; a launch of their own 457, beside sixteen wavefronts 490, beside the sums and into the rows without a pair alone 470.
-// (311 MB 97.5 in a launch of their own and 92 beside sixteen wavefronts, 623 MB 122.5, or 120.5, and 125.)
-constexpr int64_t kManyZeros = 512 << 20;                  // bytes
+// another: 20483 rows of 4096 into 151936 450 us in all; a launch of their own 457, beside sixteen wavefronts 490, beside the sums and into the rows without a pair alone 470.
+// Where one ends and the other begins, us in all, beside the sort or few rows' sums and in order: 20483 rows of 1024 in bf16 into 311 MB 77 and 85, 377 MB 99 and 98, 438 MB 113 and 107, 623 MB 144
+// and 136; 2897 of 1024 in fp32 into 311 MB 56 and 59, 377 MB 76 and 70, 438 MB 88 and 78; 9000 of 4096 into 344 MB 92 and 100, 410 MB 109 and 108; 40000 of 512 into 311 MB 95 and 100, 369 MB 110 and
+// 111, 430 MB 124 and 121; 500 of 1024 into 344 MB 65 and 56.
+constexpr int64_t kManyZeros = 360 << 20;                  // bytes
 constexpr size_t kZeroLds = 52000;
 __global__ void __launch_bounds__(256) zero_kernel(f32x4* to, int64_t chunks) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
