@@ -4,7 +4,7 @@
 // of a pair (i, i + R / 2) are its own, and pairs of neighbours are anyway.  The R / 2 sines and cosines of a row are formed by a lane each and go to all heads of the
 // row through LDS: a wavefront takes whole rows, of few rows parts of them.
 //
-// Bound by HBM: 14.4 thousand rows of 28 + 4 heads of 128 in bf16, 212 MB, take 37 us, 5.7 TB/s (a copy: 5.0); 20.6 thousand of 32 + 8 forward 63 us (377 MB), backward 105 (566 MB; 97 where
+// Bound by HBM: 14.4 thousand rows of 28 + 4 heads of 128 in bf16, 212 MB, take 37.5 us, 5.7 TB/s (a copy: 5.0); 20.6 thousand of 32 + 8 forward 65 us (377 MB), backward 107 (566 MB; 97 where
 // the forward pass has not just read the rows past the caches) and 5 for the weights' gradients.  64 rows of 32 + 8, the step of a decoding batch, 3.7 us (6.1 with a wavefront per row).
 #include "nat_internal.h"
 #include "mfma_tile.hip.h"
@@ -201,7 +201,7 @@ __device__ __forceinline__ void norm_of(const float (&x)[8], const float (&y)[8]
 
 // Inputs are read past the caches, which the results fill for the next launch: 20.6 thousand rows of 32 + 8 heads 63 us, otherwise 77, between launches that write the inputs and read the
 // results 222 and 227, 14.4 thousand of 28 + 4 115 and 124.  (Results past the caches: 79 instead of 71 with the launch that reads them.)
-// Without loads ahead: 76 registers, six wavefronts per SIMD.  With them, as in the backward pass, 102 and four: 14.4 thousand rows of 28 + 4 heads 36 instead of 33 us.
+// Without loads ahead: 83 registers, five wavefronts per SIMD.  With them, as in the backward pass, 102 and four: 14.4 thousand rows of 28 + 4 heads 36 instead of 33 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * kWaves) heads_fwd_kernel(HeadsArgs a) {
   constexpr bool kOnce = D == 128 && sizeof(T) == 2;

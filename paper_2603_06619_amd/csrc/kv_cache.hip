@@ -177,7 +177,7 @@ struct Stored {
 };
 
 // The sequence of a packed row is searched for by the lanes that read it, once for the two rows that each of them reads: a chain of five or six loads, after which both rows of keys and of
-// values are under way.  106 MB of 6 sequences from 8 bits in 18.4 us, 5.8 TB/s, most of it written, where a copy writes half; 102 MB from 4 bits in 18.1, behind a launch that fills the
+// values are under way.  106 MB of 6 sequences from 8 bits in 18.4 us (18.9 with a profiler), 5.8 TB/s, most of it written, where a copy writes half; 102 MB from 4 bits in 18.1 (19.0), behind a launch that fills the
 // Infinity Cache and with one that reads the rows 56 (a row per lane 20.3, 20.9 and 64; four rows 19.2, 18.1 and 57).
 constexpr int kReadRows = 2;
 template <int D, int kFormat>
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(256) kv_read_kernel(ReadArgs a) {
 // where there is more than one.  Every cached byte is read once for all heads of the group; the products cost nothing beside that (a group of fewer than 16 heads
 // leaves columns of them empty).  The next 32 tokens are in registers while these are worked on: at two wavefronts per SIMD, 64 KB in flight per compute unit.
 // 128 sequences of up to 8192 tokens (32 heads on 8 of 128, 8-bit) 235 us, 5.3 TB/s; one of 32768 (28 on 4, bf16) 15.5 us, 4.3 TB/s: 256 tokens per
-// workgroup, of which the first loads are a third of the time.  The first from 4 bits 125 us, 5.3 TB/s.
+// workgroup, of which the first loads are a third of the time.  The first from 4 bits 123 us, 5.4 TB/s.
 // Rounded to fewer bits are the probabilities, to bf16 for the product (with an 8-bit row's power of two in them, which rounds nothing).  From 4 bits, where values are exact in bf16, what
 // that rounding leaves is a second bf16, and both are multiplied: together good to 2^-16.  A group of up to 8 query heads leaves half of the columns empty; there these are kHalves, and the second
 // numbers take that half (lanes n >= 8, which hold the scores of head n - 8), so that there are no more products than before; larger groups have twice as many.  Error in the 2-norm 0.0017, the
@@ -294,9 +294,10 @@ struct TokenTile {
     else return 32 * s + 8 * g;
   }
 
-  // Of a cache in 4 bits past the chip's caches: nobody reads it again before the next token, and the other layers come in between.  128 sequences of up to 8192 tokens 126 us, otherwise
-  // 141; after a launch that has filled the Infinity Cache 126 and 174, 16 of up to 16384 46 and 60, one of 32768 16.5 and 21.4, 128 of up to 2048 with heads of 64 31.6 and 38.5 (which,
-  // called again and again, the cache holds: 31 and 29).  Tables that name the same pages for two, four or eight sequences next to each other: 112, 105 and 100, otherwise 109, 99 and 98.
+  // Of a cache in 4 bits past the chip's caches: nobody reads it again before the next token, and the other layers come in between.  128 sequences of up to 8192 tokens 128.5 us, otherwise
+  // 142; after a launch that has filled the Infinity Cache 126 and 175, 16 of up to 16384 45 and 62, one of 32768 16.4 and 21.5, 128 of up to 2048 with heads of 64 26.6 and 34 (which,
+  // called again and again, the cache holds: 27.4 and 26.9).  Tables that name the same pages for two, four or eight sequences next to each other, after such a launch: 112, 108 and 103,
+  // otherwise 116, 104 and 103.
   template <typename V>
   __device__ __forceinline__ static V once(const V* p) {
     if constexpr (kFp4) return __builtin_nontemporal_load(p);
@@ -402,8 +403,8 @@ __global__ void __launch_bounds__(256, kFormat == NAT_KV_FP4 ? 4 : 2) decode_ker
     const int last = (end - 1) / 16, b = t0 / 16;
     t.load(a.c, __builtin_amdgcn_readfirstlane(pages[b]), __builtin_amdgcn_readfirstlane(pages[b < last ? b + 1 : last]), head, first + t0, lane);
   };
-  // In 4 bits one tile, loaded again as soon as its keys and values have been read: 124 registers, four workgroups per compute unit (128 sequences of up to 8192 tokens, loads
-  // through the caches: 141 us; with a second tile 145, three workgroups; with a third 157).
+  // In 4 bits one tile, loaded again as soon as its keys and values have been read: 125 registers, four workgroups per compute unit (128 sequences of up to 8192 tokens 128.5 us; with a second
+  // tile 136, three workgroups; of up to 2048 40 and 45, with heads of 64 27.4 and 28.4; 100 of up to 3000 55.4 and 52).
   constexpr int kTiles = kFormat == NAT_KV_FP4 ? 1 : 2;
   auto step = [&](TokenTile<D, kFormat>& t, int t0, int ahead) {
     const int last = (end - 1) / 16, b0 = t0 / 16;
@@ -624,8 +625,8 @@ bool stride_ok(int64_t s, int64_t row) { return s == 0 || (s >= row && s % 8 == 
 // lengths of a batch differ, and short chunks even them out), or 512 chunks of 256 tokens at least (two steps of each wavefront), and never more than 4096 tokens.  256 sequences of
 // 304 tokens (8 key heads of 128, 8-bit) take 45 us in one chunk each, 66 in two with the join; 8 of 4096 tokens 23 in chunks of 512, 25 of 256; lengths from 33 to 8192 in
 // 128 sequences 101 us in four chunks each, 110 in two.
-// From 4 bits, where a token is half as many bytes, 2048 tokens take the place of 1024: 128 sequences of up to 2048 (8 key heads of 128) 39.4 us, in two chunks each 44.9; with heads of 64 25.8
-// and 31.2; 100 of up to 3000 54.9 and 52.5.
+// From 4 bits, where a token is half as many bytes, 2048 tokens take the place of 1024: 128 sequences of up to 2048 (8 key heads of 128) 40.1 us, in two chunks each 45.5; with heads of 64 27.4
+// and 31.6; of up to 8192 128.5 and 129.3; but 100 of up to 3000 55.4 and 52.9.
 constexpr int kFewTokens = 1024;
 int chunk_of(int64_t n_seqs, int64_t blocks, int64_t most, int64_t few) {
   auto min = [](int64_t x, int64_t y) { return x < y ? x : y; };
