@@ -622,14 +622,15 @@ nat_status nat_embed_bwd(const int32_t* d_ids, int64_t n_rows, const void* d_dou
  *                16 to 256;
  *   d_free_pages [n_pages] int32, only read;  d_counts [1 or more] int32: n_free (clamped to [0, n_pages]);
  *   d_counts_out [2] int32 out: pages that are left, sequences refused;  d_seq_lens_out [n_seqs] int32 out: len_i + new_i, or len_i if
- *                refused.  d_counts_out may be d_counts, and d_seq_lens_out d_seq_lens; no other results may overlap inputs or one another;
+ *                refused.  d_counts_out may be d_counts, and d_seq_lens_out d_seq_lens; no other arrays that are written (the table and the workspace too)
+ *                may overlap others;
  *   d_start      [n_seqs] int32 out: len_i, or -1 if refused;
  *   d_cu_new     [n_seqs + 1] int32 out: offsets of the new tokens' rows, refused ones included (a step's rows keep their places; offsets
  *                that do not fit 31 bits are 2^31 - 1);
  *   d_slots      [rows_cap] int64 out: slot of row cu_new[i] + j, for nat_kv_write: -1 for refused sequences, for pages outside
  *                [0, n_pages) and behind the last row;  d_position_ids [rows_cap] int32 out or NULL: len_i + j (0 behind the last row);
  *   d_ws / ws_bytes: at least nat_kv_reserve_workspace_bytes, 256-byte aligned.
- * Errors: NULL pointer, n_seqs < 0, rows_cap outside [0, 2^31), n_pages < 0, table_width < 0 -> NAT_INVALID_ARG; page_size, n_seqs > 2^24,
+ * Errors: NULL pointer, arrays that overlap, n_seqs < 0, rows_cap outside [0, 2^31), n_pages < 0, table_width < 0 -> NAT_INVALID_ARG; page_size, n_seqs > 2^24,
  * table_width * page_size >= 2^31 -> NAT_BAD_SHAPE; NAT_WORKSPACE_TOO_SMALL.
  */
 size_t nat_kv_reserve_workspace_bytes(int32_t n_seqs);
@@ -646,7 +647,7 @@ nat_status nat_kv_reserve(int32_t* d_block_table, int32_t table_width, int32_t n
  * A page that is named at several of these places, or is on the stack already, goes back once more for each, and would then be given to several
  * sequences: of rows that name the same pages one alone has them here, and only when the others no longer read them, the other rows have -1 in these places.
  *   d_keep_lens  [n_seqs] int32 (negative: 0);  d_counts_out [2] int32 out: free pages, and 0;  d_seq_lens_out [n_seqs] int32 out:
- *                what is kept.  d_counts_out may be d_counts, and d_seq_lens_out d_seq_lens; no other arrays may overlap.  d_ws: nat_kv_release_workspace_bytes, 256-byte aligned.
+ *                what is kept.  d_counts_out may be d_counts, and d_seq_lens_out d_seq_lens; no other written ones may overlap others.  d_ws: nat_kv_release_workspace_bytes, 256-byte aligned.
  * Errors as nat_kv_reserve.
  */
 size_t nat_kv_release_workspace_bytes(int32_t n_seqs);

@@ -267,6 +267,24 @@ nat_status page_args(const int32_t* d_block_table, int32_t width, int32_t n_seqs
 
 size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
+struct Array { const void* at; int64_t bytes; };
+bool same_memory(const Array& a, const Array& b) {
+  const uintptr_t x = (uintptr_t)a.at, y = (uintptr_t)b.at;
+  return a.at && b.at && a.bytes > 0 && b.bytes > 0 && x < y + (uint64_t)b.bytes && y < x + (uint64_t)a.bytes;
+}
+// Whether an array that is written shares memory with another, which other workgroups may have yet to read or write.  The first two that are written, counts and lengths, may be the first two that
+// are read.
+template <int kWritten, int kRead>
+bool overlap(const Array (&written)[kWritten], const Array (&read)[kRead]) {
+  for (int i = 0; i < kWritten; ++i) {
+    for (int j = i + 1; j < kWritten; ++j)
+      if (same_memory(written[i], written[j])) return true;
+    for (int j = 0; j < kRead; ++j)
+      if (same_memory(written[i], read[j]) && !(i == j && i < 2 && written[i].at == read[j].at)) return true;
+  }
+  return false;
+}
+
 }  // namespace
 }  // namespace nat
 
@@ -286,6 +304,11 @@ extern "C" nat_status nat_kv_reserve(int32_t* d_block_table, int32_t table_width
   if (!d_cu_new || (n_seqs > 0 && !d_start) || (rows_cap > 0 && !d_slots)) return NAT_INVALID_ARG;
   if (n_seqs > 0 && (!d_ws || ws_bytes < nat_kv_reserve_workspace_bytes(n_seqs))) return NAT_WORKSPACE_TOO_SMALL;
   if ((uintptr_t)d_ws & 255) return NAT_INVALID_ARG;
+  const int64_t n4 = (int64_t)n_seqs * 4;
+  if (overlap<8, 4>({{d_counts_out, 8}, {d_seq_lens_out, n4}, {d_block_table, n4 * table_width}, {d_start, n4}, {d_cu_new, n4 + 4}, {d_slots, rows_cap * 8},
+                     {d_position_ids, rows_cap * 4}, {d_ws, n4}},
+                    {{d_counts, 4}, {d_seq_lens, n4}, {d_new_lens, n4}, {d_free_pages, (int64_t)n_pages * 4}}))
+    return NAT_INVALID_ARG;
   a.start = d_start;
   a.cu = d_cu_new;
   a.slots = d_slots;
@@ -320,6 +343,10 @@ extern "C" nat_status nat_kv_release(const int32_t* d_block_table, int32_t table
   if (st != NAT_OK) return st;
   if (n_seqs > 0 && (!d_ws || ws_bytes < nat_kv_release_workspace_bytes(n_seqs))) return NAT_WORKSPACE_TOO_SMALL;
   if ((uintptr_t)d_ws & 255) return NAT_INVALID_ARG;
+  const int64_t n4 = (int64_t)n_seqs * 4;
+  if (overlap<4, 4>({{d_counts_out, 8}, {d_seq_lens_out, n4}, {d_free_pages, (int64_t)n_pages * 4}, {d_ws, n_seqs > 0 ? n4 + 4 : 0}},
+                    {{d_counts, 4}, {d_seq_lens, n4}, {d_keep_lens, n4}, {d_block_table, n4 * table_width}}))
+    return NAT_INVALID_ARG;
   a.ws = (int32_t*)d_ws;
   hipStream_t s = (hipStream_t)stream;
   ProfScope prof(PC_PAGES, s);
